@@ -309,6 +309,30 @@ enum { SK_TOP2_STATIC_BYTES = 1 << 20 };
 int sk_top2_static(const float* logits, int32_t rows, int32_t vocab, int64_t row_stride,
                    int32_t* idx1, int32_t* idx2, float* val1, float* val2, float* gap, void* hip_stream);
 
+/*
+ * LOG PROBABILITIES of given tokens, with entropy and the best alternatives: the softmax over a logit row from which the paper's
+ * confidence (Sec. 3.9.2) takes only the two largest entries.  Independent of any pool.
+ * logits: DEVICE [rows][row_stride] of dtype (SK_F32 | SK_BF16), the first `vocab` entries of a row count; aligned to its elements
+ * only (any row_stride >= vocab).  tokens: DEVICE int32 [rows][n_tokens], n_tokens >= 0 (may be NULL when 0); one outside
+ * 0..vocab-1 (padding) is not looked up and its log probability is written as 0.
+ * Outputs, DEVICE, fp32 unless stated; with log softmax(x)[t] = x[t] - lse:
+ *   logprob     [rows][n_tokens]   log softmax(x)[token]
+ *   lse         [rows]             log sum exp of the row                             (may be NULL)
+ *   entropy     [rows]             -sum p log p, natural logarithm, 0 log 0 = 0       (may be NULL)
+ *   top_idx     [rows][n_top]      int32, the n_top largest logits' indices, largest first; equal logits: the lower index first
+ *   top_logprob [rows][n_top]      their log probabilities                            (may be NULL)
+ * n_top: 0..SK_LOGPROBS_MAX_TOP, at most vocab.  Statistics are held in fp32.  Logits of -inf have probability 0 and take what
+ * places of top_idx are left in the order of their indices; a row of nothing else has lse and log probabilities -inf and entropy 0.
+ * A row with NaN or +inf has lse, entropy and log probabilities NaN, and indices that are valid and differ.
+ * workspace: DEVICE scratch of sk_logprobs_workspace_bytes(rows, vocab, n_top) bytes, 16-byte aligned, owned by the caller (NULL if that
+ * is 0); calls that overlap in time need one each.  Kernels only: the call can be captured in a HIP graph.
+ */
+enum { SK_LOGPROBS_MAX_TOP = 32, SK_LOGPROBS_MAX_ROWS = 1 << 20, SK_LOGPROBS_MAX_VOCAB = 1 << 21 };
+size_t sk_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t n_top);
+int sk_logprobs(const void* logits, int dtype, int32_t rows, int32_t vocab, int64_t row_stride,
+                const int32_t* tokens, int32_t n_tokens, int32_t n_top, void* workspace, size_t workspace_bytes,
+                float* logprob, float* lse, float* entropy, int32_t* top_idx, float* top_logprob, void* hip_stream);
+
 /* Byte offset inside kv_mem of element (block, kv_head, is_v, slot, dim), so a harness can
  * address the pool without knowing the layout.  Negative on bad arguments. */
 int64_t sk_pool_element_offset(const sk_pool* pool, int64_t block, int32_t kv_head, int32_t is_v,

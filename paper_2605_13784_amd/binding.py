@@ -17,6 +17,7 @@ SK_POOL_METADATA_ONLY = 1
 
 SK_SITE_RING, SK_SITE_UPLOAD, SK_SITE_BLOCK_COPY, SK_SITE_SCATTER, SK_SITE_ATTENTION, SK_SITE_COMBINE, SK_SITE_PLAN = 1, 2, 3, 4, 5, 6, 7
 SK_TOP2_STATIC_BYTES = 1 << 20
+SK_LOGPROBS_MAX_TOP, SK_LOGPROBS_MAX_ROWS, SK_LOGPROBS_MAX_VOCAB = 32, 1 << 20, 1 << 21
 
 SK_OK = 0
 SK_E_INVAL, SK_E_SHAPE, SK_E_DTYPE, SK_E_NOMEM, SK_E_BADSESSION = -1, -2, -3, -4, -5
@@ -69,6 +70,7 @@ EXPORTS = [
     "sk_pool_set_profiling", "sk_pool_read_profile",
     "sk_pool_element_offset", "sk_pool_get_stats", "sk_pool_last_launch", "sk_strerror",
     "sk_last_hip_error", "sk_version", "sk_top2_workspace_bytes", "sk_top2", "sk_top2_static",
+    "sk_logprobs_workspace_bytes", "sk_logprobs",
     "sk_pool_inject_failure", "sk_probe_read", "sk_probe_mfma",
 ]
 
@@ -118,6 +120,9 @@ def lib():
     L.sk_top2_workspace_bytes.argtypes = [i32, i32]
     L.sk_top2.argtypes = [vp, i32, i32, i64, vp, ctypes.c_size_t, vp, vp, vp, vp, vp, vp]
     L.sk_top2_static.argtypes = [vp, i32, i32, i64, vp, vp, vp, vp, vp, vp]
+    L.sk_logprobs_workspace_bytes.restype = ctypes.c_size_t
+    L.sk_logprobs_workspace_bytes.argtypes = [i32, i32, i32]
+    L.sk_logprobs.argtypes = [vp, ctypes.c_int, i32, i32, i64, vp, i32, i32, vp, ctypes.c_size_t, vp, vp, vp, vp, vp, vp]
     L.sk_pool_inject_failure.argtypes = [vp, i32, i32]
     L.sk_probe_read.argtypes = [vp, ctypes.c_size_t, i32, i32, vp, vp]
     L.sk_probe_mfma.argtypes = [i32, i32, vp, ctypes.c_size_t, vp, P(ctypes.c_double), vp]
@@ -408,6 +413,38 @@ def sk_top2(logits, stream=None, workspace=None, outputs=None):
     _ck(lib().sk_top2(logits.data_ptr() if rows else None, rows, vocab, logits.stride(0) if rows else vocab, _p(workspace),
                       workspace.numel(), _p(idx1), _p(idx2), _p(val1), _p(val2), _p(gap), _stream(stream)), "sk_top2")
     return idx1, idx2, val1, val2, gap
+
+
+def logprobs_outputs(rows, n_tokens, n_top, device):
+    """Output tensors of sk_logprobs: (logprob [rows, n_tokens], lse [rows], entropy [rows], top_idx [rows, n_top], top_logprob)."""
+    f32 = dict(dtype=torch.float32, device=device)
+    return (torch.empty((rows, n_tokens), **f32), torch.empty(rows, **f32), torch.empty(rows, **f32),
+            torch.empty((rows, n_top), dtype=torch.int32, device=device), torch.empty((rows, n_top), **f32))
+
+
+def sk_logprobs(logits, tokens=None, n_top=0, workspace=None, outputs=None, stream=None):
+    """logits: CUDA float32 or bfloat16 tensor [rows, vocab] (rows may be strided); tokens: CUDA int32 [rows, n_tokens] (or [rows]) or
+    None.  Returns (logprob [rows, n_tokens], lse [rows], entropy [rows], top_idx [rows, n_top], top_logprob [rows, n_top])."""
+    assert logits.is_cuda and logits.dtype in (torch.float32, torch.bfloat16) and logits.dim() == 2 and (logits.stride(1) == 1 or logits.shape[1] == 1)
+    rows, vocab = logits.shape
+    n_tokens = 0
+    if tokens is not None:
+        tokens = tokens.view(rows, 1) if tokens.dim() == 1 else tokens
+        assert tokens.dtype == torch.int32 and tokens.device == logits.device and tokens.shape[0] == rows and tokens.dim() == 2
+        n_tokens = tokens.shape[1]
+    if outputs is None:
+        outputs = logprobs_outputs(rows, n_tokens, n_top, logits.device)
+    logprob, lse, entropy, top_idx, top_logprob = outputs
+    for t, shape, dtype in ((logprob, (rows, n_tokens), torch.float32), (lse, (rows,), torch.float32), (entropy, (rows,), torch.float32),
+                            (top_idx, (rows, n_top), torch.int32), (top_logprob, (rows, n_top), torch.float32)):
+        assert t is None or (t.shape == shape and t.dtype == dtype and t.device == logits.device)
+    if workspace is None:
+        workspace = torch.empty(max(lib().sk_logprobs_workspace_bytes(rows, vocab, n_top), 16), dtype=torch.uint8, device=logits.device)
+    # (a single row may have any stride)
+    _ck(lib().sk_logprobs(logits.data_ptr() if rows else None, _dt(logits.dtype), rows, vocab, logits.stride(0) if rows > 1 else vocab, _p(tokens), n_tokens,
+                          n_top, _p(workspace), workspace.numel() * workspace.element_size(), _p(logprob), _p(lse), _p(entropy), _p(top_idx), _p(top_logprob),
+                          _stream(stream)), "sk_logprobs")
+    return outputs
 
 
 def sk_probe_read(buf, n_workgroups, sink, stream=None, nbytes=None, non_temporal=False):

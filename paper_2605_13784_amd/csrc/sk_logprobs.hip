@@ -1,0 +1,422 @@
+// Log probabilities of given tokens, normaliser, entropy and best alternatives of logit rows (include/sk.h: sk_logprobs), gfx950.
+//
+// One pass over the logits.  A wave keeps, per lane, the running maximum m and the sums of a softmax against it,
+//   S = sum exp(x - m),   Z = sum exp(x - m) (x - m),
+// which move to a larger maximum m' = m - delta (delta < 0) by S' = e^delta S, Z' = e^delta (Z + delta S).  Then
+//   lse = m + log S,   log p(t) = (x_t - m) - log S,   entropy = log S - Z / S,
+// the last a sum of two terms that are never negative, so that nothing cancels in a row that is nearly certain.
+// The best alternatives come from the same registers: a wave knows a bound that at least `n_top` of the logits it has seen
+// reach, appends what lies above to a short list in LDS, and cuts the list back to the best n_top when it is full, which raises the
+// bound.  The bound is first the n_top-th largest of the 64 lanes' maxima, found by counting lanes bit by bit.
+// Bound: reading the logits once; about ten vector instructions per logit beside it.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+#include <limits.h>
+#include "../../include/sk.h"
+#include "sk_internal.h"
+
+namespace {
+
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+
+constexpr int kTile = 2048;           // logits that a wave takes at once, 32 in a lane
+constexpr int kWaves = 4;
+constexpr int kList = 256;            // entries of a wave's list of candidates
+constexpr float kLog2e = 1.4426950408889634f;
+
+struct Args {
+    const void* logits;
+    int64_t row_stride;
+    int32_t rows, vocab, n_tokens, n_top;
+    int32_t parts, tiles;             // workgroups to a row; tiles that each of their waves takes
+    const int32_t* tokens;
+    float *logprob, *lse, *entropy;
+    int32_t* top_idx;
+    float* top_logprob;
+    float4* stats;                    // [rows][parts * kWaves]: m, S, Z
+    uint64_t* keys;                   // [rows][parts * kWaves][n_top]
+};
+
+__device__ __forceinline__ uint32_t rank_of(const float x)      // orders floats as unsigned numbers; -0 is +0
+{
+    const uint32_t u = __float_as_uint(x + 0.0f);
+    return u ^ (uint32_t)((int32_t)u >> 31 | INT32_MIN);
+}
+__device__ __forceinline__ float value_of(const uint32_t r)
+{
+    return __uint_as_float(r & 0x80000000u ? r ^ 0x80000000u : ~r);
+}
+constexpr uint32_t kRankNone = 0x007fffffu;       // of -inf
+
+__device__ __forceinline__ int lanes(const bool b) { return __popcll(__ballot(b)); }
+__device__ __forceinline__ int lanes_before(const uint64_t m)
+{
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
+}
+__device__ __forceinline__ void wave_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); __builtin_amdgcn_wave_barrier(); }
+
+// Largest bound that at least k of the wave's numbers reach (N of them in a lane), found from the top bit down; the search ends where
+// exactly k reach it.  `hits` receives how many do.
+template <int N>
+__device__ __forceinline__ uint32_t bound_of(const uint32_t (&r)[N], const int k, int& hits)
+{
+    uint32_t t = 0;
+    hits = 64 * N;
+    for (int b = 31; b >= 0; --b) {
+        const uint32_t c = t | 1u << b;
+        int n = 0;
+#pragma unroll
+        for (int j = 0; j < N; ++j) n += lanes(r[j] >= c);
+        if (n >= k) { t = c; hits = n; }
+        if (n == k) break;
+    }
+    return t;
+}
+
+// A wave's candidates: rank << 32 | ~index, so that of equal logits the one of lower index is the larger key.
+struct Top {
+    uint64_t* list;         // LDS, kList entries
+    int n, k;
+    float floor;            // a logit that is smaller is none of the best; one that equals it only with an index below floor_idx
+    int32_t floor_idx;
+
+    __device__ __forceinline__ void init(uint64_t* l, const int kk) { list = l; n = 0; k = kk; floor = -__builtin_inff(); floor_idx = INT_MIN; }
+
+    // Cuts the list to its k best.
+    __device__ __forceinline__ void cut(const int lane)
+    {
+        constexpr int N = kList / 64;
+        if (n <= k) return;
+        wave_order();
+        uint32_t hi[N], lo[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const bool in = 64 * j + lane < n;
+            const uint64_t x = in ? list[64 * j + lane] : 0;
+            hi[j] = (uint32_t)(x >> 32); lo[j] = (uint32_t)x;
+        }
+        int hits;
+        const uint32_t t = bound_of(hi, k, hits);
+        uint32_t tie = 0;                                 // of equal ranks, those whose ~index reaches this
+        if (hits > k) {
+            int over = 0;
+            uint32_t l[N];
+#pragma unroll
+            for (int j = 0; j < N; ++j) { over += lanes(hi[j] > t); l[j] = hi[j] == t ? lo[j] : 0; }
+            int h;
+            tie = bound_of(l, k - over, h);
+            floor_idx = (int32_t)~tie;
+        } else floor_idx = INT_MIN;                   // (what lies in front of a row has negative indices)
+        floor = t <= kRankNone ? -__builtin_inff() : value_of(t);
+        int at = 0;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const bool stays = hi[j] > t || (hi[j] == t && lo[j] >= tie);
+            const uint64_t m = __ballot(stays);
+            if (stays) list[at + lanes_before(m)] = (uint64_t)hi[j] << 32 | lo[j];
+            at += __popcll(m);
+        }
+        n = at;
+        wave_order();
+    }
+    __device__ __forceinline__ void append(const bool add, const uint64_t key, const int lane)
+    {
+        const uint64_t m = __ballot(add);
+        if (!m) return;
+        if (add) list[n + lanes_before(m)] = key;
+        n += __popcll(m);
+        if (n > kList - 64) cut(lane);
+    }
+    __device__ __forceinline__ bool takes(const float x, const int32_t i) const
+    {
+        return x > floor || (x == floor && i < floor_idx);
+    }
+};
+
+// The 32 logits of this lane in tile `tile` of a row; what lies outside the row is -inf.  `row`: rounded down to 16 bytes, `skip` the
+// elements of another row that come first.
+template <bool BF16>
+__device__ __forceinline__ void load_tile(const unsigned char* __restrict__ row, const int skip, const int64_t total, const int tile, const int lane, float (&x)[32])
+{
+    constexpr int V = BF16 ? 8 : 4, NV = 32 / V;          // logits to a 16-byte piece, pieces to a lane
+    const int64_t first = (int64_t)tile * kTile;
+    u32x4 p[NV];
+    if (first >= skip && first + kTile <= total) {
+        const u32x4* src = (const u32x4*)row + first / V + lane;
+#pragma unroll
+        for (int u = 0; u < NV; ++u) p[u] = __builtin_nontemporal_load(src + 64 * u);
+    } else {                                              // pieces that reach over an end are put together from what lies inside
+#pragma unroll
+        for (int u = 0; u < NV; ++u) {
+            const int64_t e = first + (int64_t)V * (lane + 64 * u);
+            if (e >= skip && e + V <= total) p[u] = __builtin_nontemporal_load((const u32x4*)row + e / V);
+            else {
+                uint32_t w[V];
+#pragma unroll
+                for (int c = 0; c < V; ++c) {
+                    const bool in = e + c >= skip && e + c < total;
+                    if (BF16) w[c] = in ? ((const uint16_t*)row)[e + c] : 0xff80u;
+                    else w[c] = in ? ((const uint32_t*)row)[e + c] : 0xff800000u;
+                }
+                if (BF16) p[u] = u32x4{w[0] | w[1 % V] << 16, w[2 % V] | w[3 % V] << 16, w[4 % V] | w[5 % V] << 16, w[6 % V] | w[7 % V] << 16};
+                else p[u] = u32x4{w[0], w[1], w[2], w[3]};
+            }
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < NV; ++u)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            if (BF16) { x[u * V + 2 * c] = __uint_as_float(p[u][c] << 16); x[u * V + 2 * c + 1] = __uint_as_float(p[u][c] & 0xffff0000u); }
+            else x[u * V + c] = __uint_as_float(p[u][c]);
+        }
+}
+
+struct Sums { float m, s, z; };
+
+__device__ __forceinline__ float exp_of(const float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
+__device__ __forceinline__ float finite_or_0(const float m) { return m == -__builtin_inff() ? 0.f : m; }
+
+// The sums of `a`, moved to the maximum M >= a.m (not -inf).  A side that saw nothing but -inf (or NaN, which stays one) has no z.
+__device__ __forceinline__ Sums moved(const Sums a, const float M)
+{
+    const float d = a.m - M, f = exp_of(d);
+    return Sums{M, a.s * f, a.m == -__builtin_inff() ? 0.f : f * (a.z + d * a.s)};
+}
+
+__device__ __forceinline__ Sums wave_sums(Sums a)
+{
+    float M = a.m;
+#pragma unroll
+    for (int i = 32; i >= 1; i >>= 1) M = fmaxf(M, __shfl_xor(M, i, 64));
+    a = moved(a, finite_or_0(M));
+#pragma unroll
+    for (int i = 32; i >= 1; i >>= 1) { a.s += __shfl_xor(a.s, i, 64); a.z += __shfl_xor(a.z, i, 64); }
+    a.m = M;
+    return a;
+}
+
+// The row's results from its sums and its list (the best n_top in no order, fewer where fewer logits are above -inf), by one wave.
+template <bool BF16>
+__device__ __forceinline__ void write_row(const Args& A, const int r, const Sums a, const Top& top, const int lane)
+{
+    const float log_s = logf(a.s), m = finite_or_0(a.m);
+    const bool none = a.s == 0.f;                         // nothing above -inf
+    const unsigned char* row = (const unsigned char*)A.logits + (int64_t)r * A.row_stride * (BF16 ? 2 : 4);
+    auto at = [&](const int32_t i) { return BF16 ? __uint_as_float((uint32_t)((const uint16_t*)row)[i] << 16) : ((const float*)row)[i]; };
+    auto log_p = [&](const float x) { return none ? -__builtin_inff() : (x - m) - log_s; };
+    if (lane == 0) {
+        if (A.lse) A.lse[r] = none ? -__builtin_inff() : m + log_s;
+        if (A.entropy) A.entropy[r] = none ? 0.f : log_s - a.z / a.s;
+    }
+    for (int j = lane; j < A.n_tokens; j += 64) {
+        const int32_t t = A.tokens[(int64_t)r * A.n_tokens + j];
+        A.logprob[(int64_t)r * A.n_tokens + j] = t >= 0 && t < A.vocab ? log_p(at(t)) : 0.f;
+    }
+    if (A.n_top > 0) {
+        const bool in = lane < top.n;
+        const uint64_t key = in ? top.list[lane] : 0;
+        int place = 0;
+        for (int j = 0; j < top.n; ++j) place += top.list[j] > key;
+        // places that nothing above -inf fills go to the lowest indices that have none
+        const int32_t idx = (int32_t)~(uint32_t)key;
+        uint64_t taken = 0;
+        for (int j = 0; j < top.n; ++j) {
+            const uint32_t i = ~(uint32_t)top.list[j];
+            taken |= i < 64 ? uint64_t(1) << i : 0;
+        }
+        if (in) {
+            A.top_idx[(int64_t)r * A.n_top + place] = idx;
+            if (A.top_logprob) A.top_logprob[(int64_t)r * A.n_top + place] = log_p(at(idx));
+        }
+        const bool free = !(taken >> lane & 1);
+        const int fill = top.n + lanes_before(__ballot(free));
+        if (free && fill < A.n_top) {
+            A.top_idx[(int64_t)r * A.n_top + fill] = lane;
+            if (A.top_logprob) A.top_logprob[(int64_t)r * A.n_top + fill] = log_p(at(lane));
+        }
+    }
+}
+
+// Joins the sums and lists of a workgroup's waves; the result is valid in wave 0.
+template <bool TOP>
+__device__ __forceinline__ void join_waves(Sums& a, Top& top, uint64_t (&lists)[kWaves][kList], const int wave, const int lane)
+{
+    __shared__ float4 stat[kWaves];
+    __shared__ int count[kWaves];
+    if (TOP) top.cut(lane);
+    if (lane == 0) { stat[wave] = float4{a.m, a.s, a.z, 0.f}; if (TOP) count[wave] = top.n; }
+    __syncthreads();
+    if (wave != 0) return;
+    const float4 b = stat[lane & (kWaves - 1)];
+    a = lane < kWaves ? Sums{b.x, b.y, b.z} : Sums{-__builtin_inff(), 0.f, 0.f};
+    a = wave_sums(a);
+    if (TOP) {
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) {
+            const int n = count[w];
+            const uint64_t key = lane < n ? lists[w][lane] : 0;
+            top.append(lane < n, key, lane);
+        }
+        top.cut(lane);
+        wave_order();
+    }
+}
+
+// Workgroup (part, row): its waves take the row's tiles part * kWaves * tiles + wave, + kWaves, ..
+template <bool BF16, bool TOP>
+__global__ __launch_bounds__(64 * kWaves) void sk_logprobs_scan(const Args A)
+{
+    __shared__ uint64_t lists[kWaves][kList];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = blockIdx.x / A.parts, part = blockIdx.x - r * A.parts;
+    constexpr int EL = BF16 ? 2 : 4, V = 16 / EL;
+    const uintptr_t row = (uintptr_t)A.logits + (uintptr_t)((int64_t)r * A.row_stride * EL);
+    const int skip = (int)(row & 15) / EL;
+    const int64_t total = (int64_t)skip + A.vocab;
+    Sums a = {-__builtin_inff(), 0.f, 0.f};
+    Top top;
+    if (TOP) top.init(lists[wave], A.n_top);
+    for (int i = 0; i < A.tiles; ++i) {
+        const int tile = (part * A.tiles + i) * kWaves + wave;
+        if ((int64_t)tile * kTile >= total) break;
+        float x[32];
+        load_tile<BF16>((const unsigned char*)(row & ~(uintptr_t)15), skip, total, tile, lane, x);
+        float mx = x[0];
+#pragma unroll
+        for (int e = 1; e < 32; ++e) mx = fmaxf(mx, x[e]);
+        const float M = fmaxf(a.m, mx), Mf = finite_or_0(M);
+        a = moved(a, Mf);
+        a.m = M;
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+            const float d = x[e] - Mf, w = exp_of(d);
+            a.s += w;
+            a.z += w * fmaxf(d, -200.f);                  // e^-200 is 0 in 32 bits: a logit of -inf adds 0 and not 0 * inf
+        }
+        if (TOP) {
+            if (top.n < top.k) {                          // at least k logits reach the k-th largest of the lanes' maxima
+                int hits;
+                const uint32_t rk[1] = {mx == mx ? rank_of(mx) : 0};
+                const uint32_t t = bound_of(rk, top.k, hits);
+                if (t > kRankNone) { const float f = value_of(t); if (f > top.floor) { top.floor = f; top.floor_idx = INT_MAX; } }
+            }
+            if (__ballot(mx >= top.floor)) {
+                const int32_t i0 = (int32_t)((int64_t)tile * kTile - skip) + V * lane;
+#pragma unroll
+                for (int e = 0; e < 32; ++e) {
+                    const int32_t idx = i0 + (e / V) * 64 * V + e % V;
+                    const bool add = top.takes(x[e], idx);
+                    if (__ballot(add)) top.append(add, (uint64_t)rank_of(x[e]) << 32 | (uint32_t)~idx, lane);
+                }
+            }
+        }
+    }
+    a = wave_sums(a);
+    if (A.parts == 1) {
+        join_waves<TOP>(a, top, lists, wave, lane);
+        if (wave == 0) write_row<BF16>(A, r, a, top, lane);
+        return;
+    }
+    const int64_t slot = (int64_t)blockIdx.x * kWaves + wave;
+    if (lane == 0) A.stats[slot] = float4{a.m, a.s, a.z, 0.f};
+    if (TOP) {
+        top.cut(lane);
+        wave_order();
+        if (lane < A.n_top) A.keys[slot * A.n_top + lane] = lane < top.n ? top.list[lane] : 0;
+    }
+}
+
+// Rows cut into several parts: one workgroup to a row joins them.
+template <bool BF16, bool TOP>
+__global__ __launch_bounds__(64 * kWaves) void sk_logprobs_join(const Args A)
+{
+    __shared__ uint64_t lists[kWaves][kList];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = blockIdx.x, n = A.parts * kWaves;
+    Sums a = {-__builtin_inff(), 0.f, 0.f};
+    for (int i = threadIdx.x; i < n; i += 64 * kWaves) {
+        const float4 b = A.stats[(int64_t)r * n + i];
+        const float M = fmaxf(a.m, b.x), Mf = finite_or_0(M);
+        const Sums p = moved(a, Mf), q = moved(Sums{b.x, b.y, b.z}, Mf);
+        a = Sums{M, p.s + q.s, p.z + q.z};
+    }
+    a = wave_sums(a);
+    Top top;
+    if (TOP) {
+        top.init(lists[wave], A.n_top);
+        const int64_t all = (int64_t)n * A.n_top;
+        const uint64_t* keys = A.keys + (int64_t)r * all;
+        for (int64_t i = 64 * wave; i < all; i += 64 * kWaves) {
+            const uint64_t key = i + lane < all ? keys[i + lane] : 0;
+            const float x = value_of((uint32_t)(key >> 32));
+            top.append(key != 0 && top.takes(x, (int32_t)~(uint32_t)key), key, lane);
+        }
+    }
+    join_waves<TOP>(a, top, lists, wave, lane);
+    if (wave == 0) write_row<BF16>(A, r, a, top, lane);
+}
+
+// How a call is cut: workgroups to a row and tiles to a wave.
+void cut_rows(const int32_t rows, const int32_t vocab, int32_t& parts, int32_t& tiles)
+{
+    const int64_t all = (int64_t(vocab) + 7 + kTile - 1) / kTile, groups = (all + kWaves - 1) / kWaves;
+    // at least 1,024 workgroups where the logits suffice for that
+    int64_t t = (rows * groups + 1023) / 1024;
+    t = t < 1 ? 1 : t > groups ? groups : t;
+    parts = int32_t((groups + t - 1) / t);
+    tiles = int32_t((groups + parts - 1) / parts);
+}
+
+size_t stats_bytes(const int32_t rows, const int32_t parts) { return (size_t)rows * parts * kWaves * sizeof(float4); }
+
+}  // namespace
+
+extern "C" {
+
+size_t sk_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t n_top)
+{
+    if (rows <= 0 || vocab < 1 || n_top < 0 || n_top > SK_LOGPROBS_MAX_TOP) return 0;
+    int32_t parts, tiles;
+    cut_rows(rows, vocab, parts, tiles);
+    return parts == 1 ? 0 : stats_bytes(rows, parts) + (size_t)rows * parts * kWaves * n_top * sizeof(uint64_t);
+}
+
+int sk_logprobs(const void* logits, int dtype, int32_t rows, int32_t vocab, int64_t row_stride, const int32_t* tokens, int32_t n_tokens,
+                int32_t n_top, void* workspace, size_t workspace_bytes, float* logprob, float* lse, float* entropy,
+                int32_t* top_idx, float* top_logprob, void* hip_stream)
+{
+    if (dtype != SK_F32 && dtype != SK_BF16) return SK_E_DTYPE;
+    if (rows < 0 || rows > SK_LOGPROBS_MAX_ROWS || vocab < 1 || vocab > SK_LOGPROBS_MAX_VOCAB || row_stride < vocab) return SK_E_INVAL;
+    if (n_tokens < 0 || n_top < 0 || n_top > SK_LOGPROBS_MAX_TOP || n_top > vocab) return SK_E_INVAL;
+    if (rows == 0) return SK_OK;
+    if (!logits || (n_tokens > 0 && (!tokens || !logprob)) || (n_top > 0 && !top_idx)) return SK_E_INVAL;
+    if ((uintptr_t)logits % (dtype == SK_BF16 ? 2 : 4) || (uintptr_t)workspace % 16) return SK_E_INVAL;
+    Args A;
+    cut_rows(rows, vocab, A.parts, A.tiles);
+    const size_t need = sk_logprobs_workspace_bytes(rows, vocab, n_top);
+    if (need > 0 && !workspace) return SK_E_INVAL;
+    if (workspace_bytes < need) return SK_E_WORKSPACE;
+    A.logits = logits; A.row_stride = row_stride; A.rows = rows; A.vocab = vocab; A.n_tokens = n_tokens; A.n_top = n_top;
+    A.tokens = tokens; A.logprob = logprob; A.lse = lse; A.entropy = entropy; A.top_idx = top_idx; A.top_logprob = top_logprob;
+    A.stats = (float4*)workspace;
+    A.keys = (uint64_t*)((unsigned char*)workspace + stats_bytes(rows, A.parts));
+    hipStream_t st = (hipStream_t)hip_stream;
+    const dim3 grid((unsigned)rows * (unsigned)A.parts), block(64 * kWaves);
+#define SK_LOGPROBS(kernel, grid)                                                                                   \
+    do {                                                                                                            \
+        if (dtype == SK_BF16) {                                                                                     \
+            if (n_top > 0) hipLaunchKernelGGL((kernel<true, true>), grid, block, 0, st, A);                         \
+            else hipLaunchKernelGGL((kernel<true, false>), grid, block, 0, st, A);                                  \
+        } else {                                                                                                    \
+            if (n_top > 0) hipLaunchKernelGGL((kernel<false, true>), grid, block, 0, st, A);                        \
+            else hipLaunchKernelGGL((kernel<false, false>), grid, block, 0, st, A);                                 \
+        }                                                                                                           \
+    } while (0)
+    SK_LOGPROBS(sk_logprobs_scan, grid);
+    if (A.parts > 1) SK_LOGPROBS(sk_logprobs_join, dim3(rows));
+#undef SK_LOGPROBS
+    return hipGetLastError() == hipSuccess ? SK_OK : SK_E_HIP;
+}
+
+}  // extern "C"
