@@ -257,6 +257,31 @@ int sk_session_freeze(sk_pool* pool, int32_t id, int64_t n_frozen);
 int sk_session_evict_oldest(sk_pool* pool, int32_t id, int64_t n_tokens, void* hip_stream);
 
 /*
+ * ATTENTION WEIGHT PER CACHED TOKEN: what sk_session_evict_lowest ranks tokens by.  q [n_tok][Hq][d] (pool dtype) and
+ * lse [n_tok][Hq] DEVICE are a call's query rows and the log-sum-exps that it wrote for them; for every KV head g and retained token j
+ *   mass_out[g][j] = keep * mass_in[g][j] + sum over tokens i and query heads h of group g of exp(scale * q[i][h] . k[g][j] - lse[i][h])
+ * causal == 0 (behind sk_session_query): every token sees every retained one.  causal != 0 (behind sk_session_append): the
+ * n_tok tokens are the session's newest, token i sees retained tokens 0..length - n_tok + i.  A query's own K/V are not cached and
+ * receive nothing.  keep: 1 adds up, below 1 older calls fade, 0 starts anew (mass_in is not read then; NULL is the same).  A row whose
+ * lse is infinite (padding: it attended to nothing) adds nothing, whatever its q holds.  n_tok == 0 scales only.
+ * mass_in, mass_out: DEVICE float [Hkv][stride], 4-byte aligned, strides in elements, at least the session's length; entries from
+ * the length on are neither read nor written.  mass_out may be mass_in (same pointer and stride) and must not overlap it otherwise, nor
+ * another item's arrays.  The caller keeps these arrays beside the session: an append's tokens come behind the last entry (put 0
+ * there, or pass keep 0), sk_session_evict_lowest moves the entries with the tokens, sk_session_evict_oldest(n) takes out
+ * n entries behind the frozen ones.  Sums are fp32, in an order that depends on the shapes only.  Nothing of the session changes; the
+ * call enqueues kernels only and can be captured like sk_session_query.
+ * The batched form does the same for item i's rows cu_tokens[i]..cu_tokens[i+1]-1 and its own arrays (HOST arrays, the pointers in
+ * them DEVICE; causal NULL: all 0; mass_in NULL: none).  A session may appear once.
+ */
+int sk_session_attention_mass(sk_pool* pool, int32_t id, const void* q, const float* lse, int32_t n_tok, int32_t causal,
+                              const float* mass_in, int64_t mass_in_stride, float keep,
+                              float* mass_out, int64_t mass_out_stride, void* hip_stream);
+int sk_batch_attention_mass(sk_pool* pool, int32_t n_items, const int32_t* session_id, const int32_t* causal,
+                            const int32_t* cu_tokens, const void* q, const float* lse,
+                            const float* const* mass_in, const int64_t* mass_in_stride, float keep,
+                            float* const* mass_out, const int64_t* mass_out_stride, void* hip_stream);
+
+/*
  * FORK (Sec. 3.7 prefix-aware grouped prefill: followers alias the leader's state; Sec. 3.10
  * metadata-only sequence aliasing).  Creates a session whose cache is the first n_prefix retained
  * tokens of session src (including src's frozen region and evicted range as far as the prefix

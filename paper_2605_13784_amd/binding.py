@@ -70,6 +70,7 @@ EXPORTS = [
     "sk_pool_set_profiling", "sk_pool_read_profile",
     "sk_pool_element_offset", "sk_pool_get_stats", "sk_pool_last_launch", "sk_strerror",
     "sk_last_hip_error", "sk_version", "sk_top2_workspace_bytes", "sk_top2", "sk_top2_static",
+    "sk_session_attention_mass", "sk_batch_attention_mass",
     "sk_logprobs_workspace_bytes", "sk_logprobs",
     "sk_pool_inject_failure", "sk_probe_read", "sk_probe_mfma",
 ]
@@ -120,6 +121,8 @@ def lib():
     L.sk_top2_workspace_bytes.argtypes = [i32, i32]
     L.sk_top2.argtypes = [vp, i32, i32, i64, vp, ctypes.c_size_t, vp, vp, vp, vp, vp, vp]
     L.sk_top2_static.argtypes = [vp, i32, i32, i64, vp, vp, vp, vp, vp, vp]
+    L.sk_session_attention_mass.argtypes = [vp, i32, vp, vp, i32, i32, vp, i64, ctypes.c_float, vp, i64, vp]
+    L.sk_batch_attention_mass.argtypes = [vp, i32, P(i32), P(i32), P(i32), vp, vp, P(vp), P(i64), ctypes.c_float, P(vp), P(i64), vp]
     L.sk_logprobs_workspace_bytes.restype = ctypes.c_size_t
     L.sk_logprobs_workspace_bytes.argtypes = [i32, i32, i32]
     L.sk_logprobs.argtypes = [vp, ctypes.c_int, i32, i32, i64, vp, i32, i32, vp, ctypes.c_size_t, vp, vp, vp, vp, vp, vp]
@@ -371,6 +374,42 @@ class Pool:
         if lse_s is not None:
             lse_s = lse_s.view(NQ, Sfx, self.Hq)
         return out_p, lse_p, out_s, lse_s
+
+    def _mass(self, t, n):
+        """Checks an array of accumulated weights: float32 [Hkv, >= n], entries of a row next to each other."""
+        assert t.dtype == torch.float32 and t.dim() == 2 and t.shape[0] == self.Hkv and t.shape[1] >= n and (t.stride(1) == 1 or t.shape[1] <= 1)
+        return t.data_ptr(), (t.stride(0) if self.Hkv > 1 else max(n, 1))
+
+    def sk_session_attention_mass(self, sid, q, lse, causal=False, mass_in=None, keep=1.0, mass_out=None, stream=None):
+        """mass_in, mass_out: float32 [Hkv, capacity]; mass_out left out: mass_in in place, or a new [Hkv, length]."""
+        n = self.sk_session_length(sid)
+        if mass_out is None:
+            mass_out = mass_in if mass_in is not None else torch.empty((self.Hkv, n), dtype=torch.float32, device=self.device)
+        assert q is None or (q.dtype == self.torch_dtype and lse.dtype == torch.float32 and lse.numel() == q.shape[0] * self.Hq)
+        pi, si = self._mass(mass_in, n) if mass_in is not None and keep != 0 else (None, 0)
+        po, so = self._mass(mass_out, n)
+        _ck(lib().sk_session_attention_mass(self.h, sid, _p(q), _p(lse), 0 if q is None else q.shape[0], int(bool(causal)), pi, si, keep, po, so,
+                                            _stream(stream)), "sk_session_attention_mass")
+        return mass_out
+
+    def sk_batch_attention_mass(self, session_ids, cu_tokens, q, lse, causal=None, mass_in=None, keep=1.0, mass_out=None, stream=None):
+        """The same for a ragged step: mass_in and mass_out are lists of arrays, one a session."""
+        n = len(session_ids)
+        lengths = [self.sk_session_length(s) for s in session_ids]
+        if mass_out is None:
+            mass_out = mass_in if mass_in is not None else [torch.empty((self.Hkv, m), dtype=torch.float32, device=self.device) for m in lengths]
+        assert q.dtype == self.torch_dtype and lse.dtype == torch.float32 and q.shape[0] >= cu_tokens[-1] and lse.numel() == q.shape[0] * self.Hq
+
+        def host(arrays):
+            got = [self._mass(t, m) for t, m in zip(arrays, lengths, strict=True)]
+            return (ctypes.c_void_p * n)(*[x for x, _ in got]), (ctypes.c_int64 * n)(*[x for _, x in got])
+
+        pi, si = host(mass_in) if mass_in is not None and keep != 0 else (None, None)
+        po, so = host(mass_out)
+        _ck(lib().sk_batch_attention_mass(self.h, n, (ctypes.c_int32 * n)(*session_ids), None if causal is None else (ctypes.c_int32 * n)(*map(int, causal)),
+                                          (ctypes.c_int32 * (n + 1))(*cu_tokens), _p(q), _p(lse), pi, si, keep, po, so, _stream(stream)),
+            "sk_batch_attention_mass")
+        return mass_out
 
     def sk_session_gather(self, sid, first=0, count=None, stream=None):
         if count is None:

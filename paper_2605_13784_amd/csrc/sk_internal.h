@@ -174,6 +174,21 @@ struct sk_commit {
     sk_scatter item[SK_COMMIT_ITEMS];
 };
 
+// What an operator in a file of its own needs to know of a pool and one of its sessions (sk_pool.cpp).
+struct sk_pool;
+struct sk_session_view {
+    sk_geom g;
+    bool device;              // false: metadata-only pool
+    int32_t tbl_off;          // int32 offset of the session's block table in sk_geom::tables
+    int32_t max_batch_tokens;
+    int64_t retained;         // tokens the session holds: storage indices [0, frozen) and [win, win + retained - frozen)
+    int64_t frozen, win;
+};
+int sk_view_session(const sk_pool* p, int32_t id, sk_session_view* out);     // SK_OK | SK_E_INVAL | SK_E_BADSESSION
+bool sk_sessions_differ(sk_pool* p, int32_t n, const int32_t* id);           // ids of live sessions
+int sk_note_hip_error(int hip_error);                                        // for sk_last_hip_error; returns SK_E_HIP
+void sk_count_launch(sk_pool* p);
+
 // Launchers implemented in sk_kernels.hip (return hipError_t as int).
 int sk_launch_scatter(const sk_geom& g, const void* k, const void* v, const sk_scatter* items,
                       int32_t n_items, int32_t* tables_rw, unsigned char* kv_rw,

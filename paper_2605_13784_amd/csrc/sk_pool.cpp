@@ -37,6 +37,7 @@ struct Session {
     int64_t frozen = 0, win = 0;
     std::vector<int32_t> blocks;
     mutable bool may_share = false;      // forked, or a fork: other sessions may hold some of its blocks too (holds_shared)
+    uint64_t named = 0;                  // the last list that was found to name it (sk_sessions_differ)
     int64_t retained() const { return frozen + (len - win); }
 };
 
@@ -125,6 +126,7 @@ struct sk_pool {
     std::deque<int32_t> free_blocks;
     std::vector<Session> sessions;
     std::vector<int32_t> free_ids;
+    uint64_t lists_named = 0;            // lists looked through by sk_sessions_differ
     int64_t blocks_in_use = 0;
     std::vector<int32_t> refcnt;         // sessions holding each block (forks share the blocks of a prefix)
     // pinned staging ring for uploaded lists
@@ -1335,6 +1337,35 @@ int launch_list(sk_pool* p, ListPlan& P, const ScatterBatch* sb, int n_sb, ListG
 }
 
 }  // namespace
+
+// ---- for the operators in files of their own (sk_internal.h) ----
+
+int sk_view_session(const sk_pool* p, int32_t id, sk_session_view* out)
+{
+    if (!p) return SK_E_INVAL;
+    const Session* s = get_session(p, id);
+    if (!s) return SK_E_BADSESSION;
+    out->g = p->geom;
+    out->device = p->device;
+    out->tbl_off = int32_t(int64_t(id) * p->L.max_blocks_per_session);
+    out->max_batch_tokens = p->L.max_batch_tokens;
+    out->retained = s->retained(); out->frozen = s->frozen; out->win = s->win;
+    return SK_OK;
+}
+
+bool sk_sessions_differ(sk_pool* p, int32_t n, const int32_t* id)
+{
+    const uint64_t list = ++p->lists_named;
+    for (int32_t i = 0; i < n; ++i) {
+        Session& s = p->sessions[(size_t)id[i]];
+        if (s.named == list) return false;
+        s.named = list;
+    }
+    return true;
+}
+
+int sk_note_hip_error(int e) { g_last_hip = e; return SK_E_HIP; }
+void sk_count_launch(sk_pool* p) { p->stats.launches++; }
 
 extern "C" {
 

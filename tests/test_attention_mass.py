@@ -1,0 +1,307 @@
+"""sk_session_attention_mass / sk_batch_attention_mass: the attention weight of every cached token summed over a call's rows, against
+the formula in 64 bits.
+
+Tolerance, relative, as every term of a sum is positive.  With u = 2^-24: a score of d products that are exact (bf16) or
+rounded once (fp32) is off by at most (d + 1) u |q| |k| before the scale; the scale in log2 units, the row's log-sum-exp in log2
+units and their difference are rounded to u of themselves each, which an exponential turns into a relative 2 u ln 2 (|s| + |lse|) log2 e
+= 2 u (|s| + |lse|) at most, as is s times the rounding of the scale; the hardware's exponential is within 2 u; the R rows of a
+KV head meet in at most R + 8 additions of u each; keep * mass_in and the last addition round twice more."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2605_13784_amd as sk
+from workloads import synth
+
+SHAPES = {"layer": synth.CFG2, "f32": synth.CFG1, "d64": synth.Shape("bf16", 32, 8, 64), "group7": synth.Shape("bf16", 28, 4, 128),
+          "one_kv_head": synth.Shape("bf16", 33, 1, 64), "f32_wide": synth.Shape("f32", 8, 2, 128), "no_groups": synth.Shape("bf16", 5, 5, 128)}
+
+
+def _session(shape, gen, n, block, frozen=0, evicted=0, n_more=0, max_sessions=1):
+    """A pool with a session of n retained tokens in blocks of no order, and its keys as the pool holds them."""
+    blocks = -(-(n + evicted + n_more) // block) + 2
+    pool = sk.Pool(shape.dtype, shape.n_q_heads, shape.n_kv_heads, shape.head_dim, block, blocks, max_sessions=max_sessions, max_batch_tokens=8192, kv_fill=0xFF)
+    pool.sk_pool_set_alloc_order(synth.permutation(gen, blocks))
+    sid = pool.sk_session_create()
+    _, k, v = synth.draw_qkv(gen, n + evicted, shape)
+    for t in range(0, n + evicted, 8192):
+        pool.sk_session_append(sid, None, k[t:t + 8192].cuda(), v[t:t + 8192].cuda())
+    if frozen:
+        pool.sk_session_freeze(sid, frozen)
+    if evicted:
+        pool.sk_session_evict_oldest(sid, evicted)
+    return pool, sid, torch.cat([k[:frozen], k[frozen + evicted:]])
+
+
+def _expected(shape, q, k, lse, causal, scale=None):
+    """(sums, relative tolerance) in 64 bits."""
+    T, n, G = q.shape[0], k.shape[0], shape.group
+    scale = scale or 1.0 / math.sqrt(shape.head_dim)
+    total = torch.zeros((shape.n_kv_heads, n), dtype=torch.float64)
+    most = 0.0
+    for h in range(shape.n_q_heads):
+        qh, kh = q[:, h].double(), k[:, h // G].double()
+        s = scale * (qh @ kh.t())
+        live = torch.isfinite(lse[:, h])
+        w = torch.where(live[:, None], torch.exp(s - lse[:, h].double()[:, None]), torch.zeros((), dtype=torch.float64))
+        if causal:
+            w = torch.tril(w, diagonal=n - T)
+        total[h // G] += w.sum(0)
+        if live.any():
+            most = max(most, float(scale * qh[live].norm(dim=1).max() * kh.norm(dim=1).max()))
+    u = 2.0 ** -24
+    ll = lse[torch.isfinite(lse)].abs().max() if torch.isfinite(lse).any() else 0.0
+    return total, u * ((shape.head_dim + 1) * most + 4 * (most + float(ll)) + T * G + 16)
+
+
+def _close(got, want, tol):
+    got = got.double().cpu()
+    assert torch.isfinite(got).all()
+    worst = ((got - want).abs() - tol * want.abs()).max()
+    assert worst <= 1e-37, "off by %.3e beyond the tolerance" % worst          # (what is below the least normal number may vanish)
+
+
+def _lse(shape, gen, q, k, causal, scale=None):
+    """Near the rows' log-sum-exp (an input like any other here)."""
+    T, n, G = q.shape[0], k.shape[0], shape.group
+    out = torch.empty((T, shape.n_q_heads))
+    for h in range(shape.n_q_heads):
+        s = (scale or shape.head_dim ** -0.5) * (q[:, h].float() @ k[:, h // G].float().t())
+        if causal:
+            s = torch.where(torch.tril(torch.ones_like(s), diagonal=n - T) > 0, s, torch.full_like(s, -math.inf))
+        out[:, h] = torch.logsumexp(s, 1)
+    return out
+
+
+CASES = [("layer", 1, 1, False, 16), ("layer", 1, 1, True, 16), ("layer", 31, 1, False, 16), ("layer", 33, 9, True, 16), ("layer", 64, 64, True, 16),
+         ("layer", 65, 40, False, 64), ("layer", 129, 129, True, 16), ("layer", 1000, 1, False, 16), ("layer", 1037, 77, True, 256), ("layer", 2600, 300, True, 16),
+         ("layer", 9001, 130, True, 64), ("layer", 9001, 8, False, 16), ("layer", 20000, 33, False, 16),
+         ("f32", 1, 1, True, 16), ("f32", 63, 20, True, 16), ("f32", 1024, 16, False, 16), ("f32", 1001, 200, True, 64), ("f32_wide", 700, 50, True, 16),
+         ("f32_wide", 8200, 3, False, 16), ("d64", 130, 131 - 1, True, 16), ("d64", 3001, 17, False, 1024), ("d64", 12000, 257, True, 16),
+         ("group7", 500, 41, True, 16), ("group7", 9001, 77, True, 64), ("one_kv_head", 777, 3, False, 16), ("one_kv_head", 4000, 100, True, 16),
+         ("no_groups", 900, 70, True, 16)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name,n,T,causal,block", CASES)
+def test_against_the_formula(name, n, T, causal, block):
+    shape = SHAPES[name]
+    gen = synth.generator(9, stream=n + T)
+    pool, sid, k = _session(shape, gen, n, block)
+    q = synth.draw(gen, (T, shape.n_q_heads, shape.head_dim), shape.dtype)
+    lse = _lse(shape, gen, q, k, causal)
+    before = torch.rand((shape.n_kv_heads, n + 5), generator=gen)
+    want, tol = _expected(shape, q, k, lse, causal)
+    got = pool.sk_session_attention_mass(sid, q.cuda(), lse.cuda(), causal=causal)
+    torch.cuda.synchronize()
+    assert got.shape == (shape.n_kv_heads, n)
+    _close(got, want, tol)
+    # on top of what is there, in place, with room behind the session's end that stays as it is; the same bits each time
+    place = before.cuda()
+    assert pool.sk_session_attention_mass(sid, q.cuda(), lse.cuda(), causal=causal, mass_in=place, keep=0.75) is place
+    again = torch.full_like(place, -7.0)
+    pool.sk_session_attention_mass(sid, q.cuda(), lse.cuda(), causal=causal, mass_in=before.cuda(), keep=0.75, mass_out=again)
+    torch.cuda.synchronize()
+    _close(place[:, :n], want + 0.75 * before[:, :n].double(), tol)
+    assert torch.equal(place[:, n:].cpu(), before[:, n:]) and torch.equal(again[:, :n], place[:, :n]) and (again[:, n:] == -7.0).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", ["layer", "f32"])
+@pytest.mark.parametrize("frozen,evicted,block", [(0, 5, 16), (37, 10, 16), (64, 100, 64), (100, 333, 256), (500, 3, 16)])
+def test_sessions_with_evicted_tokens(name, frozen, evicted, block):
+    shape = SHAPES[name]
+    gen = synth.generator(9, stream=frozen + evicted)
+    n = 611
+    pool, sid, k = _session(shape, gen, n, block, frozen, evicted)
+    for T, causal in ((3, False), (45, True)):
+        q = synth.draw(gen, (T, shape.n_q_heads, shape.head_dim), shape.dtype)
+        lse = _lse(shape, gen, q, k, causal)
+        want, tol = _expected(shape, q, k, lse, causal)
+        _close(pool.sk_session_attention_mass(sid, q.cuda(), lse.cuda(), causal=causal), want, tol)
+
+
+@pytest.mark.gpu
+def test_weights_of_an_append_and_of_queries_add_up_to_their_rows():
+    """Beside the calls that they belong to: every row gives each KV head's tokens a weight of 1 in all (a query's own tokens apart)."""
+    shape = synth.CFG2
+    gen = synth.generator(9, stream=1)
+    pool, sid, k = _session(shape, gen, 900, 16, n_more=200)
+    q, k2, v2 = (x.cuda() for x in synth.draw_qkv(gen, 200, shape))
+    _, lse = pool.sk_session_append(sid, q, k2, v2)
+    mass = pool.sk_session_attention_mass(sid, q, lse, causal=True)
+    # lse of the library within 1e-3 (its stated tolerance): each row's weights add up to e^+-1e-3
+    assert torch.all((mass.double().sum(1) / (200 * shape.group) - 1).abs() <= 1.1e-3)
+    assert (mass[:, -1] > 0).all()
+    _, lse = pool.sk_session_query(sid, q[:32])
+    more = pool.sk_session_attention_mass(sid, q[:32], lse, mass_in=mass, mass_out=torch.empty_like(mass))
+    assert torch.all(((more.double().sum(1) - mass.double().sum(1)) / (32 * shape.group) - 1).abs() <= 1.1e-3)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", ["layer", "f32", "d64"])
+def test_rows_that_are_left_out_and_sums_that_are_not_read(name):
+    shape = SHAPES[name]
+    gen = synth.generator(9, stream=2)
+    n, T = 300, 40
+    pool, sid, k = _session(shape, gen, n, 16)
+    q = synth.draw(gen, (T, shape.n_q_heads, shape.head_dim), shape.dtype)
+    lse = _lse(shape, gen, q, k, False)
+    clean = q.clone()
+    lse[5], lse[17, 3], lse[39] = math.inf, -math.inf, math.inf
+    q[5], q[17, 3], q[39] = math.nan, math.inf, math.nan
+    want, tol = _expected(shape, clean, k, lse, False)
+    nothing = torch.full((shape.n_kv_heads, n), math.nan, device="cuda")
+    _close(pool.sk_session_attention_mass(sid, q.cuda(), lse.cuda(), mass_in=nothing, keep=0.0), want, tol)
+    # a call of such rows only, and one of no rows: what was there, scaled
+    before = torch.rand((shape.n_kv_heads, n), generator=gen).cuda()
+    for rows in (1, 0):
+        out = pool.sk_session_attention_mass(sid, q[5:5 + rows].cuda(), lse[5:5 + rows].cuda(), mass_in=before, keep=0.5, mass_out=torch.empty_like(before))
+        assert torch.equal(out, 0.5 * before)
+
+
+@pytest.mark.gpu
+def test_batch_against_single_calls_and_the_formula():
+    shape = synth.CFG2
+    gen = synth.generator(9, stream=3)
+    lengths, tokens, causal = [1, 700, 0, 64, 2000, 129, 31], [1, 50, 0, 64, 0, 5, 2], [1, 1, 0, 1, 0, 0, 0]
+    pool = sk.Pool("bf16", 32, 8, 128, 16, 400, max_sessions=60, kv_fill=0xFF)
+    pool.sk_pool_set_alloc_order(synth.permutation(gen, 400))
+    sids, keys = [], []
+    for n in lengths:
+        sids.append(pool.sk_session_create())
+        _, k, v = synth.draw_qkv(gen, n, shape)
+        if n:
+            pool.sk_session_append(sids[-1], None, k.cuda(), v.cuda())
+        keys.append(k)
+    cu = [0] + [int(x) for x in np.cumsum(tokens)]
+    q = synth.draw(gen, (cu[-1], 32, 128), "bf16")
+    lse = torch.cat([_lse(shape, gen, q[a:b], k, c) if b > a else torch.empty((0, 32)) for a, b, k, c in zip(cu, cu[1:], keys, causal)])
+    before = [torch.rand((8, n + i), generator=gen).cuda() for i, n in enumerate(lengths)]
+    out = pool.sk_batch_attention_mass(sids, cu, q.cuda(), lse.cuda(), causal=causal, mass_in=before, keep=0.5, mass_out=[torch.full_like(b, -3.0) for b in before])
+    fresh = pool.sk_batch_attention_mass(sids, cu, q.cuda(), lse.cuda(), causal=causal)
+    torch.cuda.synchronize()
+    for i, n in enumerate(lengths):
+        a, b = cu[i], cu[i + 1]
+        if n:
+            want, tol = _expected(shape, q[a:b], keys[i], lse[a:b], causal[i])
+            _close(fresh[i], want, tol)
+            _close(out[i][:, :n], want + 0.5 * before[i][:, :n].cpu().double(), tol)
+        assert (out[i][:, n:] == -3.0).all()
+    # more sessions than one launch carries: forks of one
+    forks = [pool.sk_session_fork(sids[5], 129 - i % 3) for i in range(53)]
+    cu = list(range(54))
+    got = pool.sk_batch_attention_mass(forks, cu, q[:53].cuda(), lse[:53].cuda())
+    torch.cuda.synchronize()
+    for i in (0, 1, 2, 46, 47, 48, 49, 52):
+        want, tol = _expected(shape, q[i:i + 1], keys[5][:129 - i % 3], lse[i:i + 1], False)
+        _close(got[i], want, tol)
+
+
+@pytest.mark.gpu
+def test_captured_and_replayed():
+    shape = synth.CFG2
+    gen = synth.generator(9, stream=4)
+    n, T = 700, 20
+    pool, sid, k = _session(shape, gen, n, 16)
+    q = synth.draw(gen, (T, 32, 128), "bf16").cuda()
+    lse = torch.zeros((T, 32), device="cuda")
+    mass = torch.zeros((8, n), device="cuda")
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        pool.sk_session_attention_mass(sid, q, lse, mass_in=mass, keep=0.5)
+    torch.cuda.synchronize()
+    want = torch.zeros_like(mass)
+    for _ in range(4):
+        x = synth.draw(gen, (T, 32, 128), "bf16")
+        q.copy_(x.cuda())
+        lse.copy_(_lse(shape, gen, x, k, False).cuda())
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        pool.sk_session_attention_mass(sid, q, lse, mass_in=want, keep=0.5)
+        torch.cuda.synchronize()
+        assert torch.equal(mass, want)
+
+
+@pytest.mark.gpu
+def test_another_scale_and_arrays_between_each_other():
+    """Rows of several sessions' sums in one tensor [Hkv][sessions][capacity]; a pool with a softmax scale of its own."""
+    gen = synth.generator(9, stream=5)
+    shape = synth.Shape("bf16", 8, 4, 64)
+    pool = sk.Pool("bf16", 8, 4, 64, 16, 64, max_sessions=2, softmax_scale=0.3)
+    all_mass = torch.zeros((4, 2, 40), device="cuda")
+    sids, keys = [], []
+    for n in (40, 33):
+        sids.append(pool.sk_session_create())
+        _, k, v = synth.draw_qkv(gen, n, shape)
+        pool.sk_session_append(sids[-1], None, k.cuda(), v.cuda())
+        keys.append(k)
+    q = synth.draw(gen, (2, 8, 64), "bf16")
+    lse = torch.cat([_lse(shape, gen, q[i:i + 1], keys[i], False, 0.3) for i in range(2)])
+    views = [all_mass[:, i] for i in range(2)]
+    pool.sk_batch_attention_mass(sids, [0, 1, 2], q.cuda(), lse.cuda(), mass_in=views)
+    torch.cuda.synchronize()
+    for i, n in enumerate((40, 33)):
+        want, tol = _expected(shape, q[i:i + 1], keys[i], lse[i:i + 1], False, 0.3)
+        _close(all_mass[:, i, :n], want, tol)
+    assert (all_mass[:, 1, 33:] == 0).all()
+
+
+def _refusals(pool, sid, other, device):
+    """Statuses of calls on a session of 40 tokens (2 KV heads); `other` is an empty one."""
+    import ctypes
+    L = sk.lib()
+    P, I64 = ctypes.c_void_p, ctypes.c_int64
+    a = 1 << 20                                               # addresses that a refused call does not use
+    good = dict(id=sid, q=a, lse=a, T=3, causal=0, i=a, si=64, keep=1.0, o=a, so=64)
+
+    def call(**kw):
+        x = {**good, **kw}
+        return L.sk_session_attention_mass(pool.h, x["id"], x["q"], x["lse"], x["T"], x["causal"], x["i"], x["si"], x["keep"], x["o"], x["so"], None)
+
+    assert call(id=9) == sk.SK_E_BADSESSION and call(T=-1) == sk.SK_E_INVAL and call(T=41, causal=1) == sk.SK_E_INVAL
+    assert L.sk_session_attention_mass(None, 0, a, a, 1, 0, None, 0, 1.0, a, 64, None) == sk.SK_E_INVAL
+    if device:
+        for bad in (dict(q=None), dict(lse=None), dict(o=None), dict(q=a + 8), dict(lse=a + 4), dict(i=a + 2), dict(o=a + 1), dict(so=39), dict(si=39),
+                    dict(i=a + 4 * 30), dict(i=a - 4), dict(so=65), dict(i=a + 64 * 4 * 1)):
+            assert call(**bad) == sk.SK_E_INVAL, bad
+        assert call(T=5000) == sk.SK_E_WORKSPACE
+    else:
+        assert call() == sk.SK_E_NODEVICE
+
+    def batch(ids, cu, **kw):
+        n = len(ids)
+        x = {"q": a, "lse": a, "o": [a * (i + 1) for i in range(n)], **kw}
+        return L.sk_batch_attention_mass(pool.h, n, (ctypes.c_int32 * n)(*ids), None, (ctypes.c_int32 * (n + 1))(*cu), x["q"], x["lse"], None, None, 1.0,
+                                         (P * n)(*x["o"]), (I64 * n)(*[64] * n), None)
+
+    assert batch([sid, 7], [0, 1, 2]) == sk.SK_E_BADSESSION and batch([sid, sid], [0, 1, 2]) == sk.SK_E_INVAL
+    assert batch([sid, other], [0, 2, 1]) == sk.SK_E_INVAL and batch([sid, other], [1, 2, 3]) == sk.SK_E_INVAL
+    assert batch([sid], [0, 1]) == sk.SK_E_NODEVICE if not device else batch([sid], [0, 1], o=[None]) == sk.SK_E_INVAL
+    assert L.sk_batch_attention_mass(pool.h, 0, None, None, None, None, None, None, None, 1.0, None, None, None) == sk.SK_OK
+    assert L.sk_batch_attention_mass(pool.h, 1, None, None, None, None, None, None, None, 1.0, None, None, None) == sk.SK_E_INVAL
+    assert L.sk_batch_attention_mass(pool.h, -1, None, None, None, None, None, None, None, 1.0, None, None, None) == sk.SK_E_INVAL
+
+
+def test_refusals_without_a_gpu():
+    pool = sk.Pool("bf16", 4, 2, 64, 16, 16, max_sessions=3, metadata_only=True)
+    sid, other = pool.sk_session_create(), pool.sk_session_create()
+    pool.reserve(sid, 40)
+    _refusals(pool, sid, other, False)
+
+
+@pytest.mark.gpu
+def test_refusals():
+    pool = sk.Pool("bf16", 4, 2, 64, 16, 16, max_sessions=3)
+    sid, other = pool.sk_session_create(), pool.sk_session_create()
+    x = torch.zeros((40, 2, 64), dtype=torch.bfloat16, device="cuda")
+    pool.sk_session_append(sid, None, x, x)
+    _refusals(pool, sid, other, True)
+    # an empty session: nothing to do
+    assert sk.lib().sk_session_attention_mass(pool.h, other, None, None, 0, 0, None, 0, 1.0, None, 0, None) == sk.SK_OK
+    torch.cuda.synchronize()
