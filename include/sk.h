@@ -282,6 +282,29 @@ int sk_batch_attention_mass(sk_pool* pool, int32_t n_items, const int32_t* sessi
                             float* const* mass_out, const int64_t* mass_out_stride, void* hip_stream);
 
 /*
+ * EVICTION BY WEIGHT: like sk_session_evict_oldest a way to hold a session to a budget (Alg. 1, the capacity check in front of the
+ * append), but what leaves is what the rows since have looked at least.  Of the retained tokens that are neither frozen nor
+ * among the n_recent newest, the n_evict of lowest mass_in leave; equal sums: the older token first; a NaN counts as larger than
+ * any number.  per_head != 0: every KV head by its own row of mass_in, so that token j of the session is another one for each head
+ * (their number is the same: the session has one length); per_head == 0: the same tokens for all heads, by the sum of the rows,
+ * added in fp32 in the order of the heads.  The others keep their order and move together, K and V bit for bit, in front of
+ * them the frozen tokens; sk_session_length falls by n_evict, blocks behind the new end return to the free list, and positions are the
+ * caller's concern as for sk_session_evict_oldest.
+ * mass_in, mass_out: DEVICE float [Hkv][stride] as sk_session_attention_mass keeps them (4-byte aligned, strides at least the length).
+ * mass_out[g][j] receives the sums of the tokens that stay, in their new places, and 0 in the n_evict places behind the new end.
+ * It may be mass_in (same pointer and stride; no other overlap) or NULL (the caller keeps no sums).
+ * A block that another session holds too is not written: what stays of it goes to a block from the free list (SK_E_NOMEM if they do not
+ * suffice; a session that shares none needs none).  More than there are to choose from: SK_E_INVAL.  SK_E_WORKSPACE if the lists of what stays
+ * (about 4 bytes a token and KV head, 8 bytes a token with per_head == 0) exceed the part of the workspace that holds split partials
+ * (at least 134 MB for 128 dims, 67 MB for 64).
+ * All or nothing.  Kernels only, ordered on hip_stream like the session's other calls; host metadata change with every call, so a
+ * capture of it cannot be replayed.  On a metadata-only pool the host half alone runs.
+ */
+int sk_session_evict_lowest(sk_pool* pool, int32_t id, const float* mass_in, int64_t mass_in_stride,
+                            int64_t n_evict, int64_t n_recent, int32_t per_head,
+                            float* mass_out, int64_t mass_out_stride, void* hip_stream);
+
+/*
  * FORK (Sec. 3.7 prefix-aware grouped prefill: followers alias the leader's state; Sec. 3.10
  * metadata-only sequence aliasing).  Creates a session whose cache is the first n_prefix retained
  * tokens of session src (including src's frozen region and evicted range as far as the prefix
@@ -424,7 +447,8 @@ enum { SK_SITE_NONE = 0, SK_SITE_RING = 1,   /* waiting for a pinned upload slot
        SK_SITE_UPLOAD = 2,                   /* host-to-device copy of a list or block table */
        SK_SITE_BLOCK_COPY = 3,               /* copy of a shared or partly filled block */
        SK_SITE_SCATTER = 4, SK_SITE_ATTENTION = 5, SK_SITE_COMBINE = 6,   /* kernel launches */
-       SK_SITE_PLAN = 7 };                   /* the lists of a batched call do not fit */
+       SK_SITE_PLAN = 7,                     /* the lists of a batched call do not fit */
+       SK_SITE_EVICT_SELECT = 8, SK_SITE_EVICT_MOVE = 9 };      /* kernel launches of sk_session_evict_lowest */
 int sk_pool_inject_failure(sk_pool* pool, int32_t site, int32_t countdown);
 
 const char* sk_strerror(int status);     /* static storage */

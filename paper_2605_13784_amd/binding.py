@@ -16,6 +16,7 @@ SK_OP_APPEND, SK_OP_QUERY_A, SK_OP_QUERY_B = 0, 1, 2
 SK_POOL_METADATA_ONLY = 1
 
 SK_SITE_RING, SK_SITE_UPLOAD, SK_SITE_BLOCK_COPY, SK_SITE_SCATTER, SK_SITE_ATTENTION, SK_SITE_COMBINE, SK_SITE_PLAN = 1, 2, 3, 4, 5, 6, 7
+SK_SITE_EVICT_SELECT, SK_SITE_EVICT_MOVE = 8, 9
 SK_TOP2_STATIC_BYTES = 1 << 20
 SK_LOGPROBS_MAX_TOP, SK_LOGPROBS_MAX_ROWS, SK_LOGPROBS_MAX_VOCAB = 32, 1 << 20, 1 << 21
 
@@ -70,7 +71,7 @@ EXPORTS = [
     "sk_pool_set_profiling", "sk_pool_read_profile",
     "sk_pool_element_offset", "sk_pool_get_stats", "sk_pool_last_launch", "sk_strerror",
     "sk_last_hip_error", "sk_version", "sk_top2_workspace_bytes", "sk_top2", "sk_top2_static",
-    "sk_session_attention_mass", "sk_batch_attention_mass",
+    "sk_session_evict_lowest", "sk_session_attention_mass", "sk_batch_attention_mass",
     "sk_logprobs_workspace_bytes", "sk_logprobs",
     "sk_pool_inject_failure", "sk_probe_read", "sk_probe_mfma",
 ]
@@ -121,6 +122,7 @@ def lib():
     L.sk_top2_workspace_bytes.argtypes = [i32, i32]
     L.sk_top2.argtypes = [vp, i32, i32, i64, vp, ctypes.c_size_t, vp, vp, vp, vp, vp, vp]
     L.sk_top2_static.argtypes = [vp, i32, i32, i64, vp, vp, vp, vp, vp, vp]
+    L.sk_session_evict_lowest.argtypes = [vp, i32, vp, i64, i64, i64, i32, vp, i64, vp]
     L.sk_session_attention_mass.argtypes = [vp, i32, vp, vp, i32, i32, vp, i64, ctypes.c_float, vp, i64, vp]
     L.sk_batch_attention_mass.argtypes = [vp, i32, P(i32), P(i32), P(i32), vp, vp, P(vp), P(i64), ctypes.c_float, P(vp), P(i64), vp]
     L.sk_logprobs_workspace_bytes.restype = ctypes.c_size_t
@@ -390,6 +392,18 @@ class Pool:
         po, so = self._mass(mass_out, n)
         _ck(lib().sk_session_attention_mass(self.h, sid, _p(q), _p(lse), 0 if q is None else q.shape[0], int(bool(causal)), pi, si, keep, po, so,
                                             _stream(stream)), "sk_session_attention_mass")
+        return mass_out
+
+    def sk_session_evict_lowest(self, sid, mass_in, n_evict, n_recent=0, per_head=True, mass_out=None, stream=None):
+        """mass_in: float32 [Hkv, capacity]; the sums of what stays go to mass_out, left out: mass_in in place.  Metadata-only pools:
+        mass_in None."""
+        pi, si, po, so = None, 0, None, 0
+        if self.kv_mem is not None:
+            n = self.sk_session_length(sid)
+            mass_out = mass_in if mass_out is None else mass_out
+            (pi, si), (po, so) = self._mass(mass_in, n), self._mass(mass_out, n)
+        _ck(lib().sk_session_evict_lowest(self.h, sid, pi, si, int(n_evict), int(n_recent), int(bool(per_head)), po, so,
+                                          _stream(stream) if self.kv_mem is not None else None), "sk_session_evict_lowest")
         return mass_out
 
     def sk_batch_attention_mass(self, session_ids, cu_tokens, q, lse, causal=None, mass_in=None, keep=1.0, mass_out=None, stream=None):

@@ -185,9 +185,43 @@ struct sk_session_view {
     int64_t frozen, win;
 };
 int sk_view_session(const sk_pool* p, int32_t id, sk_session_view* out);     // SK_OK | SK_E_INVAL | SK_E_BADSESSION
+// An eviction by weight, host side (sk_pool.cpp): sk_evict_begin checks and plans it and changes nothing, sk_evict_end carries it out
+// once its kernels are on the stream.  Storage indices as in sk_pool.cpp: the tokens behind the frozen ones lie at [win, len).
+struct sk_evict {
+    sk_session_view v;
+    int32_t id;
+    int64_t len, new_len;     // storage end before and behind
+    int64_t n_evict, n_cand;  // tokens that leave, and among how many of [win, len), from win on, they are looked for
+    int64_t first;            // storage index from which slots are written again: the start of a 16-token group, of a block if that is shared
+    int64_t blk0, n_blk;      // blocks that hold [first, new_len): their entries of the table
+    int64_t n_fresh;          // of those, how many another session holds too: they are written to blocks from the free list
+    const int32_t* table;     // pinned: the n_blk entries as they will be (n_fresh > 0, device pools)
+    int slot;
+    unsigned char* scratch;   // device memory that no other call of the pool is using (its split partials)
+    size_t scratch_bytes;
+    int32_t* tables_rw;
+    unsigned char* kv_rw;
+};
+int sk_evict_begin(sk_pool* p, int32_t id, int64_t n_evict, int64_t n_recent, sk_evict* out);
+void sk_evict_listed(sk_pool* p, const sk_evict& e, void* stream);           // a kernel that reads e.table is on the stream
+void sk_evict_undo(sk_pool* p, const sk_evict& e, void* stream);             // its kernels will not all run: the device table as it was
+void sk_evict_end(sk_pool* p, const sk_evict& e);
+bool sk_injected(sk_pool* p, int site);                                      // sk_pool_inject_failure
+
 bool sk_sessions_differ(sk_pool* p, int32_t n, const int32_t* id);           // ids of live sessions
 int sk_note_hip_error(int hip_error);                                        // for sk_last_hip_error; returns SK_E_HIP
 void sk_count_launch(sk_pool* p);
+
+// Whether arrays of `rows` rows of n floats meet other than in the same place, for a call's arrays of sums that it reads and write.
+static inline bool sk_rows_overlap(const float* a, int64_t stride_a, const float* b, int64_t stride_b, int64_t rows, int64_t n)
+{
+    if (a == b && stride_a == stride_b) return false;
+    const int64_t d = b - a;
+    if (d >= (rows - 1) * stride_a + n || -d >= (rows - 1) * stride_b + n) return false;
+    if (stride_a != stride_b) return true;
+    const int64_t m = ((d % stride_a) + stride_a) % stride_a;      // rows of one array between those of the other
+    return m < n || stride_a - m < n;
+}
 
 // Launchers implemented in sk_kernels.hip (return hipError_t as int).
 int sk_launch_scatter(const sk_geom& g, const void* k, const void* v, const sk_scatter* items,

@@ -196,17 +196,6 @@ struct Call {
     const int64_t* out_stride;
 };
 
-// Whether arrays of `rows` rows of n floats meet other than in the same place.
-bool overlap(const float* a, int64_t stride_a, const float* b, int64_t stride_b, int64_t rows, int64_t n)
-{
-    if (a == b && stride_a == stride_b) return false;
-    const int64_t d = b - a;
-    if (d >= (rows - 1) * stride_a + n || -d >= (rows - 1) * stride_b + n) return false;
-    if (stride_a != stride_b) return true;
-    const int64_t m = ((d % stride_a) + stride_a) % stride_a;      // rows of one array between those of the other
-    return m < n || stride_a - m < n;
-}
-
 int check(sk_pool* p, const Call& C)
 {
     if (C.cu_tokens[0] != 0) return SK_E_INVAL;
@@ -220,7 +209,7 @@ int check(sk_pool* p, const Call& C)
         if (n == 0) continue;
         if (!C.out[i] || (uintptr_t)C.out[i] & 3 || C.out_stride[i] < n) return SK_E_INVAL;
         if (C.in && C.keep != 0.f && (!C.in[i] || (uintptr_t)C.in[i] & 3 || C.in_stride[i] < n ||
-                                      overlap(C.in[i], C.in_stride[i], C.out[i], C.out_stride[i], V.g.Hkv, n))) return SK_E_INVAL;
+                                      sk_rows_overlap(C.in[i], C.in_stride[i], C.out[i], C.out_stride[i], V.g.Hkv, n))) return SK_E_INVAL;
         if (T > 0 && (!C.q || !C.lse || ((uintptr_t)C.q | (uintptr_t)C.lse) & 15)) return SK_E_INVAL;
     }
     if (!sk_sessions_differ(p, C.n_items, C.session_id)) return SK_E_INVAL;

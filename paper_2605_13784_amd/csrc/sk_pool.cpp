@@ -1364,6 +1364,79 @@ bool sk_sessions_differ(sk_pool* p, int32_t n, const int32_t* id)
     return true;
 }
 
+bool sk_injected(sk_pool* p, int site) { return inject(p, site); }
+
+int sk_evict_begin(sk_pool* p, int32_t id, int64_t n_evict, int64_t n_recent, sk_evict* out)
+{
+    sk_evict& e = *out;
+    const int rc = sk_view_session(p, id, &e.v);
+    if (rc) return rc;
+    const Session& s = p->sessions[(size_t)id];
+    const int64_t B = p->d.block_tokens, m = s.len - s.win;
+    if (n_evict < 0 || n_recent < 0 || n_evict > m - std::min(n_recent, m)) return SK_E_INVAL;
+    e.id = id;
+    e.len = s.len; e.new_len = s.len - n_evict; e.n_evict = n_evict; e.n_cand = m - std::min(n_recent, m);
+    e.n_fresh = 0; e.table = nullptr; e.slot = 0;
+    // Which tokens leave is known on the device only: every slot from win on may be written again, and a block of those that another
+    // session holds too is replaced.
+    e.blk0 = s.win / B;
+    e.n_blk = std::max<int64_t>(0, (e.new_len + B - 1) / B - e.blk0);
+    if (n_evict > 0)
+        for (int64_t b = 0; b < e.n_blk; ++b) e.n_fresh += p->refcnt[(size_t)s.blocks[size_t(e.blk0 + b)]] > 1;
+    if (e.n_fresh > (int64_t)p->free_blocks.size()) return SK_E_NOMEM;
+    e.first = s.win / 16 * 16;
+    if (e.n_fresh > 0 && p->refcnt[(size_t)s.blocks[(size_t)e.blk0]] > 1) e.first = e.blk0 * B;
+    unsigned char* ws = (unsigned char*)p->d.workspace;
+    e.scratch = p->device ? ws + p->L.off_part_ml : nullptr;
+    e.scratch_bytes = p->L.off_eph - p->L.off_part_ml;
+    e.tables_rw = p->device ? (int32_t*)(ws + p->L.off_tables) : nullptr;
+    e.kv_rw = (unsigned char*)p->d.kv_mem;
+    if (e.n_fresh > 0) {
+        unsigned char* host;
+        const int rc2 = ring_acquire(p, &e.slot, &host);
+        if (rc2) return rc2;
+        size_t next = 0;
+        if (host)
+            for (int64_t b = 0; b < e.n_blk; ++b) {
+                const int32_t blk = s.blocks[size_t(e.blk0 + b)];
+                ((int32_t*)host)[b] = p->refcnt[(size_t)blk] > 1 ? p->free_blocks[next++] : blk;
+            }
+        e.table = (const int32_t*)host;
+    }
+    return SK_OK;
+}
+
+void sk_evict_listed(sk_pool* p, const sk_evict& e, void* stream) { if (e.table) ring_busy(p, e.slot, (hipStream_t)stream); }
+
+void sk_evict_undo(sk_pool* p, const sk_evict& e, void* stream)
+{
+    if (!e.table) return;
+    const std::vector<int32_t>& blocks = p->sessions[(size_t)e.id].blocks;
+    (void)hipMemcpyAsync(e.tables_rw + e.v.tbl_off + e.blk0, blocks.data() + e.blk0, size_t(e.n_blk) * 4, hipMemcpyHostToDevice, (hipStream_t)stream);
+    (void)hipStreamSynchronize((hipStream_t)stream);      // (from memory that is not pinned)
+}
+
+void sk_evict_end(sk_pool* p, const sk_evict& e)
+{
+    Session& s = p->sessions[(size_t)e.id];
+    if (e.n_fresh > 0)
+        for (int64_t b = 0; b < e.n_blk; ++b) {
+            int32_t& blk = s.blocks[size_t(e.blk0 + b)];
+            if (p->refcnt[(size_t)blk] <= 1) continue;
+            p->refcnt[(size_t)blk]--;                     // still held by the others
+            blk = p->free_blocks.front();
+            p->free_blocks.pop_front();
+            p->refcnt[(size_t)blk] = 1;
+            p->blocks_in_use++;
+        }
+    s.len = e.new_len;
+    while ((int64_t)s.blocks.size() > e.blk0 + e.n_blk) {
+        release_block(p, s.blocks.back());
+        s.blocks.pop_back();
+    }
+    p->stats.tokens_evicted += e.n_evict;
+}
+
 int sk_note_hip_error(int e) { g_last_hip = e; return SK_E_HIP; }
 void sk_count_launch(sk_pool* p) { p->stats.launches++; }
 
@@ -2016,7 +2089,7 @@ int sk_session_fork(sk_pool* p, int32_t src_id, int64_t n_prefix, int32_t* out_i
 
 int sk_pool_inject_failure(sk_pool* p, int32_t site, int32_t countdown)
 {
-    if (!p || site < 0 || site > SK_SITE_PLAN || countdown < 0) return SK_E_INVAL;
+    if (!p || site < 0 || site > SK_SITE_EVICT_MOVE || countdown < 0) return SK_E_INVAL;
     p->inject_site = countdown > 0 ? site : 0;
     p->inject_countdown = countdown;
     return SK_OK;

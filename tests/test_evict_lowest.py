@@ -1,0 +1,352 @@
+"""sk_session_evict_lowest: which tokens leave (by sum, then by age), that the others are there bit for bit and in order, what
+becomes of blocks, forks and sums, and attention over what is left.  Everything but that last part is exact."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import oracle
+import paper_2605_13784_amd as sk
+from gpu_common import compare
+from workloads import synth
+
+D64 = synth.Shape("bf16", 8, 4, 64)
+ODD = synth.Shape("bf16", 6, 3, 128)
+F32_WIDE = synth.Shape("f32", 4, 2, 128)
+
+
+class Model:
+    """What the session holds, by hand: K and V [n][Hkv][d] as raw bits (row j is every head's own j-th token), sums [Hkv][n]."""
+
+    def __init__(self, shape, k, v, frozen=0):
+        self.shape, self.K, self.V, self.frozen = shape, k, v, frozen
+
+    def evict(self, mass, n_evict, n_recent, per_head):
+        n, hkv = self.K.shape[0], self.shape.n_kv_heads
+        m = n - n_evict
+        last = max(n - n_recent, self.frozen)
+        rows = mass
+        if not per_head:
+            total = mass[0].copy()
+            for g in range(1, hkv):
+                total = total + mass[g]                    # fp32, head by head
+            rows = np.repeat(total[None], hkv, 0)
+        K, V, out = np.empty_like(self.K[:m]), np.empty_like(self.V[:m]), np.zeros_like(mass)
+        for g in range(hkv):
+            gone = self.frozen + np.argsort(rows[g, self.frozen:last], kind="stable")[:n_evict]
+            left = np.delete(np.arange(n), gone)
+            K[:, g], V[:, g], out[g, :m] = self.K[left, g], self.V[left, g], mass[g, left]
+        self.K, self.V = K, V
+        return out
+
+
+def _check(pool, sid, model):
+    assert pool.sk_session_length(sid) == model.K.shape[0]
+    if model.K.shape[0]:
+        k, v = pool.sk_session_gather(sid)
+        torch.cuda.synchronize()
+        np.testing.assert_array_equal(synth.to_raw(k.cpu()), model.K)
+        np.testing.assert_array_equal(synth.to_raw(v.cpu()), model.V)
+
+
+def _attend(pool, sid, model, gen, T=5):
+    """A query over what is left, against the oracle."""
+    shape = model.shape
+    q = synth.draw(gen, (T, shape.n_q_heads, shape.head_dim), shape.dtype)
+    out, lse = pool.sk_session_query(sid, q.cuda())
+    ro, rl = oracle.attention(shape.dtype, synth.to_raw(q), model.K, model.V, None, None, None, shape.n_q_heads, shape.n_kv_heads, shape.head_dim,
+                              shape.head_dim ** -0.5)
+    compare("query", out, lse, ro, rl, shape.dtype)
+
+
+def _make(shape, gen, n, block, frozen=0, evicted=0, spare=9, max_sessions=3):
+    blocks = -(-(n + evicted) // block) + spare
+    pool = sk.Pool(shape.dtype, shape.n_q_heads, shape.n_kv_heads, shape.head_dim, block, blocks, max_sessions=max_sessions, max_batch_tokens=8192, kv_fill=0xFF)
+    pool.sk_pool_set_alloc_order(synth.permutation(gen, blocks))
+    sid = pool.sk_session_create()
+    _, k, v = synth.draw_qkv(gen, n + evicted, shape)
+    for t in range(0, n + evicted, 8192):
+        pool.sk_session_append(sid, None, k[t:t + 8192].cuda(), v[t:t + 8192].cuda())
+    if frozen:
+        pool.sk_session_freeze(sid, frozen)
+    if evicted:
+        pool.sk_session_evict_oldest(sid, evicted)
+    k, v = (synth.to_raw(torch.cat([x[:frozen], x[frozen + evicted:]])) for x in (k, v))
+    return pool, sid, Model(shape, k, v, frozen)
+
+
+def _mass(gen, hkv, n, kind="spread"):
+    if kind == "spread":
+        return torch.exp(1.5 * torch.randn((hkv, n), generator=gen))
+    if kind == "equal":
+        return torch.full((hkv, n), 0.25)
+    if kind == "zero":
+        return torch.zeros((hkv, n)) * torch.where(torch.arange(n) % 2 == 0, 1.0, -1.0)      # +0 and -0 are equal
+    if kind == "few":
+        return torch.randint(0, 4, (hkv, n), generator=gen).float()
+    if kind == "rising":
+        return torch.arange(n).float().repeat(hkv, 1) * 2.0 ** -10
+    if kind == "falling":
+        return -torch.arange(n).float().repeat(hkv, 1)
+    if kind == "near":                                         # differ in the last bits only
+        return (torch.full((hkv, n), 1.0).view(torch.int32) + torch.randint(0, 50, (hkv, n), generator=gen, dtype=torch.int32)).view(torch.float32)
+    assert kind == "odd"                                       # negative sums, infinities and NaN
+    x = torch.randn((hkv, n), generator=gen)
+    x[:, ::7], x[:, 3::11], x[:, 5::13] = float("nan"), float("inf"), -float("inf")
+    return x
+
+
+CASES = [(D64, 200, 16, 0, 0, 100, 0, True), (D64, 200, 16, 0, 0, 1, 0, True), (D64, 200, 16, 0, 0, 200, 0, True), (D64, 200, 16, 0, 0, 0, 0, True),
+         (D64, 1, 16, 0, 0, 1, 0, True), (D64, 17, 16, 3, 0, 5, 4, False), (D64, 333, 64, 37, 0, 63, 50, True), (D64, 333, 64, 64, 0, 64, 0, False),
+         (D64, 1000, 256, 100, 0, 65, 1000 - 100 - 65, True), (D64, 1000, 1024, 1, 0, 500, 10, True), (D64, 700, 16, 20, 35, 300, 64, True),
+         (D64, 700, 64, 0, 100, 333, 1, False), (ODD, 650, 16, 15, 3, 129, 17, True), (ODD, 1500, 64, 500, 70, 900, 100, True),
+         (synth.CFG2, 2600, 16, 0, 0, 1300, 64, True), (synth.CFG2, 4099, 16, 100, 5, 257, 300, True), (synth.CFG2, 9001, 64, 500, 1000, 4000, 333, False),
+         (synth.CFG1, 500, 16, 0, 0, 250, 10, True), (synth.CFG1, 777, 64, 33, 40, 100, 0, False), (F32_WIDE, 600, 16, 10, 20, 64, 64, True),
+         (D64, 30000, 16, 0, 0, 1000, 0, True), (D64, 30000, 256, 1234, 77, 15000, 5000, True), (D64, 40000, 16, 0, 0, 39000, 0, False)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape,n,block,frozen,evicted,n_evict,n_recent,per_head", CASES)
+def test_what_leaves_and_what_stays(shape, n, block, frozen, evicted, n_evict, n_recent, per_head):
+    gen = synth.generator(10, stream=n + n_evict)
+    pool, sid, model = _make(shape, gen, n, block, frozen, evicted)
+    mass = _mass(gen, shape.n_kv_heads, n + 3)
+    place = mass.cuda()
+    free = pool.sk_pool_blocks_free()
+    held = len(pool.sk_session_block_table(sid))
+    want = model.evict(mass[:, :n].numpy(), n_evict, n_recent, per_head)
+    assert pool.sk_session_evict_lowest(sid, place, n_evict, n_recent, per_head) is place
+    torch.cuda.synchronize()
+    np.testing.assert_array_equal(place[:, :n].cpu().numpy(), want)
+    assert torch.equal(place[:, n:].cpu(), mass[:, n:])
+    _check(pool, sid, model)
+    assert held - len(pool.sk_session_block_table(sid)) == pool.sk_pool_blocks_free() - free >= n_evict // block
+    if n > n_evict:
+        _attend(pool, sid, model, gen)
+    # it goes on: tokens are appended, and some leave again
+    q, k, v = synth.draw_qkv(gen, 100 if n < 20000 else 40, shape)
+    model.K, model.V = np.concatenate([model.K, synth.to_raw(k)]), np.concatenate([model.V, synth.to_raw(v)])
+    pool.sk_session_append(sid, q.cuda(), k.cuda(), v.cuda())
+    n2 = model.K.shape[0]
+    mass = _mass(gen, shape.n_kv_heads, n2, "few")
+    more = min(n2 - frozen, 37)
+    want = model.evict(mass.numpy(), more, 0, not per_head)
+    out = pool.sk_session_evict_lowest(sid, mass.cuda(), more, 0, not per_head, mass_out=torch.full((shape.n_kv_heads, n2 + 1), -1.0, device="cuda"))
+    torch.cuda.synchronize()
+    np.testing.assert_array_equal(out[:, :n2].cpu().numpy(), want)
+    assert (out[:, n2:] == -1.0).all()
+    _check(pool, sid, model)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("per_head", [True, False])
+@pytest.mark.parametrize("kind", ["equal", "zero", "few", "rising", "falling", "near", "odd"])
+@pytest.mark.parametrize("n", [90, 3000])
+def test_orders_of_sums(n, kind, per_head):
+    gen = synth.generator(10, stream=n)
+    pool, sid, model = _make(D64, gen, n, 16, 11)
+    mass = _mass(gen, 4, n, kind)
+    before = mass.cuda()
+    with np.errstate(invalid="ignore"):
+        want = model.evict(mass.numpy(), n // 3, 7, per_head)
+    out = pool.sk_session_evict_lowest(sid, before, n // 3, 7, per_head, mass_out=torch.empty_like(before))
+    torch.cuda.synchronize()
+    np.testing.assert_array_equal(out.cpu().numpy(), want)
+    _check(pool, sid, model)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape,block,frozen,evicted,prefix", [(D64, 16, 0, 0, 500), (D64, 64, 100, 70, 391), (synth.CFG2, 16, 37, 0, 320), (F32_WIDE, 16, 10, 20, 333)])
+def test_forks_keep_what_they_share(shape, block, frozen, evicted, prefix):
+    """A fork is cut, then its source, then the fork again: blocks that both hold are replaced and never written."""
+    gen = synth.generator(10, stream=prefix)
+    n = 500
+    pool, a, model = _make(shape, gen, n, block, frozen, evicted, spare=2 * (n // block + 3))
+    b = pool.sk_session_fork(a, prefix)
+    other = Model(shape, model.K[:prefix], model.V[:prefix], min(frozen, prefix))
+    for sid, mine, n_evict in ((b, other, 200), (a, model, 150), (b, other, 30), (a, model, 1)):
+        mass = _mass(gen, shape.n_kv_heads, mine.K.shape[0])
+        want = mine.evict(mass.numpy(), n_evict, 20, True)
+        place = mass.cuda()
+        pool.sk_session_evict_lowest(sid, place, n_evict, 20)
+        torch.cuda.synchronize()
+        np.testing.assert_array_equal(place.cpu().numpy(), want)
+        _check(pool, a, model)
+        _check(pool, b, other)
+        _attend(pool, sid, mine, gen)
+    pool.sk_session_destroy(a)
+    _check(pool, b, other)
+    pool.sk_session_destroy(b)
+    assert pool.sk_pool_blocks_free() == pool.desc.n_blocks
+
+
+@pytest.mark.gpu
+def test_stream_held_to_a_budget():
+    """The operators as they are used together: append, its weights, a question, its weights and log probabilities, eviction down
+    to the budget; the model follows with the sums that the library reports."""
+    shape = synth.CFG2
+    gen = synth.generator(10, stream=5)
+    pool, sid, model = _make(shape, gen, 64, 16, spare=80)
+    pool.sk_session_freeze(sid, 16)
+    model.frozen = 16
+    mass = torch.zeros((8, 1200), device="cuda")
+    head = torch.randn((32 * 128, 1000), generator=gen).cuda()
+    for step, L in enumerate([300, 77, 256, 1, 130, 300]):
+        q, k, v = synth.draw_qkv(gen, L, shape)
+        out, lse = pool.sk_session_append(sid, q.cuda(), k.cuda(), v.cuda())
+        model.K, model.V = np.concatenate([model.K, synth.to_raw(k)]), np.concatenate([model.V, synth.to_raw(v)])
+        pool.sk_session_attention_mass(sid, q.cuda(), lse, causal=True, mass_in=mass, keep=0.9)
+        q = synth.draw(gen, (9, 32, 128), "bf16")
+        out, lse = pool.sk_session_query(sid, q.cuda())
+        pool.sk_session_attention_mass(sid, q.cuda(), lse, mass_in=mass)
+        logits = out.view(9, -1) @ head
+        logprob, _, entropy, top, top_logprob = sk.sk_logprobs(logits, n_top=3)
+        i1, i2, _, _, gap = sk.sk_top2(logits)
+        torch.cuda.synchronize()
+        assert torch.equal(top[:, 0], i1) and torch.equal(top[:, 1], i2) and (entropy >= 0).all()
+        n = model.K.shape[0]
+        # both calls' rows give every KV head a weight of one each (to the library's 1e-3 in lse)
+        if n > 500:
+            sums = mass[:, :n].cpu().numpy().copy()
+            want = model.evict(sums, n - 500, 64, step % 2 == 0)
+            pool.sk_session_evict_lowest(sid, mass, n - 500, 64, step % 2 == 0)
+            torch.cuda.synchronize()
+            np.testing.assert_array_equal(mass[:, :n].cpu().numpy(), want)
+            assert (mass[:, 500:] == 0).all()
+        _check(pool, sid, model)
+        _attend(pool, sid, model, gen, 33)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("site", [sk.SK_SITE_RING, sk.SK_SITE_EVICT_SELECT, sk.SK_SITE_EVICT_MOVE])
+def test_call_that_fails_on_the_device_leaves_the_session(site):
+    gen = synth.generator(10, stream=6)
+    pool, a, model = _make(D64, gen, 300, 16, spare=40)
+    b = pool.sk_session_fork(a, 300)
+    mass = _mass(gen, 4, 300)
+    place = mass.cuda()
+    free = pool.sk_pool_blocks_free()
+    pool.sk_pool_inject_failure(site, 1)
+    with pytest.raises(sk.SkError) as e:
+        pool.sk_session_evict_lowest(b, place, 100)
+    assert e.value.status == sk.SK_E_HIP
+    torch.cuda.synchronize()
+    assert torch.equal(place.cpu(), mass) and pool.sk_pool_blocks_free() == free
+    _check(pool, a, model)
+    _check(pool, b, model)
+    other = Model(D64, model.K, model.V)
+    other.evict(mass.numpy(), 100, 0, True)
+    pool.sk_session_evict_lowest(b, place, 100)
+    _check(pool, b, other)
+    _check(pool, a, model)
+
+
+# ---- host half, without a GPU ---------------------------------------------------------------------------
+
+def _meta(**kw):
+    args = dict(dtype="bf16", n_q_heads=8, n_kv_heads=4, head_dim=64, block_tokens=16, n_blocks=64, max_sessions=4, metadata_only=True)
+    return sk.Pool(**{**args, **kw})
+
+
+def _state(p, sids):
+    return [(p.sk_session_length(s), p.sk_session_block_table(s)) for s in sids], p.sk_pool_blocks_free()
+
+
+def test_host_half_and_refusals_without_a_gpu():
+    p = _meta()
+    a = p.sk_session_create()
+    p.reserve(a, 200)
+    p.sk_session_freeze(a, 30)
+    free = p.sk_pool_blocks_free()
+    before = _state(p, [a])
+    for n_evict, n_recent in ((171, 0), (100, 71), (1, 170), (1, 500), (-1, 0), (1, -1)):
+        with pytest.raises(sk.SkError) as e:
+            p.sk_session_evict_lowest(a, None, n_evict, n_recent)
+        assert e.value.status == sk.SK_E_INVAL
+    with pytest.raises(sk.SkError) as e:
+        p.sk_session_evict_lowest(3, None, 0)
+    assert e.value.status == sk.SK_E_BADSESSION
+    assert sk.lib().sk_session_evict_lowest(None, 0, None, 0, 0, 0, 0, None, 0, None) == sk.SK_E_INVAL
+    assert _state(p, [a]) == before
+    p.sk_session_evict_lowest(a, None, 0, 500)                # nothing to evict: as it was
+    assert _state(p, [a]) == before
+    p.sk_session_evict_lowest(a, None, 100, 70)
+    assert p.sk_session_length(a) == 100 and p.sk_pool_blocks_free() == free + 6
+    assert p.sk_session_block_table(a) == before[0][0][1][:7]      # the blocks in front stay where they are
+    p.sk_session_evict_oldest(a, 20)                          # and the window goes on behind it
+    p.sk_session_evict_lowest(a, None, 50)
+    assert p.sk_session_length(a) == 30 and p.sk_pool_get_stats()["tokens_evicted"] == 170
+    with pytest.raises(sk.SkError):
+        p.sk_session_evict_lowest(a, None, 1)                 # only the frozen tokens are left
+    p.reserve(a, 5)
+    assert p.sk_session_length(a) == 35
+
+
+def test_shared_blocks_are_replaced_and_counted():
+    p = _meta(n_blocks=20)
+    a = p.sk_session_create()
+    p.reserve(a, 160)                                         # 10 blocks
+    p.sk_session_freeze(a, 40)
+    b = p.sk_session_fork(a, 155)                             # shares 9, holds a copy of the last: 9 free
+    tables = _state(p, [a, b])[0]
+    assert p.sk_pool_blocks_free() == 9
+    p.sk_session_evict_lowest(b, None, 20)                    # 135 tokens, blocks 2..8 are replaced, the last one goes
+    assert p.sk_session_length(b) == 135 and p.sk_pool_blocks_free() == 9 - 7 + 1
+    tb = p.sk_session_block_table(b)
+    assert tb[:2] == tables[0][1][:2] and not set(tb[2:]) & set(tables[0][1]) and p.sk_session_block_table(a) == tables[0][1]
+    c = p.sk_session_fork(a, 160)
+    before = _state(p, [a, b, c])
+    with pytest.raises(sk.SkError) as e:
+        p.sk_session_evict_lowest(c, None, 1)                 # 8 blocks to replace, 3 free
+    assert e.value.status == sk.SK_E_NOMEM and _state(p, [a, b, c]) == before
+    p.sk_session_evict_lowest(c, None, 80)                    # 80 left: blocks 2, 3 and 4
+    assert p.sk_pool_blocks_free() == 0
+    for s in (a, b, c):
+        p.sk_session_destroy(s)
+    assert p.sk_pool_blocks_free() == 20
+
+
+@pytest.mark.parametrize("site", [sk.SK_SITE_RING, sk.SK_SITE_EVICT_SELECT, sk.SK_SITE_EVICT_MOVE])
+def test_call_that_fails_changes_nothing(site):
+    p = _meta()
+    a = p.sk_session_create()
+    p.reserve(a, 200)
+    b = p.sk_session_fork(a, 200)
+    before = _state(p, [a, b])
+    p.sk_pool_inject_failure(site, 1)
+    with pytest.raises(sk.SkError) as e:
+        p.sk_session_evict_lowest(b, None, 50)
+    assert e.value.status == sk.SK_E_HIP and _state(p, [a, b]) == before
+    p.sk_session_evict_lowest(b, None, 50)
+    assert p.sk_session_length(b) == 150
+
+
+def test_injected_sites_end_with_the_eviction():
+    p = _meta()
+    assert sk.lib().sk_pool_inject_failure(p.h, sk.SK_SITE_EVICT_MOVE + 1, 1) == sk.SK_E_INVAL
+    assert sk.lib().sk_pool_inject_failure(p.h, -1, 1) == sk.SK_E_INVAL
+
+
+@pytest.mark.gpu
+def test_refusals():
+    pool, sid, model = _make(D64, synth.generator(10), 100, 16)
+    L, a = sk.lib(), 1 << 20                                  # an address that a refused call does not use
+    good = dict(i=a, si=128, n=10, r=0, o=a, so=128)
+
+    def call(**kw):
+        x = {**good, **kw}
+        return L.sk_session_evict_lowest(pool.h, sid, x["i"], x["si"], x["n"], x["r"], 1, x["o"], x["so"], None)
+
+    for bad in (dict(i=None), dict(i=a + 2), dict(si=99), dict(o=a + 1), dict(so=99), dict(so=129), dict(o=a + 400), dict(o=a - 4), dict(o=a + 128 * 4),
+                dict(n=101), dict(n=50, r=51), dict(n=-1), dict(r=-1)):
+        assert call(**bad) == sk.SK_E_INVAL, bad
+    _check(pool, sid, model)
+    empty = pool.sk_session_create()
+    assert L.sk_session_evict_lowest(pool.h, empty, None, 0, 0, 5, 1, None, 0, None) == sk.SK_OK
+    assert L.sk_session_evict_lowest(pool.h, empty, None, 0, 1, 0, 1, None, 0, None) == sk.SK_E_INVAL
+    # no sums kept
+    mass = _mass(synth.generator(10, stream=7), 4, 100).cuda()
+    assert L.sk_session_evict_lowest(pool.h, sid, ctypes.c_void_p(mass.data_ptr()), 100, 10, 0, 0, None, 0, ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)) == sk.SK_OK
+    model.evict(mass.cpu().numpy(), 10, 0, False)
+    _check(pool, sid, model)
