@@ -13,9 +13,11 @@
 #include <stdint.h>
 #include <limits.h>
 #include "../../include/sk.h"
-#include "sk_internal.h"
+#include "sk_order.h"
 
 namespace {
+
+using namespace sk_order;
 
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
@@ -37,42 +39,6 @@ struct Args {
     uint64_t* keys;                   // [rows][parts * kWaves][n_top]
 };
 
-__device__ __forceinline__ uint32_t rank_of(const float x)      // orders floats as unsigned numbers; -0 is +0
-{
-    const uint32_t u = __float_as_uint(x + 0.0f);
-    return u ^ (uint32_t)((int32_t)u >> 31 | INT32_MIN);
-}
-__device__ __forceinline__ float value_of(const uint32_t r)
-{
-    return __uint_as_float(r & 0x80000000u ? r ^ 0x80000000u : ~r);
-}
-constexpr uint32_t kRankNone = 0x007fffffu;       // of -inf
-
-__device__ __forceinline__ int lanes(const bool b) { return __popcll(__ballot(b)); }
-__device__ __forceinline__ int lanes_before(const uint64_t m)
-{
-    return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
-}
-__device__ __forceinline__ void wave_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); __builtin_amdgcn_wave_barrier(); }
-
-// Largest bound that at least k of the wave's numbers reach (N of them in a lane), found from the top bit down; the search ends where
-// exactly k reach it.  `hits` receives how many do.
-template <int N>
-__device__ __forceinline__ uint32_t bound_of(const uint32_t (&r)[N], const int k, int& hits)
-{
-    uint32_t t = 0;
-    hits = 64 * N;
-    for (int b = 31; b >= 0; --b) {
-        const uint32_t c = t | 1u << b;
-        int n = 0;
-#pragma unroll
-        for (int j = 0; j < N; ++j) n += lanes(r[j] >= c);
-        if (n >= k) { t = c; hits = n; }
-        if (n == k) break;
-    }
-    return t;
-}
-
 // A wave's candidates: rank << 32 | ~index, so that of equal logits the one of lower index is the larger key.
 struct Top {
     uint64_t* list;         // LDS, kList entries
@@ -82,22 +48,22 @@ struct Top {
 
     __device__ __forceinline__ void init(uint64_t* l, const int kk) { list = l; n = 0; k = kk; floor = -__builtin_inff(); floor_idx = INT_MIN; }
 
-    // Cuts the list to its k best.
+    // Cuts a list of more than k entries to its k best.
     __device__ __forceinline__ void cut(const int lane)
     {
         constexpr int N = kList / 64;
-        if (n <= k) return;
         wave_order();
         uint32_t hi[N], lo[N];
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-            const bool in = 64 * j + lane < n;
-            const uint64_t x = in ? list[64 * j + lane] : 0;
+            const uint64_t x = 64 * j + lane < n ? list[64 * j + lane] : 0;
             hi[j] = (uint32_t)(x >> 32); lo[j] = (uint32_t)x;
         }
         int hits;
         const uint32_t t = bound_of(hi, k, hits);
         uint32_t tie = 0;                                 // of equal ranks, those whose ~index reaches this
+        floor = t <= kRankNone ? -__builtin_inff() : value_of(t);
+        floor_idx = INT_MIN;                              // (what lies in front of a row has negative indices)
         if (hits > k) {
             int over = 0;
             uint32_t l[N];
@@ -106,8 +72,7 @@ struct Top {
             int h;
             tie = bound_of(l, k - over, h);
             floor_idx = (int32_t)~tie;
-        } else floor_idx = INT_MIN;                   // (what lies in front of a row has negative indices)
-        floor = t <= kRankNone ? -__builtin_inff() : value_of(t);
+        }
         int at = 0;
 #pragma unroll
         for (int j = 0; j < N; ++j) {
@@ -119,17 +84,27 @@ struct Top {
         n = at;
         wave_order();
     }
-    __device__ __forceinline__ void append(const bool add, const uint64_t key, const int lane)
+    // Adds the keys of the lanes in `m`; the caller has seen that there is room for them.
+    __device__ __forceinline__ void add(const uint64_t m, const bool mine, const uint64_t key)
     {
-        const uint64_t m = __ballot(add);
-        if (!m) return;
-        if (add) list[n + lanes_before(m)] = key;
+        if (mine) list[n + lanes_before(m)] = key;
         n += __popcll(m);
-        if (n > kList - 64) cut(lane);
     }
+    __device__ __forceinline__ bool full() const { return n > kList - 64; }
     __device__ __forceinline__ bool takes(const float x, const int32_t i) const
     {
         return x > floor || (x == floor && i < floor_idx);
+    }
+    // The smallest number that is taken among those whose indices are `first` and higher.
+    __device__ __forceinline__ float least(const int32_t first) const
+    {
+        return floor_idx <= first ? value_of(rank_of(floor) + 1) : floor;
+    }
+    // Before numbers of which at least k reach rank t are offered: none below that is among the best.
+    __device__ __forceinline__ void raise(const uint32_t t)
+    {
+        const float f = value_of(t);
+        if (t > kRankNone && f > floor) { floor = f; floor_idx = INT_MAX; }
     }
 };
 
@@ -196,70 +171,88 @@ __device__ __forceinline__ Sums wave_sums(Sums a)
     return a;
 }
 
-// The row's results from its sums and its list (the best n_top in no order, fewer where fewer logits are above -inf), by one wave.
 template <bool BF16>
-__device__ __forceinline__ void write_row(const Args& A, const int r, const Sums a, const Top& top, const int lane)
-{
-    const float log_s = logf(a.s), m = finite_or_0(a.m);
-    const bool none = a.s == 0.f;                         // nothing above -inf
-    const unsigned char* row = (const unsigned char*)A.logits + (int64_t)r * A.row_stride * (BF16 ? 2 : 4);
-    auto at = [&](const int32_t i) { return BF16 ? __uint_as_float((uint32_t)((const uint16_t*)row)[i] << 16) : ((const float*)row)[i]; };
-    auto log_p = [&](const float x) { return none ? -__builtin_inff() : (x - m) - log_s; };
-    if (lane == 0) {
-        if (A.lse) A.lse[r] = none ? -__builtin_inff() : m + log_s;
-        if (A.entropy) A.entropy[r] = none ? 0.f : log_s - a.z / a.s;
+struct Row {
+    const unsigned char* logits;
+    float m, log_s;
+    bool none;                        // nothing above -inf
+    __device__ __forceinline__ Row(const Args& A, const int r) : logits((const unsigned char*)A.logits + (int64_t)r * A.row_stride * (BF16 ? 2 : 4)) {}
+    __device__ __forceinline__ void of(const Sums a) { m = finite_or_0(a.m); log_s = logf(a.s); none = a.s == 0.f; }
+    __device__ __forceinline__ float at(const int32_t i) const
+    {
+        return BF16 ? __uint_as_float((uint32_t)((const uint16_t*)logits)[i] << 16) : ((const float*)logits)[i];
     }
-    for (int j = lane; j < A.n_tokens; j += 64) {
-        const int32_t t = A.tokens[(int64_t)r * A.n_tokens + j];
-        A.logprob[(int64_t)r * A.n_tokens + j] = t >= 0 && t < A.vocab ? log_p(at(t)) : 0.f;
-    }
-    if (A.n_top > 0) {
-        const bool in = lane < top.n;
-        const uint64_t key = in ? top.list[lane] : 0;
-        int place = 0;
-        for (int j = 0; j < top.n; ++j) place += top.list[j] > key;
-        // places that nothing above -inf fills go to the lowest indices that have none
-        const int32_t idx = (int32_t)~(uint32_t)key;
-        uint64_t taken = 0;
-        for (int j = 0; j < top.n; ++j) {
-            const uint32_t i = ~(uint32_t)top.list[j];
-            taken |= i < 64 ? uint64_t(1) << i : 0;
-        }
-        if (in) {
-            A.top_idx[(int64_t)r * A.n_top + place] = idx;
-            if (A.top_logprob) A.top_logprob[(int64_t)r * A.n_top + place] = log_p(at(idx));
-        }
-        const bool free = !(taken >> lane & 1);
-        const int fill = top.n + lanes_before(__ballot(free));
-        if (free && fill < A.n_top) {
-            A.top_idx[(int64_t)r * A.n_top + fill] = lane;
-            if (A.top_logprob) A.top_logprob[(int64_t)r * A.n_top + fill] = log_p(at(lane));
-        }
-    }
-}
+    __device__ __forceinline__ float log_p(const float x) const { return none ? -__builtin_inff() : (x - m) - log_s; }
+};
 
-// Joins the sums and lists of a workgroup's waves; the result is valid in wave 0.
-template <bool TOP>
-__device__ __forceinline__ void join_waves(Sums& a, Top& top, uint64_t (&lists)[kWaves][kList], const int wave, const int lane)
+// Joins the sums and lists (of at most 64 entries) of a workgroup's waves and writes the row's results.
+template <bool BF16, bool TOP>
+__device__ __forceinline__ void finish_row(const Args& A, const int r, Sums a, Top& top, uint64_t (&lists)[kWaves][kList], const int wave, const int lane)
 {
     __shared__ float4 stat[kWaves];
     __shared__ int count[kWaves];
-    if (TOP) top.cut(lane);
     if (lane == 0) { stat[wave] = float4{a.m, a.s, a.z, 0.f}; if (TOP) count[wave] = top.n; }
+    Row<BF16> row(A, r);
+    int32_t t = -1;
+    float x = 0.f;
+    if (wave == 1 && lane < A.n_tokens) {                 // on their way while the others arrive
+        t = A.tokens[(int64_t)r * A.n_tokens + lane];
+        if (t >= 0 && t < A.vocab) x = row.at(t);
+    }
     __syncthreads();
-    if (wave != 0) return;
-    const float4 b = stat[lane & (kWaves - 1)];
-    a = lane < kWaves ? Sums{b.x, b.y, b.z} : Sums{-__builtin_inff(), 0.f, 0.f};
-    a = wave_sums(a);
-    if (TOP) {
+    if (!TOP && wave != 1) return;
+    a = Sums{-__builtin_inff(), 0.f, 0.f};
+    float M = a.m;
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) {
-            const int n = count[w];
-            const uint64_t key = lane < n ? lists[w][lane] : 0;
-            top.append(lane < n, key, lane);
+    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, stat[w].x);
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        const Sums b = moved(Sums{stat[w].x, stat[w].y, stat[w].z}, finite_or_0(M));
+        a.s += b.s; a.z += b.z;
+    }
+    a.m = M;
+    row.of(a);
+    if (wave == 1) {
+        if (lane == 0) {
+            if (A.lse) A.lse[r] = row.none ? -__builtin_inff() : row.m + row.log_s;
+            if (A.entropy) A.entropy[r] = row.none ? 0.f : row.log_s - a.z / a.s;
         }
-        top.cut(lane);
-        wave_order();
+        for (int j = lane; j < A.n_tokens; j += 64) {
+            if (j >= 64) {
+                t = A.tokens[(int64_t)r * A.n_tokens + j];
+                if (t >= 0 && t < A.vocab) x = row.at(t);
+            }
+            A.logprob[(int64_t)r * A.n_tokens + j] = t >= 0 && t < A.vocab ? row.log_p(x) : 0.f;
+        }
+    }
+    if (!TOP) return;
+    // A key's place is the number of larger ones in all the lists.
+    const bool in = lane < top.n;
+    const uint64_t key = in ? lists[wave][lane] : 0;
+    int place = 0, n = 0;
+    for (int w = 0; w < kWaves; ++w) {
+        const int c = count[w];
+        n += c;
+#pragma unroll 4
+        for (int j = 0; j < c; ++j) place += lists[w][j] > key;
+    }
+    if (in && place < A.n_top) {
+        A.top_idx[(int64_t)r * A.n_top + place] = (int32_t)~(uint32_t)key;
+        if (A.top_logprob) A.top_logprob[(int64_t)r * A.n_top + place] = row.log_p(value_of((uint32_t)(key >> 32)));
+    }
+    if (n < A.n_top && wave == 0) {                       // the other places go to the lowest indices that have none
+        uint64_t taken = 0;
+        for (int w = 0; w < kWaves; ++w)
+            for (int j = 0; j < count[w]; ++j) {
+                const uint32_t i = ~(uint32_t)lists[w][j];
+                taken |= i < 64 ? uint64_t(1) << i : 0;
+            }
+        const bool free = !(taken >> lane & 1);
+        const int fill = n + lanes_before(__ballot(free));
+        if (free && fill < A.n_top) {
+            A.top_idx[(int64_t)r * A.n_top + fill] = lane;
+            if (A.top_logprob) A.top_logprob[(int64_t)r * A.n_top + fill] = row.log_p(row.at(lane));
+        }
     }
 }
 
@@ -282,9 +275,14 @@ __global__ __launch_bounds__(64 * kWaves) void sk_logprobs_scan(const Args A)
         if ((int64_t)tile * kTile >= total) break;
         float x[32];
         load_tile<BF16>((const unsigned char*)(row & ~(uintptr_t)15), skip, total, tile, lane, x);
-        float mx = x[0];
+        float part[4];                                    // maxima of eight logits each
 #pragma unroll
-        for (int e = 1; e < 32; ++e) mx = fmaxf(mx, x[e]);
+        for (int e = 0; e < 4; ++e) {
+            part[e] = x[8 * e];
+#pragma unroll
+            for (int f = 1; f < 8; ++f) part[e] = fmaxf(part[e], x[8 * e + f]);
+        }
+        const float mx = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
         const float M = fmaxf(a.m, mx), Mf = finite_or_0(M);
         a = moved(a, Mf);
         a.m = M;
@@ -295,35 +293,58 @@ __global__ __launch_bounds__(64 * kWaves) void sk_logprobs_scan(const Args A)
             a.z += w * fmaxf(d, -200.f);                  // e^-200 is 0 in 32 bits: a logit of -inf adds 0 and not 0 * inf
         }
         if (TOP) {
-            if (top.n < top.k) {                          // at least k logits reach the k-th largest of the lanes' maxima
-                int hits;
-                const uint32_t rk[1] = {mx == mx ? rank_of(mx) : 0};
-                const uint32_t t = bound_of(rk, top.k, hits);
-                if (t > kRankNone) { const float f = value_of(t); if (f > top.floor) { top.floor = f; top.floor_idx = INT_MAX; } }
+            if (top.n < top.k) {                          // the k-th largest of the lanes' maxima, if as many lanes have one
+                const uint32_t rk[1] = {mx > -__builtin_inff() ? rank_of(mx) : 0};
+                int hits = lanes(rk[0] != 0);
+                if (hits >= top.k) top.raise(bound_of(rk, top.k, hits));
             }
-            if (__ballot(mx >= top.floor)) {
-                const int32_t i0 = (int32_t)((int64_t)tile * kTile - skip) + V * lane;
+            const int32_t first = (int32_t)((int64_t)tile * kTile - skip);
+            const float least = top.least(first);
+            int done = 32;                                // of the 32 steps, a logit of each lane
+            if (__ballot(mx >= least)) {
 #pragma unroll
-                for (int e = 0; e < 32; ++e) {
-                    const int32_t idx = i0 + (e / V) * 64 * V + e % V;
-                    const bool add = top.takes(x[e], idx);
-                    if (__ballot(add)) top.append(add, (uint64_t)rank_of(x[e]) << 32 | (uint32_t)~idx, lane);
+                for (int p = 0; p < 4; ++p) {
+                    if (done < 32 || !__ballot(part[p] >= least)) continue;
+#pragma unroll
+                    for (int e = 8 * p; e < 8 * p + 8; ++e) {
+                        const uint64_t m = __ballot(x[e] >= least);
+                        if (!m) continue;
+                        if (top.full()) { done = e; break; }
+                        top.add(m, x[e] >= least, (uint64_t)rank_of(x[e]) << 32 | (uint32_t)~(first + V * lane + (e / V) * 64 * V + e % V));
+                    }
                 }
+            }
+            // A list that is full before the tile is through (thousands of equal logits, as a mask writes them) is cut in
+            // between, and the rest of the tile read again, a logit at a time.  (Nothing of this stands behind each of the steps above:
+            // a kernel of one tile runs most of its code once, from a cold instruction cache.)
+            for (;;) {
+#pragma clang loop unroll(disable)
+                for (; done < 32 && !top.full(); ++done) {
+                    const int32_t idx = first + V * lane + (done / V) * 64 * V + done % V;
+                    float y = -__builtin_inff();
+                    if (idx >= 0 && idx < A.vocab) y = BF16 ? __uint_as_float((uint32_t)((const uint16_t*)row)[idx] << 16) : ((const float*)row)[idx];
+                    const bool takes = top.takes(y, idx);
+                    top.add(__ballot(takes), takes, (uint64_t)rank_of(y) << 32 | (uint32_t)~idx);
+                }
+                if (top.n > 64) top.cut(lane);
+                if (done == 32) break;
             }
         }
     }
     a = wave_sums(a);
     if (A.parts == 1) {
-        join_waves<TOP>(a, top, lists, wave, lane);
-        if (wave == 0) write_row<BF16>(A, r, a, top, lane);
+        finish_row<BF16, TOP>(A, r, a, top, lists, wave, lane);
         return;
     }
     const int64_t slot = (int64_t)blockIdx.x * kWaves + wave;
     if (lane == 0) A.stats[slot] = float4{a.m, a.s, a.z, 0.f};
-    if (TOP) {
-        top.cut(lane);
+    if (TOP) {                                            // its best in order, 0 in the places that none fills
         wave_order();
-        if (lane < A.n_top) A.keys[slot * A.n_top + lane] = lane < top.n ? top.list[lane] : 0;
+        const uint64_t key = lane < top.n ? top.list[lane] : 0;
+        int place = lane < top.n ? 0 : lane;
+#pragma unroll 4
+        for (int j = 0; j < top.n; ++j) place += top.list[j] > key && key;
+        if (place < A.n_top) A.keys[slot * A.n_top + place] = key;
     }
 }
 
@@ -347,14 +368,42 @@ __global__ __launch_bounds__(64 * kWaves) void sk_logprobs_join(const Args A)
         top.init(lists[wave], A.n_top);
         const int64_t all = (int64_t)n * A.n_top;
         const uint64_t* keys = A.keys + (int64_t)r * all;
-        for (int64_t i = 64 * wave; i < all; i += 64 * kWaves) {
-            const uint64_t key = i + lane < all ? keys[i + lane] : 0;
-            const float x = value_of((uint32_t)(key >> 32));
-            top.append(key != 0 && top.takes(x, (int32_t)~(uint32_t)key), key, lane);
+        constexpr int N = 8;
+        for (int64_t i0 = threadIdx.x; i0 - threadIdx.x < all; i0 += N * 64 * kWaves) {
+            uint64_t key[N];
+#pragma unroll
+            for (int j = 0; j < N; ++j) key[j] = i0 + j * 64 * kWaves < all ? keys[i0 + j * 64 * kWaves] : 0;
+            if (top.n < top.k) {                          // as in the scan, by the lanes' maxima
+                uint32_t most[1] = {(uint32_t)(key[0] >> 32)};
+#pragma unroll
+                for (int j = 1; j < N; ++j) most[0] = max(most[0], (uint32_t)(key[j] >> 32));
+                int hits = lanes(most[0] != 0);
+                if (hits >= top.k) top.raise(bound_of(most, top.k, hits));
+            }
+            auto takes = [&](const uint64_t x) { return x != 0 && top.takes(value_of((uint32_t)(x >> 32)), (int32_t)~(uint32_t)x); };
+            int done = N;
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const bool t = takes(key[j]);
+                const uint64_t m = __ballot(t);
+                if (!m) continue;
+                if (top.full()) { done = j; break; }
+                top.add(m, t, key[j]);
+            }
+            for (;;) {
+#pragma clang loop unroll(disable)
+                for (; done < N && !top.full(); ++done) {
+                    const int64_t i = i0 + done * 64 * kWaves;
+                    const uint64_t x = i < all ? keys[i] : 0;
+                    const bool t = takes(x);
+                    top.add(__ballot(t), t, x);
+                }
+                if (top.n > 64) top.cut(lane);
+                if (done == N) break;
+            }
         }
     }
-    join_waves<TOP>(a, top, lists, wave, lane);
-    if (wave == 0) write_row<BF16>(A, r, a, top, lane);
+    finish_row<BF16, TOP>(A, r, a, top, lists, wave, lane);
 }
 
 // How a call is cut: workgroups to a row and tiles to a wave.
