@@ -295,7 +295,7 @@ int sk_batch_attention_mass(sk_pool* pool, int32_t n_items, const int32_t* sessi
  * It may be mass_in (same pointer and stride; no other overlap) or NULL (the caller keeps no sums).
  * A block that another session holds too is not written: what stays of it goes to a block from the free list (SK_E_NOMEM if they do not
  * suffice; a session that shares none needs none).  More than there are to choose from: SK_E_INVAL.  SK_E_WORKSPACE if the lists of what stays
- * (about 4 bytes a token and KV head, 8 bytes a token with per_head == 0) exceed the part of the workspace that holds split partials
+ * (about 8 bytes a token and KV head, 12 bytes a token with per_head == 0) exceed the part of the workspace that holds split partials
  * (at least 134 MB for 128 dims, 67 MB for 64).
  * All or nothing.  Kernels only, ordered on hip_stream like the session's other calls; host metadata change with every call, so a
  * capture of it cannot be replayed.  On a metadata-only pool the host half alone runs.

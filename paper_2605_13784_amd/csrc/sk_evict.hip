@@ -1,10 +1,12 @@
 // Eviction of the tokens with the lowest accumulated weight (include/sk.h: sk_session_evict_lowest), gfx950.
 //
-// Two launches.  The first finds, per list (a KV head, or all together), the n-th smallest sum as a number of 32 bits that orders
-// like the float, eleven bits at a time by histograms, and writes the indices of what stays in order.  The second moves: a
-// workgroup takes 64 consecutive slots of one KV head, reads what goes there and writes it.  K and V bytes are copied, never computed with.
-// Bound: the selection by round trips to the L2 (a workgroup for each list), the move by HBM (what stays is read once and written
-// once; V, transposed in groups of 16 tokens, is read in whole groups).
+// First what leaves: per list (a KV head, or all together) the n-th smallest sum, as a number of 32 bits that orders like the float,
+// found by histograms of its leading bits and, among the few that share those, by counting lanes; then the indices of what
+// stays are written in order.  One launch with a workgroup to a list where the list fits LDS; longer lists are cut among workgroups, in
+// five launches.  Then the move: a workgroup takes 64 consecutive slots of one KV head, reads what goes there and writes it.  K and V
+// bytes are copied, never computed with.
+// Bound: the selection by latency, the move by HBM (what stays is read once and written once; V, transposed in groups of 16
+// tokens, is read in whole groups).
 //
 // Moving in place.  A token never moves to a higher slot.  A workgroup first reads all that it will write, then says so, and writes
 // once those before it, whose tokens lie in its 64 slots, have said so too.  Workgroups take their slots in the order in which they
@@ -14,14 +16,20 @@
 #include <stdint.h>
 #include "../../include/sk.h"
 #include "sk_internal.h"
+#include "sk_order.h"
 
 namespace {
+
+using namespace sk_order;
 
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
 constexpr int kSlots = 64;            // slots that a workgroup of the move takes
-constexpr int kBins = 2048;
-constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
+constexpr int kSelectThreads = 1024;
+constexpr int kBinBits = 13, kBins = 1 << kBinBits;       // leading bits that a histogram counts
+constexpr int kKept = 30 * 1024;      // sums that one workgroup keeps in LDS; longer lists are cut into
+constexpr int kPart = 4096, kPartThreads = 256;           // parts of this many
+constexpr int kFew = 256;             // sums that one wave finishes the search among
 
 struct Args {
     sk_geom g;
@@ -45,144 +53,342 @@ struct Args {
     uint32_t* started;                // [Hkv]
     uint32_t* has_read;               // [Hkv][n_chunks]
     int32_t n_old;
+    // ... of lists that are cut into parts
+    int32_t n_parts;
+    uint32_t* histogram;              // [n_lists][kBins]
+    uint32_t* some;                   // [n_lists][n_cand]: sums that share the leading bits of the n-th smallest
+    uint32_t *n_some, *emitting;      // [n_lists] each: how many; parts that have started to write what stays
+    uint64_t* counted;                // [n_lists][n_parts]: of a part, sums below the n-th smallest, and equal ones + 1
+    uint2* found;                     // [n_lists]: the n-th smallest, and how many that equal it leave
+    int64_t n_clear;                  // words from `started` on that are cleared
 };
 
-__device__ __forceinline__ uint32_t rank_of(const float x)      // orders floats as unsigned numbers; -0 is +0, NaN the largest
-{
-    const uint32_t u = __float_as_uint(x + 0.0f);
-    return x != x ? 0xffffffffu : u ^ (uint32_t)((int32_t)u >> 31 | INT32_MIN);
-}
+// Orders sums as unsigned numbers, of which the lowest leave first; a NaN is larger than any.  (The complement of none of them is 0.)
+__device__ __forceinline__ uint32_t place_of(const float x) { return x != x ? 0xfffffffeu : rank_of(x); }
 
-__device__ __forceinline__ int lanes_before(const uint64_t m)
-{
-    return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
-}
-
-// Exclusive sum over the workgroup's threads; `all` receives the total.
-__device__ __forceinline__ int before_me(const int x, int& all, int* waves /*[kSelectWaves]*/)
+// Exclusive sum over the workgroup's threads.
+template <int WAVES>
+__device__ __forceinline__ int before_me(const int x, int* waves)
 {
     int s = x;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
     for (int i = 1; i < 64; i <<= 1) { const int y = __shfl_up(s, i, 64); s += lane >= i ? y : 0; }
-    __syncthreads();
     if (lane == 63) waves[wave] = s;
     __syncthreads();
     int base = 0;
-    all = 0;
-    for (int w = 0; w < kSelectWaves; ++w) { base += w < wave ? waves[w] : 0; all += waves[w]; }
+    for (int w = 0; w < WAVES; ++w) base += w < wave ? waves[w] : 0;
     return base + s - x;
 }
 
-// Workgroups 0 .. n_lists - 1: one list each.  The others clear what the move counts with, and put the table in place.
-__global__ __launch_bounds__(kSelectThreads) void sk_evict_select(const Args A)
+// Clears what the launches behind count with, puts the table in place, and lists the newest, which all stay: workgroup i of n.
+__device__ __forceinline__ void prepare(const Args& A, const int i, const int n)
 {
-    __shared__ int bins[kBins];
-    __shared__ int waves[kSelectWaves], found[2];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int list = blockIdx.x;
-    if (list >= A.n_lists) {
-        const int64_t i0 = (int64_t)(list - A.n_lists) * kSelectThreads + tid, step = (int64_t)(gridDim.x - A.n_lists) * kSelectThreads;
-        for (int64_t i = i0; i < (int64_t)A.g.Hkv * (A.n_chunks + 1); i += step) A.started[i] = 0;      // (has_read lies behind it)
-        if (A.n_fresh > 0) {
-            int32_t* table = A.tables_rw + A.tbl_off + A.blk0;
-            for (int64_t i = i0; i < A.n_old; i += step) {
-                A.old_table[i] = table[i];
-                if (i < A.n_blk) table[i] = A.table_new[i];
+    const int64_t first = (int64_t)i * blockDim.x + threadIdx.x, step = (int64_t)n * blockDim.x;
+    for (int64_t k = first; k < A.n_clear; k += step) A.started[k] = 0;
+    if (A.n_fresh > 0) {
+        int32_t* table = A.tables_rw + A.tbl_off + A.blk0;
+        for (int64_t k = first; k < A.n_old; k += step) {
+            A.old_table[k] = table[k];
+            if (k < A.n_blk) table[k] = A.table_new[k];
+        }
+    }
+    const int64_t kept = A.new_len - A.win, newest = kept - (A.n_cand - A.n_evict);
+    for (int64_t k = first; k < newest * A.n_lists; k += step) {
+        const int64_t list = k / newest, j = A.n_cand - A.n_evict + k % newest;
+        A.keep[list * kept + j] = (int32_t)(j + A.n_evict);
+    }
+}
+
+__device__ __forceinline__ const float* sums_of(const Args& A, const int list)
+{
+    return A.per_head ? A.in + list * A.in_stride + A.frozen : A.sums;
+}
+
+struct Search {
+    uint32_t bins[kBins], few[kFew];
+    int waves[kSelectThreads / 64];
+    uint32_t bin;
+    int before, count, n_few, left;
+};
+
+// The bin in which the left-th smallest lies, from the counts of the bins (own = kBins / threads consecutive ones to a thread, at(k) the
+// k-th of them); `before`: how many lie below it.
+template <int THREADS, class At>
+__device__ __forceinline__ void find_bin(const At at, const int left, int* waves, uint32_t& bin, int& before, int& count)
+{
+    constexpr int own = kBins / THREADS;
+    uint32_t n[own];
+    int mine = 0;
+#pragma unroll
+    for (int k = 0; k < own; ++k) { n[k] = at(k); mine += n[k]; }
+    int b = before_me<THREADS / 64>(mine, waves);
+    if (b < left && left <= b + mine) {
+#pragma unroll
+        for (int k = 0; k < own; ++k) {
+            if (b < left && left <= b + (int)n[k]) { bin = threadIdx.x * own + k; before = b; count = n[k]; }
+            b += n[k];
+        }
+    }
+    __syncthreads();
+}
+
+// The left-th smallest of 4 * n4 numbers (four at a time: keys(i), any that pad the end 0xffffffff), whose bits from `shift` on
+// are those of `limit` or do not count; `left` becomes the number of those equal to it that are among the left smallest.  All threads.
+template <class Keys>
+__device__ __forceinline__ void search(Search& S, const Keys keys, const int n4, int shift, uint32_t& limit, int& left)
+{
+    const int tid = threadIdx.x, lane = tid & 63;
+    constexpr int own = kBins / kSelectThreads;
+    while (shift > 0) {
+        const int above = shift, width = shift < kBinBits ? shift : kBinBits;
+        shift -= width;
+        for (int b = tid; b < kBins / 4; b += kSelectThreads) ((u32x4*)S.bins)[b] = u32x4{0, 0, 0, 0};
+        if (tid == 0) S.n_few = 0;
+        __syncthreads();
+        const uint32_t mask = (1u << width) - 1;
+#pragma unroll 2
+        for (int i = tid; i < n4; i += kSelectThreads) {
+            const u32x4 x = keys(i);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t b = x[e] >> shift & mask;
+                // a thread's bins lie kSelectThreads words apart: no two lanes meet in a bank when it adds them up
+                if (above == 32 || x[e] >> above == limit >> above) atomicAdd(&S.bins[b % own * kSelectThreads + b / own], 1u);
             }
         }
+        __syncthreads();
+        find_bin<kSelectThreads>([&](const int k) { return S.bins[k * kSelectThreads + tid]; }, left, S.waves, S.bin, S.before, S.count);
+        limit |= S.bin << shift;
+        left -= S.before;
+        if (shift == 0 || S.count > kFew) { __syncthreads(); continue; }
+        // few share these bits: one wave looks at all of them
+#pragma unroll 2
+        for (int i = tid; i < n4; i += kSelectThreads) {
+            const u32x4 x = keys(i);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (x[e] >> shift == limit >> shift) S.few[atomicAdd(&S.n_few, 1)] = x[e];
+        }
+        __syncthreads();
+        if (tid < 64) {
+            constexpr int N = kFew / 64;
+            uint32_t y[N];                                // complements: the largest of those are looked for
+#pragma unroll
+            for (int j = 0; j < N; ++j) y[j] = 64 * j + lane < S.n_few ? ~S.few[64 * j + lane] : 0;
+            int hits, more = 0;
+            const uint32_t t = bound_of(y, left, hits);
+#pragma unroll
+            for (int j = 0; j < N; ++j) more += lanes(y[j] > t);
+            if (lane == 0) { S.bin = ~t; S.left = hits == left ? 0x7fffffff : left - more; }      // (all that reach t leave)
+        }
+        __syncthreads();
+        limit = S.bin; left = S.left;
         return;
     }
-    const int c = A.n_cand;
-    const float* in = A.in + list * A.in_stride + A.frozen;
-    if (!A.per_head) {
-        for (int i = tid; i < c; i += kSelectThreads) {
-            float s = in[i];
-            for (int h = 1; h < A.g.Hkv; ++h) s += in[h * A.in_stride + i];
-            A.sums[i] = s;
-        }
-        in = A.sums;
-        __syncthreads();
+}
+
+// Whether a sum stays, by the n-th smallest; `same_before`: how many of its equals lie in front of the wave's 64.
+__device__ __forceinline__ bool stays(const bool there, const uint32_t x, const uint32_t limit, const int left, int& same_before)
+{
+    const uint64_t eq = __ballot(there && x == limit);
+    bool s = there && x > limit;
+    if (eq) {
+        if (there && x == limit) s = same_before + lanes_before(eq) >= left;
+        same_before += __popcll(eq);
     }
-    // the n_evict-th smallest: `prefix` its leading bits, `left` its place among the sums that share them
-    uint32_t prefix = 0;
+    return s;
+}
+
+// One choice for all heads: the sum of the rows, head by head.
+__global__ __launch_bounds__(256) void sk_evict_sums(const Args A)
+{
+    const int i = blockIdx.x * 256 + threadIdx.x;
+    if (i >= A.n_cand) return;
+    const float* in = A.in + A.frozen + i;
+    float s = in[0];
+#pragma unroll 8
+    for (int h = 1; h < A.g.Hkv; ++h) s += in[h * A.in_stride];
+    A.sums[i] = s;
+}
+
+// Workgroups 0 .. n_lists - 1: one list each, of at most kKept candidates.  The others prepare.
+__global__ __launch_bounds__(kSelectThreads) void sk_evict_select(const Args A)
+{
+    __shared__ Search S;
+    __shared__ uint32_t kept[kKept];
+    __shared__ int n_less[kSelectThreads / 64], n_same[kSelectThreads / 64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int list = blockIdx.x;
+    if (list >= A.n_lists) { prepare(A, list - A.n_lists, gridDim.x - A.n_lists); return; }
+    const int c = A.n_cand, n4 = (c + 3) / 4;
+    const float* in = sums_of(A, list);
+#pragma unroll 8
+    for (int i = tid; i < 4 * n4; i += kSelectThreads) kept[i] = i < c ? place_of(in[i]) : 0xffffffffu;
+    uint32_t limit = 0;
     int left = A.n_evict;
-    if (A.n_evict > 0) {
-#pragma unroll
-        for (int pass = 0; pass < 3; ++pass) {
-            const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, width = pass == 2 ? 10 : 11;
-            for (int b = tid; b < kBins; b += kSelectThreads) bins[b] = 0;
-            __syncthreads();
-            for (int i0 = tid; i0 < c; i0 += 4 * kSelectThreads) {
-                float x[4];
-#pragma unroll
-                for (int u = 0; u < 4; ++u) x[u] = i0 + u * kSelectThreads < c ? in[i0 + u * kSelectThreads] : 0.f;
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const uint32_t r = rank_of(x[u]);
-                    const bool in_it = i0 + u * kSelectThreads < c && (pass == 0 || r >> (shift + width) == prefix >> (shift + width));
-                    const int b = (int)(r >> shift & ((1u << width) - 1));
-                    // (sums that are all the same, zeros above all, would queue up at one counter)
-                    const uint64_t who = __ballot(in_it);
-                    if (!who) continue;
-                    const int one = __shfl(b, __ffsll((unsigned long long)who) - 1, 64);
-                    if (__ballot(in_it && b == one) == who) { if (lane == 0) atomicAdd(&bins[one], __popcll(who)); }
-                    else if (in_it) atomicAdd(&bins[b], 1);
-                }
-            }
-            __syncthreads();
-            int all;
-            const int x0 = bins[2 * tid], x1 = bins[2 * tid + 1];
-            const int at = before_me(x0 + x1, all, waves);
-            if (at < left && left <= at + x0) { found[0] = 2 * tid; found[1] = at; }
-            else if (at + x0 < left && left <= at + x0 + x1) { found[0] = 2 * tid + 1; found[1] = at + x0; }
-            __syncthreads();
-            prefix |= (uint32_t)found[0] << shift;
-            left -= found[1];
-            __syncthreads();
-        }
-    }
-    // What stays: each wave a stretch of the candidates; of the sums that equal the n_evict-th smallest the first `left` leave.
-    const bool none = A.n_evict == 0;
-    const int stretch = ((c + kSelectWaves - 1) / kSelectWaves + 63) & ~63;
-    const int a = wave * stretch < c ? wave * stretch : c, b = a + stretch < c ? a + stretch : c;
+    if (left > 0) search(S, [&](const int i) { return ((const u32x4*)kept)[i]; }, n4, 32, limit, left);
+    else __syncthreads();
+    // what stays: a wave takes a stretch of E rows of 64
+    const int E = (c + kSelectThreads - 1) / kSelectThreads, begin = wave * E * 64, end = begin + E * 64 < c ? begin + E * 64 : c;
     int less = 0, same = 0;
-    for (int i = a; i < b; i += 64) {
-        const bool in_it = i + lane < b;
-        const uint32_t r = in_it ? rank_of(in[i + lane]) : 0xffffffffu;
-        less += __popcll(__ballot(in_it && r < prefix));
-        same += __popcll(__ballot(in_it && r == prefix));
-    }
-    __shared__ int n_less[kSelectWaves], n_same[kSelectWaves];
+    for (int i = begin + lane; i < end; i += 64) { less += kept[i] < limit; same += kept[i] == limit; }
+#pragma unroll
+    for (int i = 32; i >= 1; i >>= 1) { less += __shfl_xor(less, i, 64); same += __shfl_xor(same, i, 64); }
     if (lane == 0) { n_less[wave] = less; n_same[wave] = same; }
     __syncthreads();
     int same_before = 0, less_before = 0;
     for (int w = 0; w < wave; ++w) { same_before += n_same[w]; less_before += n_less[w]; }
-    if (none) { same_before = less_before = 0; left = 0; }
-    int at = a - (none ? 0 : less_before + (same_before < left ? same_before : left));
+    int at = begin - less_before - (same_before < left ? same_before : left);
     int32_t* keep = A.keep + (int64_t)list * (A.new_len - A.win);
-    for (int i = a; i < b; i += 64) {
-        const bool in_it = i + lane < b;
-        const uint32_t r = in_it ? rank_of(in[i + lane]) : 0;
-        const uint64_t eq = __ballot(in_it && r == prefix);
-        const bool stays = in_it && (none || r > prefix || (r == prefix && same_before + lanes_before(eq) >= left));
-        const uint64_t m = __ballot(stays);
-        if (stays) keep[at + lanes_before(m)] = i + lane;
+#pragma unroll 2
+    for (int i = begin + lane; i - lane < end; i += 64) {
+        const bool s = stays(i < end, kept[i < end ? i : 0], limit, left, same_before);
+        const uint64_t m = __ballot(s);
+        if (s) keep[at + lanes_before(m)] = i;
         at += __popcll(m);
-        same_before += __popcll(eq);
     }
-    for (int i = c - A.n_evict + tid; i < A.new_len - A.win; i += kSelectThreads) keep[i] = i + A.n_evict;      // the newest
+}
+
+// ---- longer lists: workgroup (part, list) of 256 threads takes kPart candidates, 16 to a thread ----
+
+__global__ __launch_bounds__(kSelectThreads) void sk_evict_prepare(const Args A) { prepare(A, blockIdx.x, gridDim.x); }
+
+// The candidates of a part: thread t's e-th is the part's 1,024 (t / 64) + 64 e + t % 64.
+__device__ __forceinline__ void load_part(const Args& A, const int list, const int part, uint32_t (&x)[kPart / kPartThreads])
+{
+    const float* in = sums_of(A, list);
+    const int first = part * kPart + (threadIdx.x >> 6) * (kPart / 4) + (threadIdx.x & 63);
+    float f[kPart / kPartThreads];
+#pragma unroll
+    for (int e = 0; e < kPart / kPartThreads; ++e) f[e] = in[first + 64 * e < A.n_cand ? first + 64 * e : A.n_cand - 1];
+#pragma unroll
+    for (int e = 0; e < kPart / kPartThreads; ++e) x[e] = first + 64 * e < A.n_cand ? place_of(f[e]) : 0xffffffffu;
+}
+
+__global__ __launch_bounds__(kPartThreads) void sk_evict_count(const Args A)
+{
+    __shared__ uint32_t bins[kBins];
+    const int list = blockIdx.x % A.n_lists, part = blockIdx.x / A.n_lists;
+    uint32_t x[kPart / kPartThreads];
+    load_part(A, list, part, x);
+    for (int b = threadIdx.x; b < kBins / 4; b += kPartThreads) ((u32x4*)bins)[b] = u32x4{0, 0, 0, 0};
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < kPart / kPartThreads; ++e) if (x[e] != 0xffffffffu) atomicAdd(&bins[x[e] >> (32 - kBinBits)], 1u);
+    __syncthreads();
+    for (int b = threadIdx.x; b < kBins; b += kPartThreads)
+        if (bins[b]) atomicAdd(&A.histogram[(int64_t)list * kBins + b], bins[b]);
+}
+
+// The candidates that share the leading bits of the n-th smallest.
+__global__ __launch_bounds__(kPartThreads) void sk_evict_gather(const Args A)
+{
+    __shared__ uint32_t some[kPart], bin;
+    __shared__ int waves[kPartThreads / 64], before, count, n, at;
+    const int list = blockIdx.x % A.n_lists, part = blockIdx.x / A.n_lists;
+    uint32_t x[kPart / kPartThreads];
+    load_part(A, list, part, x);
+    if (threadIdx.x == 0) n = 0;
+    const uint32_t* h = A.histogram + (int64_t)list * kBins + threadIdx.x * (kBins / kPartThreads);
+    find_bin<kPartThreads>([&](const int k) { return h[k]; }, A.n_evict, waves, bin, before, count);
+#pragma unroll
+    for (int e = 0; e < kPart / kPartThreads; ++e)
+        if (x[e] >> (32 - kBinBits) == bin && x[e] != 0xffffffffu) some[atomicAdd(&n, 1)] = x[e];
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        if (n > 0) at = atomicAdd(&A.n_some[list], (uint32_t)n);
+        if (part == 0) A.found[list] = uint2{bin << (32 - kBinBits), (uint32_t)(A.n_evict - before)};
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += kPartThreads) A.some[(int64_t)list * A.n_cand + at + i] = some[i];
+}
+
+// The n-th smallest itself, one workgroup to a list.
+__global__ __launch_bounds__(kSelectThreads) void sk_evict_search(const Args A)
+{
+    __shared__ Search S;
+    __shared__ uint32_t kept[kKept];
+    const int list = blockIdx.x, n = A.n_some[list], n4 = (n + 3) / 4;
+    const uint32_t* some = A.some + (int64_t)list * A.n_cand;
+    uint32_t limit = A.found[list].x;
+    int left = A.found[list].y;
+    auto at = [&](const int i) { return i < n ? some[i] : 0xffffffffu; };
+    if (n <= kKept) {
+#pragma unroll 8
+        for (int i = threadIdx.x; i < 4 * n4; i += kSelectThreads) kept[i] = at(i);
+        search(S, [&](const int i) { return ((const u32x4*)kept)[i]; }, n4, 32 - kBinBits, limit, left);
+    } else search(S, [&](const int i) { return u32x4{at(4 * i), at(4 * i + 1), at(4 * i + 2), at(4 * i + 3)}; }, n4, 32 - kBinBits, limit, left);
+    if (threadIdx.x == 0) A.found[list] = uint2{limit, (uint32_t)left};
+}
+
+// What stays, in order: a part counts what leaves, says so, and adds up what the parts before it have said.  Parts are handed out in
+// the order in which workgroups start, so each waits only for workgroups that are running and have nothing to wait for before they say it.
+__global__ __launch_bounds__(kPartThreads) void sk_evict_emit(const Args A)
+{
+    __shared__ int ticket, n_less[kPartThreads / 64], n_same[kPartThreads / 64], less_of[kPartThreads / 64], same_of[kPartThreads / 64];
+    const int list = blockIdx.x % A.n_lists, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (threadIdx.x == 0) ticket = (int)__hip_atomic_fetch_add(&A.emitting[list], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    const int part = ticket;
+    uint32_t x[kPart / kPartThreads];
+    load_part(A, list, part, x);
+    uint32_t limit = 0;
+    int left = 0;
+    if (A.n_evict > 0) { limit = A.found[list].x; left = (int)A.found[list].y; }
+    int less = 0, same = 0;
+#pragma unroll
+    for (int e = 0; e < kPart / kPartThreads; ++e) { less += x[e] < limit; same += x[e] == limit; }
+#pragma unroll
+    for (int i = 32; i >= 1; i >>= 1) { less += __shfl_xor(less, i, 64); same += __shfl_xor(same, i, 64); }
+    if (lane == 0) { n_less[wave] = less; n_same[wave] = same; }
+    __syncthreads();
+    uint64_t* counted = A.counted + (int64_t)list * A.n_parts;
+    if (threadIdx.x == 0) {
+        int l = 0, s = 0;
+        for (int w = 0; w < kPartThreads / 64; ++w) { l += n_less[w]; s += n_same[w]; }
+        __hip_atomic_store(&counted[part], (uint64_t)l << 32 | (uint32_t)(s + 1), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    less = same = 0;
+    for (int p = threadIdx.x; p < part; p += kPartThreads) {
+        uint64_t y;
+        while ((y = __hip_atomic_load(&counted[p], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) == 0) __builtin_amdgcn_s_sleep(1);
+        less += (int)(y >> 32); same += (int)(uint32_t)y - 1;
+    }
+#pragma unroll
+    for (int i = 32; i >= 1; i >>= 1) { less += __shfl_xor(less, i, 64); same += __shfl_xor(same, i, 64); }
+    if (lane == 0) { less_of[wave] = less; same_of[wave] = same; }
+    __syncthreads();
+    int less_before = 0, same_before = 0;
+    for (int w = 0; w < kPartThreads / 64; ++w) {
+        less_before += less_of[w] + (w < wave ? n_less[w] : 0);
+        same_before += same_of[w] + (w < wave ? n_same[w] : 0);
+    }
+    const int begin = part * kPart + wave * (kPart / 4);
+    int at = begin - less_before - (same_before < left ? same_before : left);
+    int32_t* keep = A.keep + (int64_t)list * (A.new_len - A.win);
+#pragma unroll
+    for (int e = 0; e < kPart / kPartThreads; ++e) {
+        const int i = begin + 64 * e + lane;
+        const bool s = stays(i < A.n_cand, x[e], limit, left, same_before);
+        const uint64_t m = __ballot(s);
+        if (s) keep[at + lanes_before(m)] = i;
+        at += __popcll(m);
+    }
 }
 
 __device__ __forceinline__ void used(u32x4& x) { asm volatile("" : "+v"(x)); }
 
 // Workgroup (chunk, KV head) of the move.
 template <int D, bool F32>
-__global__ __launch_bounds__(256) void sk_evict_move(const Args A)
+__global__ __launch_bounds__(256, F32 ? 2 : 4) void sk_evict_move(const Args A)
 {
     constexpr int ROWB = D * (F32 ? 4 : 2), PR = ROWB / 16, N = kSlots * PR / 256;     // 16-byte pieces of a row, of a thread
     __shared__ int64_t from[kSlots];      // byte offset of the slot's block and KV head
     __shared__ int slot[kSlots];          // slot within that block
+    __shared__ uint8_t pick[kSlots];      // bf16: which of the groups that go to this slot's one, slot within it
+    __shared__ int64_t group_at[kSlots];  // bf16: byte offset of V of the groups that go to group g, from 16 g on
+    __shared__ int n_groups[kSlots / 16];
     __shared__ int64_t to[kSlots / 16];   // of the four groups: byte offset of the block and KV head
     __shared__ int last_moves, ticket;
     const int tid = threadIdx.x;
@@ -208,6 +414,15 @@ __global__ __launch_bounds__(256) void sk_evict_move(const Args A)
             from[tid] = (int64_t)source[(src >> A.g.log2B) - A.blk0] * A.g.blk_stride;
             slot[tid] = src & (A.g.B - 1);
             if (tid == n_valid - 1) last_moves = src != t;
+            if (!F32) {                   // tokens of one group of 16 slots share the loads of it
+                const int before = __shfl_up(src, 1, 64);
+                const bool first = tid % 16 == 0 || src >> 4 != before >> 4;
+                const uint64_t m = __ballot(first) >> (tid & 48) & 0xffff;
+                const int g = __popcll(m & ((2u << (tid & 15)) - 1)) - 1;
+                pick[tid] = (uint8_t)(g << 4 | (src & 15));
+                if (first) group_at[(tid & 48) + g] = from[tid] + A.g.v_off + (int64_t)((src & (A.g.B - 1)) >> 4) * (D * 32);
+                if (tid % 16 == 15) n_groups[tid >> 4] = g + 1;
+            }
         }
     } else if (tid < kSlots + kSlots / 16) {
         const int t = t0 + 16 * (tid - kSlots);
@@ -231,16 +446,35 @@ __global__ __launch_bounds__(256) void sk_evict_move(const Args A)
             if (F32) v[i] = *(const u32x4*)(row + A.g.v_off);
         }
         if constexpr (!F32) {
+            // A thread holds one dimension of a group: 32 bytes of each group that something comes from, kBatch groups at a time,
+            // of which it picks 16 bits for each of the 16 slots.  (Which, is the same for the whole wave.)
             const int dim = tid % D;
+            constexpr int kBatch = 4;
 #pragma unroll
             for (int i = 0; i < kSlots / 16 / VG; ++i) {
-                const int group = tid / D + VG * i;
-                uint32_t w[8];
+                const int group = __builtin_amdgcn_readfirstlane(tid / D + VG * i), n = __builtin_amdgcn_readfirstlane(n_groups[group]);
+                uint32_t w[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+                const uint32_t mine = pick[16 * group + (tid & 15)];
+                for (int g0 = 0; g0 < n; g0 += kBatch) {
+                    typedef __attribute__((ext_vector_type(32))) uint32_t u32x32;
+                    u32x32 x;
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int r = 16 * group + e;
-                    const uint32_t x = *(const uint16_t*)(kv + from[r] + A.g.v_off + ((slot[r] >> 4) * D + dim) * 32 + (slot[r] & 15) * 2);
-                    w[e >> 1] = e & 1 ? w[e >> 1] | x << 16 : x;
+                    for (int j = 0; j < kBatch; ++j) {
+                        const int g = g0 + j < n ? g0 + j : n - 1;
+                        const u32x4* p = (const u32x4*)(kv + group_at[16 * group + g] + dim * 32);
+                        const u32x4 a = p[0], b = p[1];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) { x[8 * j + e] = a[e]; x[8 * j + 4 + e] = b[e]; }
+                    }
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const uint32_t from_slot = __builtin_amdgcn_readlane(mine, e);
+                        const uint32_t g = (from_slot >> 4) - g0;
+                        if (g < kBatch) {
+                            const uint32_t y = x[g * 8 + (from_slot >> 1 & 7)] >> (from_slot & 1) * 16;
+                            w[e >> 1] |= e & 1 ? y << 16 : y & 0xffffu;
+                        }
+                    }
                 }
                 v[2 * i] = u32x4{w[0], w[1], w[2], w[3]};
                 v[2 * i + 1] = u32x4{w[4], w[5], w[6], w[7]};
@@ -315,7 +549,7 @@ extern "C" int sk_session_evict_lowest(sk_pool* p, int32_t id, const float* mass
     int64_t chunks = 0;
     if (V.device && n > 0) {
         A.g = V.g;
-        A.tbl_off = V.tbl_off; A.per_head = per_head ? 1 : 0; A.n_lists = per_head ? (int32_t)Hkv : 1;
+        A.tbl_off = V.tbl_off; A.per_head = per_head || Hkv == 1 ? 1 : 0; A.n_lists = A.per_head ? (int32_t)Hkv : 1;
         A.win = (int32_t)V.win; A.frozen = (int32_t)V.frozen; A.len = (int32_t)E.len; A.new_len = (int32_t)E.new_len; A.first = (int32_t)E.first;
         A.n_evict = (int32_t)E.n_evict; A.n_cand = (int32_t)E.n_cand;
         A.blk0 = (int32_t)E.blk0; A.n_blk = (int32_t)E.n_blk; A.n_fresh = (int32_t)E.n_fresh;
@@ -332,22 +566,50 @@ extern "C" int sk_session_evict_lowest(sk_pool* p, int32_t id, const float* mass
         A.old_table = take<int32_t>(at, A.n_old);
         A.started = take<uint32_t>(at, Hkv * (chunks + 1));
         A.has_read = A.started + Hkv;
+        A.n_clear = Hkv * (chunks + 1);
+        if (A.n_cand > kKept) {
+            const int64_t lists = A.n_lists;
+            A.n_parts = (A.n_cand + kPart - 1) / kPart;
+            A.n_some = take<uint32_t>(at, lists);
+            A.emitting = take<uint32_t>(at, lists);
+            A.histogram = take<uint32_t>(at, lists * kBins);
+            A.counted = take<uint64_t>(at, lists * A.n_parts);
+            A.n_clear = (uint32_t*)at - A.started;
+            A.some = take<uint32_t>(at, lists * A.n_cand);
+            A.found = take<uint2>(at, lists);
+        }
         if ((size_t)(at - E.scratch) > E.scratch_bytes || chunks * Hkv >= (int64_t(1) << 31)) return SK_E_WORKSPACE;
     }
     // (nothing to evict and no sums to copy: nothing to do on the device)
     const bool runs = V.device && n > 0 && (n_evict > 0 || (mass_out && mass_out != mass_in));
+    int launches = 2;
     hipStream_t st = (hipStream_t)hip_stream;
     if (sk_injected(p, SK_SITE_EVICT_SELECT)) return SK_E_HIP;
     if (runs) {
-        const int64_t others = (Hkv * (chunks + 1) + A.n_old) / (8 * kSelectThreads) + 1;
-        hipLaunchKernelGGL(sk_evict_select, dim3((unsigned)(A.n_lists + (others < 64 ? others : 64))), dim3(kSelectThreads), 0, st, A);
+        if (!A.per_head && A.n_cand > 0) {
+            hipLaunchKernelGGL(sk_evict_sums, dim3((unsigned)((A.n_cand + 255) / 256)), dim3(256), 0, st, A);
+            ++launches;
+        }
+        const int64_t work = A.n_clear + A.n_old + A.n_lists * n_recent;
+        const unsigned others = (unsigned)(work / (8 * kSelectThreads) < 63 ? work / (8 * kSelectThreads) + 1 : 64);
+        if (A.n_parts == 0) hipLaunchKernelGGL(sk_evict_select, dim3(A.n_lists + others), dim3(kSelectThreads), 0, st, A);
+        else {
+            const dim3 parts((unsigned)A.n_lists * (unsigned)A.n_parts);
+            hipLaunchKernelGGL(sk_evict_prepare, dim3(others), dim3(kSelectThreads), 0, st, A);
+            if (n_evict > 0) {
+                hipLaunchKernelGGL(sk_evict_count, parts, dim3(kPartThreads), 0, st, A);
+                hipLaunchKernelGGL(sk_evict_gather, parts, dim3(kPartThreads), 0, st, A);
+                hipLaunchKernelGGL(sk_evict_search, dim3(A.n_lists), dim3(kSelectThreads), 0, st, A);
+            }
+            hipLaunchKernelGGL(sk_evict_emit, parts, dim3(kPartThreads), 0, st, A);
+            launches += n_evict > 0 ? 4 : 1;
+        }
         const int e = (int)hipGetLastError();
         sk_evict_listed(p, E, hip_stream);
         if (e) {      // (an error that an earlier call left behind shows up here too, with the kernel on the stream)
             sk_evict_undo(p, E, hip_stream);
             return sk_note_hip_error(e);
         }
-        sk_count_launch(p);
     }
     int e = sk_injected(p, SK_SITE_EVICT_MOVE) ? (int)hipErrorUnknown : 0;
     if (runs && !e) {
@@ -365,7 +627,7 @@ extern "C" int sk_session_evict_lowest(sk_pool* p, int32_t id, const float* mass
         if (runs) sk_evict_undo(p, E, hip_stream);
         return sk_note_hip_error(e);
     }
-    if (runs) sk_count_launch(p);
+    for (; runs && launches > 0; --launches) sk_count_launch(p);
     sk_evict_end(p, E);
     return SK_OK;
 }

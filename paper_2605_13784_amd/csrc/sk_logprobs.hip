@@ -410,8 +410,11 @@ __global__ __launch_bounds__(64 * kWaves) void sk_logprobs_join(const Args A)
 void cut_rows(const int32_t rows, const int32_t vocab, int32_t& parts, int32_t& tiles)
 {
     const int64_t all = (int64_t(vocab) + 7 + kTile - 1) / kTile, groups = (all + kWaves - 1) / kWaves;
-    // at least 1,024 workgroups where the logits suffice for that
-    int64_t t = (rows * groups + 1023) / 1024;
+    // Up to 2,048 workgroups: eight to a CU hide each other's start, and what a row cut in parts has more (the second launch, a list
+    // for every part) is spread over them.  us for 200 x 50,257 (fp32, bf16), 20 alternatives, by this number: 512 23.9, 26.9;
+    // 1,024 22.3, 24.2; 2,048 19.5, 21.9; 4,096 19.6, 22.0; 600 x 128,256: 65.7, 66.2; 62.3, 58.0; 61.7, 64.2; 67.1, 72.5.  Rows that make
+    // two workgroups' work each are left whole once there is one for every CU: 500 x 16,384, 5: 14.2 -> 12.1.
+    int64_t t = groups <= 2 && rows >= 256 ? groups : (rows * groups + 2047) / 2048;
     t = t < 1 ? 1 : t > groups ? groups : t;
     parts = int32_t((groups + t - 1) / t);
     tiles = int32_t((groups + parts - 1) / parts);
