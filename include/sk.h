@@ -293,8 +293,9 @@ int sk_batch_attention_mass(sk_pool* pool, int32_t n_items, const int32_t* sessi
  * mass_in, mass_out: DEVICE float [Hkv][stride] as sk_session_attention_mass keeps them (4-byte aligned, strides at least the length).
  * mass_out[g][j] receives the sums of the tokens that stay, in their new places, and 0 in the n_evict places behind the new end.
  * It may be mass_in (same pointer and stride; no other overlap) or NULL (the caller keeps no sums).
- * A block that another session holds too is not written: what stays of it goes to a block from the free list (SK_E_NOMEM if they do not
- * suffice; a session that shares none needs none).  More than there are to choose from: SK_E_INVAL.  SK_E_WORKSPACE if the lists of what stays
+ * What stays goes to blocks from the free list, and those that it lay in are given back, if the free list has as many; if not, it moves
+ * within the session's own blocks by way of the workspace, which takes longer, and only blocks that another session holds too, which are never
+ * written, are replaced (SK_E_NOMEM if the free ones do not suffice for that; a session that shares none needs none).  More than there are to choose from: SK_E_INVAL.  SK_E_WORKSPACE if the lists of what stays
  * (about 8 bytes a token and KV head, 12 bytes a token with per_head == 0) exceed the part of the workspace that holds split partials
  * (at least 134 MB for 128 dims, 67 MB for 64).
  * All or nothing.  Kernels only, ordered on hip_stream like the session's other calls; host metadata change with every call, so a

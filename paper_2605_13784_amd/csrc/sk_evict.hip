@@ -8,10 +8,12 @@
 // Bound: the selection by latency, the move by HBM (what stays is read once and written once; V, transposed in groups of 16
 // tokens, is read in whole groups).
 //
-// Moving in place.  A token never moves to a higher slot.  A workgroup first reads all that it will write, then says so, and writes
-// once those before it, whose tokens lie in its 64 slots, have said so too.  Workgroups take their slots in the order in which they
-// start (a counter), so everyone waits only for workgroups that are running already and wait for nobody in order to read:
-// every wait ends.
+// Where the tokens go.  If the free list has a block for every one that would be written, what stays goes there and the old blocks
+// are given back: nothing that is read is written.  If not, stretches of what stays go to the workspace in their new order and
+// from there to their places, a launch each: a token never moves to a higher slot, so that no stretch writes over what a later one reads.
+// (Moving in place in one launch was built and measured: workgroups that read 64 slots, say so, and write when those before them whose
+// tokens lie there have said so.  Its three device-scope round trips for each workgroup, one behind the other, cost more than the
+// way by the workspace: 131,072 tokens to 65,536 370 us, 14,800 of 64 dims to 11,303 37 us; to free blocks 130 and 10 us.)
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 #include "../../include/sk.h"
@@ -33,7 +35,7 @@ constexpr int kFew = 256;             // sums that one wave finishes the search 
 
 struct Args {
     sk_geom g;
-    int32_t tbl_off, n_lists, per_head, in_place;
+    int32_t tbl_off, n_lists, per_head;
     int32_t win, frozen;
     int32_t len, new_len, first;      // storage indices, see sk_evict
     int32_t n_evict, n_cand;
@@ -50,9 +52,10 @@ struct Args {
     int32_t* keep;                    // [n_lists][new_len - win]: what stays, counted from win, ascending
     float* sums;                      // per_head == 0: [n_cand]
     int32_t* old_table;               // n_fresh > 0: the n_blk entries and those behind them that are read, as they were
-    uint32_t* started;                // [Hkv]
-    uint32_t* has_read;               // [Hkv][n_chunks]
+    float* old_sums;                  // out == in: a copy of in's entries behind the frozen ones, [Hkv][len - win]
     int32_t n_old;
+    unsigned char* staged;            // chunk by chunk and head by head K and V as they will lie, or null: to their places at once
+    int32_t chunk0;                   // first chunk of a launch
     // ... of lists that are cut into parts
     int32_t n_parts;
     uint32_t* histogram;              // [n_lists][kBins]
@@ -60,7 +63,8 @@ struct Args {
     uint32_t *n_some, *emitting;      // [n_lists] each: how many; parts that have started to write what stays
     uint64_t* counted;                // [n_lists][n_parts]: of a part, sums below the n-th smallest, and equal ones + 1
     uint2* found;                     // [n_lists]: the n-th smallest, and how many that equal it leave
-    int64_t n_clear;                  // words from `started` on that are cleared
+    uint32_t* clear;                  // n_clear words that are cleared: the counts above
+    int64_t n_clear;
 };
 
 // Orders sums as unsigned numbers, of which the lowest leave first; a NaN is larger than any.  (The complement of none of them is 0.)
@@ -70,10 +74,7 @@ __device__ __forceinline__ uint32_t place_of(const float x) { return x != x ? 0x
 template <int WAVES>
 __device__ __forceinline__ int before_me(const int x, int* waves)
 {
-    int s = x;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int i = 1; i < 64; i <<= 1) { const int y = __shfl_up(s, i, 64); s += lane >= i ? y : 0; }
+    const int s = wave_running_sum(x), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     if (lane == 63) waves[wave] = s;
     __syncthreads();
     int base = 0;
@@ -85,7 +86,11 @@ __device__ __forceinline__ int before_me(const int x, int* waves)
 __device__ __forceinline__ void prepare(const Args& A, const int i, const int n)
 {
     const int64_t first = (int64_t)i * blockDim.x + threadIdx.x, step = (int64_t)n * blockDim.x;
-    for (int64_t k = first; k < A.n_clear; k += step) A.started[k] = 0;
+    for (int64_t k = first; k < A.n_clear; k += step) A.clear[k] = 0;
+    if (A.old_sums) {
+        const int64_t m = A.len - A.win;
+        for (int64_t k = first; k < m * A.g.Hkv; k += step) A.old_sums[k] = A.in[k / m * A.in_stride + A.frozen + k % m];
+    }
     if (A.n_fresh > 0) {
         int32_t* table = A.tables_rw + A.tbl_off + A.blk0;
         for (int64_t k = first; k < A.n_old; k += step) {
@@ -108,44 +113,47 @@ __device__ __forceinline__ const float* sums_of(const Args& A, const int list)
 struct Search {
     uint32_t bins[kBins], few[kFew];
     int waves[kSelectThreads / 64];
-    uint32_t bin;
+    uint32_t bin, lowest, highest;
     int before, count, n_few, left;
 };
 
-// The bin in which the left-th smallest lies, from the counts of the bins (own = kBins / threads consecutive ones to a thread, at(k) the
-// k-th of them); `before`: how many lie below it.
-template <int THREADS, class At>
-__device__ __forceinline__ void find_bin(const At at, const int left, int* waves, uint32_t& bin, int& before, int& count)
+// The bin in which the left-th smallest lies, from the counts of the bins in LDS, kBins / threads consecutive ones to a thread;
+// `before`: how many lie below it.
+template <int THREADS>
+__device__ __forceinline__ void find_bin(const uint32_t* bins, const int left, int* waves, uint32_t& bin, int& before, int& count)
 {
     constexpr int own = kBins / THREADS;
-    uint32_t n[own];
+    u32x4 n[own / 4];
     int mine = 0;
 #pragma unroll
-    for (int k = 0; k < own; ++k) { n[k] = at(k); mine += n[k]; }
+    for (int k = 0; k < own / 4; ++k) { n[k] = ((const u32x4*)bins)[threadIdx.x * (own / 4) + k]; mine += n[k].x + n[k].y + n[k].z + n[k].w; }
     int b = before_me<THREADS / 64>(mine, waves);
     if (b < left && left <= b + mine) {
 #pragma unroll
         for (int k = 0; k < own; ++k) {
-            if (b < left && left <= b + (int)n[k]) { bin = threadIdx.x * own + k; before = b; count = n[k]; }
-            b += n[k];
+            const int m = n[k / 4][k % 4];
+            if (b < left && left <= b + m) { bin = threadIdx.x * own + k; before = b; count = m; }
+            b += m;
         }
     }
     __syncthreads();
 }
 
-// The left-th smallest of 4 * n4 numbers (four at a time: keys(i), any that pad the end 0xffffffff), whose bits from `shift` on
-// are those of `limit` or do not count; `left` becomes the number of those equal to it that are among the left smallest.  All threads.
+__device__ __forceinline__ void empty(Search& S)
+{
+    for (int b = threadIdx.x; b < kBins / 4; b += kSelectThreads) ((u32x4*)S.bins)[b] = u32x4{0, 0, 0, 0};
+    if (threadIdx.x == 0) S.n_few = 0;
+}
+
+// The left-th smallest of 4 * n4 numbers (four at a time: keys(i); any that pad the end are as large as others at least), among those
+// whose bits from `shift` on are those of `limit` (the bins are empty at the start); `left` becomes the number of those equal to it that are among the left smallest.  All threads.
 template <class Keys>
 __device__ __forceinline__ void search(Search& S, const Keys keys, const int n4, int shift, uint32_t& limit, int& left)
 {
     const int tid = threadIdx.x, lane = tid & 63;
-    constexpr int own = kBins / kSelectThreads;
     while (shift > 0) {
         const int above = shift, width = shift < kBinBits ? shift : kBinBits;
         shift -= width;
-        for (int b = tid; b < kBins / 4; b += kSelectThreads) ((u32x4*)S.bins)[b] = u32x4{0, 0, 0, 0};
-        if (tid == 0) S.n_few = 0;
-        __syncthreads();
         const uint32_t mask = (1u << width) - 1;
 #pragma unroll 2
         for (int i = tid; i < n4; i += kSelectThreads) {
@@ -153,15 +161,19 @@ __device__ __forceinline__ void search(Search& S, const Keys keys, const int n4,
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const uint32_t b = x[e] >> shift & mask;
-                // a thread's bins lie kSelectThreads words apart: no two lanes meet in a bank when it adds them up
-                if (above == 32 || x[e] >> above == limit >> above) atomicAdd(&S.bins[b % own * kSelectThreads + b / own], 1u);
+                if (above == 32 || x[e] >> above == limit >> above) atomicAdd(&S.bins[b], 1u);
             }
         }
         __syncthreads();
-        find_bin<kSelectThreads>([&](const int k) { return S.bins[k * kSelectThreads + tid]; }, left, S.waves, S.bin, S.before, S.count);
+        find_bin<kSelectThreads>(S.bins, left, S.waves, S.bin, S.before, S.count);
         limit |= S.bin << shift;
         left -= S.before;
-        if (shift == 0 || S.count > kFew) { __syncthreads(); continue; }
+        if (shift == 0) break;
+        if (S.count > kFew) {
+            empty(S);
+            __syncthreads();
+            continue;
+        }
         // few share these bits: one wave looks at all of them
 #pragma unroll 2
         for (int i = tid; i < n4; i += kSelectThreads) {
@@ -223,18 +235,39 @@ __global__ __launch_bounds__(kSelectThreads) void sk_evict_select(const Args A)
     if (list >= A.n_lists) { prepare(A, list - A.n_lists, gridDim.x - A.n_lists); return; }
     const int c = A.n_cand, n4 = (c + 3) / 4;
     const float* in = sums_of(A, list);
-#pragma unroll 8
-    for (int i = tid; i < 4 * n4; i += kSelectThreads) kept[i] = i < c ? place_of(in[i]) : 0xffffffffu;
+    empty(S);
+    if (tid == 0) { S.lowest = 0xffffffffu; S.highest = 0; }
+    __syncthreads();
+    uint32_t hi = 0, lo = 0;              // largest, and largest complement
+    for (int i0 = tid; i0 < 4 * n4; i0 += 8 * kSelectThreads) {       // (a loop's rest of single loads would be a round trip each)
+        float f[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = in[i0 + e * kSelectThreads < c ? i0 + e * kSelectThreads : c - 1];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int i = i0 + e * kSelectThreads;
+            const uint32_t x = i < c ? place_of(f[e]) : 0xffffffffu;
+            if (i < 4 * n4) kept[i] = x;
+            if (i < c) { hi = hi > x ? hi : x; lo = lo > ~x ? lo : ~x; }
+        }
+    }
+    hi = wave_max(hi); lo = wave_max(lo);
+    if (lane == 0) { atomicMax(&S.highest, hi); atomicMin(&S.lowest, ~lo); }
+    __syncthreads();
+    // The bits that are looked through start where the sums differ: bins for the range that there is.  (Bins for all floats are
+    // few for the octaves of real sums: the lanes of a wave queue up at them, and hundreds share one.)
     uint32_t limit = 0;
     int left = A.n_evict;
-    if (left > 0) search(S, [&](const int i) { return ((const u32x4*)kept)[i]; }, n4, 32, limit, left);
-    else __syncthreads();
+    if (left > 0) {
+        const uint32_t base = S.lowest, range = S.highest - base;
+        search(S, [&](const int i) { return ((const u32x4*)kept)[i] - base; }, n4, range ? 32 - __builtin_clz(range) : 0, limit, left);
+        limit += base;
+    }
     // what stays: a wave takes a stretch of E rows of 64
     const int E = (c + kSelectThreads - 1) / kSelectThreads, begin = wave * E * 64, end = begin + E * 64 < c ? begin + E * 64 : c;
     int less = 0, same = 0;
     for (int i = begin + lane; i < end; i += 64) { less += kept[i] < limit; same += kept[i] == limit; }
-#pragma unroll
-    for (int i = 32; i >= 1; i >>= 1) { less += __shfl_xor(less, i, 64); same += __shfl_xor(same, i, 64); }
+    less = wave_sum(less); same = wave_sum(same);
     if (lane == 0) { n_less[wave] = less; n_same[wave] = same; }
     __syncthreads();
     int same_before = 0, less_before = 0;
@@ -284,14 +317,17 @@ __global__ __launch_bounds__(kPartThreads) void sk_evict_count(const Args A)
 // The candidates that share the leading bits of the n-th smallest.
 __global__ __launch_bounds__(kPartThreads) void sk_evict_gather(const Args A)
 {
-    __shared__ uint32_t some[kPart], bin;
+    __shared__ uint32_t bins[kBins], some[kPart], bin;
     __shared__ int waves[kPartThreads / 64], before, count, n, at;
     const int list = blockIdx.x % A.n_lists, part = blockIdx.x / A.n_lists;
     uint32_t x[kPart / kPartThreads];
     load_part(A, list, part, x);
     if (threadIdx.x == 0) n = 0;
-    const uint32_t* h = A.histogram + (int64_t)list * kBins + threadIdx.x * (kBins / kPartThreads);
-    find_bin<kPartThreads>([&](const int k) { return h[k]; }, A.n_evict, waves, bin, before, count);
+#pragma unroll
+    for (int b = 0; b < kBins / 4 / kPartThreads; ++b)
+        ((u32x4*)bins)[b * kPartThreads + threadIdx.x] = ((const u32x4*)(A.histogram + (int64_t)list * kBins))[b * kPartThreads + threadIdx.x];
+    __syncthreads();
+    find_bin<kPartThreads>(bins, A.n_evict, waves, bin, before, count);
 #pragma unroll
     for (int e = 0; e < kPart / kPartThreads; ++e)
         if (x[e] >> (32 - kBinBits) == bin && x[e] != 0xffffffffu) some[atomicAdd(&n, 1)] = x[e];
@@ -314,11 +350,24 @@ __global__ __launch_bounds__(kSelectThreads) void sk_evict_search(const Args A)
     uint32_t limit = A.found[list].x;
     int left = A.found[list].y;
     auto at = [&](const int i) { return i < n ? some[i] : 0xffffffffu; };
+    empty(S);
     if (n <= kKept) {
-#pragma unroll 8
-        for (int i = threadIdx.x; i < 4 * n4; i += kSelectThreads) kept[i] = at(i);
+        for (int i0 = threadIdx.x; i0 < 4 * n4; i0 += 4 * kSelectThreads) {
+            uint32_t x[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = some[i0 + e * kSelectThreads < n ? i0 + e * kSelectThreads : n - 1];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int i = i0 + e * kSelectThreads;
+                if (i < 4 * n4) kept[i] = i < n ? x[e] : 0xffffffffu;
+            }
+        }
+        __syncthreads();
         search(S, [&](const int i) { return ((const u32x4*)kept)[i]; }, n4, 32 - kBinBits, limit, left);
-    } else search(S, [&](const int i) { return u32x4{at(4 * i), at(4 * i + 1), at(4 * i + 2), at(4 * i + 3)}; }, n4, 32 - kBinBits, limit, left);
+    } else {
+        __syncthreads();
+        search(S, [&](const int i) { return u32x4{at(4 * i), at(4 * i + 1), at(4 * i + 2), at(4 * i + 3)}; }, n4, 32 - kBinBits, limit, left);
+    }
     if (threadIdx.x == 0) A.found[list] = uint2{limit, (uint32_t)left};
 }
 
@@ -339,8 +388,7 @@ __global__ __launch_bounds__(kPartThreads) void sk_evict_emit(const Args A)
     int less = 0, same = 0;
 #pragma unroll
     for (int e = 0; e < kPart / kPartThreads; ++e) { less += x[e] < limit; same += x[e] == limit; }
-#pragma unroll
-    for (int i = 32; i >= 1; i >>= 1) { less += __shfl_xor(less, i, 64); same += __shfl_xor(same, i, 64); }
+    less = wave_sum(less); same = wave_sum(same);
     if (lane == 0) { n_less[wave] = less; n_same[wave] = same; }
     __syncthreads();
     uint64_t* counted = A.counted + (int64_t)list * A.n_parts;
@@ -355,8 +403,7 @@ __global__ __launch_bounds__(kPartThreads) void sk_evict_emit(const Args A)
         while ((y = __hip_atomic_load(&counted[p], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) == 0) __builtin_amdgcn_s_sleep(1);
         less += (int)(y >> 32); same += (int)(uint32_t)y - 1;
     }
-#pragma unroll
-    for (int i = 32; i >= 1; i >>= 1) { less += __shfl_xor(less, i, 64); same += __shfl_xor(same, i, 64); }
+    less = wave_sum(less); same = wave_sum(same);
     if (lane == 0) { less_of[wave] = less; same_of[wave] = same; }
     __syncthreads();
     int less_before = 0, same_before = 0;
@@ -377,7 +424,37 @@ __global__ __launch_bounds__(kPartThreads) void sk_evict_emit(const Args A)
     }
 }
 
-__device__ __forceinline__ void used(u32x4& x) { asm volatile("" : "+v"(x)); }
+// Writes what a workgroup holds of a chunk: thread t the pieces t, t + 256, .. of its K rows and, fp32, of its V rows; bf16, two pieces of
+// dimension t % D of the 16-slot group t / D, + 256 / D, ..
+template <int D, bool F32, int N>
+__device__ __forceinline__ void put(const Args& A, const int head, const int t0, const int n_valid, const int64_t* to, const u32x4 (&k)[N], const u32x4 (&v)[N])
+{
+    constexpr int ROWB = D * (F32 ? 4 : 2), PR = ROWB / 16, VG = 256 / D;
+    const int tid = threadIdx.x;
+    unsigned char* dst = A.kv_rw + (int64_t)head * A.g.head_stride;
+    const int s0 = t0 & (A.g.B - 1);      // (a group of 16 slots lies in one block; blocks hold whole groups)
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int p = tid + 256 * i, r = p / PR;
+        if (r < n_valid) {
+            unsigned char* row = dst + to[r >> 4] + (int64_t)((s0 + r) & (A.g.B - 1)) * ROWB + (p % PR) * 16;
+            *(u32x4*)row = k[i];
+            if (F32) *(u32x4*)(row + A.g.v_off) = v[i];
+        }
+    }
+    if constexpr (!F32) {
+        const int dim = tid % D;
+#pragma unroll
+        for (int i = 0; i < kSlots / 16 / VG; ++i) {
+            const int group = tid / D + VG * i;
+            if (16 * group < n_valid) {
+                unsigned char* at = dst + to[group] + A.g.v_off + ((((s0 + 16 * group) & (A.g.B - 1)) >> 4) * D + dim) * 32;
+                *(u32x4*)at = v[2 * i];
+                *(u32x4*)(at + 16) = v[2 * i + 1];
+            }
+        }
+    }
+}
 
 // Workgroup (chunk, KV head) of the move.
 template <int D, bool F32>
@@ -390,16 +467,10 @@ __global__ __launch_bounds__(256, F32 ? 2 : 4) void sk_evict_move(const Args A)
     __shared__ int64_t group_at[kSlots];  // bf16: byte offset of V of the groups that go to group g, from 16 g on
     __shared__ int n_groups[kSlots / 16];
     __shared__ int64_t to[kSlots / 16];   // of the four groups: byte offset of the block and KV head
-    __shared__ int last_moves, ticket;
+    __shared__ int last_moves;
     const int tid = threadIdx.x;
     const int Hkv = A.g.Hkv;
-    int chunk = blockIdx.x / Hkv;
-    const int head = blockIdx.x - chunk * Hkv;
-    if (A.in_place) {
-        if (tid == 0) ticket = (int)__hip_atomic_fetch_add(&A.started[head], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        __syncthreads();
-        chunk = ticket;
-    }
+    const int chunk = A.chunk0 + blockIdx.x / Hkv, head = blockIdx.x % Hkv;
     const int t0 = A.first + chunk * kSlots;
     const int n_valid = A.new_len - t0 < kSlots ? A.new_len - t0 : kSlots;               // slots that hold something afterwards
     const unsigned char* kv = A.g.kv + (int64_t)head * A.g.head_stride;
@@ -430,7 +501,7 @@ __global__ __launch_bounds__(256, F32 ? 2 : 4) void sk_evict_move(const Args A)
     }
     // the sums that go to these places
     float sum = 0.f;
-    const float* in = A.in + head * A.in_stride + A.frozen - A.win;                      // by storage index, from win on
+    const float* in = A.old_sums ? A.old_sums + (int64_t)head * (A.len - A.win) - A.win : A.in + head * A.in_stride + A.frozen - A.win;    // by storage index, from win on
     if (A.out && tid < n_valid && t0 + tid >= A.win) sum = in[src];
     __syncthreads();
     // where nothing in front has left and no block is replaced, everything is in its place
@@ -481,19 +552,6 @@ __global__ __launch_bounds__(256, F32 ? 2 : 4) void sk_evict_move(const Args A)
             }
         }
     }
-    if (A.in_place) {
-        // all of it has arrived: say so, and wait for those whose tokens lie in these slots
-#pragma unroll
-        for (int i = 0; i < N; ++i) if (moves) { used(k[i]); used(v[i]); }
-        asm volatile("" : "+v"(sum));
-        __syncthreads();
-        uint32_t* flags = A.has_read + (int64_t)head * A.n_chunks;
-        if (tid == 0) __hip_atomic_store(&flags[chunk], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        const int back = (A.n_evict + kSlots - 1) / kSlots;
-        for (int f = (chunk > back ? chunk - back : 0) + tid; f < chunk; f += 256)
-            while (__hip_atomic_load(&flags[f], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == 0) __builtin_amdgcn_s_sleep(1);
-        __syncthreads();
-    }
     if (A.out) {
         float* out = A.out + head * A.out_stride + A.frozen - A.win;
         if (tid < kSlots && t0 + tid >= A.win && t0 + tid < A.len) out[t0 + tid] = sum;
@@ -501,29 +559,36 @@ __global__ __launch_bounds__(256, F32 ? 2 : 4) void sk_evict_move(const Args A)
             for (int j = tid; j < A.frozen; j += 256) A.out[head * A.out_stride + j] = A.in[head * A.in_stride + j];
     }
     if (!moves) return;
-    unsigned char* dst = A.kv_rw + (int64_t)head * A.g.head_stride;
-    const int s0 = t0 & (A.g.B - 1);      // (a group of 16 slots lies in one block; blocks hold whole groups)
+    if (A.staged) {
+        u32x4* dst = (u32x4*)(A.staged + (int64_t)blockIdx.x * (2 * kSlots * ROWB)) + tid;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const int p = tid + 256 * i, r = p / PR;
-        if (r < n_valid) {
-            unsigned char* row = dst + to[r >> 4] + (int64_t)((s0 + r) & (A.g.B - 1)) * ROWB + (p % PR) * 16;
-            *(u32x4*)row = k[i];
-            if (F32) *(u32x4*)(row + A.g.v_off) = v[i];
-        }
+        for (int i = 0; i < N; ++i) { dst[256 * i] = k[i]; dst[256 * (N + i)] = v[i]; }
+        return;
     }
-    if constexpr (!F32) {
-        const int dim = tid % D;
+    put<D, F32>(A, head, t0, n_valid, to, k, v);
+}
+
+// The chunks of a launch from the workspace to their places.
+template <int D, bool F32>
+__global__ __launch_bounds__(256) void sk_evict_put(const Args A)
+{
+    constexpr int ROWB = D * (F32 ? 4 : 2), N = kSlots * (ROWB / 16) / 256;
+    __shared__ int64_t to[kSlots / 16];
+    const int chunk = A.chunk0 + blockIdx.x / A.g.Hkv, head = blockIdx.x % A.g.Hkv;
+    const int t0 = A.first + chunk * kSlots, n_valid = A.new_len - t0 < kSlots ? A.new_len - t0 : kSlots, last = t0 + n_valid - 1;
+    if (n_valid <= 0) return;
+    const int32_t* keep = A.keep + (A.per_head ? (int64_t)head * (A.new_len - A.win) : 0);
+    if (A.n_fresh == 0 && (last < A.win || A.win + keep[last - A.win] == last)) return;      // (did not move, see there)
+    if (threadIdx.x < kSlots / 16) {
+        const int t = t0 + 16 * threadIdx.x;
+        if (t < A.new_len) to[threadIdx.x] = (int64_t)A.g.tables[A.tbl_off + (t >> A.g.log2B)] * A.g.blk_stride;
+    }
+    const u32x4* src = (const u32x4*)(A.staged + (int64_t)blockIdx.x * (2 * kSlots * ROWB)) + threadIdx.x;
+    u32x4 k[N], v[N];
 #pragma unroll
-        for (int i = 0; i < kSlots / 16 / VG; ++i) {
-            const int group = tid / D + VG * i;
-            if (16 * group < n_valid) {
-                unsigned char* at = dst + to[group] + A.g.v_off + ((((s0 + 16 * group) & (A.g.B - 1)) >> 4) * D + dim) * 32;
-                *(u32x4*)at = v[2 * i];
-                *(u32x4*)(at + 16) = v[2 * i + 1];
-            }
-        }
-    }
+    for (int i = 0; i < N; ++i) { k[i] = src[256 * i]; v[i] = src[256 * (N + i)]; }
+    __syncthreads();
+    put<D, F32>(A, head, t0, n_valid, to, k, v);
 }
 
 template <class T> T* take(unsigned char*& at, int64_t n) { T* p = (T*)at; at += (size_t(n) * sizeof(T) + 255) / 256 * 256; return p; }
@@ -546,7 +611,7 @@ extern "C" int sk_session_evict_lowest(sk_pool* p, int32_t id, const float* mass
     rc = sk_evict_begin(p, id, n_evict, n_recent, &E);
     if (rc) return rc;
     Args A = {};
-    int64_t chunks = 0;
+    int64_t chunks = 0, round = 0;
     if (V.device && n > 0) {
         A.g = V.g;
         A.tbl_off = V.tbl_off; A.per_head = per_head || Hkv == 1 ? 1 : 0; A.n_lists = A.per_head ? (int32_t)Hkv : 1;
@@ -554,7 +619,6 @@ extern "C" int sk_session_evict_lowest(sk_pool* p, int32_t id, const float* mass
         A.n_evict = (int32_t)E.n_evict; A.n_cand = (int32_t)E.n_cand;
         A.blk0 = (int32_t)E.blk0; A.n_blk = (int32_t)E.n_blk; A.n_fresh = (int32_t)E.n_fresh;
         A.in = mass_in; A.in_stride = mass_in_stride; A.out = mass_out; A.out_stride = mass_out_stride;
-        A.in_place = E.n_fresh < E.n_blk || mass_out == mass_in;
         A.table_new = E.table; A.tables_rw = E.tables_rw; A.kv_rw = E.kv_rw;
         chunks = (E.len - E.first + kSlots - 1) / kSlots;
         if (chunks < 1) chunks = 1;                       // (no token behind the frozen ones: their sums are copied)
@@ -564,25 +628,30 @@ extern "C" int sk_session_evict_lowest(sk_pool* p, int32_t id, const float* mass
         A.keep = take<int32_t>(at, (int64_t)A.n_lists * (E.new_len - V.win));
         A.sums = take<float>(at, A.per_head ? 0 : E.n_cand);
         A.old_table = take<int32_t>(at, A.n_old);
-        A.started = take<uint32_t>(at, Hkv * (chunks + 1));
-        A.has_read = A.started + Hkv;
-        A.n_clear = Hkv * (chunks + 1);
+        A.old_sums = mass_out == mass_in ? take<float>(at, Hkv * (E.len - V.win)) : nullptr;
         if (A.n_cand > kKept) {
             const int64_t lists = A.n_lists;
             A.n_parts = (A.n_cand + kPart - 1) / kPart;
-            A.n_some = take<uint32_t>(at, lists);
+            A.clear = A.n_some = take<uint32_t>(at, lists);
             A.emitting = take<uint32_t>(at, lists);
             A.histogram = take<uint32_t>(at, lists * kBins);
             A.counted = take<uint64_t>(at, lists * A.n_parts);
-            A.n_clear = (uint32_t*)at - A.started;
+            A.n_clear = (uint32_t*)at - A.clear;
             A.some = take<uint32_t>(at, lists * A.n_cand);
             A.found = take<uint2>(at, lists);
+        }
+        round = chunks;
+        if (E.n_fresh < E.n_blk && n_evict > 0) {         // by way of the workspace, as many chunks at a time as it holds
+            A.staged = at;
+            const int64_t chunk_bytes = Hkv * 2 * kSlots * V.g.d * V.g.elem;
+            round = (int64_t)(E.scratch_bytes - (size_t)(at - E.scratch)) / chunk_bytes;
+            if (at > E.scratch + E.scratch_bytes || round < 1) return SK_E_WORKSPACE;
         }
         if ((size_t)(at - E.scratch) > E.scratch_bytes || chunks * Hkv >= (int64_t(1) << 31)) return SK_E_WORKSPACE;
     }
     // (nothing to evict and no sums to copy: nothing to do on the device)
     const bool runs = V.device && n > 0 && (n_evict > 0 || (mass_out && mass_out != mass_in));
-    int launches = 2;
+    int launches = 1;
     hipStream_t st = (hipStream_t)hip_stream;
     if (sk_injected(p, SK_SITE_EVICT_SELECT)) return SK_E_HIP;
     if (runs) {
@@ -590,7 +659,7 @@ extern "C" int sk_session_evict_lowest(sk_pool* p, int32_t id, const float* mass
             hipLaunchKernelGGL(sk_evict_sums, dim3((unsigned)((A.n_cand + 255) / 256)), dim3(256), 0, st, A);
             ++launches;
         }
-        const int64_t work = A.n_clear + A.n_old + A.n_lists * n_recent;
+        const int64_t work = A.n_clear + A.n_old + A.n_lists * (E.len - V.win - E.n_cand) + (A.old_sums ? Hkv * (E.len - V.win) : 0);
         const unsigned others = (unsigned)(work / (8 * kSelectThreads) < 63 ? work / (8 * kSelectThreads) + 1 : 64);
         if (A.n_parts == 0) hipLaunchKernelGGL(sk_evict_select, dim3(A.n_lists + others), dim3(kSelectThreads), 0, st, A);
         else {
@@ -613,15 +682,25 @@ extern "C" int sk_session_evict_lowest(sk_pool* p, int32_t id, const float* mass
     }
     int e = sk_injected(p, SK_SITE_EVICT_MOVE) ? (int)hipErrorUnknown : 0;
     if (runs && !e) {
-        const dim3 grid((unsigned)(chunks * Hkv)), block(256);
-        if (A.g.elem == 4) {
-            if (A.g.d == 128) hipLaunchKernelGGL((sk_evict_move<128, true>), grid, block, 0, st, A);
-            else hipLaunchKernelGGL((sk_evict_move<64, true>), grid, block, 0, st, A);
-        } else {
-            if (A.g.d == 128) hipLaunchKernelGGL((sk_evict_move<128, false>), grid, block, 0, st, A);
-            else hipLaunchKernelGGL((sk_evict_move<64, false>), grid, block, 0, st, A);
+        for (int64_t c = 0; c < chunks && !e; c += round) {
+            const dim3 grid((unsigned)((chunks - c < round ? chunks - c : round) * Hkv)), block(256);
+            A.chunk0 = (int32_t)c;
+#define SK_EVICT(kernel)                                                                                            \
+    do {                                                                                                            \
+        if (A.g.elem == 4) {                                                                                        \
+            if (A.g.d == 128) hipLaunchKernelGGL((kernel<128, true>), grid, block, 0, st, A);                       \
+            else hipLaunchKernelGGL((kernel<64, true>), grid, block, 0, st, A);                                     \
+        } else {                                                                                                    \
+            if (A.g.d == 128) hipLaunchKernelGGL((kernel<128, false>), grid, block, 0, st, A);                      \
+            else hipLaunchKernelGGL((kernel<64, false>), grid, block, 0, st, A);                                    \
+        }                                                                                                           \
+        ++launches;                                                                                                 \
+    } while (0)
+            SK_EVICT(sk_evict_move);
+            if (A.staged) SK_EVICT(sk_evict_put);
+#undef SK_EVICT
+            e = (int)hipGetLastError();
         }
-        e = (int)hipGetLastError();
     }
     if (e) {
         if (runs) sk_evict_undo(p, E, hip_stream);

@@ -192,9 +192,10 @@ struct sk_evict {
     int32_t id;
     int64_t len, new_len;     // storage end before and behind
     int64_t n_evict, n_cand;  // tokens that leave, and among how many of [win, len), from win on, they are looked for
-    int64_t first;            // storage index from which slots are written again: the start of a 16-token group, of a block if that is shared
+    int64_t first;            // storage index from which slots are written again: the start of a 16-token group, of a block if that is replaced
     int64_t blk0, n_blk;      // blocks that hold [first, new_len): their entries of the table
-    int64_t n_fresh;          // of those, how many another session holds too: they are written to blocks from the free list
+    int64_t n_fresh;          // of those, how many are replaced by blocks from the free list
+    bool all_fresh;           // all of them, as the free list has so many; otherwise those that another session holds too
     const int32_t* table;     // pinned: the n_blk entries as they will be (n_fresh > 0, device pools)
     int slot;
     unsigned char* scratch;   // device memory that no other call of the pool is using (its split partials)

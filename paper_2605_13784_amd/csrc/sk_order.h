@@ -31,6 +31,23 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t x)
     { const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false); return max((uint32_t)r[0], (uint32_t)r[1]); }
 }
 
+__device__ __forceinline__ int wave_sum(int x)
+{
+    x += (int)dpp<0xB1>((uint32_t)x); x += (int)dpp<0x4E>((uint32_t)x); x += (int)dpp<0x141>((uint32_t)x); x += (int)dpp<0x140>((uint32_t)x);
+    { const auto r = __builtin_amdgcn_permlane16_swap((uint32_t)x, (uint32_t)x, false, false); x = (int)r[0] + (int)r[1]; }
+    { const auto r = __builtin_amdgcn_permlane32_swap((uint32_t)x, (uint32_t)x, false, false); return (int)r[0] + (int)r[1]; }
+}
+
+// Sum over the lanes up to and with this one: within a row of 16 lanes by shifts of it, then the last lane of a row added to the
+// rows behind it.
+__device__ __forceinline__ int wave_running_sum(int x)
+{
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true); x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true); x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false); x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+    return x;
+}
+
 // A bound that at least k of the wave's numbers reach (N of them in a lane; 0: none), as high as it can be, or one that exactly k reach;
 // `hits` receives how many do.  At least k are above 0.  Found by counting lanes, from the highest bit in which the numbers differ down.
 template <int N>

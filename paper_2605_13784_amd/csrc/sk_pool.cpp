@@ -1366,6 +1366,8 @@ bool sk_sessions_differ(sk_pool* p, int32_t n, const int32_t* id)
 
 bool sk_injected(sk_pool* p, int site) { return inject(p, site); }
 
+static bool evict_replaces(const sk_pool* p, const sk_evict& e, int32_t block) { return e.all_fresh || p->refcnt[(size_t)block] > 1; }
+
 int sk_evict_begin(sk_pool* p, int32_t id, int64_t n_evict, int64_t n_recent, sk_evict* out)
 {
     sk_evict& e = *out;
@@ -1377,15 +1379,17 @@ int sk_evict_begin(sk_pool* p, int32_t id, int64_t n_evict, int64_t n_recent, sk
     e.id = id;
     e.len = s.len; e.new_len = s.len - n_evict; e.n_evict = n_evict; e.n_cand = m - std::min(n_recent, m);
     e.n_fresh = 0; e.table = nullptr; e.slot = 0;
-    // Which tokens leave is known on the device only: every slot from win on may be written again, and a block of those that another
-    // session holds too is replaced.
+    // Which tokens leave is known on the device only: every slot from win on may be written again.  The blocks of those are
+    // replaced, all of them if the free list has as many, and otherwise the ones that another session holds too.
     e.blk0 = s.win / B;
     e.n_blk = std::max<int64_t>(0, (e.new_len + B - 1) / B - e.blk0);
     if (n_evict > 0)
         for (int64_t b = 0; b < e.n_blk; ++b) e.n_fresh += p->refcnt[(size_t)s.blocks[size_t(e.blk0 + b)]] > 1;
     if (e.n_fresh > (int64_t)p->free_blocks.size()) return SK_E_NOMEM;
+    e.all_fresh = n_evict > 0 && e.n_blk <= (int64_t)p->free_blocks.size();
+    if (e.all_fresh) e.n_fresh = e.n_blk;
     e.first = s.win / 16 * 16;
-    if (e.n_fresh > 0 && p->refcnt[(size_t)s.blocks[(size_t)e.blk0]] > 1) e.first = e.blk0 * B;
+    if (e.n_fresh > 0 && evict_replaces(p, e, s.blocks[(size_t)e.blk0])) e.first = e.blk0 * B;
     unsigned char* ws = (unsigned char*)p->d.workspace;
     e.scratch = p->device ? ws + p->L.off_part_ml : nullptr;
     e.scratch_bytes = p->L.off_eph - p->L.off_part_ml;
@@ -1399,7 +1403,7 @@ int sk_evict_begin(sk_pool* p, int32_t id, int64_t n_evict, int64_t n_recent, sk
         if (host)
             for (int64_t b = 0; b < e.n_blk; ++b) {
                 const int32_t blk = s.blocks[size_t(e.blk0 + b)];
-                ((int32_t*)host)[b] = p->refcnt[(size_t)blk] > 1 ? p->free_blocks[next++] : blk;
+                ((int32_t*)host)[b] = evict_replaces(p, e, blk) ? p->free_blocks[next++] : blk;
             }
         e.table = (const int32_t*)host;
     }
@@ -1422,12 +1426,13 @@ void sk_evict_end(sk_pool* p, const sk_evict& e)
     if (e.n_fresh > 0)
         for (int64_t b = 0; b < e.n_blk; ++b) {
             int32_t& blk = s.blocks[size_t(e.blk0 + b)];
-            if (p->refcnt[(size_t)blk] <= 1) continue;
-            p->refcnt[(size_t)blk]--;                     // still held by the others
+            if (!evict_replaces(p, e, blk)) continue;
+            const int32_t old = blk;
             blk = p->free_blocks.front();
             p->free_blocks.pop_front();
             p->refcnt[(size_t)blk] = 1;
             p->blocks_in_use++;
+            release_block(p, old);                        // (behind those that are taken)
         }
     s.len = e.new_len;
     while ((int64_t)s.blocks.size() > e.blk0 + e.n_blk) {

@@ -103,14 +103,17 @@ CASES = [(D64, 200, 16, 0, 0, 100, 0, True), (D64, 200, 16, 0, 0, 1, 0, True), (
          (D64, 700, 64, 0, 100, 333, 1, False), (ODD, 650, 16, 15, 3, 129, 17, True), (ODD, 1500, 64, 500, 70, 900, 100, True),
          (synth.CFG2, 2600, 16, 0, 0, 1300, 64, True), (synth.CFG2, 4099, 16, 100, 5, 257, 300, True), (synth.CFG2, 9001, 64, 500, 1000, 4000, 333, False),
          (synth.CFG1, 500, 16, 0, 0, 250, 10, True), (synth.CFG1, 777, 64, 33, 40, 100, 0, False), (F32_WIDE, 600, 16, 10, 20, 64, 64, True),
-         (D64, 30000, 16, 0, 0, 1000, 0, True), (D64, 30000, 256, 1234, 77, 15000, 5000, True), (D64, 40000, 16, 0, 0, 39000, 0, False)]
+         (D64, 30000, 16, 0, 0, 1000, 0, True), (D64, 30000, 256, 1234, 77, 15000, 5000, True), (D64, 40000, 16, 0, 0, 39000, 0, False),
+         (synth.CFG2, 36000, 16, 7, 0, 1500, 0, True)]         # the last in two stretches where it moves by way of the workspace
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("room", [False, True])               # free blocks for what stays, or too few
 @pytest.mark.parametrize("shape,n,block,frozen,evicted,n_evict,n_recent,per_head", CASES)
-def test_what_leaves_and_what_stays(shape, n, block, frozen, evicted, n_evict, n_recent, per_head):
+def test_what_leaves_and_what_stays(shape, n, block, frozen, evicted, n_evict, n_recent, per_head, room):
     gen = synth.generator(10, stream=n + n_evict)
-    pool, sid, model = _make(shape, gen, n, block, frozen, evicted)
+    pool, sid, model = _make(shape, gen, n, block, frozen, evicted, spare=9 + (n // block if room else 0))
+    before = pool.sk_session_block_table(sid)
     mass = _mass(gen, shape.n_kv_heads, n + 3)
     place = mass.cuda()
     free = pool.sk_pool_blocks_free()
@@ -121,6 +124,10 @@ def test_what_leaves_and_what_stays(shape, n, block, frozen, evicted, n_evict, n
     np.testing.assert_array_equal(place[:, :n].cpu().numpy(), want)
     assert torch.equal(place[:, n:].cpu(), mass[:, n:])
     _check(pool, sid, model)
+    if room and n_evict and n > n_evict + frozen + block:
+        assert not set(pool.sk_session_block_table(sid)[frozen // block + 2 + evicted // block:]) & set(before)
+    elif not room and n > n_evict + 20 * block + frozen:
+        assert pool.sk_session_block_table(sid) == before[:len(pool.sk_session_block_table(sid))]
     assert held - len(pool.sk_session_block_table(sid)) == pool.sk_pool_blocks_free() - free >= n_evict // block
     if n > n_evict:
         _attend(pool, sid, model, gen)
@@ -273,7 +280,8 @@ def test_host_half_and_refusals_without_a_gpu():
     assert _state(p, [a]) == before
     p.sk_session_evict_lowest(a, None, 100, 70)
     assert p.sk_session_length(a) == 100 and p.sk_pool_blocks_free() == free + 6
-    assert p.sk_session_block_table(a) == before[0][0][1][:7]      # the blocks in front stay where they are
+    table = p.sk_session_block_table(a)                       # what is frozen stays where it is, the rest goes to free blocks
+    assert table[:1] == before[0][0][1][:1] and len(table) == 7 and not set(table[1:]) & set(before[0][0][1])
     p.sk_session_evict_oldest(a, 20)                          # and the window goes on behind it
     p.sk_session_evict_lowest(a, None, 50)
     assert p.sk_session_length(a) == 30 and p.sk_pool_get_stats()["tokens_evicted"] == 170
@@ -281,6 +289,17 @@ def test_host_half_and_refusals_without_a_gpu():
         p.sk_session_evict_lowest(a, None, 1)                 # only the frozen tokens are left
     p.reserve(a, 5)
     assert p.sk_session_length(a) == 35
+
+
+def test_a_full_pool_needs_no_blocks():
+    p = _meta(n_blocks=15)
+    a = p.sk_session_create()
+    p.reserve(a, 200)                                         # 13 blocks, 2 free
+    table = p.sk_session_block_table(a)
+    p.sk_session_evict_lowest(a, None, 100, 70)               # 7 blocks would be written: in place
+    assert p.sk_session_length(a) == 100 and p.sk_session_block_table(a) == table[:7] and p.sk_pool_blocks_free() == 8
+    p.sk_session_evict_lowest(a, None, 1)
+    assert p.sk_session_length(a) == 99 and not set(p.sk_session_block_table(a)) & set(table[:7]) and p.sk_pool_blocks_free() == 8
 
 
 def test_shared_blocks_are_replaced_and_counted():
