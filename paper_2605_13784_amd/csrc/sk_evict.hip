@@ -624,7 +624,7 @@ extern "C" int sk_session_evict_lowest(sk_pool* p, int32_t id, const float* mass
         if (chunks < 1) chunks = 1;                       // (no token behind the frozen ones: their sums are copied)
         A.n_chunks = (int32_t)chunks;
         A.n_old = (int32_t)((E.len + V.g.B - 1) / V.g.B - E.blk0);
-        unsigned char* at = E.scratch;
+        unsigned char* at = V.scratch;
         A.keep = take<int32_t>(at, (int64_t)A.n_lists * (E.new_len - V.win));
         A.sums = take<float>(at, A.per_head ? 0 : E.n_cand);
         A.old_table = take<int32_t>(at, A.n_old);
@@ -644,10 +644,10 @@ extern "C" int sk_session_evict_lowest(sk_pool* p, int32_t id, const float* mass
         if (E.n_fresh < E.n_blk && n_evict > 0) {         // by way of the workspace, as many chunks at a time as it holds
             A.staged = at;
             const int64_t chunk_bytes = Hkv * 2 * kSlots * V.g.d * V.g.elem;
-            round = (int64_t)(E.scratch_bytes - (size_t)(at - E.scratch)) / chunk_bytes;
-            if (at > E.scratch + E.scratch_bytes || round < 1) return SK_E_WORKSPACE;
+            round = (int64_t)(V.scratch_bytes - (size_t)(at - V.scratch)) / chunk_bytes;
+            if (at > V.scratch + V.scratch_bytes || round < 1) return SK_E_WORKSPACE;
         }
-        if ((size_t)(at - E.scratch) > E.scratch_bytes || chunks * Hkv >= (int64_t(1) << 31)) return SK_E_WORKSPACE;
+        if ((size_t)(at - V.scratch) > V.scratch_bytes || chunks * Hkv >= (int64_t(1) << 31)) return SK_E_WORKSPACE;
     }
     // (nothing to evict and no sums to copy: nothing to do on the device)
     const bool runs = V.device && n > 0 && (n_evict > 0 || (mass_out && mass_out != mass_in));

@@ -183,6 +183,8 @@ struct sk_session_view {
     int32_t max_batch_tokens;
     int64_t retained;         // tokens the session holds: storage indices [0, frozen) and [win, win + retained - frozen)
     int64_t frozen, win;
+    unsigned char* scratch;   // device memory that no other call of the pool is using (its split partials)
+    size_t scratch_bytes;
 };
 int sk_view_session(const sk_pool* p, int32_t id, sk_session_view* out);     // SK_OK | SK_E_INVAL | SK_E_BADSESSION
 // An eviction by weight, host side (sk_pool.cpp): sk_evict_begin checks and plans it and changes nothing, sk_evict_end carries it out
@@ -198,8 +200,6 @@ struct sk_evict {
     bool all_fresh;           // all of them, as the free list has so many; otherwise those that another session holds too
     const int32_t* table;     // pinned: the n_blk entries as they will be (n_fresh > 0, device pools)
     int slot;
-    unsigned char* scratch;   // device memory that no other call of the pool is using (its split partials)
-    size_t scratch_bytes;
     int32_t* tables_rw;
     unsigned char* kv_rw;
 };

@@ -1350,6 +1350,8 @@ int sk_view_session(const sk_pool* p, int32_t id, sk_session_view* out)
     out->tbl_off = int32_t(int64_t(id) * p->L.max_blocks_per_session);
     out->max_batch_tokens = p->L.max_batch_tokens;
     out->retained = s->retained(); out->frozen = s->frozen; out->win = s->win;
+    out->scratch = p->device ? (unsigned char*)p->d.workspace + p->L.off_part_ml : nullptr;
+    out->scratch_bytes = p->L.off_eph - p->L.off_part_ml;
     return SK_OK;
 }
 
@@ -1391,8 +1393,6 @@ int sk_evict_begin(sk_pool* p, int32_t id, int64_t n_evict, int64_t n_recent, sk
     e.first = s.win / 16 * 16;
     if (e.n_fresh > 0 && evict_replaces(p, e, s.blocks[(size_t)e.blk0])) e.first = e.blk0 * B;
     unsigned char* ws = (unsigned char*)p->d.workspace;
-    e.scratch = p->device ? ws + p->L.off_part_ml : nullptr;
-    e.scratch_bytes = p->L.off_eph - p->L.off_part_ml;
     e.tables_rw = p->device ? (int32_t*)(ws + p->L.off_tables) : nullptr;
     e.kv_rw = (unsigned char*)p->d.kv_mem;
     if (e.n_fresh > 0) {
