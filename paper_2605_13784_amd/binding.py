@@ -231,6 +231,8 @@ class Pool:
         h = ctypes.c_void_p()
         _ck(lib().sk_pool_create(ctypes.byref(self.desc), ctypes.byref(h)), "sk_pool_create")
         self.h = h
+        self._len = ctypes.c_int64()
+        self._len_ref = ctypes.byref(self._len)
 
     def close(self):
         if self.h:
@@ -377,21 +379,28 @@ class Pool:
             lse_s = lse_s.view(NQ, Sfx, self.Hq)
         return out_p, lse_p, out_s, lse_s
 
+    def _length(self, sid):
+        _ck(lib().sk_session_length(self.h, sid, self._len_ref), "sk_session_length")
+        return self._len.value
+
     def _mass(self, t, n):
-        """Checks an array of accumulated weights: float32 [Hkv, >= n], entries of a row next to each other."""
-        assert t.dtype == torch.float32 and t.dim() == 2 and t.shape[0] == self.Hkv and t.shape[1] >= n and (t.stride(1) == 1 or t.shape[1] <= 1)
-        return t.data_ptr(), (t.stride(0) if self.Hkv > 1 else max(n, 1))
+        """Checks an array of accumulated weights: float32 [Hkv, >= n], entries of a row next to each other.  -> address, row stride"""
+        rows, cols = t.shape
+        stride, step = t.stride()
+        assert t.dtype is torch.float32 and rows == self.Hkv and cols >= n and (step == 1 or cols <= 1) and t.is_cuda
+        return t.data_ptr(), (stride if rows > 1 else max(n, 1))
 
     def sk_session_attention_mass(self, sid, q, lse, causal=False, mass_in=None, keep=1.0, mass_out=None, stream=None):
-        """mass_in, mass_out: float32 [Hkv, capacity]; mass_out left out: mass_in in place, or a new [Hkv, length]."""
-        n = self.sk_session_length(sid)
+        """q [tokens, Hq, d], lse [tokens, Hq] of a call's rows; mass_in, mass_out: float32 [Hkv, capacity]; mass_out left out: mass_in in
+        place, or a new [Hkv, length]."""
+        n, n_tok = self._length(sid), 0 if q is None else q.shape[0]
         if mass_out is None:
             mass_out = mass_in if mass_in is not None else torch.empty((self.Hkv, n), dtype=torch.float32, device=self.device)
-        assert q is None or (q.dtype == self.torch_dtype and lse.dtype == torch.float32 and lse.numel() == q.shape[0] * self.Hq)
-        pi, si = self._mass(mass_in, n) if mass_in is not None and keep != 0 else (None, 0)
+        assert q is None or (q.dtype is self.torch_dtype and lse.dtype is torch.float32 and q.numel() == n_tok * self.Hq * self.d and lse.numel() == n_tok * self.Hq)
         po, so = self._mass(mass_out, n)
-        _ck(lib().sk_session_attention_mass(self.h, sid, _p(q), _p(lse), 0 if q is None else q.shape[0], int(bool(causal)), pi, si, keep, po, so,
-                                            _stream(stream)), "sk_session_attention_mass")
+        pi, si = (None, 0) if mass_in is None or keep == 0 else (po, so) if mass_in is mass_out else self._mass(mass_in, n)
+        _ck(lib().sk_session_attention_mass(self.h, sid, _p(q), _p(lse), n_tok, int(bool(causal)), pi, si, keep, po, so, _stream(stream)),
+            "sk_session_attention_mass")
         return mass_out
 
     def sk_session_evict_lowest(self, sid, mass_in, n_evict, n_recent=0, per_head=True, mass_out=None, stream=None):
@@ -399,7 +408,7 @@ class Pool:
         mass_in None."""
         pi, si, po, so = None, 0, None, 0
         if self.kv_mem is not None:
-            n = self.sk_session_length(sid)
+            n = self._length(sid)
             mass_out = mass_in if mass_out is None else mass_out
             (pi, si), (po, so) = self._mass(mass_in, n), self._mass(mass_out, n)
         _ck(lib().sk_session_evict_lowest(self.h, sid, pi, si, int(n_evict), int(n_recent), int(bool(per_head)), po, so,
@@ -409,10 +418,10 @@ class Pool:
     def sk_batch_attention_mass(self, session_ids, cu_tokens, q, lse, causal=None, mass_in=None, keep=1.0, mass_out=None, stream=None):
         """The same for a ragged step: mass_in and mass_out are lists of arrays, one a session."""
         n = len(session_ids)
-        lengths = [self.sk_session_length(s) for s in session_ids]
+        lengths = [self._length(s) for s in session_ids]
         if mass_out is None:
             mass_out = mass_in if mass_in is not None else [torch.empty((self.Hkv, m), dtype=torch.float32, device=self.device) for m in lengths]
-        assert q.dtype == self.torch_dtype and lse.dtype == torch.float32 and q.shape[0] >= cu_tokens[-1] and lse.numel() == q.shape[0] * self.Hq
+        assert q.dtype is self.torch_dtype and lse.dtype is torch.float32 and q.numel() >= cu_tokens[-1] * self.Hq * self.d and lse.numel() >= cu_tokens[-1] * self.Hq
 
         def host(arrays):
             got = [self._mass(t, m) for t, m in zip(arrays, lengths, strict=True)]
@@ -488,9 +497,9 @@ def sk_logprobs(logits, tokens=None, n_top=0, workspace=None, outputs=None, stre
     if outputs is None:
         outputs = logprobs_outputs(rows, n_tokens, n_top, logits.device)
     logprob, lse, entropy, top_idx, top_logprob = outputs
-    for t, shape, dtype in ((logprob, (rows, n_tokens), torch.float32), (lse, (rows,), torch.float32), (entropy, (rows,), torch.float32),
-                            (top_idx, (rows, n_top), torch.int32), (top_logprob, (rows, n_top), torch.float32)):
-        assert t is None or (t.shape == shape and t.dtype == dtype and t.device == logits.device)
+    assert top_idx is None or (top_idx.dtype is torch.int32 and top_idx.numel() == rows * n_top and top_idx.is_cuda)
+    for t, n in ((logprob, rows * n_tokens), (lse, rows), (entropy, rows), (top_logprob, rows * n_top)):
+        assert t is None or (t.dtype is torch.float32 and t.numel() == n and t.is_cuda)
     if workspace is None:
         workspace = torch.empty(max(lib().sk_logprobs_workspace_bytes(rows, vocab, n_top), 16), dtype=torch.uint8, device=logits.device)
     # (a single row may have any stride)

@@ -30,7 +30,8 @@ constexpr int kSlots = 64;            // slots that a workgroup of the move take
 constexpr int kSelectThreads = 1024;
 constexpr int kBinBits = 13, kBins = 1 << kBinBits;       // leading bits that a histogram counts
 constexpr int kKept = 30 * 1024;      // sums that one workgroup keeps in LDS; longer lists are cut into
-constexpr int kPart = 4096, kPartThreads = 256;           // parts of this many
+constexpr int kPart = 4096, kPartThreads = 256;           // parts of this many, whose histograms have
+constexpr int kPartBits = 11, kPartBins = 1 << kPartBits; // fewer bins to clear, merge and look through
 constexpr int kFew = 256;             // sums that one wave finishes the search among
 
 struct Args {
@@ -58,7 +59,7 @@ struct Args {
     int32_t chunk0;                   // first chunk of a launch
     // ... of lists that are cut into parts
     int32_t n_parts;
-    uint32_t* histogram;              // [n_lists][kBins]
+    uint32_t* histogram;              // [n_lists][kPartBins]
     uint32_t* some;                   // [n_lists][n_cand]: sums that share the leading bits of the n-th smallest
     uint32_t *n_some, *emitting;      // [n_lists] each: how many; parts that have started to write what stays
     uint64_t* counted;                // [n_lists][n_parts]: of a part, sums below the n-th smallest, and equal ones + 1
@@ -117,12 +118,12 @@ struct Search {
     int before, count, n_few, left;
 };
 
-// The bin in which the left-th smallest lies, from the counts of the bins in LDS, kBins / threads consecutive ones to a thread;
+// The bin in which the left-th smallest lies, from the counts of the bins in LDS, BINS / THREADS consecutive ones to a thread;
 // `before`: how many lie below it.
-template <int THREADS>
+template <int THREADS, int BINS>
 __device__ __forceinline__ void find_bin(const uint32_t* bins, const int left, int* waves, uint32_t& bin, int& before, int& count)
 {
-    constexpr int own = kBins / THREADS;
+    constexpr int own = BINS / THREADS;
     u32x4 n[own / 4];
     int mine = 0;
 #pragma unroll
@@ -165,7 +166,7 @@ __device__ __forceinline__ void search(Search& S, const Keys keys, const int n4,
             }
         }
         __syncthreads();
-        find_bin<kSelectThreads>(S.bins, left, S.waves, S.bin, S.before, S.count);
+        find_bin<kSelectThreads, kBins>(S.bins, left, S.waves, S.bin, S.before, S.count);
         limit |= S.bin << shift;
         left -= S.before;
         if (shift == 0) break;
@@ -266,6 +267,7 @@ __global__ __launch_bounds__(kSelectThreads) void sk_evict_select(const Args A)
     // what stays: a wave takes a stretch of E rows of 64
     const int E = (c + kSelectThreads - 1) / kSelectThreads, begin = wave * E * 64, end = begin + E * 64 < c ? begin + E * 64 : c;
     int less = 0, same = 0;
+#pragma unroll 4
     for (int i = begin + lane; i < end; i += 64) { less += kept[i] < limit; same += kept[i] == limit; }
     less = wave_sum(less); same = wave_sum(same);
     if (lane == 0) { n_less[wave] = less; n_same[wave] = same; }
@@ -274,12 +276,18 @@ __global__ __launch_bounds__(kSelectThreads) void sk_evict_select(const Args A)
     for (int w = 0; w < wave; ++w) { same_before += n_same[w]; less_before += n_less[w]; }
     int at = begin - less_before - (same_before < left ? same_before : left);
     int32_t* keep = A.keep + (int64_t)list * (A.new_len - A.win);
-#pragma unroll 2
-    for (int i = begin + lane; i - lane < end; i += 64) {
-        const bool s = stays(i < end, kept[i < end ? i : 0], limit, left, same_before);
-        const uint64_t m = __ballot(s);
-        if (s) keep[at + lanes_before(m)] = i;
-        at += __popcll(m);
+    for (int i0 = begin + lane; i0 - lane < end; i0 += 4 * 64) {
+        uint32_t x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = kept[i0 + 64 * e < end ? i0 + 64 * e : 0];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int i = i0 + 64 * e;
+            const bool s = stays(i < end, x[e], limit, left, same_before);
+            const uint64_t m = __ballot(s);
+            if (s) keep[at + lanes_before(m)] = i;
+            at += __popcll(m);
+        }
     }
 }
 
@@ -301,40 +309,40 @@ __device__ __forceinline__ void load_part(const Args& A, const int list, const i
 
 __global__ __launch_bounds__(kPartThreads) void sk_evict_count(const Args A)
 {
-    __shared__ uint32_t bins[kBins];
+    __shared__ uint32_t bins[kPartBins];
     const int list = blockIdx.x % A.n_lists, part = blockIdx.x / A.n_lists;
     uint32_t x[kPart / kPartThreads];
     load_part(A, list, part, x);
-    for (int b = threadIdx.x; b < kBins / 4; b += kPartThreads) ((u32x4*)bins)[b] = u32x4{0, 0, 0, 0};
+    for (int b = threadIdx.x; b < kPartBins / 4; b += kPartThreads) ((u32x4*)bins)[b] = u32x4{0, 0, 0, 0};
     __syncthreads();
 #pragma unroll
-    for (int e = 0; e < kPart / kPartThreads; ++e) if (x[e] != 0xffffffffu) atomicAdd(&bins[x[e] >> (32 - kBinBits)], 1u);
+    for (int e = 0; e < kPart / kPartThreads; ++e) if (x[e] != 0xffffffffu) atomicAdd(&bins[x[e] >> (32 - kPartBits)], 1u);
     __syncthreads();
-    for (int b = threadIdx.x; b < kBins; b += kPartThreads)
-        if (bins[b]) atomicAdd(&A.histogram[(int64_t)list * kBins + b], bins[b]);
+    for (int b = threadIdx.x; b < kPartBins; b += kPartThreads)
+        if (bins[b]) atomicAdd(&A.histogram[(int64_t)list * kPartBins + b], bins[b]);
 }
 
 // The candidates that share the leading bits of the n-th smallest.
 __global__ __launch_bounds__(kPartThreads) void sk_evict_gather(const Args A)
 {
-    __shared__ uint32_t bins[kBins], some[kPart], bin;
+    __shared__ uint32_t bins[kPartBins], some[kPart], bin;
     __shared__ int waves[kPartThreads / 64], before, count, n, at;
     const int list = blockIdx.x % A.n_lists, part = blockIdx.x / A.n_lists;
     uint32_t x[kPart / kPartThreads];
     load_part(A, list, part, x);
     if (threadIdx.x == 0) n = 0;
 #pragma unroll
-    for (int b = 0; b < kBins / 4 / kPartThreads; ++b)
-        ((u32x4*)bins)[b * kPartThreads + threadIdx.x] = ((const u32x4*)(A.histogram + (int64_t)list * kBins))[b * kPartThreads + threadIdx.x];
+    for (int b = 0; b < kPartBins / 4 / kPartThreads; ++b)
+        ((u32x4*)bins)[b * kPartThreads + threadIdx.x] = ((const u32x4*)(A.histogram + (int64_t)list * kPartBins))[b * kPartThreads + threadIdx.x];
     __syncthreads();
-    find_bin<kPartThreads>(bins, A.n_evict, waves, bin, before, count);
+    find_bin<kPartThreads, kPartBins>(bins, A.n_evict, waves, bin, before, count);
 #pragma unroll
     for (int e = 0; e < kPart / kPartThreads; ++e)
-        if (x[e] >> (32 - kBinBits) == bin && x[e] != 0xffffffffu) some[atomicAdd(&n, 1)] = x[e];
+        if (x[e] >> (32 - kPartBits) == bin && x[e] != 0xffffffffu) some[atomicAdd(&n, 1)] = x[e];
     __syncthreads();
     if (threadIdx.x == 0) {
         if (n > 0) at = atomicAdd(&A.n_some[list], (uint32_t)n);
-        if (part == 0) A.found[list] = uint2{bin << (32 - kBinBits), (uint32_t)(A.n_evict - before)};
+        if (part == 0) A.found[list] = uint2{bin << (32 - kPartBits), (uint32_t)(A.n_evict - before)};
     }
     __syncthreads();
     for (int i = threadIdx.x; i < n; i += kPartThreads) A.some[(int64_t)list * A.n_cand + at + i] = some[i];
@@ -363,10 +371,10 @@ __global__ __launch_bounds__(kSelectThreads) void sk_evict_search(const Args A)
             }
         }
         __syncthreads();
-        search(S, [&](const int i) { return ((const u32x4*)kept)[i]; }, n4, 32 - kBinBits, limit, left);
+        search(S, [&](const int i) { return ((const u32x4*)kept)[i]; }, n4, 32 - kPartBits, limit, left);
     } else {
         __syncthreads();
-        search(S, [&](const int i) { return u32x4{at(4 * i), at(4 * i + 1), at(4 * i + 2), at(4 * i + 3)}; }, n4, 32 - kBinBits, limit, left);
+        search(S, [&](const int i) { return u32x4{at(4 * i), at(4 * i + 1), at(4 * i + 2), at(4 * i + 3)}; }, n4, 32 - kPartBits, limit, left);
     }
     if (threadIdx.x == 0) A.found[list] = uint2{limit, (uint32_t)left};
 }
@@ -634,7 +642,7 @@ extern "C" int sk_session_evict_lowest(sk_pool* p, int32_t id, const float* mass
             A.n_parts = (A.n_cand + kPart - 1) / kPart;
             A.clear = A.n_some = take<uint32_t>(at, lists);
             A.emitting = take<uint32_t>(at, lists);
-            A.histogram = take<uint32_t>(at, lists * kBins);
+            A.histogram = take<uint32_t>(at, lists * kPartBins);
             A.counted = take<uint64_t>(at, lists * A.n_parts);
             A.n_clear = (uint32_t*)at - A.clear;
             A.some = take<uint32_t>(at, lists * A.n_cand);
