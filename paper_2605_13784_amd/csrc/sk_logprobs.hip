@@ -275,14 +275,14 @@ __global__ __launch_bounds__(64 * kWaves) void sk_logprobs_scan(const Args A)
         if ((int64_t)tile * kTile >= total) break;
         float x[32];
         load_tile<BF16>((const unsigned char*)(row & ~(uintptr_t)15), skip, total, tile, lane, x);
-        float part[4];                                    // maxima of eight logits each
+        float most[4];                                    // maxima of eight logits each
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            part[e] = x[8 * e];
+            most[e] = x[8 * e];
 #pragma unroll
-            for (int f = 1; f < 8; ++f) part[e] = fmaxf(part[e], x[8 * e + f]);
+            for (int f = 1; f < 8; ++f) most[e] = fmaxf(most[e], x[8 * e + f]);
         }
-        const float mx = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
+        const float mx = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
         const float M = fmaxf(a.m, mx), Mf = finite_or_0(M);
         a = moved(a, Mf);
         a.m = M;
@@ -304,7 +304,7 @@ __global__ __launch_bounds__(64 * kWaves) void sk_logprobs_scan(const Args A)
             if (__ballot(mx >= least)) {
 #pragma unroll
                 for (int p = 0; p < 4; ++p) {
-                    if (done < 32 || !__ballot(part[p] >= least)) continue;
+                    if (done < 32 || !__ballot(most[p] >= least)) continue;
 #pragma unroll
                     for (int e = 8 * p; e < 8 * p + 8; ++e) {
                         const uint64_t m = __ballot(x[e] >= least);
@@ -410,11 +410,14 @@ __global__ __launch_bounds__(64 * kWaves) void sk_logprobs_join(const Args A)
 void cut_rows(const int32_t rows, const int32_t vocab, int32_t& parts, int32_t& tiles)
 {
     const int64_t all = (int64_t(vocab) + 7 + kTile - 1) / kTile, groups = (all + kWaves - 1) / kWaves;
-    // Up to 2,048 workgroups: eight to a CU hide each other's start, and what a row cut in parts has more (the second launch, a list
-    // for every part) is spread over them.  us for 200 x 50,257 (fp32, bf16), 20 alternatives, by this number: 512 23.9, 26.9;
-    // 1,024 22.3, 24.2; 2,048 19.5, 21.9; 4,096 19.6, 22.0; 600 x 128,256: 65.7, 66.2; 62.3, 58.0; 61.7, 64.2; 67.1, 72.5.  Rows that make
-    // two workgroups' work each are left whole once there is one for every CU: 500 x 16,384, 5: 14.2 -> 12.1.
-    int64_t t = groups <= 2 && rows >= 256 ? groups : (rows * groups + 2047) / 2048;
+    // A row cut in parts has a list and an end for every part, and a second launch joins them; whole, the bound of its list holds for more
+    // tiles.  us with 20 alternatives, logits not in a cache (fp32, bf16), 1, 2, 4, 8, 16 parts:
+    //   1,024 x 128,256   90.8  99.5  97.9  97.7 103 / 76.5 89.4 97.0 100 114       200 x 50,257   31.4 28.1 23.7 21.8 / 32.9 30.6 25.1 23.1
+    //     600 x 128,256   66.3  64.9  63.8  63.2 65.8 / 67.3 59.6 64.9 66.0 72.7     64 x 128,256   52.2 37.7 26.7 21.9 19.5 / 53.8 40.5 28.5 23.4 19.3
+    //     300 x 128,256   58.0  46.3  40.4  40.1 39.8 / 59.2 49.0 40.2 41.5 42.9    1,024 x 32,000   32.4 37.3 / 32.2 38.8
+    // So whole from three rows to a CU, two for rows of at most two workgroups' work (500 x 16,384, 5: 14.2 -> 12.1), and else about 2,048
+    // workgroups, eight to a CU.
+    int64_t t = rows >= (groups <= 2 ? 256 : 768) ? groups : (rows * groups + 2047) / 2048;
     t = t < 1 ? 1 : t > groups ? groups : t;
     parts = int32_t((groups + t - 1) / t);
     tiles = int32_t((groups + parts - 1) / parts);
