@@ -83,9 +83,13 @@ CASES = [("layer", 1, 1, False, 16), ("layer", 1, 1, True, 16), ("layer", 31, 1,
          ("group7", 500, 41, True, 16), ("group7", 9001, 77, True, 64), ("one_kv_head", 777, 3, False, 16), ("one_kv_head", 4000, 100, True, 16),
          ("no_groups", 900, 70, True, 16)]
 
+# Keys or rows enough that a wave holds 128 keys, that the rows are cut into parts, or both.
+LONG = [("layer", 30011, 40, True, 64), ("d64", 29000, 33, False, 16), ("layer", 2100, 280, True, 16), ("one_kv_head", 60001, 63, True, 64),
+        ("one_kv_head", 5000, 63, False, 16), ("f32", 5001, 150, True, 16), ("f32_wide", 4097, 130, False, 64)]
+
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("name,n,T,causal,block", CASES)
+@pytest.mark.parametrize("name,n,T,causal,block", CASES + LONG)
 def test_against_the_formula(name, n, T, causal, block):
     shape = SHAPES[name]
     gen = synth.generator(9, stream=n + T)
@@ -201,14 +205,37 @@ def test_batch_against_single_calls_and_the_formula():
 
 
 @pytest.mark.gpu
-def test_captured_and_replayed():
-    shape = synth.CFG2
+def test_batch_of_sessions_whose_rows_are_cut_into_parts():
+    shape = SHAPES["one_kv_head"]
+    gen = synth.generator(9, stream=6)
+    lengths, tokens, causal = [3000, 10, 5000, 129, 700], [40, 2, 63, 0, 20], [1, 0, 1, 0, 0]
+    pool = sk.Pool("bf16", 33, 1, 64, 16, 600, max_sessions=5, max_batch_tokens=8192, kv_fill=0xFF)
+    sids, keys = [], []
+    for n in lengths:
+        sids.append(pool.sk_session_create())
+        _, k, v = synth.draw_qkv(gen, n, shape)
+        pool.sk_session_append(sids[-1], None, k.cuda(), v.cuda())
+        keys.append(k)
+    cu = [0] + [int(x) for x in np.cumsum(tokens)]
+    q = synth.draw(gen, (cu[-1], 33, 64), "bf16")
+    lse = torch.cat([_lse(shape, gen, q[a:b], k, c) if b > a else torch.empty((0, 33)) for a, b, k, c in zip(cu, cu[1:], keys, causal)])
+    got = pool.sk_batch_attention_mass(sids, cu, q.cuda(), lse.cuda(), causal=causal)
+    torch.cuda.synchronize()
+    for i in range(5):
+        want, tol = _expected(shape, q[cu[i]:cu[i + 1]], keys[i], lse[cu[i]:cu[i + 1]], causal[i]) if tokens[i] else (torch.zeros((1, 129), dtype=torch.float64), 0.0)
+        _close(got[i], want, tol)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name,n,T", [("layer", 700, 20), ("layer", 2100, 280), ("one_kv_head", 5000, 63)])      # the last two in parts
+def test_captured_and_replayed(name, n, T):
+    shape = SHAPES[name]
     gen = synth.generator(9, stream=4)
-    n, T = 700, 20
     pool, sid, k = _session(shape, gen, n, 16)
-    q = synth.draw(gen, (T, 32, 128), "bf16").cuda()
-    lse = torch.zeros((T, 32), device="cuda")
-    mass = torch.zeros((8, n), device="cuda")
+    rows = (T, shape.n_q_heads, shape.head_dim)
+    q = synth.draw(gen, rows, "bf16").cuda()
+    lse = torch.zeros(rows[:2], device="cuda")
+    mass = torch.zeros((shape.n_kv_heads, n), device="cuda")
     stream = torch.cuda.Stream()
     stream.wait_stream(torch.cuda.current_stream())
     graph = torch.cuda.CUDAGraph()
@@ -217,7 +244,7 @@ def test_captured_and_replayed():
     torch.cuda.synchronize()
     want = torch.zeros_like(mass)
     for _ in range(4):
-        x = synth.draw(gen, (T, 32, 128), "bf16")
+        x = synth.draw(gen, rows, "bf16")
         q.copy_(x.cuda())
         lse.copy_(_lse(shape, gen, x, k, False).cuda())
         torch.cuda.synchronize()

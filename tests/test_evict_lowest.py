@@ -164,6 +164,24 @@ def test_orders_of_sums(n, kind, per_head):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("per_head", [True, False])
+@pytest.mark.parametrize("kind", ["equal", "zero", "few", "rising", "falling", "near", "odd"])
+def test_orders_of_long_lists(kind, per_head):
+    """More candidates than one workgroup looks through, and as many that share their leading bits."""
+    gen = synth.generator(10, stream=8)
+    n = 70001
+    pool, sid, model = _make(D64, gen, n, 64, 1003, spare=1200)
+    mass = _mass(gen, 4, n, kind)
+    place = mass.cuda()
+    with np.errstate(invalid="ignore"):
+        want = model.evict(mass.numpy(), 30007, 513, per_head)
+    pool.sk_session_evict_lowest(sid, place, 30007, 513, per_head)
+    torch.cuda.synchronize()
+    np.testing.assert_array_equal(place.cpu().numpy(), want)
+    _check(pool, sid, model)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("shape,block,frozen,evicted,prefix", [(D64, 16, 0, 0, 500), (D64, 64, 100, 70, 391), (synth.CFG2, 16, 37, 0, 320), (F32_WIDE, 16, 10, 20, 333)])
 def test_forks_keep_what_they_share(shape, block, frozen, evicted, prefix):
     """A fork is cut, then its source, then the fork again: blocks that both hold are replaced and never written."""
