@@ -152,10 +152,11 @@ struct Sums { float m, s, z; };
 __device__ __forceinline__ float exp_of(const float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
 __device__ __forceinline__ float finite_or_0(const float m) { return m == -__builtin_inff() ? 0.f : m; }
 
-// The sums of `a`, moved to the maximum M >= a.m (not -inf).  A side that saw nothing but -inf (or NaN, which stays one) has no z.
+// The sums of `a`, moved to the maximum M >= a.m (not -inf).  A side that saw nothing but -inf (or NaN, which stays one) has no z.  (e^-200 is
+// 0 in 32 bits: a side that saw nothing but a mask's 1e38s counts 0, and not 0 times a product that is infinite.)
 __device__ __forceinline__ Sums moved(const Sums a, const float M)
 {
-    const float d = a.m - M, f = exp_of(d);
+    const float d = fmaxf(a.m - M, -200.f), f = exp_of(d);
     return Sums{M, a.s * f, a.m == -__builtin_inff() ? 0.f : f * (a.z + d * a.s)};
 }
 

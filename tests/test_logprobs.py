@@ -24,10 +24,10 @@ def _expected(x, tokens, n_top):
     z = x.double()
     m = z.max(1, keepdim=True)[0]
     none = torch.isneginf(m)
-    e = torch.exp(z - torch.where(none, torch.zeros_like(m), m))
-    s = e.sum(1, keepdim=True)
+    m0 = torch.where(none, torch.zeros_like(m), m)
+    s = torch.exp(z - m0).sum(1, keepdim=True)
     lse = torch.where(none, m, m + torch.log(s))
-    p = torch.where(none, torch.full_like(z, -np.inf), z - lse)
+    p = torch.where(none, torch.full_like(z, -np.inf), (z - m0) - torch.log(s))           # (z - lse is 0 where m is 1e38: 64 bits do not hold m + log s)
     q = torch.where(none, torch.zeros_like(z), torch.exp(p))
     entropy = -torch.where(q > 0, q * p, torch.zeros_like(q)).sum(1)
     valid = (tokens >= 0) & (tokens < x.shape[1])
@@ -140,6 +140,29 @@ def test_without_tokens_or_alternatives():
     torch.cuda.synchronize()
     assert got[1] is None and int(got[3][0, 0]) == int(x[0].argmax())
     assert sk.sk_logprobs(x.cuda()[:0])[1].shape == (0,)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [70, 300, 5000, 50257])
+def test_masks_of_the_lowest_value(vocab, dtype):
+    """Tokens masked with the type's lowest number: alone, in stretches that a lane, a wave or a workgroup sees nothing else of, everywhere,
+    and beside the largest numbers, where differences overflow."""
+    t = synth.torch_dtype(dtype)
+    low, high = torch.finfo(t).min, torch.finfo(t).max
+    x = (2.5 * torch.randn((8, vocab), generator=synth.generator(8, stream=9))).to(t).float()
+    x[0, ::2] = low
+    x[1, : vocab - 9] = low
+    x[2, 9:] = low
+    x[3, :] = low
+    x[4, torch.arange(vocab) % 64 != 5] = low
+    x[5, :] = low
+    x[5, 7:16] = high
+    x[6, 20:] = low
+    x[6, 3] = high
+    x[7, vocab // 3:] = -0.5 * high
+    tokens = torch.tensor([[1], [vocab - 1], [0], [2], [5], [8], [3], [0]], dtype=torch.int32)
+    _check(x.to(t).cuda(), x, tokens, 1)
 
 
 @pytest.mark.gpu
