@@ -293,11 +293,12 @@ int sk_batch_attention_mass(sk_pool* pool, int32_t n_items, const int32_t* sessi
  * mass_in, mass_out: DEVICE float [Hkv][stride] as sk_session_attention_mass keeps them (4-byte aligned, strides at least the length).
  * mass_out[g][j] receives the sums of the tokens that stay, in their new places, and 0 in the n_evict places behind the new end.
  * It may be mass_in (same pointer and stride; no other overlap) or NULL (the caller keeps no sums).
- * What stays goes to blocks from the free list, and those that it lay in are given back, if the free list has as many; if not, it moves
- * within the session's own blocks by way of the workspace, which takes longer, and only blocks that another session holds too, which are never
- * written, are replaced (SK_E_NOMEM if the free ones do not suffice for that; a session that shares none needs none).  More than there are to choose from: SK_E_INVAL.  SK_E_WORKSPACE if the lists of what stays
- * (about 8 bytes a token and KV head, 12 bytes a token with per_head == 0) exceed the part of the workspace that holds split partials
- * (at least 134 MB for 128 dims, 67 MB for 64).
+ * What stays goes to blocks from the free list, and those that it lay in are given back, if the free list has as many; if not, it
+ * moves within the session's own blocks by way of the workspace, which takes longer, and only blocks that another session holds too,
+ * which are never written, are replaced (SK_E_NOMEM if the free ones do not suffice for that; a session that shares none needs none).
+ * More than there are to choose from: SK_E_INVAL.  SK_E_WORKSPACE if the lists that the call makes (at most 12 bytes a token and KV
+ * head with per_head != 0, else 12 a token, and 4 a token and KV head where mass_out is mass_in) exceed the part of the workspace that
+ * holds split partials (at least 134 MB for 128 dims, 67 MB for 64).
  * All or nothing.  Kernels only, ordered on hip_stream like the session's other calls; host metadata change with every call, so a
  * capture of it cannot be replayed.  On a metadata-only pool the host half alone runs.
  */
