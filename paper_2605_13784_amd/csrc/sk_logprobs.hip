@@ -7,7 +7,8 @@
 // the last a sum of two terms that are never negative, so that nothing cancels in a row that is nearly certain.
 // The best alternatives come from the same registers: a wave knows a bound that at least `n_top` of the logits it has seen
 // reach, appends what lies above to a short list in LDS, and cuts the list back to the best n_top when it is full, which raises the
-// bound.  The bound is first the n_top-th largest of the 64 lanes' maxima, found by counting lanes bit by bit.
+// bound.  The bound is first the n_top-th largest of the 64 lanes' maxima, found by counting lanes two bits at a time; the waves of a workgroup
+// tell each other theirs, and what the highest leaves of their lists is put in order by counting larger ones.
 // Bound: reading the logits once; about ten vector instructions per logit beside it.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -22,7 +23,8 @@ using namespace sk_order;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
 constexpr int kTile = 2048;           // logits that a wave takes at once, 32 in a lane
-constexpr int kWaves = 4;
+constexpr int kWaves = 4;             // of a workgroup, where a row is cut into parts or there are many
+constexpr int kWavesAlone = 16;       // of one that takes a whole row, where there are few
 constexpr int kList = 256;            // entries of a wave's list of candidates
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -43,10 +45,11 @@ struct Args {
 struct Top {
     uint64_t* list;         // LDS, kList entries
     int n, k;
+    uint32_t* bound;        // LDS: the highest rank that some wave knows n_top logits of its row to reach
     float floor;            // a logit that is smaller is none of the best; one that equals it only with an index below floor_idx
     int32_t floor_idx;
 
-    __device__ __forceinline__ void init(uint64_t* l, const int kk) { list = l; n = 0; k = kk; floor = -__builtin_inff(); floor_idx = INT_MIN; }
+    __device__ __forceinline__ void init(uint64_t* l, uint32_t* b, const int kk) { list = l; bound = b; n = 0; k = kk; floor = -__builtin_inff(); floor_idx = INT_MIN; }
 
     // Cuts a list of more than k entries to its k best.
     __device__ __forceinline__ void cut(const int lane)
@@ -105,6 +108,12 @@ struct Top {
     {
         const float f = value_of(t);
         if (t > kRankNone && f > floor) { floor = f; floor_idx = INT_MAX; }
+    }
+    // Tells the other waves, and hears from them.
+    __device__ __forceinline__ void share(const int lane)
+    {
+        if (lane == 0) atomicMax(bound, rank_of(floor));
+        raise(__builtin_amdgcn_readfirstlane(__hip_atomic_load(bound, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP)));
     }
 };
 
@@ -186,13 +195,25 @@ struct Row {
     __device__ __forceinline__ float log_p(const float x) const { return none ? -__builtin_inff() : (x - m) - log_s; }
 };
 
-// Joins the sums and lists (of at most 64 entries) of a workgroup's waves and writes the row's results.
-template <bool BF16, bool TOP>
-__device__ __forceinline__ void finish_row(const Args& A, const int r, Sums a, Top& top, uint64_t (&lists)[kWaves][kList], const int wave, const int lane)
+// Joins the sums and lists (of at most 64 entries) of a workgroup's W waves and writes the row's results.
+template <bool BF16, bool TOP, int W>
+__device__ __forceinline__ void finish_row(const Args& A, const int r, Sums a, const Top& top, const int wave, const int lane)
 {
-    __shared__ float4 stat[kWaves];
-    __shared__ int count[kWaves];
-    if (lane == 0) { stat[wave] = float4{a.m, a.s, a.z, 0.f}; if (TOP) count[wave] = top.n; }
+    __shared__ float4 stat[W];
+    __shared__ __attribute__((aligned(16))) uint64_t best[TOP ? 64 * W : 1];
+    __shared__ int n_best, places[TOP ? 64 * W : 1];
+    if (TOP) {
+        uint32_t known = rank_of(top.floor);
+        if (2 * top.n > 3 * top.k) {                      // (a list of several tiles says more than the bound that it came in by)
+            const uint32_t rk[1] = {lane < top.n ? (uint32_t)(top.list[lane] >> 32) : 0};
+            int hits;
+            known = bound_of(rk, top.k, hits);
+        }
+        if (lane == 0) atomicMax(top.bound, known);
+    }
+    if (lane == 0) stat[wave] = float4{a.m, a.s, a.z, 0.f};
+    if (TOP) places[threadIdx.x] = 0;
+    if (threadIdx.x == 0) n_best = 0;
     Row<BF16> row(A, r);
     int32_t t = -1;
     float x = 0.f;
@@ -201,13 +222,40 @@ __device__ __forceinline__ void finish_row(const Args& A, const int r, Sums a, T
         if (t >= 0 && t < A.vocab) x = row.at(t);
     }
     __syncthreads();
-    if (!TOP && wave != 1) return;
+    if (TOP) {
+        // What the highest of the waves' bounds leaves.
+        const uint32_t least = *top.bound;
+        const uint64_t key = lane < top.n ? top.list[lane] : 0;
+        const uint64_t m = __ballot((uint32_t)(key >> 32) >= least && key != 0);
+        if (m) {
+            int at = 0;
+            if (lane == 0) at = atomicAdd(&n_best, __popcll(m));
+            at = __builtin_amdgcn_readfirstlane(at);
+            if (m >> lane & 1) best[at + lanes_before(m)] = key;
+        }
+        __syncthreads();
+    }
+    const int n = TOP ? n_best : 0, i = threadIdx.x;
+    // A key's place is the number of larger ones.  Of more than a wave's, the waves that no keys are left for count in a part of the others.
+    int place = 0;
+    if (TOP && n > 64) {
+        const int groups = (n + 63) / 64, shares = W / groups, group = wave % groups, share = wave / groups;
+        if (share < shares) {
+            const uint64_t key = best[64 * group + lane];
+#pragma unroll 8
+            for (int j = share; j < n; j += shares) place += best[j] > key;
+            atomicAdd(&places[64 * group + lane], place);
+        }
+        __syncthreads();
+        place = places[i];
+    }
+    if (wave > 1 && 64 * wave >= n) return;
     a = Sums{-__builtin_inff(), 0.f, 0.f};
     float M = a.m;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, stat[w].x);
+    for (int w = 0; w < W; ++w) M = fmaxf(M, stat[w].x);
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
+    for (int w = 0; w < W; ++w) {
         const Sums b = moved(Sums{stat[w].x, stat[w].y, stat[w].z}, finite_or_0(M));
         a.s += b.s; a.z += b.z;
     }
@@ -227,27 +275,23 @@ __device__ __forceinline__ void finish_row(const Args& A, const int r, Sums a, T
         }
     }
     if (!TOP) return;
-    // A key's place is the number of larger ones in all the lists.
-    const bool in = lane < top.n;
-    const uint64_t key = in ? lists[wave][lane] : 0;
-    int place = 0, n = 0;
-    for (int w = 0; w < kWaves; ++w) {
-        const int c = count[w];
-        n += c;
-#pragma unroll 4
-        for (int j = 0; j < c; ++j) place += lists[w][j] > key;
-    }
-    if (in && place < A.n_top) {
-        A.top_idx[(int64_t)r * A.n_top + place] = (int32_t)~(uint32_t)key;
-        if (A.top_logprob) A.top_logprob[(int64_t)r * A.n_top + place] = row.log_p(value_of((uint32_t)(key >> 32)));
+    if (64 * wave < n) {
+        const uint64_t key = i < n ? best[i] : 0;
+        if (n <= 64) {
+#pragma unroll 8
+            for (int j = 0; j < n; ++j) place += best[j] > key;
+        }
+        if (i < n && place < A.n_top) {
+            A.top_idx[(int64_t)r * A.n_top + place] = (int32_t)~(uint32_t)key;
+            if (A.top_logprob) A.top_logprob[(int64_t)r * A.n_top + place] = row.log_p(value_of((uint32_t)(key >> 32)));
+        }
     }
     if (n < A.n_top && wave == 0) {                       // the other places go to the lowest indices that have none
         uint64_t taken = 0;
-        for (int w = 0; w < kWaves; ++w)
-            for (int j = 0; j < count[w]; ++j) {
-                const uint32_t i = ~(uint32_t)lists[w][j];
-                taken |= i < 64 ? uint64_t(1) << i : 0;
-            }
+        for (int j = 0; j < n; ++j) {
+            const uint32_t k = ~(uint32_t)best[j];
+            taken |= k < 64 ? uint64_t(1) << k : 0;
+        }
         const bool free = !(taken >> lane & 1);
         const int fill = n + lanes_before(__ballot(free));
         if (free && fill < A.n_top) {
@@ -257,11 +301,11 @@ __device__ __forceinline__ void finish_row(const Args& A, const int r, Sums a, T
     }
 }
 
-// Workgroup (part, row): its waves take the row's tiles part * kWaves * tiles + wave, + kWaves, ..
-template <bool BF16, bool TOP>
-__global__ __launch_bounds__(64 * kWaves) void sk_logprobs_scan(const Args A)
+// Workgroup (part, row): its W waves take the row's tiles part * W * tiles + wave, + W, ..
+template <bool BF16, bool TOP, int W>
+__global__ __launch_bounds__(64 * W) void sk_logprobs_scan(const Args A)
 {
-    __shared__ uint64_t lists[kWaves][kList];
+    __shared__ uint64_t lists[W][kList];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = blockIdx.x / A.parts, part = blockIdx.x - r * A.parts;
     constexpr int EL = BF16 ? 2 : 4, V = 16 / EL;
@@ -270,9 +314,14 @@ __global__ __launch_bounds__(64 * kWaves) void sk_logprobs_scan(const Args A)
     const int64_t total = (int64_t)skip + A.vocab;
     Sums a = {-__builtin_inff(), 0.f, 0.f};
     Top top;
-    if (TOP) top.init(lists[wave], A.n_top);
+    __shared__ uint32_t bound;
+    if (TOP) {
+        top.init(lists[wave], &bound, A.n_top);
+        if (threadIdx.x == 0) bound = 0;
+        __syncthreads();
+    }
     for (int i = 0; i < A.tiles; ++i) {
-        const int tile = (part * A.tiles + i) * kWaves + wave;
+        const int tile = (part * A.tiles + i) * W + wave;
         if ((int64_t)tile * kTile >= total) break;
         float x[32];
         load_tile<BF16>((const unsigned char*)(row & ~(uintptr_t)15), skip, total, tile, lane, x);
@@ -294,11 +343,12 @@ __global__ __launch_bounds__(64 * kWaves) void sk_logprobs_scan(const Args A)
             a.z += w * fmaxf(d, -200.f);                  // e^-200 is 0 in 32 bits: a logit of -inf adds 0 and not 0 * inf
         }
         if (TOP) {
-            if (top.n < top.k) {                          // the k-th largest of the lanes' maxima, if as many lanes have one
+            if (top.floor == -__builtin_inff()) {                          // the k-th largest of the lanes' maxima, if as many lanes have one
                 const uint32_t rk[1] = {mx > -__builtin_inff() ? rank_of(mx) : 0};
                 int hits = lanes(rk[0] != 0);
                 if (hits >= top.k) top.raise(bound_of(rk, top.k, hits));
             }
+            top.share(lane);
             const int32_t first = (int32_t)((int64_t)tile * kTile - skip);
             const float least = top.least(first);
             int done = 32;                                // of the 32 steps, a logit of each lane
@@ -333,11 +383,11 @@ __global__ __launch_bounds__(64 * kWaves) void sk_logprobs_scan(const Args A)
         }
     }
     a = wave_sums(a);
-    if (A.parts == 1) {
-        finish_row<BF16, TOP>(A, r, a, top, lists, wave, lane);
+    if (W == kWavesAlone || A.parts == 1) {
+        finish_row<BF16, TOP, W>(A, r, a, top, wave, lane);
         return;
     }
-    const int64_t slot = (int64_t)blockIdx.x * kWaves + wave;
+    const int64_t slot = (int64_t)blockIdx.x * W + wave;
     if (lane == 0) A.stats[slot] = float4{a.m, a.s, a.z, 0.f};
     if (TOP) {                                            // its best in order, 0 in the places that none fills
         wave_order();
@@ -365,8 +415,11 @@ __global__ __launch_bounds__(64 * kWaves) void sk_logprobs_join(const Args A)
     }
     a = wave_sums(a);
     Top top;
+    __shared__ uint32_t bound;
     if (TOP) {
-        top.init(lists[wave], A.n_top);
+        top.init(lists[wave], &bound, A.n_top);
+        if (threadIdx.x == 0) bound = 0;
+        __syncthreads();
         const int64_t all = (int64_t)n * A.n_top;
         const uint64_t* keys = A.keys + (int64_t)r * all;
         constexpr int N = 8;
@@ -374,13 +427,14 @@ __global__ __launch_bounds__(64 * kWaves) void sk_logprobs_join(const Args A)
             uint64_t key[N];
 #pragma unroll
             for (int j = 0; j < N; ++j) key[j] = i0 + j * 64 * kWaves < all ? keys[i0 + j * 64 * kWaves] : 0;
-            if (top.n < top.k) {                          // as in the scan, by the lanes' maxima
+            if (top.floor == -__builtin_inff()) {                          // as in the scan, by the lanes' maxima
                 uint32_t most[1] = {(uint32_t)(key[0] >> 32)};
 #pragma unroll
                 for (int j = 1; j < N; ++j) most[0] = max(most[0], (uint32_t)(key[j] >> 32));
                 int hits = lanes(most[0] != 0);
                 if (hits >= top.k) top.raise(bound_of(most, top.k, hits));
             }
+            top.share(lane);
             auto takes = [&](const uint64_t x) { return x != 0 && top.takes(value_of((uint32_t)(x >> 32)), (int32_t)~(uint32_t)x); };
             int done = N;
 #pragma unroll
@@ -404,20 +458,29 @@ __global__ __launch_bounds__(64 * kWaves) void sk_logprobs_join(const Args A)
             }
         }
     }
-    finish_row<BF16, TOP>(A, r, a, top, lists, wave, lane);
+    finish_row<BF16, TOP, kWaves>(A, r, a, top, wave, lane);
 }
 
-// How a call is cut: workgroups to a row and tiles to a wave.
-void cut_rows(const int32_t rows, const int32_t vocab, int32_t& parts, int32_t& tiles)
+// How a call is cut: waves of a workgroup, workgroups to a row and tiles to a wave.
+void cut_rows(const int32_t rows, const int32_t vocab, int32_t& waves, int32_t& parts, int32_t& tiles)
 {
-    const int64_t all = (int64_t(vocab) + 7 + kTile - 1) / kTile, groups = (all + kWaves - 1) / kWaves;
-    // A row cut in parts has a list and an end for every part, and a second launch joins them; whole, the bound of its list holds for more
+    const int64_t all = (int64_t(vocab) + 7 + kTile - 1) / kTile, groups = (all + kWaves - 1) / kWaves, rounds = (all + kWavesAlone - 1) / kWavesAlone;
+    // Up to a row to a CU: a workgroup of sixteen waves takes all of it, in one launch; where its waves take several tiles each, from as many rows
+    // on that parts of them would fill the device anyhow.  us in parts / alone, 5 and 20 alternatives:
+    //   fp32    1 x 9,000  10.7 / 7.5, 12.0 / 9.0     200 x 9,000  12.7 / 8.7, 14.3 / 9.9     1 x 32,000  10.2 / 9.5, 12.0 / 12.4    200 x 32,000  15.5 / 11.5, 17.6 / 15.7
+    //          64 x 50,257 13.1 / 13.3, 15.4 / 16.6   200 x 50,257 17.8 / 14.4, 20.6 / 17.6  128 x 128,256 21.8 / 21.2, 25.2 / 28.5  200 x 128,256 28.3 / 23.4, 33.4 / 29.4
+    //   bf16   64 x 50,257 14.0 / 12.5, 16.5 / 16.5   200 x 50,257 18.9 / 13.5, 22.5 / 17.2    1 x 128,256 11.6 / 18.0, 14.4 / 25.0  200 x 128,256 27.0 / 21.5, 32.5 / 30.0
+    // (300 rows are a second round: 300 x 32,000 17.2 / 20.1.)  What one group of four waves takes at once is as fast either way.
+    waves = kWavesAlone; parts = 1; tiles = (int32_t)rounds;
+    if (rows <= 256 && groups > 1 && rows >= 64 * (rounds - 1)) return;
+    // Else a row cut in parts has a list and an end for every part, and a second launch joins them; whole, the bound of its list holds for more
     // tiles.  us with 20 alternatives, logits not in a cache (fp32, bf16), 1, 2, 4, 8, 16 parts:
-    //   1,024 x 128,256   90.8  99.5  97.9  97.7 103 / 76.5 89.4 97.0 100 114       200 x 50,257   31.4 28.1 23.7 21.8 / 32.9 30.6 25.1 23.1
-    //     600 x 128,256   66.3  64.9  63.8  63.2 65.8 / 67.3 59.6 64.9 66.0 72.7     64 x 128,256   52.2 37.7 26.7 21.9 19.5 / 53.8 40.5 28.5 23.4 19.3
-    //     300 x 128,256   58.0  46.3  40.4  40.1 39.8 / 59.2 49.0 40.2 41.5 42.9    1,024 x 32,000   32.4 37.3 / 32.2 38.8
-    // So whole from three rows to a CU, two for rows of at most two workgroups' work (500 x 16,384, 5: 14.2 -> 12.1), and else about 2,048
+    //   1,024 x 128,256   90.8  99.5  97.9  97.7 103 / 76.5 89.4 97.0 100 114       64 x 128,256   52.2 37.7 26.7 21.9 19.5 / 53.8 40.5 28.5 23.4 19.3
+    //     600 x 128,256   66.3  64.9  63.8  63.2 65.8 / 67.3 59.6 64.9 66.0 72.7   1,024 x 32,000   32.4 37.3 / 32.2 38.8
+    //     300 x 128,256   58.0  46.3  40.4  40.1 39.8 / 59.2 49.0 40.2 41.5 42.9
+    // So whole from three rows to a CU, one for rows of at most two workgroups' work (500 x 16,384, 5: 14.2 -> 12.1), and else about 2,048
     // workgroups, eight to a CU.
+    waves = kWaves;
     int64_t t = rows >= (groups <= 2 ? 256 : 768) ? groups : (rows * groups + 2047) / 2048;
     t = t < 1 ? 1 : t > groups ? groups : t;
     parts = int32_t((groups + t - 1) / t);
@@ -433,8 +496,8 @@ extern "C" {
 size_t sk_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t n_top)
 {
     if (rows <= 0 || vocab < 1 || n_top < 0 || n_top > SK_LOGPROBS_MAX_TOP) return 0;
-    int32_t parts, tiles;
-    cut_rows(rows, vocab, parts, tiles);
+    int32_t waves, parts, tiles;
+    cut_rows(rows, vocab, waves, parts, tiles);
     return parts == 1 ? 0 : stats_bytes(rows, parts) + (size_t)rows * parts * kWaves * n_top * sizeof(uint64_t);
 }
 
@@ -449,7 +512,8 @@ int sk_logprobs(const void* logits, int dtype, int32_t rows, int32_t vocab, int6
     if (!logits || (n_tokens > 0 && (!tokens || !logprob)) || (n_top > 0 && !top_idx)) return SK_E_INVAL;
     if ((uintptr_t)logits % (dtype == SK_BF16 ? 2 : 4) || (uintptr_t)workspace % 16) return SK_E_INVAL;
     Args A;
-    cut_rows(rows, vocab, A.parts, A.tiles);
+    int32_t waves;
+    cut_rows(rows, vocab, waves, A.parts, A.tiles);
     const size_t need = sk_logprobs_workspace_bytes(rows, vocab, n_top);
     if (need > 0 && !workspace) return SK_E_INVAL;
     if (workspace_bytes < need) return SK_E_WORKSPACE;
@@ -458,19 +522,21 @@ int sk_logprobs(const void* logits, int dtype, int32_t rows, int32_t vocab, int6
     A.stats = (float4*)workspace;
     A.keys = (uint64_t*)((unsigned char*)workspace + stats_bytes(rows, A.parts));
     hipStream_t st = (hipStream_t)hip_stream;
-    const dim3 grid((unsigned)rows * (unsigned)A.parts), block(64 * kWaves);
-#define SK_LOGPROBS(kernel, grid)                                                                                   \
+    const dim3 grid((unsigned)rows * (unsigned)A.parts);
+#define SK_LOGPROBS(kernel, grid, waves, ...)                                                                       \
     do {                                                                                                            \
+        const dim3 block(64 * (waves));                                                                             \
         if (dtype == SK_BF16) {                                                                                     \
-            if (n_top > 0) hipLaunchKernelGGL((kernel<true, true>), grid, block, 0, st, A);                         \
-            else hipLaunchKernelGGL((kernel<true, false>), grid, block, 0, st, A);                                  \
+            if (n_top > 0) hipLaunchKernelGGL((kernel<true, true __VA_OPT__(,) __VA_ARGS__>), grid, block, 0, st, A);          \
+            else hipLaunchKernelGGL((kernel<true, false __VA_OPT__(,) __VA_ARGS__>), grid, block, 0, st, A);                   \
         } else {                                                                                                    \
-            if (n_top > 0) hipLaunchKernelGGL((kernel<false, true>), grid, block, 0, st, A);                        \
-            else hipLaunchKernelGGL((kernel<false, false>), grid, block, 0, st, A);                                 \
+            if (n_top > 0) hipLaunchKernelGGL((kernel<false, true __VA_OPT__(,) __VA_ARGS__>), grid, block, 0, st, A);         \
+            else hipLaunchKernelGGL((kernel<false, false __VA_OPT__(,) __VA_ARGS__>), grid, block, 0, st, A);                  \
         }                                                                                                           \
     } while (0)
-    SK_LOGPROBS(sk_logprobs_scan, grid);
-    if (A.parts > 1) SK_LOGPROBS(sk_logprobs_join, dim3(rows));
+    if (waves == kWavesAlone) SK_LOGPROBS(sk_logprobs_scan, grid, kWavesAlone, kWavesAlone);
+    else SK_LOGPROBS(sk_logprobs_scan, grid, kWaves, kWaves);
+    if (A.parts > 1) SK_LOGPROBS(sk_logprobs_join, dim3(rows), kWaves);
 #undef SK_LOGPROBS
     return hipGetLastError() == hipSuccess ? SK_OK : SK_E_HIP;
 }

@@ -98,7 +98,8 @@ def _planted(x, n_top):
 
 
 SIZES = [(1, 1, 0, 1), (1, 2, 0, 2), (10, 3, 1, 3), (10, 31, 0, 8), (10, 64, 4, 32), (10, 65, 0, 32), (10, 2047, 0, 5), (10, 2048, 0, 20),
-         (10, 2049, 3, 20), (10, 8193, 0, 32), (10, 16400, 1, 1), (10, 50257, 0, 8), (1, 131072, 0, 20), (2, 262145, 0, 32), (1030, 9001, 0, 20), (1100, 130, 5, 4)]
+         (10, 2049, 3, 20), (10, 8193, 0, 32), (10, 16400, 1, 1), (10, 50257, 0, 8), (1, 131072, 0, 20), (2, 262145, 0, 32), (1030, 9001, 0, 20), (1100, 130, 5, 4),
+         (70, 40001, 3, 32), (130, 70001, 0, 7), (256, 33000, 1, 1), (12, 150001, 0, 32), (300, 20000, 0, 20)]      # several tiles to a wave of sixteen; parts
 
 
 @pytest.mark.gpu
@@ -184,10 +185,9 @@ def test_rows_with_nan_and_infinity(vocab):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("rows", [2, 1100])
-def test_captured_and_replayed_on_new_logits(rows):
+@pytest.mark.parametrize("rows,vocab", [(2, 20011), (1100, 20011), (5, 90011)])
+def test_captured_and_replayed_on_new_logits(rows, vocab):
     """Two captured calls with workspaces of their own, replayed several times with eager calls in between."""
-    vocab = 20011
     gen = synth.generator(8, stream=rows)
     x = [torch.randn((rows, vocab), generator=gen).cuda() for _ in range(2)]
     tokens = torch.randint(0, vocab, (rows, 2), generator=gen, dtype=torch.int32).cuda()
