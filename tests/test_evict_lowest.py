@@ -244,6 +244,34 @@ def test_stream_held_to_a_budget():
 
 
 @pytest.mark.gpu
+def test_blocks_at_the_end_of_a_large_pool():
+    """Offsets beyond 2^35: weights and eviction of a session in the last blocks of 40 GiB."""
+    shape, n = synth.CFG2, 700
+    gen = synth.generator(10, stream=11)
+    blocks = (40 << 30) // (64 << 10)
+    pool = sk.Pool("bf16", 32, 8, 128, 16, blocks, max_sessions=2, max_session_tokens=4096, max_batch_tokens=8192)
+    pool.sk_pool_set_alloc_order(np.arange(blocks, dtype=np.int32)[::-1].copy())
+    sid = pool.sk_session_create()
+    q, k, v = synth.draw_qkv(gen, n, shape)
+    pool.sk_session_append(sid, None, k.cuda(), v.cuda())
+    model = Model(shape, synth.to_raw(k), synth.to_raw(v))
+    out, lse = pool.sk_session_query(sid, q[:40].cuda())
+    mass = pool.sk_session_attention_mass(sid, q[:40].cuda(), lse)
+    few = pool.sk_session_attention_mass(sid, q[:5].cuda(), lse[:5])
+    torch.cuda.synchronize()
+    for T, got in ((40, mass), (5, few)):
+        w = torch.exp(torch.einsum("thd,nhd->thn", q[:T].double(), k.double().repeat_interleave(4, 1)) * 128 ** -0.5 - lse[:T].double().cpu()[:, :, None])
+        w = w.sum(0).view(8, 4, n).sum(1)
+        assert torch.all((got.double().cpu() - w).abs() <= 1e-4 * w)       # rounding: 40 * 4 terms, scores below 2^6: 2^-24 * 2^9 = 3e-5
+    want = model.evict(mass.cpu().numpy(), 300, 10, True)
+    pool.sk_session_evict_lowest(sid, mass, 300, 10)
+    torch.cuda.synchronize()
+    np.testing.assert_array_equal(mass.cpu().numpy(), want)
+    assert min(pool.sk_session_block_table(sid)) >= blocks - 100
+    _check(pool, sid, model)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("site", [sk.SK_SITE_RING, sk.SK_SITE_EVICT_SELECT, sk.SK_SITE_EVICT_MOVE])
 def test_call_that_fails_on_the_device_leaves_the_session(site):
     gen = synth.generator(10, stream=6)
