@@ -7,7 +7,7 @@
 // (S = Q K^T): a lane then holds 16 rows of ONE key, whose weights it adds in registers, and only its two halves (and the
 // waves that share keys) meet at the end.  The keys stay in registers, read once; the rows pass by.
 // Bound: K's stream from HBM for few rows (one token at 131,072 cached, 268 MB, 41 us: 6.5 TB/s, the rate of a plain read); for many
-// the exponentials and the matrix products, which overlap in part (256 tokens at 32,768, 6.9e10 operations, 75 us: 0.91 PFLOP/s).
+// the exponentials and the matrix products, which overlap in part (256 tokens at 32,768, 6.9e10 operations, 72 us: 0.95 PFLOP/s).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 #include <algorithm>
@@ -109,12 +109,12 @@ struct Place {
     __device__ __forceinline__ int64_t at(const Args& A, const int row_bytes) const { return (int64_t)block * A.g.blk_stride + (int64_t)slot * row_bytes; }
 };
 
-// Query rows of an item on their way to LDS: a workgroup of 256 threads takes ROWS of them at a time, 256 / ROWS threads a row, whose
+// Query rows of an item on their way to LDS: a workgroup of THREADS threads takes ROWS of them at a time, THREADS / ROWS threads a row, whose
 // pieces of 16 bytes lie next to each other.  In LDS rows lie 16 bytes further apart than they are long, so that the 16 rows that a
 // quarter of a wave reads at once start in different banks.
-template <int D, bool F32, int ROWS>
+template <int D, bool F32, int ROWS, int THREADS>
 struct Rows {
-    static constexpr int ROWB = D * (F32 ? 4 : 2), PITCH = ROWB + 16, TPR = 256 / ROWS, NP = ROWB / 16 / TPR;
+    static constexpr int ROWB = D * (F32 ? 4 : 2), PITCH = ROWB + 16, TPR = THREADS / ROWS, NP = ROWB / 16 / TPR;
     u32x4 piece[NP];
     float l;
     int see;
@@ -220,7 +220,7 @@ __global__ __launch_bounds__(256, F32 && D == 128 ? 4 : 6) void sk_mass_stream(c
     Place at;
     at.find(A, I, first + col);
     for (int r = 0; r < n_rows; r += 64) {
-        Rows<D, F32, 64> R;
+        Rows<D, F32, 64, 256> R;
         R.fetch(A, I, head, r, n_rows);
         R.store(rows + r * PITCH, norm + r, sees + r);
     }
@@ -241,16 +241,18 @@ __global__ __launch_bounds__(256, F32 && D == 128 ? 4 : 6) void sk_mass_stream(c
 }
 
 // Many rows: the keys stay in registers, and the rows pass by.  Workgroup (key tile, part of the rows, KV head) of four waves side by side
-// along the keys, KT x 32 each.  Rows go through LDS, 64 at a time, loaded one step ahead.  Where the keys make few workgroups the rows are
+// along the keys, KT x 32 each, or twice as many, which share a step's rows.  Rows go through LDS, 64 at a time, loaded one step ahead.  Where the keys make few workgroups the rows are
 // cut into parts, whose sums a second launch adds up.
-template <int D, bool F32, int KT>
-__global__ __launch_bounds__(256, 2) void sk_mass_rows(const Args A)
+template <int D, bool F32, int KT, int SHARES>
+__global__ __launch_bounds__(256 * SHARES, 2) void sk_mass_rows(const Args A)
 {
     constexpr int ROWB = D * (F32 ? 4 : 2), PITCH = ROWB + 16, ROWS = 64, KEYS = 128 * KT;
     __shared__ __attribute__((aligned(16))) unsigned char rows[2][ROWS * PITCH];
     __shared__ __attribute__((aligned(16))) float norm[2][ROWS];
     __shared__ __attribute__((aligned(16))) int sees[2][ROWS];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    __shared__ float others[SHARES > 1 ? KEYS : 1];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) & 3;
+    const int share = SHARES > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 8) : 0;
     const int half = lane >> 5, col = lane & 31;
     const int rest = blockIdx.x / A.g.Hkv, head = blockIdx.x - rest * A.g.Hkv;
     const int wg = rest / A.parts, part = rest - wg * A.parts;
@@ -275,7 +277,7 @@ __global__ __launch_bounds__(256, 2) void sk_mass_rows(const Args A)
     }
     const int n_rows = I.n_tok * A.g.G;
     const bool edge = k0 + 32 * KT > I.first_vis;
-    Rows<D, F32, ROWS> R;
+    Rows<D, F32, ROWS, 256 * SHARES> R;
     if (begin < end) { R.fetch(A, I, head, begin, n_rows); R.store(rows[0], norm[0], sees[0]); }
     arrived<D, F32, KT>(key);
     __syncthreads();
@@ -289,7 +291,7 @@ __global__ __launch_bounds__(256, 2) void sk_mass_rows(const Args A)
         const bool more = r0 + ROWS < end;
         if (more) R.fetch(A, I, head, r0 + ROWS, n_rows);
 #pragma unroll
-        for (int r = 0; r < ROWS; r += 32) {
+        for (int r = 32 * share; r < ROWS; r += 32 * SHARES) {
             // (apart, then to the others: a chain of as many additions as a lane has rows loses more than its terms do: 256 tokens over
             // 32,768 keys are off by 1.7e-7 of the sums' norm, 2.7e-7 in one chain, in the same time)
             float w[KT] = {};
@@ -301,8 +303,19 @@ __global__ __launch_bounds__(256, 2) void sk_mass_rows(const Args A)
         __syncthreads();
     }
 #pragma unroll
+    for (int t = 0; t < KT; ++t) sum[t] += __shfl_xor(sum[t], 32, 64);
+    if (SHARES > 1) {
+        if (share == 1 && half == 0) {
+#pragma unroll
+            for (int t = 0; t < KT; ++t) others[wave * (KT * 32) + 32 * t + col] = sum[t];
+        }
+        __syncthreads();
+        if (share == 1) return;
+#pragma unroll
+        for (int t = 0; t < KT; ++t) sum[t] += others[wave * (KT * 32) + 32 * t + col];
+    }
+#pragma unroll
     for (int t = 0; t < KT; ++t) {
-        sum[t] += __shfl_xor(sum[t], 32, 64);
         const int j = k0 + 32 * t + col;
         if (half != 0 || j >= I.n_keys) continue;
         if (A.parts > 1) { A.part_sums[(int64_t)blockIdx.x * KEYS + (j - key0)] = sum[t]; continue; }
@@ -333,8 +346,13 @@ int launch(const Args& A, const int kt, const int tiles, hipStream_t st)
 {
     const dim3 grid((unsigned)tiles * (unsigned)A.parts * (unsigned)A.g.Hkv), block(256);
     if (kt == 0) hipLaunchKernelGGL((sk_mass_stream<D, F32>), grid, block, (few_rows_bytes<D, F32>(A.lds_rows)), st, A);
-    else if (kt == 1) hipLaunchKernelGGL((sk_mass_rows<D, F32, 1>), grid, block, 0, st, A);
-    else if constexpr (!F32) hipLaunchKernelGGL((sk_mass_rows<D, F32, 4>), grid, block, 0, st, A);
+    else if constexpr (F32) hipLaunchKernelGGL((sk_mass_rows<D, F32, 1, 1>), grid, block, 0, st, A);
+    else if (kt == 4) hipLaunchKernelGGL((sk_mass_rows<D, F32, 4, 1>), grid, block, 0, st, A);
+    // At most a workgroup to a CU: eight waves, two to a SIMD, one at the matrix pipe while the other is at the vector unit.  us, four / eight:
+    // 256 tokens at 2,600 keys 24.1 / 19.9, 64 there 9.0 / 8.5; 20 tokens of 33 heads at 9,000 keys of one 14.0 / 11.6.  With more, waves of other workgroups
+    // do that: 64 at 9,001 12.7 / 17.0, 512 at 2,600 in parts 22.8 / 28.4.  (fp32: no difference.)
+    else if (A.parts == 1 && tiles * A.g.Hkv <= 256) hipLaunchKernelGGL((sk_mass_rows<D, F32, 1, 2>), grid, dim3(512), 0, st, A);
+    else hipLaunchKernelGGL((sk_mass_rows<D, F32, 1, 1>), grid, block, 0, st, A);
     if (A.parts > 1) hipLaunchKernelGGL(sk_mass_join, dim3((unsigned)tiles * (unsigned)A.g.Hkv), block, 0, st, A, 128 * kt);
     return (int)hipGetLastError();
 }
