@@ -295,6 +295,73 @@ def test_call_that_fails_on_the_device_leaves_the_session(site):
     _check(pool, a, model)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape,block,seed", [(D64, 16, 0), (D64, 16, 1), (D64, 64, 2), (synth.CFG1, 16, 3), (ODD, 16, 4), (D64, 256, 5)])
+def test_random_walk_with_other_calls(shape, block, seed):
+    """Sessions of a pool that is often full: appended to, cut in every way there is, forked, destroyed; all of them read back after each eviction."""
+    rng, gen = np.random.default_rng(seed), synth.generator(10, stream=40 + seed)
+    blocks = 2400 // block
+    pool = sk.Pool(shape.dtype, shape.n_q_heads, shape.n_kv_heads, shape.head_dim, block, blocks, max_sessions=5, max_batch_tokens=1024, kv_fill=0xFF)
+    pool.sk_pool_set_alloc_order(synth.permutation(gen, blocks))
+    models, refused, evicted = {}, 0, 0
+    for step in range(90):
+        sid = int(rng.choice(sorted(models))) if models else None
+        op = rng.choice(["append", "append", "evict", "evict", "evict", "oldest", "truncate", "fork", "freeze", "destroy"], p=[.2, .15, .2, .1, .1, .06, .05, .07, .05, .02])
+        try:
+            if sid is None or (op == "append" and len(models) < 5 and rng.random() < 0.3):
+                sid = pool.sk_session_create()
+                models[sid] = Model(shape, *(synth.to_raw(x[:0]) for x in synth.draw_qkv(gen, 1, shape)[1:]))
+                op = "append"
+            m = models[sid]
+            n = m.K.shape[0]
+            if op == "append":
+                _, k, v = synth.draw_qkv(gen, int(rng.integers(1, 500)), shape)
+                pool.sk_session_append(sid, None, k.cuda(), v.cuda())
+                m.K, m.V = np.concatenate([m.K, synth.to_raw(k)]), np.concatenate([m.V, synth.to_raw(v)])
+            elif op == "evict":
+                recent = int(rng.integers(0, 80))
+                count = int(rng.integers(0, max(n - m.frozen - recent, 0) + 1))
+                per_head, in_place = bool(rng.integers(2)), bool(rng.integers(2))
+                mass = _mass(gen, shape.n_kv_heads, n + 2, str(rng.choice(["spread", "few", "near", "equal"])))
+                place = mass.cuda()
+                out = pool.sk_session_evict_lowest(sid, place, count, min(recent, n), per_head, mass_out=None if in_place else torch.zeros_like(place))
+                torch.cuda.synchronize()
+                want = m.evict(mass[:, :n].numpy(), count, min(recent, n), per_head)
+                np.testing.assert_array_equal(out[:, :n].cpu().numpy(), want)
+                evicted += count > 0
+                for other in models:
+                    _check(pool, other, models[other])
+            elif op == "oldest":
+                count = int(rng.integers(0, max(n - m.frozen, 0) + 1)) // 3
+                pool.sk_session_evict_oldest(sid, count)
+                m.K, m.V = (np.concatenate([x[:m.frozen], x[m.frozen + count:]]) for x in (m.K, m.V))
+            elif op == "truncate":
+                count = int(rng.integers(n // 2, n + 1))
+                pool.sk_session_truncate(sid, count)
+                m.K, m.V, m.frozen = m.K[:count], m.V[:count], min(m.frozen, count)
+            elif op == "fork" and len(models) < 5:
+                prefix = int(rng.integers(0, n + 1))
+                new = pool.sk_session_fork(sid, prefix)
+                models[new] = Model(shape, m.K[:prefix], m.V[:prefix], min(m.frozen, prefix))
+            elif op == "freeze":
+                count = int(rng.integers(m.frozen, min(m.frozen + 100, n) + 1)) if n >= m.frozen else m.frozen
+                pool.sk_session_freeze(sid, count)
+                m.frozen = count
+            elif op == "destroy":
+                pool.sk_session_destroy(sid)
+                del models[sid]
+        except sk.SkError as e:
+            assert e.status == (sk.SK_E_INVAL if op == "freeze" else sk.SK_E_NOMEM), (step, op)
+            refused += 1
+    assert evicted > 5 and refused > 0
+    for sid, m in models.items():
+        _check(pool, sid, m)
+        if m.K.shape[0]:
+            _attend(pool, sid, m, gen)
+        pool.sk_session_destroy(sid)
+    assert pool.sk_pool_blocks_free() == blocks
+
+
 # ---- host half, without a GPU ---------------------------------------------------------------------------
 
 def _meta(**kw):
