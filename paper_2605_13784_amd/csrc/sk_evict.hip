@@ -213,9 +213,11 @@ __device__ __forceinline__ bool stays(const bool there, const uint32_t x, const 
     return s;
 }
 
-// One choice for all heads: the sum of the rows, head by head.
+// One choice for all heads: the sum of the rows, head by head.  The workgroups behind those of the candidates prepare.
 __global__ __launch_bounds__(256) void sk_evict_sums(const Args A)
 {
+    const int n_sums = (A.n_cand + 255) / 256;
+    if ((int)blockIdx.x >= n_sums) { prepare(A, blockIdx.x - n_sums, gridDim.x - n_sums); return; }
     const int i = blockIdx.x * 256 + threadIdx.x;
     if (i >= A.n_cand) return;
     const float* in = A.in + A.frozen + i;
@@ -225,7 +227,7 @@ __global__ __launch_bounds__(256) void sk_evict_sums(const Args A)
     A.sums[i] = s;
 }
 
-// Workgroups 0 .. n_lists - 1: one list each, of at most kKept candidates.  The others prepare.
+// Workgroups 0 .. n_lists - 1: one list each, of at most kKept candidates.  The others, if there are any, prepare.
 __global__ __launch_bounds__(kSelectThreads) void sk_evict_select(const Args A)
 {
     __shared__ Search S;
@@ -663,23 +665,24 @@ extern "C" int sk_session_evict_lowest(sk_pool* p, int32_t id, const float* mass
     hipStream_t st = (hipStream_t)hip_stream;
     if (sk_injected(p, SK_SITE_EVICT_SELECT)) return SK_E_HIP;
     if (runs) {
-        if (!A.per_head && A.n_cand > 0) {
-            hipLaunchKernelGGL(sk_evict_sums, dim3((unsigned)((A.n_cand + 255) / 256)), dim3(256), 0, st, A);
-            ++launches;
-        }
         const int64_t work = A.n_clear + A.n_old + A.n_lists * (E.len - V.win - E.n_cand) + (A.old_sums ? Hkv * (E.len - V.win) : 0);
         const unsigned others = (unsigned)(work / (8 * kSelectThreads) < 63 ? work / (8 * kSelectThreads) + 1 : 64);
-        if (A.n_parts == 0) hipLaunchKernelGGL(sk_evict_select, dim3(A.n_lists + others), dim3(kSelectThreads), 0, st, A);
+        const bool sums = !A.per_head && A.n_cand > 0;    // (a launch that the preparation goes along with)
+        if (sums) {
+            hipLaunchKernelGGL(sk_evict_sums, dim3((unsigned)((A.n_cand + 255) / 256) + others * (kSelectThreads / 256)), dim3(256), 0, st, A);
+            ++launches;
+        }
+        if (A.n_parts == 0) hipLaunchKernelGGL(sk_evict_select, dim3(A.n_lists + (sums ? 0 : others)), dim3(kSelectThreads), 0, st, A);
         else {
             const dim3 parts((unsigned)A.n_lists * (unsigned)A.n_parts);
-            hipLaunchKernelGGL(sk_evict_prepare, dim3(others), dim3(kSelectThreads), 0, st, A);
+            if (!sums) { hipLaunchKernelGGL(sk_evict_prepare, dim3(others), dim3(kSelectThreads), 0, st, A); ++launches; }
             if (n_evict > 0) {
                 hipLaunchKernelGGL(sk_evict_count, parts, dim3(kPartThreads), 0, st, A);
                 hipLaunchKernelGGL(sk_evict_gather, parts, dim3(kPartThreads), 0, st, A);
                 hipLaunchKernelGGL(sk_evict_search, dim3(A.n_lists), dim3(kSelectThreads), 0, st, A);
             }
             hipLaunchKernelGGL(sk_evict_emit, parts, dim3(kPartThreads), 0, st, A);
-            launches += n_evict > 0 ? 4 : 1;
+            launches += n_evict > 0 ? 3 : 0;
         }
         const int e = (int)hipGetLastError();
         sk_evict_listed(p, E, hip_stream);
