@@ -75,6 +75,11 @@ struct Top {
             int h;
             tie = bound_of(l, k - over, h);
             floor_idx = (int32_t)~tie;
+        } else if (t > kRankNone) {                       // what equals the bound, if anything does: a lower index, which a later step of the tile may bring, takes its place
+            uint32_t last = 0;
+#pragma unroll
+            for (int j = 0; j < N; ++j) last = max(last, hi[j] == t ? ~lo[j] : 0u);
+            floor_idx = (int32_t)__builtin_amdgcn_readfirstlane(wave_max(last));
         }
         int at = 0;
 #pragma unroll

@@ -234,3 +234,43 @@ def test_workspace_too_small_is_an_error():
     with pytest.raises(sk.SkError) as e:
         sk.sk_logprobs(x, n_top=4, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
     assert e.value.status == sk.SK_E_WORKSPACE
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,length,lower,twos", [("bf16", 2048, (0, 0), (5, 80, 81, 82)), ("f32", 2048, (100, 256), (40, 258, 296, 297))])
+def test_an_equal_logit_of_lower_index_comes_behind_a_cut(dtype, length, lower, twos):
+    """A flat row fills a wave's list in the middle of a tile, with exactly n_top logits of the largest value listed; one more of that
+    value follows, whose index is lower than some of theirs (a tile's steps are not in the order of indices)."""
+    x = torch.full((1, length), 1.0)
+    x[:, lower[0]:lower[1]] = -5.0
+    x[0, list(twos)] = 2.0
+    _check(x.to(synth.torch_dtype(dtype)).cuda(), x, torch.zeros((1, 1), dtype=torch.int32), 3)
+
+
+def _tied(rows, vocab, gen):
+    """Flat rows with a lower stretch at their start, in which a larger value is repeated many times by few lanes of one tile."""
+    x = torch.full((rows, vocab), 1.0)
+    for r in range(rows):
+        stretch = int(torch.randint(0, 400, (1,), generator=gen))
+        x[r, stretch:stretch + int(torch.randint(1, 400, (1,), generator=gen))] = -5.0
+        first = int(torch.randint(0, max(vocab - 600, 1), (1,), generator=gen)) if r % 2 else 0
+        lanes = torch.randint(0, min(64, vocab // 8), (1 + r % 9,), generator=gen)
+        for _ in range(6):
+            at = first + 8 * lanes + torch.randint(0, 8, lanes.shape, generator=gen)
+            x[r, at.clamp(max=vocab - 1)] = 2.0
+            at = first + 256 + 4 * lanes + torch.randint(0, 4, lanes.shape, generator=gen)
+            x[r, at.clamp(max=vocab - 1)] = 2.0
+    return x
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,vocab,pad", [(150, 2048, 0), (150, 2051, 2), (40, 9001, 0), (40, 40001, 3), (900, 5003, 0)])
+def test_ties_at_the_last_place_in_flat_rows(rows, vocab, pad, dtype):
+    gen = synth.generator(8, stream=rows + vocab + 1)
+    buf = torch.full((rows, vocab + pad), 3.0)
+    buf[:, :vocab] = _tied(rows, vocab, gen)
+    buf = buf.to(synth.torch_dtype(dtype))
+    x, xd = buf[:, :vocab].float(), buf.cuda()[:, :vocab]
+    for n_top in (1, 2, 3, 5, 8, 13, 20, 32):
+        _check(xd, x, torch.zeros((rows, 1), dtype=torch.int32), n_top)
