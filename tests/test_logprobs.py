@@ -274,3 +274,19 @@ def test_ties_at_the_last_place_in_flat_rows(rows, vocab, pad, dtype):
     x, xd = buf[:, :vocab].float(), buf.cuda()[:, :vocab]
     for n_top in (1, 2, 3, 5, 8, 13, 20, 32):
         _check(xd, x, torch.zeros((rows, 1), dtype=torch.int32), n_top)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_ties_over_parts_of_several_tiles(dtype):
+    """Rows in parts whose waves take two tiles each: what a later wave of a part reports has lower indices than some of an earlier one."""
+    rows, vocab = 100, 262144
+    gen = synth.generator(8, stream=12)
+    x = torch.full((rows, vocab), 1.0)
+    for r in range(rows):                                     # in tiles that are all over one part, or all over the row
+        at = torch.randint(0, 8 * 2048 if r % 2 else vocab, (20 + r,), generator=gen)
+        x[r, at] = 2.0
+    x = x.to(synth.torch_dtype(dtype))
+    assert sk.lib().sk_logprobs_workspace_bytes(rows, vocab, 32) == rows * 17 * 4 * (16 + 8 * 32)      # 17 parts of a row's 129 tiles: two to a wave
+    for n_top in (5, 32):
+        _check(x.cuda(), x.float(), torch.zeros((rows, 1), dtype=torch.int32), n_top)
