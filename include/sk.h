@@ -269,7 +269,7 @@ int sk_session_evict_oldest(sk_pool* pool, int32_t id, int64_t n_tokens, void* h
  * another item's arrays.  The caller keeps these arrays beside the session: an append's tokens come behind the last entry (put 0
  * there, or pass keep 0), sk_session_evict_lowest moves the entries with the tokens, sk_session_evict_oldest(n) takes out
  * n entries behind the frozen ones.  Sums are fp32, in an order that depends on the shapes only.  Nothing of the session changes; the
- * call enqueues kernels only and can be captured like sk_session_query.
+ * call enqueues kernels only and can be captured like sk_session_query.  What mass_out holds after SK_E_HIP is undefined.
  * The batched form does the same for item i's rows cu_tokens[i]..cu_tokens[i+1]-1 and its own arrays (HOST arrays, the pointers in
  * them DEVICE; causal NULL: all 0; mass_in NULL: none).  A session may appear once.
  */
@@ -299,7 +299,11 @@ int sk_batch_attention_mass(sk_pool* pool, int32_t n_items, const int32_t* sessi
  * More than there are to choose from: SK_E_INVAL.  SK_E_WORKSPACE if the lists that the call makes (at most 12 bytes a token and KV
  * head with per_head != 0, else 12 a token, and 4 a token and KV head where mass_out is mass_in) exceed the part of the workspace that
  * holds split partials (at least 134 MB for 128 dims, 67 MB for 64).
- * All or nothing.  Kernels only, ordered on hip_stream like the session's other calls; host metadata change with every call, so a
+ * All or nothing: a refused call changes nothing, and if a HIP call fails half way (SK_E_HIP) the session's length, block table and tokens,
+ * the free list, and sums in place are as before; what a mass_out of its own holds then is undefined.  One exception: where tokens move
+ * within the session's own blocks and a launch fails behind the first that wrote there, the K and V of the session's tokens behind the
+ * frozen ones are undefined (those of other sessions are as before): truncate it to its frozen tokens, or destroy it.
+ * Kernels only, ordered on hip_stream like the session's other calls; host metadata change with every call, so a
  * capture of it cannot be replayed.  On a metadata-only pool the host half alone runs.
  */
 int sk_session_evict_lowest(sk_pool* pool, int32_t id, const float* mass_in, int64_t mass_in_stride,

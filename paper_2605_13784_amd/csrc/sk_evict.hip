@@ -691,13 +691,15 @@ extern "C" int sk_session_evict_lowest(sk_pool* p, int32_t id, const float* mass
             return sk_note_hip_error(e);
         }
     }
-    int e = sk_injected(p, SK_SITE_EVICT_MOVE) ? (int)hipErrorUnknown : 0;
-    if (runs && !e) {
-        for (int64_t c = 0; c < chunks && !e; c += round) {
-            const dim3 grid((unsigned)((chunks - c < round ? chunks - c : round) * Hkv)), block(256);
-            A.chunk0 = (int32_t)c;
+    int e = 0;
+    bool moved = false;
+    auto failed = [&] { return sk_injected(p, SK_SITE_EVICT_MOVE) ? (int)hipErrorUnknown : 0; };
+    if (!runs) e = failed();
+    for (int64_t c = 0; runs && c < chunks && !e; c += round) {
+        const dim3 grid((unsigned)((chunks - c < round ? chunks - c : round) * Hkv)), block(256);
+        A.chunk0 = (int32_t)c;
 #define SK_EVICT(kernel)                                                                                            \
-    do {                                                                                                            \
+    if ((e = failed()) == 0) {                                                                                      \
         if (A.g.elem == 4) {                                                                                        \
             if (A.g.d == 128) hipLaunchKernelGGL((kernel<128, true>), grid, block, 0, st, A);                       \
             else hipLaunchKernelGGL((kernel<64, true>), grid, block, 0, st, A);                                     \
@@ -706,14 +708,17 @@ extern "C" int sk_session_evict_lowest(sk_pool* p, int32_t id, const float* mass
             else hipLaunchKernelGGL((kernel<64, false>), grid, block, 0, st, A);                                    \
         }                                                                                                           \
         ++launches;                                                                                                 \
-    } while (0)
-            SK_EVICT(sk_evict_move);
-            if (A.staged) SK_EVICT(sk_evict_put);
+        e = (int)hipGetLastError();                                                                                 \
+        moved = true;                                                                                               \
+    }
+        SK_EVICT(sk_evict_move)
+        if (A.staged && !e) SK_EVICT(sk_evict_put)
 #undef SK_EVICT
-            e = (int)hipGetLastError();
-        }
     }
     if (e) {
+        if (moved && A.old_sums)                          // sums in place: as they were
+            for (int64_t h = 0; h < Hkv; ++h)
+                (void)hipMemcpyAsync(mass_out + h * mass_out_stride + V.frozen, A.old_sums + h * (E.len - V.win), size_t(E.len - V.win) * 4, hipMemcpyDeviceToDevice, st);
         if (runs) sk_evict_undo(p, E, hip_stream);
         return sk_note_hip_error(e);
     }

@@ -482,3 +482,76 @@ def test_refusals():
     assert L.sk_session_evict_lowest(pool.h, sid, ctypes.c_void_p(mass.data_ptr()), 100, 10, 0, 0, None, 0, ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)) == sk.SK_OK
     model.evict(mass.cpu().numpy(), 10, 0, False)
     _check(pool, sid, model)
+
+
+MANY_HEADS = synth.Shape("bf16", 32, 32, 64)
+
+
+def _make_with_a_small_workspace(gen, n, frozen, evicted):
+    """A session of MANY_HEADS, 8 KiB a token, in a pool that has too few free blocks and a workspace that holds about 8,200 tokens of it."""
+    shape, blocks = MANY_HEADS, -(-(n + evicted) // 16) + 9
+    pool = sk.Pool("bf16", 32, 32, 64, 16, blocks, max_sessions=3, max_batch_tokens=64, kv_fill=0xFF)
+    pool.sk_pool_set_alloc_order(synth.permutation(gen, blocks))
+    sid = pool.sk_session_create()
+    k, v = (torch.randint(-0x7000, 0x7000, (n + evicted, 32, 64), generator=gen, dtype=torch.int16).view(torch.bfloat16) for _ in range(2))
+    kd, vd = k.cuda(), v.cuda()
+    for t in range(0, n + evicted, 64):
+        pool.sk_session_append(sid, None, kd[t:t + 64], vd[t:t + 64])
+    pool.sk_session_freeze(sid, frozen)
+    pool.sk_session_evict_oldest(sid, evicted)
+    k, v = (synth.to_raw(torch.cat([x[:frozen], x[frozen + evicted:]])) for x in (k, v))
+    return pool, sid, Model(shape, k, v, frozen)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,n_evict,n_recent,per_head", [(20011, 700, 50, True), (19001, 6000, 0, True), (20011, 3333, 10000, False)])
+def test_moves_in_several_stretches(n, n_evict, n_recent, per_head):
+    """Too few free blocks, and a workspace that holds less than half of what stays."""
+    gen = synth.generator(10, stream=n_evict)
+    pool, sid, model = _make_with_a_small_workspace(gen, n, 23, 11)
+    launches = pool.sk_pool_get_stats()["launches"]
+    mass = _mass(gen, 32, n)
+    place = mass.cuda()
+    want = model.evict(mass.numpy(), n_evict, n_recent, per_head)
+    pool.sk_session_evict_lowest(sid, place, n_evict, n_recent, per_head)
+    torch.cuda.synchronize()
+    assert pool.sk_pool_get_stats()["launches"] - launches >= 1 + 2 * 2 + (not per_head)       # selection, and move and put of each stretch
+    np.testing.assert_array_equal(place.cpu().numpy(), want)
+    _check(pool, sid, model)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("launch", [2, 3, 4])
+def test_a_launch_that_fails_between_the_moves(launch):
+    """Too few free blocks, sums in place: the launches are move and put, stretch by stretch.  Up to the first put nothing has changed; behind
+    it the tokens that are not frozen are undefined, and all else is as it was."""
+    n, frozen, n_evict = 19001, 23, 1500
+    gen = synth.generator(10, stream=launch)
+    pool, sid, model = _make_with_a_small_workspace(gen, n, frozen, 11)
+    fork = pool.sk_session_fork(sid, 60)
+    other = Model(MANY_HEADS, model.K[:60], model.V[:60])
+    mass = _mass(gen, 32, n + 3)
+    place = mass.cuda()
+
+    def state():
+        return pool.sk_session_length(sid), pool.sk_session_block_table(sid), pool.sk_pool_blocks_free(), pool.sk_pool_get_stats()["tokens_evicted"]
+
+    before = state()
+    pool.sk_pool_inject_failure(sk.SK_SITE_EVICT_MOVE, launch)
+    with pytest.raises(sk.SkError) as e:
+        pool.sk_session_evict_lowest(sid, place, n_evict, 5)
+    assert e.value.status == sk.SK_E_HIP
+    torch.cuda.synchronize()
+    assert state() == before and torch.equal(place.cpu(), mass)
+    _check(pool, fork, other)
+    if launch == 2:
+        _check(pool, sid, model)
+        want = model.evict(mass[:, :n].numpy(), n_evict, 5, True)
+        pool.sk_session_evict_lowest(sid, place, n_evict, 5)
+        torch.cuda.synchronize()
+        np.testing.assert_array_equal(place[:, :n].cpu().numpy(), want)
+    else:
+        pool.sk_session_truncate(sid, frozen)
+        model = Model(MANY_HEADS, model.K[:frozen], model.V[:frozen], frozen)
+    _check(pool, sid, model)
+    _check(pool, fork, other)
