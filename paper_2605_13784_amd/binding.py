@@ -180,6 +180,17 @@ def _stream(stream):
     return stream
 
 
+def _made(stream, *tensors):
+    """Tensors that a call makes here, as outputs or scratch, for a stream that is named: their memory came from the current one, and the
+    allocator may not hand it out again, however early they are dropped, before that stream has come to here."""
+    if stream is not None:
+        if not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(getattr(stream, "value", stream) or 0)
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+
+
 def _ck(status, where):
     if status != SK_OK:
         raise SkError(status, where)
@@ -323,17 +334,18 @@ class Pool:
         return int(lib().sk_pool_element_offset(self.h, block, kv_head, int(is_v), slot, dim))
 
     # -- compute ---------------------------------------------------------------------------
-    def _out(self, T, out_dtype, want_lse):
+    def _out(self, T, out_dtype, want_lse, stream):
         odt = torch.float32 if _dt(out_dtype) == SK_F32 else torch.bfloat16
         out = torch.empty((T, self.Hq, self.d), dtype=odt, device=self.device)
         lse = torch.empty((T, self.Hq), dtype=torch.float32, device=self.device) if want_lse else None
+        _made(stream, out, lse)
         return out, lse
 
     def sk_session_append(self, sid, q, k, v, out=None, lse=None, out_dtype="f32", want_lse=True, stream=None,
                           n_tokens=None):
         L = int(k.shape[0]) if n_tokens is None else int(n_tokens)
         if q is not None and out is None and self.kv_mem is not None:
-            out, lse = self._out(L, out_dtype, want_lse)
+            out, lse = self._out(L, out_dtype, want_lse, stream)
         _ck(lib().sk_session_append(self.h, sid, _p(q), _p(k), _p(v), L, _p(out), _dt(out_dtype), _p(lse),
                                     _stream(stream) if self.kv_mem is not None else None), "sk_session_append")
         return out, lse
@@ -347,7 +359,7 @@ class Pool:
                          n_splits=0, stream=None):
         nq = int(q.shape[0])
         if out is None:
-            out, lse = self._out(nq, out_dtype, want_lse)
+            out, lse = self._out(nq, out_dtype, want_lse, stream)
         _ck(lib().sk_session_query(self.h, sid, _p(q), _p(k), _p(v), nq, _p(out), _dt(out_dtype), _p(lse),
                                    int(n_splits), _stream(stream)), "sk_session_query")
         return out, lse
@@ -357,7 +369,7 @@ class Pool:
         n = len(session_ids)
         T = int(cu_tokens[-1])
         if out is None:
-            out, lse = self._out(T, out_dtype, want_lse)
+            out, lse = self._out(T, out_dtype, want_lse, stream)
         sid = (ctypes.c_int32 * n)(*[int(x) for x in session_ids])
         op = (ctypes.c_int32 * n)(*[int(x) for x in ops])
         cu = (ctypes.c_int32 * (n + 1))(*[int(x) for x in cu_tokens])
@@ -369,8 +381,8 @@ class Pool:
                                        stream=None):
         P = 0 if qp is None else int(qp.shape[0])
         NQ, Sfx = int(qs.shape[0]), int(qs.shape[1])
-        out_p, lse_p = self._out(P, out_dtype, want_lse)
-        out_s, lse_s = self._out(NQ * Sfx, out_dtype, want_lse)
+        out_p, lse_p = self._out(P, out_dtype, want_lse, stream)
+        out_s, lse_s = self._out(NQ * Sfx, out_dtype, want_lse, stream)
         _ck(lib().sk_session_query_shared_prefix(self.h, sid, _p(qp), _p(kp), _p(vp), P, _p(qs), _p(ks), _p(vs),
                                                  NQ, Sfx, _p(out_p), _p(out_s), _dt(out_dtype), _p(lse_p),
                                                  _p(lse_s), _stream(stream)), "sk_session_query_shared_prefix")
@@ -395,7 +407,10 @@ class Pool:
         place, or a new [Hkv, length]."""
         n, n_tok = self._length(sid), 0 if q is None else q.shape[0]
         if mass_out is None:
-            mass_out = mass_in if mass_in is not None else torch.empty((self.Hkv, n), dtype=torch.float32, device=self.device)
+            mass_out = mass_in
+            if mass_in is None:
+                mass_out = torch.empty((self.Hkv, n), dtype=torch.float32, device=self.device)
+                _made(stream, mass_out)
         assert q is None or (q.dtype is self.torch_dtype and lse.dtype is torch.float32 and q.numel() == n_tok * self.Hq * self.d and lse.numel() == n_tok * self.Hq)
         po, so = self._mass(mass_out, n)
         pi, si = (None, 0) if mass_in is None or keep == 0 else (po, so) if mass_in is mass_out else self._mass(mass_in, n)
@@ -420,7 +435,10 @@ class Pool:
         n = len(session_ids)
         lengths = [self._length(s) for s in session_ids]
         if mass_out is None:
-            mass_out = mass_in if mass_in is not None else [torch.empty((self.Hkv, m), dtype=torch.float32, device=self.device) for m in lengths]
+            mass_out = mass_in
+            if mass_in is None:
+                mass_out = [torch.empty((self.Hkv, m), dtype=torch.float32, device=self.device) for m in lengths]
+                _made(stream, *mass_out)
         assert q.dtype is self.torch_dtype and lse.dtype is torch.float32 and q.numel() >= cu_tokens[-1] * self.Hq * self.d and lse.numel() >= cu_tokens[-1] * self.Hq
 
         def host(arrays):
@@ -439,6 +457,7 @@ class Pool:
             count = self.sk_session_length(sid) - first
         k = torch.empty((count, self.Hkv, self.d), dtype=self.torch_dtype, device=self.device)
         v = torch.empty_like(k)
+        _made(stream, k, v)
         _ck(lib().sk_session_gather(self.h, sid, first, count, _p(k), _p(v), _stream(stream)), "sk_session_gather")
         return k, v
 
@@ -457,6 +476,7 @@ def sk_top2_static(logits, outputs=None, stream=None):
     rows, vocab = logits.shape
     if outputs is None:
         outputs = top2_outputs(rows, logits.device)
+        _made(stream, *outputs)
     idx1, idx2, val1, val2, gap = outputs
     _ck(lib().sk_top2_static(logits.data_ptr() if rows else None, rows, vocab,
                              logits.stride(0) if rows else vocab, _p(idx1), _p(idx2), _p(val1), _p(val2), _p(gap),
@@ -471,7 +491,11 @@ def sk_top2(logits, stream=None, workspace=None, outputs=None):
     rows, vocab = logits.shape
     if workspace is None:
         workspace = torch.empty(max(lib().sk_top2_workspace_bytes(rows, vocab), 16), dtype=torch.uint8, device=logits.device)
-    idx1, idx2, val1, val2, gap = outputs if outputs is not None else top2_outputs(rows, logits.device)
+        _made(stream, workspace)
+    if outputs is None:
+        outputs = top2_outputs(rows, logits.device)
+        _made(stream, *outputs)
+    idx1, idx2, val1, val2, gap = outputs
     _ck(lib().sk_top2(logits.data_ptr() if rows else None, rows, vocab, logits.stride(0) if rows else vocab, _p(workspace),
                       workspace.numel(), _p(idx1), _p(idx2), _p(val1), _p(val2), _p(gap), _stream(stream)), "sk_top2")
     return idx1, idx2, val1, val2, gap
@@ -496,12 +520,14 @@ def sk_logprobs(logits, tokens=None, n_top=0, workspace=None, outputs=None, stre
         n_tokens = tokens.shape[1]
     if outputs is None:
         outputs = logprobs_outputs(rows, n_tokens, n_top, logits.device)
+        _made(stream, *outputs)
     logprob, lse, entropy, top_idx, top_logprob = outputs
     assert top_idx is None or (top_idx.dtype is torch.int32 and top_idx.numel() == rows * n_top and top_idx.is_cuda)
     for t, n in ((logprob, rows * n_tokens), (lse, rows), (entropy, rows), (top_logprob, rows * n_top)):
         assert t is None or (t.dtype is torch.float32 and t.numel() == n and t.is_cuda)
     if workspace is None:
         workspace = torch.empty(max(lib().sk_logprobs_workspace_bytes(rows, vocab, n_top), 16), dtype=torch.uint8, device=logits.device)
+        _made(stream, workspace)
     # (a single row may have any stride)
     _ck(lib().sk_logprobs(logits.data_ptr() if rows else None, _dt(logits.dtype), rows, vocab, logits.stride(0) if rows > 1 else vocab, _p(tokens), n_tokens,
                           n_top, _p(workspace), workspace.numel() * workspace.element_size(), _p(logprob), _p(lse), _p(entropy), _p(top_idx), _p(top_logprob),

@@ -290,3 +290,41 @@ def test_ties_over_parts_of_several_tiles(dtype):
     assert sk.lib().sk_logprobs_workspace_bytes(rows, vocab, 32) == rows * 17 * 4 * (16 + 8 * 32)      # 17 parts of a row's 129 tiles: two to a wave
     for n_top in (5, 32):
         _check(x.cuda(), x.float(), torch.zeros((rows, 1), dtype=torch.int32), n_top)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("call", ["logprobs", "top2"])
+@pytest.mark.parametrize("handle", [False, True])
+def test_scratch_of_a_call_on_another_stream_is_not_handed_out_before_it_has_run(call, handle):
+    """The workspace that the binding makes and drops: as long as the stream of the call is busy, tensors of the current one do not get it."""
+    rows, vocab = (100, 262144) if call == "logprobs" else (4200, 128256)
+    L = sk.lib()
+    need = L.sk_logprobs_workspace_bytes(rows, vocab, 32) if call == "logprobs" else L.sk_top2_workspace_bytes(rows, vocab)
+    assert need > 1 << 20                                     # apart from small tensors
+    x = torch.randn((rows, vocab), device="cuda")
+    want = [t.clone() for t in (sk.sk_logprobs(x, n_top=32) if call == "logprobs" else sk.sk_top2(x))]
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    a = torch.empty(need, dtype=torch.uint8, device="cuda")
+    place = a.data_ptr()
+    del a
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(50_000_000)                         # tens of milliseconds
+    stream = side.cuda_stream if handle else side
+    got = sk.sk_logprobs(x, n_top=32, stream=stream) if call == "logprobs" else sk.sk_top2(x, stream=stream)
+    b = torch.empty(need, dtype=torch.uint8, device="cuda")
+    busy = not side.query()
+    assert busy and b.data_ptr() != place
+    torch.cuda.synchronize()
+    for g, w in zip(got, want):
+        assert torch.equal(g, w)
+    # a call on the current stream takes that place and leaves it to the next tensor
+    del b
+    torch.cuda.empty_cache()
+    a = torch.empty(need, dtype=torch.uint8, device="cuda")
+    place = a.data_ptr()
+    del a
+    got = sk.sk_logprobs(x, n_top=32) if call == "logprobs" else sk.sk_top2(x)
+    assert torch.empty(need, dtype=torch.uint8, device="cuda").data_ptr() == place
