@@ -18,3 +18,13 @@ def test_random_walk_over_the_host_library_under_asan_and_ubsan():
         assert r.returncode == 0, r.stdout[-2000:] + r.stderr[-6000:]
         assert "host walk ok" in r.stdout
         assert "runtime error" not in r.stderr and "AddressSanitizer" not in r.stderr
+
+
+def test_random_walk_over_eviction_by_weight_under_asan_and_ubsan():
+    with tempfile.TemporaryDirectory() as tmp:
+        exe = _build.build_host_check(os.path.join(HERE, "host_sanitize_evict_driver.cpp"), os.path.join(tmp, "host_check"))
+        env = dict(os.environ, ASAN_OPTIONS="detect_leaks=1:abort_on_error=0", UBSAN_OPTIONS="print_stacktrace=1")
+        r = subprocess.run([exe, "6000"], capture_output=True, text=True, timeout=600, env=env)
+        assert r.returncode == 0, r.stdout[-2000:] + r.stderr[-6000:]
+        assert "host walk ok" in r.stdout
+        assert "runtime error" not in r.stderr and "AddressSanitizer" not in r.stderr
