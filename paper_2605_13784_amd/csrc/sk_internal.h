@@ -219,7 +219,14 @@ static inline bool sk_rows_overlap(const float* a, int64_t stride_a, const float
     if (a == b && stride_a == stride_b) return false;
     const int64_t d = b - a;
     if (d >= (rows - 1) * stride_a + n || -d >= (rows - 1) * stride_b + n) return false;
-    if (stride_a != stride_b) return true;
+    if (stride_a != stride_b) {
+        for (int64_t i = 0; i < rows; ++i) {       // against the rows of b that start in front of row i of a and behind it
+            const int64_t x = i * stride_a - d, j = x < 0 ? -1 : x / stride_b;
+            if (j >= 0 && j < rows && x - j * stride_b < n) return true;
+            if (j + 1 < rows && (j + 1) * stride_b - x < n) return true;
+        }
+        return false;
+    }
     const int64_t m = ((d % stride_a) + stride_a) % stride_a;      // rows of one array between those of the other
     return m < n || stride_a - m < n;
 }
