@@ -419,13 +419,15 @@ class Pool:
         return mass_out
 
     def sk_session_evict_lowest(self, sid, mass_in, n_evict, n_recent=0, per_head=True, mass_out=None, stream=None):
-        """mass_in: float32 [Hkv, capacity]; the sums of what stays go to mass_out, left out: mass_in in place.  Metadata-only pools:
-        mass_in None."""
+        """mass_in: float32 [Hkv, capacity]; the sums of what stays go to mass_out, left out: mass_in in place; False: they are not kept, and
+        mass_in stays as it is.  Metadata-only pools: mass_in None."""
         pi, si, po, so = None, 0, None, 0
+        mass_out = mass_in if mass_out is None else None if mass_out is False else mass_out
         if self.kv_mem is not None:
             n = self._length(sid)
-            mass_out = mass_in if mass_out is None else mass_out
-            (pi, si), (po, so) = self._mass(mass_in, n), self._mass(mass_out, n)
+            pi, si = self._mass(mass_in, n)
+            if mass_out is not None:
+                po, so = self._mass(mass_out, n)
         _ck(lib().sk_session_evict_lowest(self.h, sid, pi, si, int(n_evict), int(n_recent), int(bool(per_head)), po, so,
                                           _stream(stream) if self.kv_mem is not None else None), "sk_session_evict_lowest")
         return mass_out

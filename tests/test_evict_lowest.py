@@ -555,3 +555,18 @@ def test_a_launch_that_fails_between_the_moves(launch):
         model = Model(MANY_HEADS, model.K[:frozen], model.V[:frozen], frozen)
     _check(pool, sid, model)
     _check(pool, fork, other)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("room", [False, True])
+@pytest.mark.parametrize("shape,n,block,n_evict,per_head", [(D64, 700, 16, 300, True), (ODD, 900, 64, 77, False), (F32_WIDE, 600, 16, 64, True), (D64, 33000, 64, 1000, False)])
+def test_sums_that_are_not_kept(shape, n, block, n_evict, per_head, room):
+    gen = synth.generator(10, stream=n)
+    pool, sid, model = _make(shape, gen, n, block, 20, 5, spare=9 + (n // block if room else 0))
+    mass = _mass(gen, shape.n_kv_heads, n + 1)
+    place = mass.cuda()
+    model.evict(mass[:, :n].numpy(), n_evict, 6, per_head)
+    assert pool.sk_session_evict_lowest(sid, place, n_evict, 6, per_head, mass_out=False) is None
+    torch.cuda.synchronize()
+    assert torch.equal(place.cpu(), mass)
+    _check(pool, sid, model)
