@@ -570,3 +570,28 @@ def test_sums_that_are_not_kept(shape, n, block, n_evict, per_head, room):
     torch.cuda.synchronize()
     assert torch.equal(place.cpu(), mass)
     _check(pool, sid, model)
+
+
+@pytest.mark.gpu
+def test_sums_of_a_stream_grow_by_a_weight_of_one_a_row():
+    """Sums in place over appends, queries and evictions: every row of a call adds a weight of one to each KV head, to the 1e-3 that the
+    library states for lse, and an eviction takes away what the tokens that leave had."""
+    shape = synth.CFG2
+    gen = synth.generator(10, stream=13)
+    pool, sid, model = _make(shape, gen, 64, 16, spare=80)
+    mass = torch.zeros((8, 1200), device="cuda")
+    total = torch.zeros(8, dtype=torch.float64)
+    for L in (300, 1, 77, 256):
+        q, k, v = (x.cuda() for x in synth.draw_qkv(gen, L, shape))
+        _, lse = pool.sk_session_append(sid, q, k, v)
+        pool.sk_session_attention_mass(sid, q, lse, causal=True, mass_in=mass)
+        for T in (9, 32):
+            _, lse = pool.sk_session_query(sid, q[:T]) if T <= L else pool.sk_session_query(sid, q[:1].repeat(T, 1, 1))
+            pool.sk_session_attention_mass(sid, q[:T] if T <= L else q[:1].repeat(T, 1, 1), lse, mass_in=mass)
+        torch.cuda.synchronize()
+        grown = mass.double().sum(1).cpu() - total
+        assert torch.all((grown / ((L + 41) * shape.group) - 1).abs() <= 1.1e-3)
+        n = pool.sk_session_length(sid)
+        if n > 300:
+            pool.sk_session_evict_lowest(sid, mass, n - 300, 64)
+        total = mass.double().sum(1).cpu()
