@@ -41,7 +41,6 @@ struct Args {
     int32_t len, new_len, first;      // storage indices, see sk_evict
     int32_t n_evict, n_cand;
     int32_t blk0, n_blk, n_fresh;
-    int32_t n_chunks;                 // groups of kSlots slots from `first` to len
     const float* in;
     int64_t in_stride;
     float* out;
@@ -632,7 +631,6 @@ extern "C" int sk_session_evict_lowest(sk_pool* p, int32_t id, const float* mass
         A.table_new = E.table; A.tables_rw = E.tables_rw; A.kv_rw = E.kv_rw;
         chunks = (E.len - E.first + kSlots - 1) / kSlots;
         if (chunks < 1) chunks = 1;                       // (no token behind the frozen ones: their sums are copied)
-        A.n_chunks = (int32_t)chunks;
         A.n_old = (int32_t)((E.len + V.g.B - 1) / V.g.B - E.blk0);
         unsigned char* at = V.scratch;
         A.keep = take<int32_t>(at, (int64_t)A.n_lists * (E.new_len - V.win));

@@ -31,7 +31,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 struct Args {
     const void* logits;
     int64_t row_stride;
-    int32_t rows, vocab, n_tokens, n_top;
+    int32_t vocab, n_tokens, n_top;
     int32_t parts, tiles;             // workgroups to a row; tiles that each of their waves takes
     const int32_t* tokens;
     float *logprob, *lse, *entropy;
@@ -522,7 +522,7 @@ int sk_logprobs(const void* logits, int dtype, int32_t rows, int32_t vocab, int6
     const size_t need = sk_logprobs_workspace_bytes(rows, vocab, n_top);
     if (need > 0 && !workspace) return SK_E_INVAL;
     if (workspace_bytes < need) return SK_E_WORKSPACE;
-    A.logits = logits; A.row_stride = row_stride; A.rows = rows; A.vocab = vocab; A.n_tokens = n_tokens; A.n_top = n_top;
+    A.logits = logits; A.row_stride = row_stride; A.vocab = vocab; A.n_tokens = n_tokens; A.n_top = n_top;
     A.tokens = tokens; A.logprob = logprob; A.lse = lse; A.entropy = entropy; A.top_idx = top_idx; A.top_logprob = top_logprob;
     A.stats = (float4*)workspace;
     A.keys = (uint64_t*)((unsigned char*)workspace + stats_bytes(rows, A.parts));
