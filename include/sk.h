@@ -298,7 +298,7 @@ int sk_batch_attention_mass(sk_pool* pool, int32_t n_items, const int32_t* sessi
  * which are never written, are replaced (SK_E_NOMEM if the free ones do not suffice for that; a session that shares none needs none).
  * More than there are to choose from: SK_E_INVAL.  SK_E_WORKSPACE if the lists that the call makes (at most 12 bytes a token and KV
  * head with per_head != 0, else 12 a token, and 4 a token and KV head where mass_out is mass_in) exceed the part of the workspace that
- * holds split partials (at least 134 MB for 128 dims, 67 MB for 64).
+ * holds split partials (at least 134 MB for 128 dims, 67 MB for 64), or leave no room in it for 64 tokens where they move by way of it.
  * All or nothing: a refused call changes nothing, and if a HIP call fails half way (SK_E_HIP) the session's length, block table and tokens,
  * the free list, and sums in place are as before; what a mass_out of its own holds then is undefined.  One exception: where tokens move
  * within the session's own blocks and a launch fails behind the first that wrote there, the K and V of the session's tokens behind the

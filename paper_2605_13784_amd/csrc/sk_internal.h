@@ -211,6 +211,7 @@ bool sk_injected(sk_pool* p, int site);                                      // 
 
 bool sk_sessions_differ(sk_pool* p, int32_t n, const int32_t* id);           // ids of live sessions
 int sk_note_hip_error(int hip_error);                                        // for sk_last_hip_error; returns SK_E_HIP
+static inline int sk_status_of(int hip_error) { return hip_error ? sk_note_hip_error(hip_error) : 0 /* SK_OK */; }
 void sk_count_launch(sk_pool* p);
 
 // Whether arrays of `rows` rows of n floats meet other than in the same place, for a call's arrays of sums that it reads and write.

@@ -14,6 +14,7 @@
 #include <stdint.h>
 #include <limits.h>
 #include "../../include/sk.h"
+#include "sk_internal.h"
 #include "sk_order.h"
 
 namespace {
@@ -543,7 +544,7 @@ int sk_logprobs(const void* logits, int dtype, int32_t rows, int32_t vocab, int6
     else SK_LOGPROBS(sk_logprobs_scan, grid, kWaves, kWaves);
     if (A.parts > 1) SK_LOGPROBS(sk_logprobs_join, dim3(rows), kWaves);
 #undef SK_LOGPROBS
-    return hipGetLastError() == hipSuccess ? SK_OK : SK_E_HIP;
+    return sk_status_of((int)hipGetLastError());
 }
 
 }  // extern "C"

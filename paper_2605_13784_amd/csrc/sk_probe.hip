@@ -5,6 +5,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 #include "../../include/sk.h"
+#include "sk_internal.h"
 
 namespace {
 
@@ -98,7 +99,7 @@ int sk_probe_read(const void* src, size_t bytes, int32_t n_workgroups, int32_t n
     else
         hipLaunchKernelGGL(sk_probe_read_kernel<false>, dim3((unsigned)n_workgroups), dim3(256), 0, (hipStream_t)hip_stream,
                            (const u32x4*)src, bytes / 16, 0x9e3779b9u, (uint32_t*)sink);
-    return hipGetLastError() == hipSuccess ? SK_OK : SK_E_HIP;
+    return sk_status_of((int)hipGetLastError());
 }
 
 int sk_probe_mfma(int32_t n_workgroups, int32_t iters, const void* operands, size_t operand_bytes, void* sink,
@@ -109,7 +110,7 @@ int sk_probe_mfma(int32_t n_workgroups, int32_t iters, const void* operands, siz
     hipLaunchKernelGGL(sk_probe_mfma_kernel, dim3((unsigned)n_workgroups), dim3(512), 0, (hipStream_t)hip_stream,
                        (int)iters, 0x7fc12345u, (float*)sink, (const uint4*)operands, (uint32_t)(operand_bytes / 16));
     if (flops_out) *flops_out = double(n_workgroups) * 8.0 /*waves*/ * double(iters) * 8.0 /*products*/ * (2.0 * 32 * 32 * 16);
-    return hipGetLastError() == hipSuccess ? SK_OK : SK_E_HIP;
+    return sk_status_of((int)hipGetLastError());
 }
 
 }  // extern "C"

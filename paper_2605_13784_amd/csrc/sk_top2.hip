@@ -6,6 +6,7 @@
 #include <limits.h>
 #include <mutex>
 #include "../../include/sk.h"
+#include "sk_internal.h"
 
 // First-pass pairs of sk_top2_static: part of the device image, so no call ever allocates it.  In
 // host code this name is only a handle for hipGetSymbolAddress; kernels get the address it returns.
@@ -195,11 +196,11 @@ int sk_top2(const float* logits, int32_t rows, int32_t vocab, int64_t row_stride
     if (n_chunks <= 2) {
         if (n_chunks == 1) hipLaunchKernelGGL(sk_top2_row<1>, dim3(rows), dim3(256), 0, st, logits, row_stride, vocab, idx1, idx2, val1, val2, gap);
         else hipLaunchKernelGGL(sk_top2_row<2>, dim3(rows), dim3(512), 0, st, logits, row_stride, vocab, idx1, idx2, val1, val2, gap);
-        return hipGetLastError() == hipSuccess ? SK_OK : SK_E_HIP;
+        return sk_status_of((int)hipGetLastError());
     }
     hipLaunchKernelGGL(sk_top2_partial, dim3(n_chunks, rows), dim3(256), 0, st, logits, row_stride, vocab, n_chunks, (Top2*)workspace);
     hipLaunchKernelGGL(sk_top2_final, dim3(rows), dim3(256), 0, st, (const Top2*)workspace, n_chunks, idx1, idx2, val1, val2, gap);
-    return hipGetLastError() == hipSuccess ? SK_OK : SK_E_HIP;
+    return sk_status_of((int)hipGetLastError());
 }
 
 // Device address of `scratch` on the current device, looked up once per device.
@@ -209,11 +210,14 @@ static int static_scratch(void** out)
     static void* ptr_of[kMaxDevices];
     static std::mutex mu;
     int dev = -1;
-    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return SK_E_HIP;
+    hipError_t e = hipGetDevice(&dev);
+    if (e == hipSuccess && (dev < 0 || dev >= kMaxDevices)) e = hipErrorInvalidDevice;
+    if (e != hipSuccess) return sk_note_hip_error((int)e);
     std::lock_guard<std::mutex> lock(mu);
     if (!ptr_of[dev]) {
         void* ptr = nullptr;
-        if (hipGetSymbolAddress(&ptr, HIP_SYMBOL(scratch)) != hipSuccess || !ptr) return SK_E_HIP;
+        e = hipGetSymbolAddress(&ptr, HIP_SYMBOL(scratch));
+        if (e != hipSuccess || !ptr) return sk_note_hip_error((int)(e != hipSuccess ? e : hipErrorInvalidSymbol));
         ptr_of[dev] = ptr;
     }
     *out = ptr_of[dev];

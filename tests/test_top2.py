@@ -93,3 +93,23 @@ def test_gpu_top2_workspace_too_small_is_an_error():
     with pytest.raises(sk.SkError) as e:
         sk.sk_top2(x, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
     assert e.value.status == sk.SK_E_WORKSPACE
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="calls with addresses that only a machine without a GPU may be given")
+def test_without_a_device_the_error_is_told():
+    """SK_E_HIP comes with the runtime's own error, from the calls that belong to no pool too."""
+    L, p = sk.lib(), 4096
+    calls = (lambda: L.sk_top2(p, 2, 100, 100, p, 1 << 20, p, p, p, p, p, None), lambda: L.sk_top2(p, 2, 100000, 100000, p, 1 << 20, p, p, p, p, p, None),
+             lambda: L.sk_top2_static(p, 2, 100, 100, p, p, p, p, p, None),
+             lambda: L.sk_logprobs(p, sk.SK_F32, 2, 100, 100, p, 1, 3, p, 1 << 20, p, p, p, p, p, None),
+             lambda: L.sk_probe_read(p, 4096, 1, 0, p, None))
+    meta = sk.Pool("bf16", 2, 1, 64, 16, 4, metadata_only=True)
+    for call in calls:
+        # (hipErrorUnknown, which an injected failure leaves behind, in front of each)
+        meta.sk_pool_inject_failure(sk.SK_SITE_SCATTER, 1)
+        sid = meta.sk_session_create()
+        with pytest.raises(sk.SkError):
+            meta.reserve(sid, 1)
+        meta.sk_session_destroy(sid)
+        before = L.sk_last_hip_error()
+        assert call() == sk.SK_E_HIP and L.sk_last_hip_error() not in (0, before)
