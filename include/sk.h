@@ -263,7 +263,8 @@ int sk_session_evict_oldest(sk_pool* pool, int32_t id, int64_t n_tokens, void* h
  * causal == 0 (behind sk_session_query): every token sees every retained one.  causal != 0 (behind sk_session_append): the
  * n_tok tokens are the session's newest, token i sees retained tokens 0..length - n_tok + i.  A query's own K/V are not cached and
  * receive nothing.  keep: 1 adds up, below 1 older calls fade, 0 starts anew (mass_in is not read then; NULL is the same).  A row whose
- * lse is infinite (padding: it attended to nothing) adds nothing, whatever its q holds.  n_tok == 0 scales only.
+ * lse is infinite (padding: it attended to nothing) adds nothing, whatever its q holds and, behind the keys that every token sees, whatever
+ * the keys hold (an append's padding receives nothing).  n_tok == 0 scales only.
  * mass_in, mass_out: DEVICE float [Hkv][stride], 4-byte aligned, strides in elements, at least the session's length; entries from
  * the length on are neither read nor written.  mass_out may be mass_in (same pointer and stride) and must not overlap it otherwise, nor
  * another item's arrays.  The caller keeps these arrays beside the session: an append's tokens come behind the last entry (put 0

@@ -132,7 +132,7 @@ struct Rows {
         see = I.first_vis + I.causal * tok;
     }
     // norm: log2 sum exp2, infinite for a row that is left out: its weights are exp2(0 - inf), whatever its q holds; sees: the keys that
-    // it sees
+    // it sees, none for a row that is left out (a key that only such rows would see, their own padding, may hold no number)
     __device__ __forceinline__ void store(unsigned char* rows, float* norm, int* sees) const
     {
         const int r = (int)threadIdx.x / TPR;
@@ -140,7 +140,7 @@ struct Rows {
         u32x4* p = (u32x4*)(rows + r * PITCH) + threadIdx.x % TPR * NP;
 #pragma unroll
         for (int i = 0; i < NP; ++i) p[i] = out ? u32x4{0, 0, 0, 0} : piece[i];
-        if (threadIdx.x % TPR == 0) { norm[r] = out ? __builtin_inff() : l * kLog2e; sees[r] = see; }
+        if (threadIdx.x % TPR == 0) { norm[r] = out ? __builtin_inff() : l * kLog2e; sees[r] = out ? 0 : see; }
     }
 };
 

@@ -332,3 +332,24 @@ def test_refusals():
     # an empty session: nothing to do
     assert sk.lib().sk_session_attention_mass(pool.h, other, None, None, 0, 0, None, 0, 1.0, None, 0, None) == sk.SK_OK
     torch.cuda.synchronize()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name,n,T,padded", [("layer", 700, 9, 3), ("layer", 700, 60, 20), ("f32", 300, 5, 2), ("f32", 300, 90, 33), ("d64", 30011, 40, 7), ("one_kv_head", 5000, 63, 20)])
+@pytest.mark.parametrize("value", [math.nan, math.inf])
+def test_padding_at_the_end_of_an_append_receives_nothing(name, n, T, padded, value):
+    """The last tokens of an append are padding: nothing of them is a number, their rows' lse is infinite and no other row sees their keys."""
+    shape = SHAPES[name]
+    gen = synth.generator(9, stream=n + T)
+    pool, sid, k = _session(shape, gen, n, 16, n_more=padded)
+    q = synth.draw(gen, (T, shape.n_q_heads, shape.head_dim), shape.dtype)
+    lse = _lse(shape, gen, q[:T - padded], k, True)
+    want, tol = _expected(shape, q[:T - padded], k, lse, True)
+    q[T - padded:] = value
+    lse = torch.cat([lse, torch.full((padded, shape.n_q_heads), math.inf)])
+    bad = torch.full((padded, shape.n_kv_heads, shape.head_dim), value, dtype=q.dtype, device="cuda")
+    pool.sk_session_append(sid, None, bad, bad)
+    mass = pool.sk_session_attention_mass(sid, q.cuda(), lse.cuda(), causal=True)
+    torch.cuda.synchronize()
+    _close(mass[:, :n], want, tol)
+    assert (mass[:, n:] == 0).all()
