@@ -595,3 +595,34 @@ def test_sums_of_a_stream_grow_by_a_weight_of_one_a_row():
         if n > 300:
             pool.sk_session_evict_lowest(sid, mass, n - 300, 64)
         total = mass.double().sum(1).cpu()
+
+
+@pytest.mark.gpu
+def test_a_workspace_that_holds_no_stretch_is_an_error():
+    """Thousands of KV heads and a small batch limit: 64 tokens do not fit the workspace.  Without free blocks the call is refused and changes
+    nothing, with them it needs none."""
+    heads, n = 5000, 100
+    shape = synth.Shape("bf16", heads, heads, 64)
+    pool = sk.Pool("bf16", heads, heads, 64, 16, 8, max_sessions=1, max_batch_tokens=1)
+    sid = pool.sk_session_create()
+    k = torch.randint(-0x7000, 0x7000, (n, heads, 64), generator=synth.generator(10), dtype=torch.int16).view(torch.bfloat16)
+    for t in range(n):
+        pool.sk_session_append(sid, None, k[t:t + 1].cuda(), k[t:t + 1].cuda())
+    model = Model(shape, synth.to_raw(k), synth.to_raw(k))
+    mass = _mass(synth.generator(10, stream=1), heads, n)
+    place = mass.cuda()
+    table, free = pool.sk_session_block_table(sid), pool.sk_pool_blocks_free()
+    for per_head in (True, False):
+        with pytest.raises(sk.SkError) as e:
+            pool.sk_session_evict_lowest(sid, place, 10, 0, per_head)
+        assert e.value.status == sk.SK_E_WORKSPACE
+    torch.cuda.synchronize()
+    assert pool.sk_session_block_table(sid) == table and pool.sk_pool_blocks_free() == free == 1 and torch.equal(place.cpu(), mass)
+    _check(pool, sid, model)
+    pool.sk_session_truncate(sid, 17)
+    model.K, model.V = model.K[:17], model.V[:17]
+    want = model.evict(mass[:, :17].numpy(), 3, 2, True)
+    pool.sk_session_evict_lowest(sid, place, 3, 2)
+    torch.cuda.synchronize()
+    np.testing.assert_array_equal(place[:, :17].cpu().numpy(), want)
+    _check(pool, sid, model)
