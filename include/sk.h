@@ -312,6 +312,48 @@ int sk_session_evict_lowest(sk_pool* pool, int32_t id, const float* mass_in, int
                             float* mass_out, int64_t mass_out_stride, void* hip_stream);
 
 /*
+ * POSITION ROTATION.  The attention calls take q and k position-encoded; these calls encode them on the way, and keep the cache's
+ * keys in step when positions change.  Pair i of the first rotary_dim dimensions of a row at position p turns by the angle p * inv_freq[i]:
+ *   (a, b) -> factor * (a cos - b sin, a sin + b cos)
+ * the pairs being (i, i + rotary_dim / 2), or (2 i, 2 i + 1) if interleaved != 0; the other dimensions stay as they are.  Angles are exact to
+ * 2^-31 of a turn at any position of 32 bits (negative ones turn backwards), products are fp32, and a turned element is rounded once to the pool's type.
+ *
+ * sk_pool_set_rotation gives a pool its rotation (HOST inv_freq, rotary_dim / 2 of them, finite, at most 10^6 in magnitude; copied).  rotary_dim: a
+ * multiple of 16 up to head_dim (SK_E_SHAPE).  It may be set again; what is cached stays as it is.  Metadata-only pools take it too.  Without
+ * it the calls below give SK_E_INVAL.
+ *
+ * positions: DEVICE int32, one a token, in any order; NULL: pos0, pos0 + 1, .. (within int32).  They are the caller's: nothing ties them to
+ * places in the cache.  q_out [tokens][Hq][d] receives q turned, which is what the call attends with and what
+ * sk_session_attention_mass needs afterwards; it may be q (same pointer), and overlaps no other array of the call (SK_E_INVAL).
+ *
+ * sk_rotate: q and k (either NULL, with its output) into q_out and k_out (which may be k), for sk_session_query and
+ * sk_session_query_shared_prefix, whose arguments they then are.  One kernel; can be captured and replayed, with other contents of q, k, positions too.
+ * sk_session_append_rotated: sk_session_append, with k turned on its way into the cache, v bit for bit, q turned into q_out.  q and q_out may be
+ * NULL together (and then out): commit only; out may be NULL alone: q is turned, nothing attends.  Otherwise as there.
+ * sk_batch_step_rotated: sk_batch_step likewise; positions must be given.  Own k of SK_OP_QUERY_B items are turned too, k and v of SK_OP_QUERY_A items not read.
+ * What q_out holds after SK_E_HIP is undefined.
+ *
+ * sk_session_shift: keys of the retained tokens first .. first + count - 1 turn on by a difference of positions (without factor, which they have
+ * got): deltas[j] for retained token first + j, DEVICE int32, with delta_stride >= count elements from one KV head's to the next or 0 (the same for all heads), or,
+ * deltas NULL, delta for all.  After sk_session_evict_oldest(n) the tokens behind the frozen ones move by -n; after
+ * sk_session_evict_lowest by what left in front of each.  Every call rounds the keys that it turns to the pool's type once more (bf16: by at most 2^-8 of an
+ * element); a delta of 0 leaves a key bit for bit.  V, and the keys' other dimensions, stay as they are.  Blocks that another session holds too are replaced
+ * by copies (SK_E_NOMEM if the free ones do not suffice; SK_E_WORKSPACE beyond 2^19 blocks in the stretch, then), others change in place.
+ * One kernel, ordered like the session's other calls.  All or nothing: a refused or failed call changes nothing.  Where no block is shared it can be captured, and
+ * every replay turns the keys again.  On a metadata-only pool the host half alone runs.
+ */
+int sk_pool_set_rotation(sk_pool* pool, int32_t rotary_dim, int32_t interleaved, const double* inv_freq, float factor);
+int sk_rotate(sk_pool* pool, const void* q, const void* k, int32_t n_tok, const int32_t* positions, int32_t pos0,
+              void* q_out, void* k_out, void* hip_stream);
+int sk_session_append_rotated(sk_pool* pool, int32_t id, const void* q, const void* k, const void* v, int32_t L,
+                              const int32_t* positions, int32_t pos0, void* q_out, void* out, int out_dtype, float* lse, void* hip_stream);
+int sk_batch_step_rotated(sk_pool* pool, int32_t n_items, const int32_t* session_id, const int32_t* op, const int32_t* cu_tokens,
+                          const int32_t* positions, const void* q, const void* k, const void* v,
+                          void* q_out, void* out, int out_dtype, float* lse, void* hip_stream);
+int sk_session_shift(sk_pool* pool, int32_t id, int64_t first, int64_t count, int32_t delta, const int32_t* deltas, int64_t delta_stride,
+                     void* hip_stream);
+
+/*
  * FORK (Sec. 3.7 prefix-aware grouped prefill: followers alias the leader's state; Sec. 3.10
  * metadata-only sequence aliasing).  Creates a session whose cache is the first n_prefix retained
  * tokens of session src (including src's frozen region and evicted range as far as the prefix
@@ -388,6 +430,33 @@ int sk_logprobs(const void* logits, int dtype, int32_t rows, int32_t vocab, int6
                 const int32_t* tokens, int32_t n_tokens, int32_t n_top, void* workspace, size_t workspace_bytes,
                 float* logprob, float* lse, float* entropy, int32_t* top_idx, float* top_logprob, void* hip_stream);
 
+/*
+ * VERIFICATION OF DRAFTED TOKENS by given random numbers: which of the n_draft tokens that a cheaper model has drafted behind a sequence stay, and which
+ * token follows them, such that what comes out has the target's distribution.  Independent of any pool; the tokens that do not stay are
+ * taken out of the cache by sk_session_truncate.  n_draft == 0: a plain draw from the target.
+ * target: DEVICE logits of dtype (SK_F32 | SK_BF16), [n_seq * (n_draft + 1)][target_stride], the first `vocab` entries of a row count: row
+ * s * (n_draft + 1) + i is the target's behind i drafted tokens of sequence s.  draft: the logits that the tokens were drawn from,
+ * [n_seq * n_draft][draft_stride], of the same dtype, or NULL: they were not drawn (q is 1 for the drafted token).  Both aligned to their elements only.
+ * tokens: DEVICE int32 [n_seq][n_draft]; one outside 0..vocab-1 ends its sequence's draft there.  temperature: DEVICE float [n_seq], or NULL: 1;
+ * p and q are the softmax of logit / temperature; 0 and below, and NaN: greedy.  uniform: DEVICE float [n_seq][n_draft + 1] in [0, 1).
+ * Drafted token x at place i stays, if all in front do, when uniform[s][i] * q(x) < p(x); greedy: when it is the target's largest logit's (lowest index
+ * among equals).  Behind those that stay one token is drawn, at the first place whose drafted token does not stay with the weights max(p - q, 0), behind the
+ * whole draft with p: the lowest t whose running sum of weights exceeds uniform[s][n_draft] times their total (a number below 0, or NaN, counts as 0, one from 1 on draws
+ * the last token that has a weight; where p - q leaves nothing, the drafted token is drawn).  Greedy: the largest logit's.
+ * Outputs, DEVICE: n_accepted int32 [n_seq], the tokens that stay; out_tokens int32 [n_seq][n_draft + 1], those, the one drawn, then -1;
+ * logprob float [n_seq][n_draft + 1] (may be NULL), the target's log probability at the temperature (greedy: at 1) of each, 0 behind them.
+ * They overlap no input.  A target row that has no probabilities (NaN or +inf among its logits, or nothing but -inf) keeps no token and draws -1, log probability
+ * NaN; a draft row that has none keeps no token and takes nothing off p.  Rows behind a sequence's draft are not read, nor are draft rows of greedy sequences.
+ * Sums and exponentials are held in 64 bits.  workspace: DEVICE scratch of sk_verify_workspace_bytes(..) bytes, 16-byte aligned, owned by the
+ * caller; calls that overlap in time need one each.  Kernels only: the call can be captured in a HIP graph.
+ * n_draft <= SK_VERIFY_MAX_DRAFT, n_seq * (n_draft + 1) <= SK_VERIFY_MAX_ROWS, vocab <= SK_VERIFY_MAX_VOCAB.
+ */
+enum { SK_VERIFY_MAX_DRAFT = 32, SK_VERIFY_MAX_ROWS = 1 << 20, SK_VERIFY_MAX_VOCAB = 1 << 21 };
+size_t sk_verify_workspace_bytes(int32_t n_seq, int32_t n_draft, int32_t vocab);
+int sk_verify(const void* target, int64_t target_stride, const void* draft, int64_t draft_stride, int dtype,
+              int32_t n_seq, int32_t n_draft, int32_t vocab, const int32_t* tokens, const float* uniform, const float* temperature,
+              void* workspace, size_t workspace_bytes, int32_t* n_accepted, int32_t* out_tokens, float* logprob, void* hip_stream);
+
 /* Byte offset inside kv_mem of element (block, kv_head, is_v, slot, dim), so a harness can
  * address the pool without knowing the layout.  Negative on bad arguments. */
 int64_t sk_pool_element_offset(const sk_pool* pool, int64_t block, int32_t kv_head, int32_t is_v,
@@ -453,7 +522,7 @@ int sk_probe_mfma(int32_t n_workgroups, int32_t iters, const void* operands, siz
 enum { SK_SITE_NONE = 0, SK_SITE_RING = 1,   /* waiting for a pinned upload slot */
        SK_SITE_UPLOAD = 2,                   /* host-to-device copy of a list or block table */
        SK_SITE_BLOCK_COPY = 3,               /* copy of a shared or partly filled block */
-       SK_SITE_SCATTER = 4, SK_SITE_ATTENTION = 5, SK_SITE_COMBINE = 6,   /* kernel launches */
+       SK_SITE_SCATTER = 4, SK_SITE_ATTENTION = 5, SK_SITE_COMBINE = 6,   /* kernel launches (4: rotations and shifts too) */
        SK_SITE_PLAN = 7,                     /* the lists of a batched call do not fit */
        SK_SITE_EVICT_SELECT = 8, SK_SITE_EVICT_MOVE = 9 };      /* kernel launches of sk_session_evict_lowest */
 int sk_pool_inject_failure(sk_pool* pool, int32_t site, int32_t countdown);

@@ -19,6 +19,7 @@ SK_SITE_RING, SK_SITE_UPLOAD, SK_SITE_BLOCK_COPY, SK_SITE_SCATTER, SK_SITE_ATTEN
 SK_SITE_EVICT_SELECT, SK_SITE_EVICT_MOVE = 8, 9
 SK_TOP2_STATIC_BYTES = 1 << 20
 SK_LOGPROBS_MAX_TOP, SK_LOGPROBS_MAX_ROWS, SK_LOGPROBS_MAX_VOCAB = 32, 1 << 20, 1 << 21
+SK_VERIFY_MAX_DRAFT, SK_VERIFY_MAX_ROWS, SK_VERIFY_MAX_VOCAB = 32, 1 << 20, 1 << 21
 
 SK_OK = 0
 SK_E_INVAL, SK_E_SHAPE, SK_E_DTYPE, SK_E_NOMEM, SK_E_BADSESSION = -1, -2, -3, -4, -5
@@ -72,7 +73,8 @@ EXPORTS = [
     "sk_pool_element_offset", "sk_pool_get_stats", "sk_pool_last_launch", "sk_strerror",
     "sk_last_hip_error", "sk_version", "sk_top2_workspace_bytes", "sk_top2", "sk_top2_static",
     "sk_session_evict_lowest", "sk_session_attention_mass", "sk_batch_attention_mass",
-    "sk_logprobs_workspace_bytes", "sk_logprobs",
+    "sk_logprobs_workspace_bytes", "sk_logprobs", "sk_verify_workspace_bytes", "sk_verify",
+    "sk_pool_set_rotation", "sk_rotate", "sk_session_append_rotated", "sk_batch_step_rotated", "sk_session_shift",
     "sk_pool_inject_failure", "sk_probe_read", "sk_probe_mfma",
 ]
 
@@ -128,6 +130,14 @@ def lib():
     L.sk_logprobs_workspace_bytes.restype = ctypes.c_size_t
     L.sk_logprobs_workspace_bytes.argtypes = [i32, i32, i32]
     L.sk_logprobs.argtypes = [vp, ctypes.c_int, i32, i32, i64, vp, i32, i32, vp, ctypes.c_size_t, vp, vp, vp, vp, vp, vp]
+    L.sk_pool_set_rotation.argtypes = [vp, i32, i32, P(ctypes.c_double), ctypes.c_float]
+    L.sk_rotate.argtypes = [vp, vp, vp, i32, vp, i32, vp, vp, vp]
+    L.sk_session_append_rotated.argtypes = [vp, i32, vp, vp, vp, i32, vp, i32, vp, vp, ctypes.c_int, vp, vp]
+    L.sk_batch_step_rotated.argtypes = [vp, i32, P(i32), P(i32), P(i32), vp, vp, vp, vp, vp, vp, ctypes.c_int, vp, vp]
+    L.sk_session_shift.argtypes = [vp, i32, i64, i64, i32, vp, i64, vp]
+    L.sk_verify_workspace_bytes.restype = ctypes.c_size_t
+    L.sk_verify_workspace_bytes.argtypes = [i32, i32, i32]
+    L.sk_verify.argtypes = [vp, i64, vp, i64, ctypes.c_int, i32, i32, i32, vp, vp, vp, vp, ctypes.c_size_t, vp, vp, vp, vp]
     L.sk_pool_inject_failure.argtypes = [vp, i32, i32]
     L.sk_probe_read.argtypes = [vp, ctypes.c_size_t, i32, i32, vp, vp]
     L.sk_probe_mfma.argtypes = [i32, i32, vp, ctypes.c_size_t, vp, P(ctypes.c_double), vp]
@@ -454,6 +464,78 @@ class Pool:
             "sk_batch_attention_mass")
         return mass_out
 
+    # -- position rotation -------------------------------------------------------------------
+    def sk_pool_set_rotation(self, inv_freq, interleaved=False, factor=1.0):
+        """inv_freq: an angle a position for each pair (rotary_dim / 2 numbers, float64 on the host)."""
+        f = np.ascontiguousarray(inv_freq, dtype=np.float64)
+        assert f.ndim == 1
+        _ck(lib().sk_pool_set_rotation(self.h, 2 * f.size, int(bool(interleaved)), f.ctypes.data_as(ctypes.POINTER(ctypes.c_double)), float(factor)),
+            "sk_pool_set_rotation")
+
+    def _turns(self, q, q_out, heads, n, positions, stream):
+        """Checks rows that are turned, and their positions; makes the output that was left out."""
+        assert positions is None or (positions.dtype is torch.int32 and positions.is_cuda and positions.numel() == n)
+        if q is None:
+            return None
+        assert q.dtype is self.torch_dtype and q.is_cuda and q.numel() == n * heads * self.d
+        if q_out is None:
+            q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            _made(stream, q_out)
+        assert q_out.dtype is self.torch_dtype and q_out.is_cuda and q_out.numel() == q.numel()
+        return q_out
+
+    def sk_rotate(self, q, k=None, positions=None, pos0=0, q_out=None, k_out=None, stream=None):
+        """q [tokens, Hq, d] and k [tokens, Hkv, d] (either None) turned by int32 positions [tokens], or pos0, pos0 + 1, ..  -> (q_out, k_out)"""
+        n = int((k if q is None else q).shape[0])
+        q_out = self._turns(q, q_out, self.Hq, n, positions, stream)
+        k_out = self._turns(k, k_out, self.Hkv, n, positions, stream)
+        _ck(lib().sk_rotate(self.h, _p(q), _p(k), n, _p(positions), int(pos0), _p(q_out), _p(k_out), _stream(stream)), "sk_rotate")
+        return q_out, k_out
+
+    def sk_session_append_rotated(self, sid, q, k, v, positions=None, pos0=None, q_out=None, out=None, lse=None, attend=True, out_dtype="f32",
+                                  want_lse=True, stream=None):
+        """sk_session_append with q and k turned on the way; pos0 left out: the session's length.  attend=False: q is turned, nothing attends.
+        -> (q_out, out, lse)"""
+        L = int(k.shape[0])
+        if pos0 is None:
+            pos0 = 0 if positions is not None else self._length(sid)
+        if self.kv_mem is not None:
+            q_out = self._turns(q, q_out, self.Hq, L, positions, stream)
+            assert k.dtype is self.torch_dtype and v.dtype is self.torch_dtype and k.numel() == v.numel() == L * self.Hkv * self.d
+            if q is not None and attend and out is None:
+                out, lse = self._out(L, out_dtype, want_lse, stream)
+        _ck(lib().sk_session_append_rotated(self.h, sid, _p(q), _p(k), _p(v), L, _p(positions), int(pos0), _p(q_out), _p(out), _dt(out_dtype), _p(lse),
+                                            _stream(stream) if self.kv_mem is not None else None), "sk_session_append_rotated")
+        return q_out, out, lse
+
+    def sk_batch_step_rotated(self, session_ids, ops, cu_tokens, positions, q, k, v, q_out=None, out=None, lse=None, out_dtype="f32", want_lse=True,
+                              stream=None):
+        """sk_batch_step with q and k turned on the way by int32 positions [tokens] -> (q_out, out, lse)"""
+        n, T = len(session_ids), int(cu_tokens[-1])
+        q_out = self._turns(q, q_out, self.Hq, T, positions, stream)
+        if out is None:
+            out, lse = self._out(T, out_dtype, want_lse, stream)
+        _ck(lib().sk_batch_step_rotated(self.h, n, (ctypes.c_int32 * n)(*map(int, session_ids)), (ctypes.c_int32 * n)(*map(int, ops)),
+                                        (ctypes.c_int32 * (n + 1))(*map(int, cu_tokens)), _p(positions), _p(q), _p(k), _p(v), _p(q_out), _p(out),
+                                        _dt(out_dtype), _p(lse), _stream(stream)), "sk_batch_step_rotated")
+        return q_out, out, lse
+
+    def sk_session_shift(self, sid, delta, first=0, count=None, stream=None):
+        """Turns the cached keys of retained tokens first .. first + count - 1 on by delta positions: a number, or CUDA int32 [count] or
+        [Hkv, count] (rows may be strided)."""
+        count = self._length(sid) - first if count is None else int(count)
+        deltas, stride, by = None, 0, 0
+        if isinstance(delta, torch.Tensor):
+            assert delta.dtype is torch.int32 and delta.is_cuda and delta.dim() in (1, 2) and delta.shape[-1] == count and (delta.stride(-1) == 1 or count <= 1)
+            assert delta.dim() == 1 or delta.shape[0] == self.Hkv
+            deltas = delta.data_ptr() if count else None
+            # (one row, or one that stands for all: any stride)
+            stride = delta.stride(0) if delta.dim() == 2 and self.Hkv > 1 else 0
+        else:
+            by = int(delta)
+        _ck(lib().sk_session_shift(self.h, sid, int(first), count, by, deltas, stride, _stream(stream) if self.kv_mem is not None else None),
+            "sk_session_shift")
+
     def sk_session_gather(self, sid, first=0, count=None, stream=None):
         if count is None:
             count = self.sk_session_length(sid) - first
@@ -534,6 +616,44 @@ def sk_logprobs(logits, tokens=None, n_top=0, workspace=None, outputs=None, stre
     _ck(lib().sk_logprobs(logits.data_ptr() if rows else None, _dt(logits.dtype), rows, vocab, logits.stride(0) if rows > 1 else vocab, _p(tokens), n_tokens,
                           n_top, _p(workspace), workspace.numel() * workspace.element_size(), _p(logprob), _p(lse), _p(entropy), _p(top_idx), _p(top_logprob),
                           _stream(stream)), "sk_logprobs")
+    return outputs
+
+
+def verify_outputs(n_seq, n_draft, device):
+    """Output tensors of sk_verify: (n_accepted [n_seq], tokens [n_seq, n_draft + 1], logprob [n_seq, n_draft + 1])."""
+    i32 = dict(dtype=torch.int32, device=device)
+    return torch.empty(n_seq, **i32), torch.empty((n_seq, n_draft + 1), **i32), torch.empty((n_seq, n_draft + 1), dtype=torch.float32, device=device)
+
+
+def sk_verify(target, tokens, uniform, draft=None, temperature=None, workspace=None, outputs=None, stream=None):
+    """target: CUDA float32 or bfloat16 logits [n_seq, n_draft + 1, vocab]; tokens: int32 [n_seq, n_draft]; uniform: float32 [n_seq, n_draft + 1];
+    draft: the logits that the tokens were drawn from [n_seq, n_draft, vocab], or None; temperature: float32 [n_seq] or None.  Rows of logits may be
+    strided, evenly over sequences and places.  Returns (n_accepted [n_seq], tokens [n_seq, n_draft + 1], logprob [n_seq, n_draft + 1])."""
+    assert target.is_cuda and target.dtype in (torch.float32, torch.bfloat16) and target.dim() == 3
+    n_seq, places, vocab = target.shape
+    n_draft = places - 1
+
+    def rows(x, n):                                          # address and row stride of [n_seq, n, vocab]
+        assert x.is_cuda and x.dtype is target.dtype and x.shape == (n_seq, n, vocab) and (x.stride(2) == 1 or vocab == 1)
+        stride = x.stride(1) if n > 1 else x.stride(0) if n_seq > 1 else vocab
+        assert n <= 1 or n_seq <= 1 or x.stride(0) == n * stride
+        return x.data_ptr() if x.numel() else None, stride
+
+    pt, st = rows(target, places)
+    pd, sd = (None, 0) if draft is None or n_draft == 0 else rows(draft, n_draft)
+    for t, kind, shape in ((tokens, torch.int32, (n_seq, n_draft)), (uniform, torch.float32, (n_seq, places)), (temperature, torch.float32, (n_seq,))):
+        assert (t is None and kind is torch.float32 and shape == (n_seq,)) or (t.is_cuda and t.dtype is kind and t.shape == shape)
+    if outputs is None:
+        outputs = verify_outputs(n_seq, n_draft, target.device)
+        _made(stream, *outputs)
+    n_accepted, out_tokens, logprob = outputs
+    for t, kind, n in ((n_accepted, torch.int32, n_seq), (out_tokens, torch.int32, n_seq * places), (logprob, torch.float32, n_seq * places)):
+        assert (t is None and kind is torch.float32) or (t.is_cuda and t.dtype is kind and t.numel() == n)
+    if workspace is None:
+        workspace = torch.empty(max(lib().sk_verify_workspace_bytes(n_seq, n_draft, vocab), 16), dtype=torch.uint8, device=target.device)
+        _made(stream, workspace)
+    _ck(lib().sk_verify(pt, st, pd, sd, _dt(target.dtype), n_seq, n_draft, vocab, _p(tokens), _p(uniform), _p(temperature), _p(workspace),
+                        workspace.numel() * workspace.element_size(), _p(n_accepted), _p(out_tokens), _p(logprob), _stream(stream)), "sk_verify")
     return outputs
 
 

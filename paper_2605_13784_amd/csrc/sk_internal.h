@@ -174,6 +174,32 @@ struct sk_commit {
     sk_scatter item[SK_COMMIT_ITEMS];
 };
 
+// The position rotation of a pool's layer (sk_pool_set_rotation): pair i turns by position * step[i] / 2^64 of a full turn.
+#define SK_ROTARY_MAX 128
+struct sk_rotation {
+    int32_t rotary;           // dimensions that turn, a multiple of 16; 0: no rotation set
+    int32_t interleaved;      // pairs (2 i, 2 i + 1) instead of (i, i + rotary / 2)
+    float factor;
+    uint64_t step[SK_ROTARY_MAX / 2];
+};
+
+// A call that turns its q and k on the way (sk_rotate.hip): the launches that stand in for the plain commit's.  `scatter` and
+// `scatter_args` commit or stage as sk_launch_scatter does, with k turned, and turn q into q_out; `rows` turns q and k (each may
+// be null) into q_out and k_out.
+struct sk_turned {
+    const sk_rotation* rot;
+    const int32_t* positions;     // DEVICE, one a token, or null: pos0, pos0 + 1, ..
+    int32_t pos0;
+    int32_t n_tok;
+    const void* q;                // null: no q
+    void* q_out;
+    int (*rows)(const sk_geom& g, const sk_turned& t, const void* q, const void* k, void* k_out, void* stream);
+    int (*scatter)(const sk_geom& g, const sk_turned& t, const void* k, const void* v, const sk_scatter* items, int32_t n_items,
+                   int32_t* tables_rw, unsigned char* kv_rw, unsigned char* eph_rw, void* stream);
+    int (*scatter_args)(const sk_geom& g, const sk_turned& t, const void* k, const void* v, const sk_scatter_list& items, int32_t n_items,
+                        int32_t* tables_rw, unsigned char* kv_rw, unsigned char* eph_rw, void* stream);
+};
+
 // What an operator in a file of its own needs to know of a pool and one of its sessions (sk_pool.cpp).
 struct sk_pool;
 struct sk_session_view {
@@ -207,6 +233,31 @@ int sk_evict_begin(sk_pool* p, int32_t id, int64_t n_evict, int64_t n_recent, sk
 void sk_evict_listed(sk_pool* p, const sk_evict& e, void* stream);           // a kernel that reads e.table is on the stream
 void sk_evict_undo(sk_pool* p, const sk_evict& e, void* stream);             // its kernels will not all run: the device table as it was
 void sk_evict_end(sk_pool* p, const sk_evict& e);
+// Keys of a session that change where they lie, host side (sk_pool.cpp), in the same two halves: storage indices [lo, hi), of whose
+// blocks those that another session holds too are replaced by blocks from the free list.
+struct sk_shift {
+    int32_t id;
+    int64_t len;              // storage end
+    int64_t blk0, n_blk;      // blocks that hold [lo, hi)
+    int64_t n_fresh;          // of those, how many are replaced
+    const int32_t* list;      // pinned: n_blk pairs of a block and what it is replaced by (itself, if it is not; n_fresh > 0, device pools)
+    int slot;
+    int32_t* tables_rw;
+    unsigned char* kv_rw;
+};
+int sk_shift_begin(sk_pool* p, int32_t id, int64_t lo, int64_t hi, sk_shift* out);
+void sk_shift_listed(sk_pool* p, const sk_shift& e, void* stream);
+void sk_shift_end(sk_pool* p, const sk_shift& e);
+
+sk_rotation* sk_rotation_of(sk_pool* p);
+bool sk_geom_of(const sk_pool* p, sk_geom* out);      // false: metadata-only pool
+// Whether what a call of T tokens turns lies apart from its other arrays (q_out may be q, k_out may be k; any may be null)
+bool sk_turned_apart(const sk_geom& g, const sk_turned& t, int64_t T, const void* k, const void* v, const void* k_out, const void* out, int out_dtype, const float* lse);
+// sk_session_append and sk_batch_step of rows that are turned on the way; their arguments' other checks are made
+int sk_append_turned(sk_pool* p, int32_t id, sk_turned& t, const void* k, const void* v, int32_t L, void* out, int out_dtype, float* lse, void* stream);
+int sk_batch_turned(sk_pool* p, int32_t n_items, const int32_t* session_id, const int32_t* op, const int32_t* cu_tokens, sk_turned& t,
+                    const void* k, const void* v, void* out, int out_dtype, float* lse, void* stream);
+
 bool sk_injected(sk_pool* p, int site);                                      // sk_pool_inject_failure
 
 bool sk_sessions_differ(sk_pool* p, int32_t n, const int32_t* id);           // ids of live sessions

@@ -135,6 +135,7 @@ struct sk_pool {
     bool ring_used[kRingSlots] = {};
     int ring_next = 0;
     sk_geom geom;
+    sk_rotation rot = {};
     sk_pool_stats stats = {};
     sk_launch_info last = {};
     // Tuning switches, read from the environment once when the pool is created (see sk_pool_create).
@@ -921,7 +922,8 @@ int scatter_reserve(sk_pool* p, int64_t n_items, ScatterSlot& ss)
     return ring_acquire(p, &ss.slot, &ss.host);
 }
 
-int scatter_launch(sk_pool* p, const ScatterSlot& ss, const std::vector<sk_scatter>& items, const void* k, const void* v, hipStream_t st)
+int scatter_launch(sk_pool* p, const ScatterSlot& ss, const std::vector<sk_scatter>& items, const void* k, const void* v, hipStream_t st,
+                   const sk_turned* turned = nullptr)
 {
     if (items.empty()) return SK_OK;
     unsigned char* ws = (unsigned char*)p->d.workspace;
@@ -930,8 +932,9 @@ int scatter_launch(sk_pool* p, const ScatterSlot& ss, const std::vector<sk_scatt
         if (!p->device) return SK_OK;
         sk_scatter_list lst;
         memcpy(lst.item, items.data(), items.size() * sizeof(sk_scatter));
-        int e = sk_launch_scatter_args(p->geom, k, v, lst, (int32_t)items.size(), (int32_t*)(ws + p->L.off_tables),
-                                       (unsigned char*)p->d.kv_mem, ws + p->L.off_eph, st);
+        int32_t* tables = (int32_t*)(ws + p->L.off_tables);
+        int e = turned ? turned->scatter_args(p->geom, *turned, k, v, lst, (int32_t)items.size(), tables, (unsigned char*)p->d.kv_mem, ws + p->L.off_eph, st)
+                       : sk_launch_scatter_args(p->geom, k, v, lst, (int32_t)items.size(), tables, (unsigned char*)p->d.kv_mem, ws + p->L.off_eph, st);
         if (e) { g_last_hip = e; return SK_E_HIP; }
         p->stats.launches++;
         return SK_OK;
@@ -958,8 +961,9 @@ int scatter_launch(sk_pool* p, const ScatterSlot& ss, const std::vector<sk_scatt
     } else if (inject(p, SK_SITE_UPLOAD)) return SK_E_HIP;
     if (inject(p, SK_SITE_SCATTER)) return SK_E_HIP;
     if (!p->device) return SK_OK;
-    int e = sk_launch_scatter(p->geom, k, v, list, (int32_t)items.size(),
-                              (int32_t*)(ws + p->L.off_tables), (unsigned char*)p->d.kv_mem, ws + p->L.off_eph, st);
+    int32_t* tables = (int32_t*)(ws + p->L.off_tables);
+    int e = turned ? turned->scatter(p->geom, *turned, k, v, list, (int32_t)items.size(), tables, (unsigned char*)p->d.kv_mem, ws + p->L.off_eph, st)
+                   : sk_launch_scatter(p->geom, k, v, list, (int32_t)items.size(), tables, (unsigned char*)p->d.kv_mem, ws + p->L.off_eph, st);
     if (in_place) ring_busy(p, ss.slot, st);         // whatever e is: an error that an earlier call left behind shows up here too, with the kernel on the stream
     if (e) { g_last_hip = e; return SK_E_HIP; }
     p->stats.launches++;
@@ -979,6 +983,17 @@ bool results_over_own(const sk_pool* p, int64_t T, const void* k, const void* v,
     const size_t kv = size_t(T) * p->d.n_kv_heads * p->d.head_dim * p->L.elem, rows = size_t(T) * p->d.n_q_heads;
     const size_t n_out = rows * p->d.head_dim * (out_dtype == SK_F32 ? 4 : 2);
     return overlap(out, n_out, k, kv) || overlap(out, n_out, v, kv) || overlap(lse, rows * 4, k, kv) || overlap(lse, rows * 4, v, kv);
+}
+
+// Turns a call's q and k, k into the staging area, in a launch of its own.
+int turn_rows(sk_pool* p, const sk_turned& t, const void* k, void* k_out, hipStream_t st)
+{
+    if (inject(p, SK_SITE_SCATTER)) return SK_E_HIP;
+    if (!p->device) return SK_OK;
+    const int e = t.rows(p->geom, t, t.q, k, k_out, st);
+    if (e) { g_last_hip = e; return SK_E_HIP; }
+    p->stats.launches++;
+    return SK_OK;
 }
 
 // Copies a call's own k and v, as they are, to the staging area, which holds twice max_batch_tokens rows.
@@ -1226,7 +1241,8 @@ int plan_list(sk_pool* p, const ScatterBatch* sb, int n_sb, ListGroup* groups, i
     return ring_acquire(p, &P.slot, &P.host);
 }
 
-int launch_list(sk_pool* p, ListPlan& P, const ScatterBatch* sb, int n_sb, ListGroup* groups, int n_groups, int out_dtype, hipStream_t st)
+int launch_list(sk_pool* p, ListPlan& P, const ScatterBatch* sb, int n_sb, ListGroup* groups, int n_groups, int out_dtype, hipStream_t st,
+                const sk_turned* turned = nullptr)
 {
     if (P.n_tiles == 0) return SK_OK;
     const int Hkv = p->d.n_kv_heads;
@@ -1285,12 +1301,19 @@ int launch_list(sk_pool* p, ListPlan& P, const ScatterBatch* sb, int n_sb, ListG
         if (n == 0) continue;
         if (!sb[i].items.empty() && inject(p, SK_SITE_SCATTER)) return SK_E_HIP;
         if (!p->device) continue;
-        int e = sk_launch_scatter(p->geom, sb[i].k, sb[i].v, (const sk_scatter*)(scatter_lists + off_sb[i]), (int32_t)n,
-                                  (int32_t*)(ws + p->L.off_tables), (unsigned char*)p->d.kv_mem, ws + p->L.off_eph, st);
+        const sk_scatter* list = (const sk_scatter*)(scatter_lists + off_sb[i]);
+        int32_t* tables = (int32_t*)(ws + p->L.off_tables);
+        const bool turns = turned && !sb[i].items.empty();
+        int e = turns ? turned->scatter(p->geom, *turned, sb[i].k, sb[i].v, list, (int32_t)n, tables, (unsigned char*)p->d.kv_mem, ws + p->L.off_eph, st)
+                      : sk_launch_scatter(p->geom, sb[i].k, sb[i].v, list, (int32_t)n, tables, (unsigned char*)p->d.kv_mem, ws + p->L.off_eph, st);
         if (in_place) ring_busy(p, P.slot, st);            // whatever e is (see scatter_launch)
         if (e) { g_last_hip = e; return SK_E_HIP; }
         if (!sb[i].items.empty()) P.scatter_enqueued = true;
         p->stats.launches++;
+    }
+    if (turned && n_items == 0) {               // (cache-only queries: no commit whose launch turns q)
+        int rc = turn_rows(p, *turned, nullptr, nullptr, st);
+        if (rc) return rc;
     }
     if (inject(p, SK_SITE_ATTENTION)) return SK_E_HIP;
     if (!p->device) return SK_OK;
@@ -1440,6 +1463,65 @@ void sk_evict_end(sk_pool* p, const sk_evict& e)
         s.blocks.pop_back();
     }
     p->stats.tokens_evicted += e.n_evict;
+}
+
+int sk_shift_begin(sk_pool* p, int32_t id, int64_t lo, int64_t hi, sk_shift* out)
+{
+    sk_shift& e = *out;
+    const Session& s = p->sessions[(size_t)id];
+    const int64_t B = p->d.block_tokens;
+    e = sk_shift();
+    e.id = id; e.len = s.len;
+    e.blk0 = lo / B; e.n_blk = hi > lo ? (hi + B - 1) / B - e.blk0 : 0;
+    if (s.may_share)
+        for (int64_t b = 0; b < e.n_blk; ++b) e.n_fresh += p->refcnt[(size_t)s.blocks[size_t(e.blk0 + b)]] > 1;
+    if (e.n_fresh > (int64_t)p->free_blocks.size()) return SK_E_NOMEM;
+    e.tables_rw = p->device ? (int32_t*)((unsigned char*)p->d.workspace + p->L.off_tables) : nullptr;
+    e.kv_rw = (unsigned char*)p->d.kv_mem;
+    if (e.n_fresh == 0) return SK_OK;
+    if (size_t(e.n_blk) * 8 > p->L.meta_bytes) return SK_E_WORKSPACE;
+    unsigned char* host;
+    const int rc = ring_acquire(p, &e.slot, &host);
+    if (rc) return rc;
+    size_t next = 0;
+    if (host)
+        for (int64_t b = 0; b < e.n_blk; ++b) {
+            const int32_t blk = s.blocks[size_t(e.blk0 + b)];
+            ((int32_t*)host)[2 * b] = blk;
+            ((int32_t*)host)[2 * b + 1] = p->refcnt[(size_t)blk] > 1 ? p->free_blocks[next++] : blk;
+        }
+    e.list = (const int32_t*)host;
+    return SK_OK;
+}
+
+void sk_shift_listed(sk_pool* p, const sk_shift& e, void* stream) { if (e.list) ring_busy(p, e.slot, (hipStream_t)stream); }
+
+void sk_shift_end(sk_pool* p, const sk_shift& e)
+{
+    Session& s = p->sessions[(size_t)e.id];
+    for (int64_t b = 0; e.n_fresh > 0 && b < e.n_blk; ++b) {
+        int32_t& blk = s.blocks[size_t(e.blk0 + b)];
+        if (p->refcnt[(size_t)blk] <= 1) continue;
+        p->refcnt[(size_t)blk]--;                         // still held by the others
+        blk = p->free_blocks.front();
+        p->free_blocks.pop_front();
+        p->refcnt[(size_t)blk] = 1;
+        p->blocks_in_use++;
+    }
+}
+
+sk_rotation* sk_rotation_of(sk_pool* p) { return &p->rot; }
+bool sk_geom_of(const sk_pool* p, sk_geom* out) { *out = p->geom; return p->device; }
+
+bool sk_turned_apart(const sk_geom& g, const sk_turned& t, int64_t T, const void* k, const void* v, const void* k_out, const void* out, int out_dtype, const float* lse)
+{
+    const size_t q = size_t(T) * g.Hq * g.d * g.elem, kv = size_t(T) * g.Hkv * g.d * g.elem, rows = size_t(T) * g.Hq;
+    if (t.q_out != t.q && overlap(t.q_out, q, t.q, q)) return false;
+    if (k_out != k && overlap(k_out, kv, k, kv)) return false;
+    if (overlap(t.q_out, q, t.positions, size_t(T) * 4) || overlap(k_out, kv, t.positions, size_t(T) * 4)) return false;
+    if (overlap(k_out, kv, t.q, q) || overlap(k_out, kv, t.q_out, q)) return false;
+    return !overlap(t.q_out, q, k, kv) && !overlap(t.q_out, q, v, kv) && !overlap(t.q_out, q, out, rows * g.d * (out_dtype == SK_F32 ? 4 : 2)) &&
+           !overlap(t.q_out, q, lse, rows * 4);
 }
 
 int sk_note_hip_error(int e) { g_last_hip = e; return SK_E_HIP; }
@@ -1614,8 +1696,8 @@ int sk_session_block_table(const sk_pool* p, int32_t id, const int32_t** table, 
     return SK_OK;
 }
 
-int sk_session_append(sk_pool* p, int32_t id, const void* q, const void* k, const void* v, int32_t L,
-                      void* out, int out_dtype, float* lse, void* hip_stream)
+static int append(sk_pool* p, int32_t id, const void* q, const void* k, const void* v, int32_t L,
+                  void* out, int out_dtype, float* lse, void* hip_stream, const sk_turned* turned)
 {
     if (!p) return SK_E_INVAL;
     Session* s = get_session(p, id);
@@ -1624,9 +1706,9 @@ int sk_session_append(sk_pool* p, int32_t id, const void* q, const void* k, cons
     if (L == 0) return SK_OK;
     if (L > p->L.max_batch_tokens) return SK_E_WORKSPACE;
     if (p->device) {
-        if (!k || !v || (!q) != (!out)) return SK_E_INVAL;
+        if (!k || !v || (turned ? !q && out : (!q) != (!out))) return SK_E_INVAL;
         if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned16(lse)) return SK_E_INVAL;
-        if (q) { int rc = check_out_dtype(p, out_dtype); if (rc) return rc; }
+        if (out) { int rc = check_out_dtype(p, out_dtype); if (rc) return rc; }
     }
     if (s->len + L > p->L.max_session_tokens) return SK_E_NOMEM;
     const int64_t need = blocks_needed(p, s->len, L);
@@ -1635,7 +1717,7 @@ int sk_session_append(sk_pool* p, int32_t id, const void* q, const void* k, cons
     // attention, and the ring slot of a scatter list too long for the kernel arguments
     hipStream_t st = (hipStream_t)hip_stream;
     const int64_t n = s->len;
-    const bool attend = p->device ? q != nullptr : true;
+    const bool attend = p->device ? out != nullptr : true;
     RegPlan plan;
     if (attend) {
         Variant v;
@@ -1647,7 +1729,18 @@ int sk_session_append(sk_pool* p, int32_t id, const void* q, const void* k, cons
     const bool one_launch = in_place && scatter_groups(n, L) <= SK_COMMIT_ITEMS;      // the attention launch commits too
     ScatterSlot ss;
     { int rc = scatter_reserve(p, scatter_groups(n, L), ss); if (rc) return rc; }
-    if (in_place && p->device && results_over_own(p, L, k, v, out, out_dtype, lse)) { int rc = copy_own(p, L, &k, &v, st); if (rc) return rc; }
+    if (in_place && turned) {                   // the launches behind find k turned in the staging area
+        const size_t bytes = size_t(L) * p->d.n_kv_heads * p->d.head_dim * p->L.elem;
+        unsigned char* to = p->device ? (unsigned char*)p->d.workspace + p->L.off_eph : nullptr;
+        int rc = turn_rows(p, *turned, k, to, st);
+        if (rc) return rc;
+        if (p->device && results_over_own(p, L, v, v, out, out_dtype, lse)) {
+            SK_HIP(hipMemcpyAsync(to + bytes, v, bytes, hipMemcpyDeviceToDevice, st));
+            v = to + bytes;
+        }
+        k = to;
+    }
+    else if (in_place && p->device && results_over_own(p, L, k, v, out, out_dtype, lse)) { int rc = copy_own(p, L, &k, &v, st); if (rc) return rc; }
     // from here on only a failing HIP call can stop the call; what it changed is taken back
     Undo u;
     int64_t first_new = 0;
@@ -1660,14 +1753,20 @@ int sk_session_append(sk_pool* p, int32_t id, const void* q, const void* k, cons
         plan.commit_items = (int32_t)items.size();
         memcpy(plan.commit.item, items.data(), items.size() * sizeof(sk_scatter));
         rc = inject(p, SK_SITE_SCATTER) ? SK_E_HIP : SK_OK;
-    } else rc = scatter_launch(p, ss, items, k, v, st);
+    } else rc = scatter_launch(p, ss, items, k, v, st, in_place ? nullptr : turned);
     if (rc) { rollback(p, u, false); return rc; }
     if (attend) {
-        rc = launch_regular(p, plan, q, out, out_dtype, lse, st);
+        rc = launch_regular(p, plan, turned ? turned->q_out : q, out, out_dtype, lse, st);
         if (rc) { rollback(p, u, !one_launch || plan.enqueued); return rc; }
     }
     p->stats.tokens_appended += L;
     return SK_OK;
+}
+
+int sk_session_append(sk_pool* p, int32_t id, const void* q, const void* k, const void* v, int32_t L,
+                      void* out, int out_dtype, float* lse, void* hip_stream)
+{
+    return append(p, id, q, k, v, L, out, out_dtype, lse, hip_stream, nullptr);
 }
 
 int sk_session_query(sk_pool* p, int32_t id, const void* q, const void* k, const void* v, int32_t nq,
@@ -1715,8 +1814,8 @@ int sk_session_query(sk_pool* p, int32_t id, const void* q, const void* k, const
     return SK_OK;
 }
 
-int sk_batch_step(sk_pool* p, int32_t n_items, const int32_t* session_id, const int32_t* op, const int32_t* cu_tokens,
-                  const void* q, const void* k, const void* v, void* out, int out_dtype, float* lse, void* hip_stream)
+static int batch_step(sk_pool* p, int32_t n_items, const int32_t* session_id, const int32_t* op, const int32_t* cu_tokens,
+                      const void* q, const void* k, const void* v, void* out, int out_dtype, float* lse, void* hip_stream, sk_turned* turned)
 {
     if (!p || n_items < 0) return SK_E_INVAL;
     if (n_items == 0) return SK_OK;
@@ -1760,6 +1859,11 @@ int sk_batch_step(sk_pool* p, int32_t n_items, const int32_t* session_id, const 
         if (rc) return rc;
         Variant vv;
         if (!pick_variant(p, 1, vv)) return SK_E_SHAPE;
+    }
+    if (turned) {
+        if (p->device && total > 0 && (!turned->positions || !turned->q_out || !sk_turned_apart(p->geom, *turned, total, any_kv ? k : nullptr, any_kv ? v : nullptr, nullptr, out, out_dtype, lse)))
+            return SK_E_INVAL;
+        turned->n_tok = (int32_t)total;
     }
     // From here on the sessions change; whatever stops the call afterwards (the lists do not fit the
     // workspace, a HIP call fails) takes every change back, in reverse order.
@@ -1812,7 +1916,7 @@ int sk_batch_step(sk_pool* p, int32_t n_items, const int32_t* session_id, const 
         Variant vv;
         if (!pick_variant(p, T, vv, allow_256)) { take_back(false); return SK_E_SHAPE; }
         ListGroup& g = groups[vv.id == SK_KV_MFMA64 ? 2 : vv.id == SK_KV_MFMA128 ? 1 : 0];
-        g.v = vv; g.q = q; g.out = out; g.lse = lse;
+        g.v = vv; g.q = turned ? turned->q_out : q; g.out = out; g.lse = lse;
         add_tiles(g, base, cu_tokens[i], T);
         if (vv.id == SK_KV_MFMA256 && list_narrow(p, vv)) tall.push_back({base, cu_tokens[i], T});
     }
@@ -1827,7 +1931,7 @@ int sk_batch_step(sk_pool* p, int32_t n_items, const int32_t* session_id, const 
         constexpr double kCarriedUs = 2.0;
         ListGroup low = groups[1];
         low.v = Variant{SK_KV_MFMA128, 128, 128 / p->L.G};
-        low.q = q; low.out = out; low.lse = lse;
+        low.q = turned ? turned->q_out : q; low.out = out; low.lse = lse;
         for (const Item& it : tall) add_tiles(low, it.base, it.row0, it.tokens);
         const size_t scatter = sb.items.size() * sizeof(sk_scatter);
         const ListGroup* const as_low[2] = {&low, &groups[2]};
@@ -1841,11 +1945,17 @@ int sk_batch_step(sk_pool* p, int32_t n_items, const int32_t* session_id, const 
     ListPlan plan;
     int rc = plan_list(p, &sb, 1, groups, 3, plan);
     if (rc) { take_back(false); return rc; }
-    rc = launch_list(p, plan, &sb, 1, groups, 3, out_dtype, st);
+    rc = launch_list(p, plan, &sb, 1, groups, 3, out_dtype, st, turned);
     if (rc) { take_back(plan.scatter_enqueued); return rc; }
     p->stats.tokens_appended += appended;
     p->stats.tokens_queried += queried;
     return SK_OK;
+}
+
+int sk_batch_step(sk_pool* p, int32_t n_items, const int32_t* session_id, const int32_t* op, const int32_t* cu_tokens,
+                  const void* q, const void* k, const void* v, void* out, int out_dtype, float* lse, void* hip_stream)
+{
+    return batch_step(p, n_items, session_id, op, cu_tokens, q, k, v, out, out_dtype, lse, hip_stream, nullptr);
 }
 
 int sk_session_query_shared_prefix(sk_pool* p, int32_t id, const void* qp, const void* kp, const void* vp, int32_t P,
@@ -2173,3 +2283,14 @@ int sk_last_hip_error(void) { return g_last_hip; }
 int sk_version(void) { return 2; }
 
 }  // extern "C"
+
+int sk_append_turned(sk_pool* p, int32_t id, sk_turned& t, const void* k, const void* v, int32_t L, void* out, int out_dtype, float* lse, void* stream)
+{
+    return append(p, id, t.q, k, v, L, out, out_dtype, lse, stream, &t);
+}
+
+int sk_batch_turned(sk_pool* p, int32_t n_items, const int32_t* session_id, const int32_t* op, const int32_t* cu_tokens, sk_turned& t,
+                    const void* k, const void* v, void* out, int out_dtype, float* lse, void* stream)
+{
+    return batch_step(p, n_items, session_id, op, cu_tokens, t.q, k, v, out, out_dtype, lse, stream, &t);
+}

@@ -1,0 +1,533 @@
+// Position rotation for gfx950: q and k turned by their tokens' positions on the way into the cache (sk_session_append_rotated,
+// sk_batch_step_rotated) or beside it (sk_rotate), and cached keys turned on by a difference of positions (sk_session_shift).
+//
+// Pair i of the first `rotary` dimensions is a point in the plane that a token at position p turns by the angle p f_i:
+//   (a, b) -> (a cos - b sin, a sin + b cos) * factor
+// Turns add up: what moves a key from one position to another is the turn by the difference, whatever position it had.
+//
+// Angles.  p f_i exceeds what 32 bits hold long before it does so for p: at position 10^6 a float's angle is off by 0.03.  Only the
+// part of a full turn that is left counts, and that is an integer product: step_i = f_i / (2 pi) as a fraction of 2^64, p step_i modulo 2^64,
+// of which the upper 32 bits are kept (2^-32 of a turn; step_i itself is off by 2^-65 of one a position, 2^-34 at position 2^31).  The upper two bits of
+// those, rounded, are the quadrant; what is left, at most pi / 4, goes through the series of sine and cosine, whose next terms are
+// below 2^-28.
+#include <hip/hip_runtime.h>
+#include <cmath>
+#include <cstring>
+
+#include "../../include/sk.h"
+#include "sk_internal.h"
+
+// Which products join an addition is written out: a row has the same bits whichever kernel turns it.
+#pragma clang fp contract(off)
+
+namespace {
+
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+
+// ---- the mathematics -------------------------------------------------------------------------------
+
+__device__ __forceinline__ uint32_t phase_of(const int32_t p, const uint64_t step)
+{
+    const uint32_t lo = (uint32_t)step, hi = (uint32_t)(step >> 32);
+    return __umulhi((uint32_t)p, lo) + (uint32_t)p * hi - (p < 0 ? lo : 0u);      // bits 32 to 63 of p * step
+}
+
+// cos and sin of a phase (2^32: a full turn)
+__device__ __forceinline__ f32x2 cos_sin(const uint32_t phase)
+{
+    const uint32_t quadrant = (phase + 0x20000000u) >> 30;
+    const float x = (float)(int32_t)(phase - (quadrant << 30)) * 1.4629180792671596e-09f;      // 2 pi / 2^32
+    const float y = x * x;
+    float s = fmaf(y, 2.7557319e-06f, -1.9841270e-04f);                                        // 1/9!, 1/7!, 1/5!, 1/3!
+    s = fmaf(y, s, 8.3333333e-03f);
+    s = fmaf(y, s, -1.6666667e-01f);
+    s = fmaf(y * x, s, x);
+    float c = fmaf(y, -2.7557319e-07f, 2.4801587e-05f);                                        // 1/10!, 1/8!, 1/6!, 1/4!, 1/2!
+    c = fmaf(y, c, -1.3888889e-03f);
+    c = fmaf(y, c, 4.1666667e-02f);
+    c = fmaf(y, c, -0.5f);
+    c = fmaf(y, c, 1.f);
+    const float a = quadrant & 1 ? s : c, b = quadrant & 1 ? c : s;
+    return f32x2{__uint_as_float(__float_as_uint(a) ^ ((quadrant + 1) & 2) << 30), __uint_as_float(__float_as_uint(b) ^ (quadrant & 2) << 30)};
+}
+
+// cos and sin of the eight pairs from pair0 on
+struct Turn { float c[8], s[8]; };
+__device__ __forceinline__ Turn turn_of(const sk_rotation& rot, const int pair0, const int32_t position, const float factor)
+{
+    Turn t;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const f32x2 cs = cos_sin(phase_of(position, rot.step[pair0 + i]));
+        t.c[i] = cs.x * factor; t.s[i] = cs.y * factor;
+    }
+    return t;
+}
+
+// A unit of a row: sixteen elements that one thread turns (eight pairs) or, behind the rotary dimensions, passes on.  Halves: eight
+// elements of either half; neighbours: sixteen in a row.
+template <bool F32> struct Unit { u32x4 x[F32 ? 4 : 2]; };
+struct Place { int lo, hi; };      // byte offsets of its two stretches of eight elements
+template <bool F32> __device__ __forceinline__ Place place_of(const sk_rotation& rot, const int unit)
+{
+    constexpr int EL = F32 ? 4 : 2;
+    if (16 * unit < rot.rotary && !rot.interleaved) return Place{8 * unit * EL, (rot.rotary / 2 + 8 * unit) * EL};
+    return Place{16 * unit * EL, (16 * unit + 8) * EL};
+}
+template <bool F32> __device__ __forceinline__ Unit<F32> load_unit(const unsigned char* row, const Place at)
+{
+    Unit<F32> u;
+    constexpr int H = F32 ? 2 : 1;
+#pragma unroll
+    for (int i = 0; i < H; ++i) { u.x[i] = *(const u32x4*)(row + at.lo + 16 * i); u.x[H + i] = *(const u32x4*)(row + at.hi + 16 * i); }
+    return u;
+}
+template <bool F32> __device__ __forceinline__ void store_unit(unsigned char* row, const Place at, const Unit<F32>& u)
+{
+    constexpr int H = F32 ? 2 : 1;
+#pragma unroll
+    for (int i = 0; i < H; ++i) { *(u32x4*)(row + at.lo + 16 * i) = u.x[i]; *(u32x4*)(row + at.hi + 16 * i) = u.x[H + i]; }
+}
+
+__device__ __forceinline__ float low(const uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float high(const uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+__device__ __forceinline__ uint32_t pack(const float a, const float b)       // the one rounding of a turned element
+{
+    const bf16x2 r = __builtin_convertvector(f32x2{a, b}, bf16x2);
+    return __builtin_bit_cast(uint32_t, r);
+}
+
+template <bool F32> __device__ __forceinline__ Unit<F32> turned(const Unit<F32>& u, const Turn& t, const bool interleaved)
+{
+    Unit<F32> r;
+    float a[8], b[8];
+    if constexpr (F32) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            a[i] = __uint_as_float(interleaved ? u.x[i >> 1][2 * (i & 1)] : u.x[i >> 2][i & 3]);
+            b[i] = __uint_as_float(interleaved ? u.x[i >> 1][2 * (i & 1) + 1] : u.x[2 + (i >> 2)][i & 3]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t wa = interleaved ? u.x[i >> 2][i & 3] : u.x[0][i >> 1], wb = interleaved ? wa : u.x[1][i >> 1];
+            a[i] = interleaved || !(i & 1) ? low(wa) : high(wa);
+            b[i] = interleaved || (i & 1) ? high(wb) : low(wb);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float x = fmaf(a[i], t.c[i], -(b[i] * t.s[i])), y = fmaf(a[i], t.s[i], b[i] * t.c[i]);
+        a[i] = x; b[i] = y;
+    }
+    if constexpr (F32) {
+#pragma unroll
+        for (int w = 0; w < 16; ++w) {
+            const float n = w & 1 ? b[w >> 1] : a[w >> 1], h = w < 8 ? a[w & 7] : b[w & 7];
+            r.x[w >> 2][w & 3] = __float_as_uint(interleaved ? n : h);
+        }
+    } else {
+#pragma unroll
+        for (int w = 0; w < 8; ++w) {
+            const uint32_t n = pack(a[w], b[w]), h = w < 4 ? pack(a[2 * w], a[2 * w + 1]) : pack(b[2 * w - 8], b[2 * w - 7]);
+            r.x[w >> 2][w & 3] = interleaved ? n : h;
+        }
+    }
+    return r;
+}
+
+// ---- rows beside the cache --------------------------------------------------------------------------
+
+// Workgroup `wg` of those that turn [n_tok][n_heads][D] x into y: a stretch of tokens and HEADS heads, for which a thread forms its
+// sines and cosines once.
+template <int D, bool F32, int HEADS>
+__device__ __forceinline__ void turn_rows(const sk_rotation& rot, const int32_t* positions, const int32_t pos0, const int n_tok, const int n_heads,
+                                          const void* x, void* y, const int wg)
+{
+    constexpr int U = D / 16, ROWB = D * (F32 ? 4 : 2), TOK = 256 / U;
+    const int head_groups = (n_heads + HEADS - 1) / HEADS, stretch = wg / head_groups, head0 = (wg - stretch * head_groups) * HEADS;
+    const int unit = threadIdx.x % U, tok = stretch * TOK + threadIdx.x / U;
+    if (tok >= n_tok) return;
+    const bool turns = 16 * unit < rot.rotary;
+    const Place at = place_of<F32>(rot, unit);
+    const int64_t row = ((int64_t)tok * n_heads + head0) * ROWB;
+    Unit<F32> u[HEADS];
+#pragma unroll
+    for (int h = 0; h < HEADS; ++h)
+        if (head0 + h < n_heads) u[h] = load_unit<F32>((const unsigned char*)x + row + h * ROWB, at);
+    if (turns) {
+        const Turn t = turn_of(rot, 8 * unit, positions ? positions[tok] : pos0 + tok, rot.factor);
+#pragma unroll
+        for (int h = 0; h < HEADS; ++h) u[h] = turned<F32>(u[h], t, rot.interleaved);
+    }
+#pragma unroll
+    for (int h = 0; h < HEADS; ++h)
+        if (head0 + h < n_heads) store_unit<F32>((unsigned char*)y + row + h * ROWB, at, u[h]);
+}
+
+template <int D, bool F32, int HEADS>
+__global__ __launch_bounds__(256) void sk_turn_rows(const void* q, void* q_out, const int Hq, const void* k, void* k_out, const int Hkv,
+                                                    const int32_t* positions, const int32_t pos0, const int n_tok, const int q_wgs, const sk_rotation rot)
+{
+    if ((int)blockIdx.x < q_wgs) turn_rows<D, F32, HEADS>(rot, positions, pos0, n_tok, Hq, q, q_out, blockIdx.x);
+    else turn_rows<D, F32, HEADS>(rot, positions, pos0, n_tok, Hkv, k, k_out, blockIdx.x - q_wgs);
+}
+
+// ---- the commit, turning on the way -------------------------------------------------------------------
+
+// One (16-token group, KV head) of a commit or staging list, as the plain commit does it but for k.
+template <int D, bool F32>
+__device__ __forceinline__ void commit_group(const sk_geom& g, const sk_rotation& rot, const int32_t* positions, const int32_t pos0, const void* k, const void* v,
+                                             const sk_scatter& it, const int head, int32_t* tables_rw, unsigned char* base, uint16_t* vt)
+{
+    constexpr int U = D / 16, ROWB = D * (F32 ? 4 : 2), PR = ROWB / 16, LD = D + 8;
+    const int tid = threadIdx.x, row = tid / U, unit = tid % U;
+    unsigned char* dst = base + it.dst_off + (int64_t)head * (it.to_eph ? g.eph_head_stride : g.head_stride);
+    unsigned char* vdst = dst + (it.to_eph ? g.eph_v_off : g.v_off);
+    if (it.tbl_index >= 0 && head == 0 && tid == 0) tables_rw[it.tbl_index] = it.block_id;
+    const bool mine = row < it.count;
+    const Place at = place_of<F32>(rot, unit);
+    Unit<F32> u;
+    if (mine) u = load_unit<F32>((const unsigned char*)k + ((int64_t)(it.src_tok0 + row) * g.Hkv + head) * ROWB, at);
+    constexpr int NV = (16 * PR + 255) / 256;      // pieces of v that a thread takes
+    u32x4 y[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int p = tid + 256 * i, r = p / PR;
+        if (r < it.count) y[i] = *(const u32x4*)((const unsigned char*)v + ((int64_t)(it.src_tok0 + r) * g.Hkv + head) * ROWB + (p % PR) * 16);
+    }
+    if (mine) {
+        const int tok = it.src_tok0 + row;
+        if (16 * unit < rot.rotary) u = turned<F32>(u, turn_of(rot, 8 * unit, positions ? positions[tok] : pos0 + tok, rot.factor), rot.interleaved);
+        store_unit<F32>(dst + (it.dst_slot0 + row) * ROWB, at, u);
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int p = tid + 256 * i, r = p / PR;
+        if (r < it.count) {
+            if constexpr (F32) *(u32x4*)(vdst + (it.dst_slot0 + r) * ROWB + (p % PR) * 16) = y[i];
+            else *(u32x4*)(vt + r * LD + (p % PR) * 8) = y[i];
+        }
+    }
+    if constexpr (!F32) {                           // transposed within the group of 16 slots; slots behind the last token are 0
+        __syncthreads();
+        if (tid >= 2 * D) return;
+        const int first = it.dst_slot0 & 15, dim = tid >> 1, s0 = (tid & 1) * 8 - first;
+        uint16_t* vd = (uint16_t*)vdst + (size_t)(it.dst_slot0 >> 4) * D * 16 + dim * 16 + (tid & 1) * 8;
+        uint32_t e[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) e[j] = (s0 + j >= 0 && s0 + j < it.count) ? vt[(s0 + j) * LD + dim] : 0u;
+        if (first == 0) *(u32x4*)vd = u32x4{e[0] | (e[1] << 16), e[2] | (e[3] << 16), e[4] | (e[5] << 16), e[6] | (e[7] << 16)};
+        else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (s0 + j >= 0) vd[j] = (uint16_t)e[j];
+        }
+    }
+}
+
+struct CommitArgs {
+    sk_geom g;
+    sk_div by_heads;
+    const void *k, *v, *q;
+    void* q_out;
+    const int32_t* positions;
+    int32_t pos0, n_tok, commit_wgs;
+    const sk_scatter* items;
+    int32_t* tables_rw;
+    unsigned char *kv_rw, *eph_rw;
+    sk_rotation rot;
+};
+
+template <int D, bool F32, int HEADS>
+__device__ __forceinline__ void commit_or_turn(const CommitArgs& A, const sk_scatter* items)
+{
+    __shared__ __attribute__((aligned(16))) uint16_t vt[F32 ? 8 : 16 * (D + 8)];
+    const int wg = blockIdx.x;
+    if (wg >= A.commit_wgs) { turn_rows<D, F32, HEADS>(A.rot, A.positions, A.pos0, A.n_tok, A.g.Hq, A.q, A.q_out, wg - A.commit_wgs); return; }
+    const int i = A.by_heads.mul ? (int)(__umulhi((uint32_t)wg, A.by_heads.mul) >> A.by_heads.shift) : wg, head = wg - i * A.g.Hkv;
+    const sk_scatter it = items[i];                // at once: the list may lie in host memory
+    if (it.to_eph == SK_COPY_LIST) {
+        const int at = head * 256 + threadIdx.x;
+        if (at < it.count) ((u32x4*)(A.eph_rw + it.dst_off))[at] = ((const u32x4*)items)[it.src_tok0 + at];
+        return;
+    }
+    commit_group<D, F32>(A.g, A.rot, A.positions, A.pos0, A.k, A.v, it, head, A.tables_rw, it.to_eph ? A.eph_rw : A.kv_rw, vt);
+}
+
+template <int D, bool F32, int HEADS>
+__global__ __launch_bounds__(256) void sk_turn_commit(const CommitArgs A) { commit_or_turn<D, F32, HEADS>(A, A.items); }
+template <int D, bool F32, int HEADS>
+__global__ __launch_bounds__(256) void sk_turn_commit_args(const CommitArgs A, const sk_scatter_list L) { commit_or_turn<D, F32, HEADS>(A, L.item); }
+
+// ---- keys in the cache, turned on ---------------------------------------------------------------------
+
+constexpr int kShiftTokens = 64;                   // tokens of a workgroup
+
+struct ShiftArgs {
+    sk_geom g;
+    unsigned char* kv_rw;
+    int32_t* tables_rw;
+    const int32_t* list;          // pairs of a block and what it is replaced by, from blk0 on; null: nothing is replaced
+    int32_t tbl_off, blk0;
+    int32_t start, end;           // storage indices: the first of a group, and behind the last token
+    int32_t lo, hi;               // turned: [lo, hi) without [hole_lo, hole_hi)
+    int32_t hole_lo, hole_hi;
+    int32_t delta;
+    const int32_t* deltas;        // by retained token from the stretch's first on, or null
+    int64_t delta_stride;         // from one KV head to the next
+    int32_t first;                // retained index of the stretch's first token
+    sk_rotation rot;
+};
+
+// Workgroup (64 tokens, KV head).
+template <int D, bool F32>
+__global__ __launch_bounds__(256) void sk_turn_cached(const ShiftArgs A)
+{
+    constexpr int U = D / 16, ROWB = D * (F32 ? 4 : 2), ROWS = 256 / U, N = kShiftTokens / ROWS;
+    constexpr int GB = 16 * ROWB;                  // bytes of a group's V
+    const int tid = threadIdx.x, span = blockIdx.x / A.g.Hkv, head = blockIdx.x - span * A.g.Hkv;
+    const int t0 = A.start + span * kShiftTokens, unit = tid % U;
+    unsigned char* kv = A.kv_rw + (int64_t)head * A.g.head_stride;
+    auto block_of = [&](const int t, int& from, int& to) {
+        const int b = t >> A.g.log2B;
+        if (A.list) { from = A.list[2 * (b - A.blk0)]; to = A.list[2 * (b - A.blk0) + 1]; }
+        else from = to = A.g.tables[A.tbl_off + b];
+    };
+    const Place at = place_of<F32>(A.rot, unit);
+    const bool turns = 16 * unit < A.rot.rotary;
+    Unit<F32> u[N];
+    unsigned char* to_row[N];
+    bool moves[N], writes[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int t = t0 + tid / U + i * ROWS;
+        moves[i] = turns && t >= A.lo && t < A.hi && !(t >= A.hole_lo && t < A.hole_hi);
+        writes[i] = false;
+        if (t < A.end) {
+            int from, to;
+            block_of(t, from, to);
+            const int64_t row = (int64_t)(t & (A.g.B - 1)) * ROWB;
+            writes[i] = moves[i] || from != to;
+            to_row[i] = kv + (int64_t)to * A.g.blk_stride + row;
+            if (writes[i]) u[i] = load_unit<F32>(kv + (int64_t)from * A.g.blk_stride + row, at);
+        }
+    }
+    // V of blocks that are replaced: whole groups of 16 slots
+    if (A.list) {
+        constexpr int PV = GB / 16;                // pieces of a group
+#pragma unroll
+        for (int i = 0; i < kShiftTokens / 16 * PV / 256; ++i) {
+            const int p = tid + 256 * i, t = t0 + p / PV * 16;
+            if (t >= A.end) continue;
+            int from, to;
+            block_of(t, from, to);
+            if (from == to) continue;
+            const int64_t off = A.g.v_off + (int64_t)((t & (A.g.B - 1)) >> 4) * GB + (p % PV) * 16;
+            *(u32x4*)(kv + (int64_t)to * A.g.blk_stride + off) = *(const u32x4*)(kv + (int64_t)from * A.g.blk_stride + off);
+        }
+        if (head == 0 && tid < kShiftTokens / 16) {
+            const int t = t0 + 16 * tid;
+            if (t < A.end && (t & (A.g.B - 1)) == 0) A.tables_rw[A.tbl_off + (t >> A.g.log2B)] = A.list[2 * ((t >> A.g.log2B) - A.blk0) + 1];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if (!writes[i]) continue;
+        if (moves[i]) {
+            const int t = t0 + tid / U + i * ROWS;
+            int32_t d = A.delta;
+            if (A.deltas) d = A.deltas[head * A.delta_stride + (t >= A.hole_hi ? t - (A.hole_hi - A.hole_lo) : t) - A.first];
+            if (d != 0) u[i] = turned<F32>(u[i], turn_of(A.rot, 8 * unit, d, 1.f), A.rot.interleaved);
+        }
+        store_unit<F32>(to_row[i], at, u[i]);
+    }
+}
+
+// ---- launches -----------------------------------------------------------------------------------------
+
+#define SK_BY_SHAPE(g, CALL)                                                          \
+    do {                                                                              \
+        if ((g).elem == 4) { if ((g).d == 128) { CALL(128, true); } else { CALL(64, true); } } \
+        else { if ((g).d == 128) { CALL(128, false); } else { CALL(64, false); } }    \
+    } while (0)
+
+unsigned row_wgs(const sk_geom& g, const int n_tok, const int n_heads, const int heads)
+{
+    const int tok = 256 / (g.d / 16);
+    return unsigned((n_tok + tok - 1) / tok) * unsigned((n_heads + heads - 1) / heads);
+}
+
+// Heads of a thread: four where one each would give more workgroups than the chip holds at once.
+bool four_heads(const sk_geom& g, const int n_tok) { return row_wgs(g, n_tok, g.Hq, 1) >= 2048; }
+
+int launch_rows(const sk_geom& g, const sk_turned& t, const void* q, const void* k, void* k_out, void* stream)
+{
+    const bool four = four_heads(g, t.n_tok);
+    const unsigned q_wgs = q ? row_wgs(g, t.n_tok, g.Hq, four ? 4 : 1) : 0, k_wgs = k ? row_wgs(g, t.n_tok, g.Hkv, four ? 4 : 1) : 0;
+    if (q_wgs + k_wgs == 0) return 0;
+    hipStream_t st = (hipStream_t)stream;
+#define SK_ROWS(D, F32)                                                                                                                        \
+    if (four) hipLaunchKernelGGL((sk_turn_rows<D, F32, 4>), dim3(q_wgs + k_wgs), dim3(256), 0, st, q, t.q_out, g.Hq, k, k_out, g.Hkv, t.positions, t.pos0, t.n_tok, (int)q_wgs, *t.rot); \
+    else hipLaunchKernelGGL((sk_turn_rows<D, F32, 1>), dim3(q_wgs + k_wgs), dim3(256), 0, st, q, t.q_out, g.Hq, k, k_out, g.Hkv, t.positions, t.pos0, t.n_tok, (int)q_wgs, *t.rot)
+    SK_BY_SHAPE(g, SK_ROWS);
+#undef SK_ROWS
+    return (int)hipGetLastError();
+}
+
+int launch_commit(const sk_geom& g, const sk_turned& t, const void* k, const void* v, const sk_scatter* items, const sk_scatter_list* args, int32_t n_items,
+                  int32_t* tables_rw, unsigned char* kv_rw, unsigned char* eph_rw, void* stream)
+{
+    CommitArgs A;
+    A.g = g; A.by_heads = sk_make_div((uint32_t)g.Hkv);
+    A.k = k; A.v = v; A.q = t.q; A.q_out = t.q_out;
+    A.positions = t.positions; A.pos0 = t.pos0; A.n_tok = t.n_tok;
+    A.commit_wgs = n_items * g.Hkv;
+    A.items = items; A.tables_rw = tables_rw; A.kv_rw = kv_rw; A.eph_rw = eph_rw;
+    A.rot = *t.rot;
+    const bool four = four_heads(g, t.n_tok);
+    const dim3 grid((unsigned)A.commit_wgs + (t.q ? row_wgs(g, t.n_tok, g.Hq, four ? 4 : 1) : 0)), block(256);
+    hipStream_t st = (hipStream_t)stream;
+#define SK_COMMIT(D, F32)                                                                                       \
+    if (args) { if (four) hipLaunchKernelGGL((sk_turn_commit_args<D, F32, 4>), grid, block, 0, st, A, *args);   \
+                else hipLaunchKernelGGL((sk_turn_commit_args<D, F32, 1>), grid, block, 0, st, A, *args); }      \
+    else if (four) hipLaunchKernelGGL((sk_turn_commit<D, F32, 4>), grid, block, 0, st, A);                      \
+    else hipLaunchKernelGGL((sk_turn_commit<D, F32, 1>), grid, block, 0, st, A)
+    SK_BY_SHAPE(g, SK_COMMIT);
+#undef SK_COMMIT
+    return (int)hipGetLastError();
+}
+int launch_scatter(const sk_geom& g, const sk_turned& t, const void* k, const void* v, const sk_scatter* items, int32_t n_items,
+                   int32_t* tables_rw, unsigned char* kv_rw, unsigned char* eph_rw, void* stream)
+{
+    return launch_commit(g, t, k, v, items, nullptr, n_items, tables_rw, kv_rw, eph_rw, stream);
+}
+int launch_scatter_args(const sk_geom& g, const sk_turned& t, const void* k, const void* v, const sk_scatter_list& items, int32_t n_items,
+                        int32_t* tables_rw, unsigned char* kv_rw, unsigned char* eph_rw, void* stream)
+{
+    return launch_commit(g, t, k, v, nullptr, &items, n_items, tables_rw, kv_rw, eph_rw, stream);
+}
+
+bool aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
+
+sk_turned make_turned(const sk_rotation* rot, const void* q, void* q_out, const int32_t* positions, int32_t pos0, int32_t n_tok)
+{
+    sk_turned t;
+    t.rot = rot; t.positions = positions; t.pos0 = pos0; t.n_tok = n_tok; t.q = q; t.q_out = q_out;
+    t.rows = launch_rows; t.scatter = launch_scatter; t.scatter_args = launch_scatter_args;
+    return t;
+}
+
+}  // namespace
+
+extern "C" {
+
+int sk_pool_set_rotation(sk_pool* p, int32_t rotary_dim, int32_t interleaved, const double* inv_freq, float factor)
+{
+    if (!p) return SK_E_INVAL;
+    sk_geom g;
+    sk_geom_of(p, &g);
+    if (rotary_dim <= 0 || rotary_dim % 16 || rotary_dim > g.d) return SK_E_SHAPE;
+    if (!inv_freq || !(std::fabs(factor) <= 3.0e38f)) return SK_E_INVAL;
+    for (int i = 0; i < rotary_dim / 2; ++i)
+        if (!(std::fabs(inv_freq[i]) <= 1e6)) return SK_E_INVAL;
+    sk_rotation r = {};
+    r.rotary = rotary_dim; r.interleaved = interleaved != 0; r.factor = factor;
+    for (int i = 0; i < rotary_dim / 2; ++i) {
+        // the part of a turn a position, in 64 bits of mantissa; 2^64 itself is none
+        const long double turns = (long double)inv_freq[i] / 6.283185307179586476925286766559005768L;
+        const long double part = turns - floorl(turns), scaled = roundl(part * 18446744073709551616.0L);
+        r.step[i] = scaled >= 18446744073709551616.0L ? 0 : (uint64_t)scaled;
+    }
+    *sk_rotation_of(p) = r;
+    return SK_OK;
+}
+
+int sk_rotate(sk_pool* p, const void* q, const void* k, int32_t n_tok, const int32_t* positions, int32_t pos0, void* q_out, void* k_out, void* hip_stream)
+{
+    if (!p || !sk_rotation_of(p)->rotary || n_tok < 0) return SK_E_INVAL;
+    if (n_tok == 0) return SK_OK;
+    sk_geom g;
+    if (!sk_geom_of(p, &g)) return SK_E_NODEVICE;
+    if ((!q && !k) || (!q) != (!q_out) || (!k) != (!k_out)) return SK_E_INVAL;
+    if (!aligned(q, 16) || !aligned(k, 16) || !aligned(q_out, 16) || !aligned(k_out, 16) || !aligned(positions, 4)) return SK_E_INVAL;
+    if (!positions && pos0 > INT32_MAX - (n_tok - 1)) return SK_E_INVAL;
+    if ((int64_t)n_tok * g.Hq > (int64_t(1) << 30)) return SK_E_INVAL;
+    const sk_turned t = make_turned(sk_rotation_of(p), q, q_out, positions, pos0, n_tok);
+    if (!sk_turned_apart(g, t, n_tok, k, nullptr, k_out, nullptr, SK_F32, nullptr)) return SK_E_INVAL;
+    if (sk_injected(p, SK_SITE_SCATTER)) return SK_E_HIP;
+    const int e = launch_rows(g, t, q, k, k_out, hip_stream);
+    if (e) return sk_note_hip_error(e);
+    sk_count_launch(p);
+    return SK_OK;
+}
+
+int sk_session_append_rotated(sk_pool* p, int32_t id, const void* q, const void* k, const void* v, int32_t L, const int32_t* positions, int32_t pos0,
+                              void* q_out, void* out, int out_dtype, float* lse, void* hip_stream)
+{
+    if (!p || !sk_rotation_of(p)->rotary || L < 0) return SK_E_INVAL;
+    sk_session_view V;
+    const int rc = sk_view_session(p, id, &V);
+    if (rc) return rc;
+    sk_turned t = make_turned(sk_rotation_of(p), q, q_out, positions, pos0, L);
+    if (L > 0 && !positions && pos0 > INT32_MAX - (L - 1)) return SK_E_INVAL;
+    if (L > 0 && V.device) {
+        if ((!q) != (!q_out) || !aligned(q_out, 16) || !aligned(positions, 4)) return SK_E_INVAL;
+        if (!sk_turned_apart(V.g, t, L, k, v, nullptr, out, out_dtype, lse)) return SK_E_INVAL;
+    }
+    return sk_append_turned(p, id, t, k, v, L, out, out_dtype, lse, hip_stream);
+}
+
+int sk_batch_step_rotated(sk_pool* p, int32_t n_items, const int32_t* session_id, const int32_t* op, const int32_t* cu_tokens, const int32_t* positions,
+                          const void* q, const void* k, const void* v, void* q_out, void* out, int out_dtype, float* lse, void* hip_stream)
+{
+    if (!p || !sk_rotation_of(p)->rotary) return SK_E_INVAL;
+    if (!aligned(q_out, 16) || !aligned(positions, 4)) return SK_E_INVAL;
+    sk_turned t = make_turned(sk_rotation_of(p), q, q_out, positions, 0, 0);
+    return sk_batch_turned(p, n_items, session_id, op, cu_tokens, t, k, v, out, out_dtype, lse, hip_stream);
+}
+
+int sk_session_shift(sk_pool* p, int32_t id, int64_t first, int64_t count, int32_t delta, const int32_t* deltas, int64_t delta_stride, void* hip_stream)
+{
+    if (!p || !sk_rotation_of(p)->rotary) return SK_E_INVAL;
+    sk_session_view V;
+    int rc = sk_view_session(p, id, &V);
+    if (rc) return rc;
+    if (first < 0 || count < 0 || first > V.retained - count) return SK_E_INVAL;
+    if (!aligned(deltas, 4) || (deltas && delta_stride != 0 && delta_stride < count)) return SK_E_INVAL;
+    if (count == 0 || (!deltas && delta == 0)) return SK_OK;
+    auto stored = [&](const int64_t j) { return j < V.frozen ? j : j - V.frozen + V.win; };
+    const int64_t lo = stored(first), hi = stored(first + count - 1) + 1;
+    sk_shift E;
+    rc = sk_shift_begin(p, id, lo, hi, &E);
+    if (rc) return rc;
+    if (sk_injected(p, SK_SITE_SCATTER)) return SK_E_HIP;
+    if (V.device) {
+        // an error that an earlier call of the thread left behind is told before anything is launched: what comes back behind the launch is its own
+        int e = (int)hipGetLastError();
+        if (e) return sk_note_hip_error(e);
+        ShiftArgs A = {};
+        A.g = V.g; A.kv_rw = E.kv_rw; A.tables_rw = E.tables_rw; A.list = E.list; A.tbl_off = V.tbl_off; A.blk0 = (int32_t)E.blk0;
+        // of replaced blocks everything that holds tokens, otherwise the groups of the stretch
+        const int64_t start = E.list ? E.blk0 * V.g.B : lo / 16 * 16, behind = (E.blk0 + E.n_blk) * V.g.B;
+        const int64_t end = E.list ? (behind < E.len ? behind : E.len) : hi;
+        A.start = (int32_t)start; A.end = (int32_t)end; A.lo = (int32_t)lo; A.hi = (int32_t)hi;
+        A.hole_lo = (int32_t)V.frozen; A.hole_hi = (int32_t)V.win;
+        A.delta = delta; A.deltas = deltas; A.delta_stride = delta_stride; A.first = (int32_t)first;
+        A.rot = *sk_rotation_of(p);
+        const dim3 grid((unsigned)((end - start + kShiftTokens - 1) / kShiftTokens * V.g.Hkv)), block(256);
+#define SK_SHIFT(D, F32) hipLaunchKernelGGL((sk_turn_cached<D, F32>), grid, block, 0, (hipStream_t)hip_stream, A)
+        SK_BY_SHAPE(V.g, SK_SHIFT);
+#undef SK_SHIFT
+        e = (int)hipGetLastError();
+        if (e) return sk_note_hip_error(e);
+        sk_shift_listed(p, E, hip_stream);
+        sk_count_launch(p);
+    }
+    sk_shift_end(p, E);
+    return SK_OK;
+}
+
+}  // extern "C"
