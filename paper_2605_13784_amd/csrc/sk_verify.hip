@@ -16,6 +16,9 @@
 #include "sk_internal.h"
 #include "sk_order.h"
 
+// Which products join an addition is written out: the launches have to agree on every weight.
+#pragma clang fp contract(off)
+
 namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
@@ -24,33 +27,55 @@ constexpr int kStretch = 4096;                     // logits of a workgroup in t
 constexpr int kMaxRows = 2 * SK_VERIFY_MAX_DRAFT + 1;
 
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef u32x4 __attribute__((aligned(2))) u32x4_anywhere;      // (the hardware loads 16 bytes from any address)
 
 struct Part { double sum; float max; int32_t at; };       // of a part of a row: sum of 2^((x - max) scale), lowest index of max (greedy)
+
+// What the second launch leaves for the third, a sequence.
+struct Chosen {
+    double scale, p_max, p_inv, q_max, q_inv;
+    int32_t place;            // the row that is drawn from; -1: the token is known
+    int32_t less;             // 0: p; 1: p - q; 2: p without the drafted token
+};
 
 struct Args {
     const unsigned char *target, *draft;
     int64_t target_stride, draft_stride;           // bytes
-    int32_t n_draft, vocab, parts, stretches;
+    int32_t n_draft, vocab, parts, stretches, rows;
     const int32_t* tokens;
     const float* uniform;
     const float* temperature;
     Part* part;                                    // [sequence][target rows, then draft rows][part]
+    Chosen* chosen;                                // [sequence]
     double* sums;                                  // [sequence][stretch]
     int32_t *n_accepted, *out_tokens;
     float* logprob;
 };
 
-// 2^d for d <= 0: the integer part goes to the exponent, the rest through the series of exp, whose next term is below 2^-47
+// 2^f for |f| <= 1/2: the polynomial through the values at Chebyshev's ten points, moved by 2^-46 to be 1 at 0; within 2^-44 of itself.
+__device__ __forceinline__ double power_of_fraction(const double f)
+{
+    double r = 1.0205905320493103e-07;
+    r = __builtin_fma(r, f, 1.3259645243929057e-06); r = __builtin_fma(r, f, 1.5252672925346873e-05); r = __builtin_fma(r, f, 1.5403433751254997e-04);
+    r = __builtin_fma(r, f, 1.3333558200793719e-03); r = __builtin_fma(r, f, 9.618129193934304e-03); r = __builtin_fma(r, f, 5.550410866465168e-02);
+    r = __builtin_fma(r, f, 0.2402265069564034); r = __builtin_fma(r, f, 0.6931471805599462);
+    return __builtin_fma(r, f, 1.0);
+}
+// 2^d for d <= 0
 __device__ __forceinline__ double power_of_two(double d)
 {
     d = __builtin_fmax(d, -1100.0);                // (-inf, and NaN of -inf * 0: nothing)
-    const double n = __builtin_rint(d), f = (d - n) * 0.6931471805599453;
-    double r = 1.0 / 39916800;
-    r = __builtin_fma(r, f, 1.0 / 3628800); r = __builtin_fma(r, f, 1.0 / 362880); r = __builtin_fma(r, f, 1.0 / 40320);
-    r = __builtin_fma(r, f, 1.0 / 5040); r = __builtin_fma(r, f, 1.0 / 720); r = __builtin_fma(r, f, 1.0 / 120);
-    r = __builtin_fma(r, f, 1.0 / 24); r = __builtin_fma(r, f, 1.0 / 6); r = __builtin_fma(r, f, 0.5);
-    r = __builtin_fma(r, f, 1.0); r = __builtin_fma(r, f, 1.0);
-    return __builtin_ldexp(r, (int)n);
+    const double n = __builtin_rint(d);
+    return __builtin_ldexp(power_of_fraction(d - n), (int)n);
+}
+// The same where 2^-1000 is as good as nothing: the integer part is rounded into the low bits of a sum and added to the exponent's.
+__device__ __forceinline__ double power_of_two_in_sum(double d)
+{
+    d = __builtin_fmax(d, -1000.0);
+    const double t = d + 6755399441055744.0;       // 1.5 * 2^52
+    const uint64_t r = __builtin_bit_cast(uint64_t, power_of_fraction(d - (t - 6755399441055744.0)));
+    const uint32_t n = (uint32_t)__builtin_bit_cast(uint64_t, t);
+    return __builtin_bit_cast(double, (uint64_t)((uint32_t)(r >> 32) + (n << 20)) << 32 | (uint32_t)r);
 }
 
 template <bool F32> __device__ __forceinline__ float logit(const unsigned char* row, const int i)
@@ -59,19 +84,56 @@ template <bool F32> __device__ __forceinline__ float logit(const unsigned char* 
     return __uint_as_float((uint32_t)((const uint16_t*)row)[i] << 16);
 }
 
-__device__ __forceinline__ double shuffled(const double x, const int mask)
+// Sums and maxima over a row of 16 lanes and over a wave, in every lane, by lane exchanges within the vector unit.
+template <int CTRL> __device__ __forceinline__ double dpp(const double x)
 {
     const uint64_t b = __builtin_bit_cast(uint64_t, x);
-    const uint32_t lo = __shfl_xor((int)(uint32_t)b, mask, 64), hi = __shfl_xor((int)(uint32_t)(b >> 32), mask, 64);
-    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+    return __builtin_bit_cast(double, (uint64_t)sk_order::dpp<CTRL>((uint32_t)(b >> 32)) << 32 | sk_order::dpp<CTRL>((uint32_t)b));
+}
+__device__ __forceinline__ double row_sum(double x) { x += dpp<0xB1>(x); x += dpp<0x4E>(x); x += dpp<0x141>(x); return x + dpp<0x140>(x); }
+__device__ __forceinline__ float row_max(float x)
+{
+    auto of = [](float y, uint32_t z) { return fmaxf(y, __uint_as_float(z)); };
+    x = of(x, sk_order::dpp<0xB1>(__float_as_uint(x))); x = of(x, sk_order::dpp<0x4E>(__float_as_uint(x)));
+    x = of(x, sk_order::dpp<0x141>(__float_as_uint(x))); return of(x, sk_order::dpp<0x140>(__float_as_uint(x)));
+}
+__device__ __forceinline__ int row_min(int x)
+{
+    x = min(x, (int)sk_order::dpp<0xB1>(x)); x = min(x, (int)sk_order::dpp<0x4E>(x)); x = min(x, (int)sk_order::dpp<0x141>(x));
+    return min(x, (int)sk_order::dpp<0x140>(x));
 }
 __device__ __forceinline__ double wave_sum(double x)
 {
+    x = row_sum(x);
 #pragma unroll
-    for (int m = 1; m < 64; m *= 2) x += shuffled(x, m);
+    for (int far = 0; far < 2; ++far) {
+        const uint64_t b = __builtin_bit_cast(uint64_t, x);
+        const uint32_t l = (uint32_t)b, h = (uint32_t)(b >> 32);
+        uint32_t l0, l1, h0, h1;
+        if (far) { const auto r = __builtin_amdgcn_permlane32_swap(l, l, false, false); const auto q = __builtin_amdgcn_permlane32_swap(h, h, false, false); l0 = r[0]; l1 = r[1]; h0 = q[0]; h1 = q[1]; }
+        else { const auto r = __builtin_amdgcn_permlane16_swap(l, l, false, false); const auto q = __builtin_amdgcn_permlane16_swap(h, h, false, false); l0 = r[0]; l1 = r[1]; h0 = q[0]; h1 = q[1]; }
+        x = __builtin_bit_cast(double, (uint64_t)h0 << 32 | l0) + __builtin_bit_cast(double, (uint64_t)h1 << 32 | l1);
+    }
     return x;
 }
 __device__ __forceinline__ float wave_max(const float x) { return sk_order::value_of(__builtin_amdgcn_readfirstlane(sk_order::wave_max(sk_order::rank_of(x)))); }
+__device__ __forceinline__ double of_lane(const double x, const int lane)
+{
+    const uint64_t b = __builtin_bit_cast(uint64_t, x);
+    return __builtin_bit_cast(double, (uint64_t)(uint32_t)__shfl((int)(b >> 32), lane, 64) << 32 | (uint32_t)__shfl((int)(uint32_t)b, lane, 64));
+}
+// Sum over the lanes in front of this one.
+__device__ __forceinline__ double wave_sum_before(double x, const int lane)
+{
+    double sum = x;
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) {
+        const double y = of_lane(sum, lane - m);
+        if (lane >= m) sum += y;
+    }
+    const double y = of_lane(sum, lane - 1);
+    return lane ? y : 0.0;
+}
 
 // The exponent's factor of a sequence: log2(e) / T; greedy sequences, whose log probabilities are those of the logits as they are, have T = 1.
 __device__ __forceinline__ double scale_of(const Args& A, const int seq, bool& greedy)
@@ -81,12 +143,15 @@ __device__ __forceinline__ double scale_of(const Args& A, const int seq, bool& g
     return 1.4426950408889634 / (greedy ? 1.0 : (double)t);
 }
 
-// Tokens that a sequence has drafted: those in front of the first outside the vocabulary.
-__device__ __forceinline__ int drafted(const Args& A, const int seq)
+// Tokens that a sequence has drafted, those in front of the first outside the vocabulary, from one a lane.
+__device__ __forceinline__ int drafted(const Args& A, const int32_t token)
+{
+    return __builtin_ctzll(__ballot((int)(threadIdx.x & 63) >= A.n_draft || (uint32_t)token >= (uint32_t)A.vocab));      // (fewer than a wave's lanes)
+}
+__device__ __forceinline__ int32_t token_of_lane(const Args& A, const int seq)
 {
     const int lane = threadIdx.x & 63;
-    const bool ends = lane >= A.n_draft || (uint32_t)A.tokens[(int64_t)seq * A.n_draft + lane] >= (uint32_t)A.vocab;
-    return __builtin_ctzll(__ballot(ends));        // (fewer than a wave's lanes)
+    return lane < A.n_draft ? A.tokens[(int64_t)seq * A.n_draft + lane] : -1;
 }
 
 __device__ __forceinline__ const unsigned char* row_of(const Args& A, const int seq, const int r)
@@ -98,267 +163,292 @@ __device__ __forceinline__ const unsigned char* row_of(const Args& A, const int 
 // ---- first launch: maximum and sum of a part of a row ----
 
 template <bool F32>
-__global__ __launch_bounds__(kThreads) void sk_verify_rows(const Args A, const int rows)
+__global__ __launch_bounds__(kThreads) void sk_verify_rows(const Args A)
 {
     constexpr int EL = F32 ? 4 : 2, N = 16 / EL;
     __shared__ Part of_wave[kWaves];
-    const int part = blockIdx.x % A.parts, row = blockIdx.x / A.parts, seq = row / rows, r = row - seq * rows;
-    const int n = drafted(A, seq), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int part = blockIdx.x % A.parts, row = blockIdx.x / A.parts, seq = row / A.rows, r = row - seq * A.rows;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int n = drafted(A, token_of_lane(A, seq));
     bool greedy;
     const double scale = scale_of(A, seq, greedy);
     if (r <= A.n_draft ? r > n : greedy || r - A.n_draft - 1 >= n) return;
     const unsigned char* x = row_of(A, seq, r);
-    // pieces of 16 bytes as they lie in memory; the first and last may reach beyond the row
-    const int lead = (int)((uintptr_t)x & 15) / EL;
-    float v[kPieces * N];
     const float none = -__builtin_inff();
+    const int at0 = (part * kPieces * kThreads + (int)threadIdx.x) * N;      // piece i: N logits from at0 + i * kThreads * N on
+    float v[kPieces * N];
+    if (A.vocab >= N) {
+        // A piece that reaches behind the row is read N logits in front of its end, of which those count that are its own.
+        u32x4 w[kPieces];
 #pragma unroll
-    for (int i = 0; i < kPieces; ++i) {
-        const int at = ((part * kPieces + i) * kThreads + (int)threadIdx.x) * N - lead;
-        if (at >= 0 && at + N <= A.vocab) {
-            const u32x4 w = *(const u32x4*)(x + (int64_t)at * EL);
+        for (int i = 0; i < kPieces; ++i) w[i] = *(const u32x4_anywhere*)(x + (int64_t)min(at0 + i * kThreads * N, A.vocab - N) * EL);
 #pragma unroll
-            for (int e = 0; e < N; ++e)
-                v[i * N + e] = F32 ? __uint_as_float(w[e % 4]) : __uint_as_float(e & 1 ? w[e / 2 % 4] & 0xffff0000u : w[e / 2 % 4] << 16);
-        } else {
+        for (int i = 0; i < kPieces; ++i) {
+            const int behind = at0 + i * kThreads * N - (A.vocab - N);
 #pragma unroll
-            for (int e = 0; e < N; ++e) v[i * N + e] = at + e >= 0 && at + e < A.vocab ? logit<F32>(x, at + e) : none;
+            for (int e = 0; e < N; ++e) {
+                const float y = F32 ? __uint_as_float(w[i][e % 4]) : __uint_as_float(e & 1 ? w[i][e / 2 % 4] & 0xffff0000u : w[i][e / 2 % 4] << 16);
+                v[i * N + e] = e >= behind ? y : none;
+            }
         }
+    } else {
+#pragma unroll
+        for (int i = 0; i < kPieces * N; ++i) v[i] = i < N && at0 + i < A.vocab ? logit<F32>(x, at0 + i) : none;
     }
     float m = none;
     bool bad = false;
 #pragma unroll
     for (int i = 0; i < kPieces * N; ++i) { m = fmaxf(m, v[i]); bad |= !(v[i] < __builtin_inff()); }
     m = wave_max(m);
-    const float m0 = m == none ? 0.f : m;
-    double sum = 0.0;
+    const double m0 = m == none ? 0.0 : (double)m;
+    double sum[2] = {0.0, 0.0};
 #pragma unroll
-    for (int i = 0; i < kPieces * N; ++i) sum += power_of_two(((double)v[i] - (double)m0) * scale);
-    sum = wave_sum(sum);
+    for (int i = 0; i < kPieces * N; ++i) sum[i & 1] += power_of_two_in_sum(((double)v[i] - m0) * scale);
+    double total = wave_sum(sum[0] + sum[1]);
     int at = INT32_MAX;
     if (greedy) {
 #pragma unroll
         for (int i = kPieces * N - 1; i >= 0; --i)
-            if (v[i] == m) at = ((part * kPieces + i / N) * kThreads + (int)threadIdx.x) * N - lead + i % N;
+            if (v[i] == m) {
+                const int first = at0 + i / N * kThreads * N;
+                at = (A.vocab >= N ? min(first, A.vocab - N) : first) + i % N;
+            }
 #pragma unroll
         for (int s = 1; s < 64; s *= 2) at = min(at, __shfl_xor(at, s, 64));
     }
-    if (__ballot(bad)) sum = __builtin_nan("");
-    if (lane == 0) of_wave[wave] = Part{sum, m, at};
+    if (m == none) total = 0.0;
+    if (__ballot(bad)) total = __builtin_nan("");
+    if (lane == 0) of_wave[wave] = Part{total, m, at};
     __syncthreads();
-    if (threadIdx.x == 0) {
-        Part p = of_wave[0];
-        for (int w = 1; w < kWaves; ++w) {
-            const Part o = of_wave[w];
-            const float top = fmaxf(p.max, o.max), t0 = top == none ? 0.f : top;
-            const int32_t first = p.max > o.max ? p.at : p.max < o.max ? o.at : min(p.at, o.at);
-            p = Part{p.sum * power_of_two(((double)p.max - t0) * scale) + o.sum * power_of_two(((double)o.max - t0) * scale), top, first};
-        }
-        A.part[((int64_t)seq * rows + r) * A.parts + part] = p;
+    if (threadIdx.x < 64) {                        // lanes 0 to 3 have the waves'
+        const Part p = lane < kWaves ? of_wave[lane] : Part{0.0, none, INT32_MAX};
+        const float top = row_max(p.max);
+        const double t0 = top == none ? 0.0 : (double)top;
+        const double all = row_sum(p.sum * power_of_two(((double)p.max - t0) * scale));
+        const int first = row_min(p.max == top ? p.at : INT32_MAX);
+        if (lane == 0) A.part[((int64_t)seq * A.rows + r) * A.parts + part] = Part{all, top, first};
     }
 }
 
-// ---- which tokens stay ----
+// ---- second launch: which tokens stay, and the sums of the stretches of the row that is drawn from ----
 
 struct Row { double total; float max; int32_t at; };      // of a whole row: sum of 2^((x - max) scale); 0: no probabilities
-struct Decision {
-    Row row[kMaxRows];
-    int n;                    // drafted
-    int accepted;
-    bool greedy, valid;       // valid: the row that is drawn from has probabilities
-    bool less;                // the draft's probabilities are taken off
-    double scale;
-};
-
-template <bool F32>
-__device__ __forceinline__ void decide(const Args& A, const int rows, const int seq, Decision& D)
-{
-    const int n = drafted(A, seq), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    bool greedy;
-    const double scale = scale_of(A, seq, greedy);
-    const float none = -__builtin_inff();
-    const int n_rows = n + 1 + (A.draft && !greedy ? n : 0);
-    for (int i = wave; i < n_rows; i += kWaves) {
-        const int r = i <= n ? i : A.n_draft + 1 + (i - n - 1);
-        const Part* p = A.part + ((int64_t)seq * rows + r) * A.parts;
-        float m = none;
-        for (int c = lane; c < A.parts; c += 64) m = fmaxf(m, p[c].max);
-        m = wave_max(m);
-        const float m0 = m == none ? 0.f : m;
-        double sum = 0.0;
-        int at = INT32_MAX;
-        for (int c = lane; c < A.parts; c += 64) {
-            const Part o = p[c];
-            sum += o.sum * power_of_two(((double)o.max - m0) * scale);
-            if (o.max == m) at = min(at, o.at);
-        }
-        sum = wave_sum(sum);
-#pragma unroll
-        for (int s = 1; s < 64; s *= 2) at = min(at, __shfl_xor(at, s, 64));
-        if (lane == 0) D.row[r] = Row{sum > 0.0 ? sum : 0.0, m, at};      // (NaN: none)
-    }
-    __syncthreads();
-    if (wave == 0) {
-        bool stays = false;
-        if (lane < n) {
-            const int32_t t = A.tokens[(int64_t)seq * A.n_draft + lane];
-            const Row p = D.row[lane];
-            if (p.total == 0.0) stays = false;
-            else if (greedy) stays = t == p.at;
-            else {
-                const double px = power_of_two(((double)logit<F32>(row_of(A, seq, lane), t) - (double)p.max) * scale) / p.total;
-                double qx = 1.0;
-                bool none_drafted = false;
-                if (A.draft) {
-                    const Row q = D.row[A.n_draft + 1 + lane];
-                    none_drafted = q.total == 0.0;
-                    qx = none_drafted ? 1.0 : power_of_two(((double)logit<F32>(row_of(A, seq, A.n_draft + 1 + lane), t) - (double)q.max) * scale) / q.total;
-                }
-                stays = !none_drafted && (double)A.uniform[(int64_t)seq * (A.n_draft + 1) + lane] * qx < px;
-            }
-        }
-        const uint64_t out = ~__ballot(stays);
-        if (lane == 0) {
-            const int a = min(n, out ? __builtin_ctzll(out) : 64);
-            D.n = n; D.accepted = a; D.greedy = greedy; D.scale = scale;
-            D.valid = D.row[a].total > 0.0;
-            D.less = a < n && (!A.draft || (!greedy && D.row[A.n_draft + 1 + a].total > 0.0));
-        }
-    }
-    __syncthreads();
-}
 
 // What a logit of the row that is drawn from counts for.
 template <bool F32> struct Weights {
     const unsigned char *p, *q;
-    double scale, p_max, p_inv, q_max, q_inv;
-    int32_t without;          // a draft without probabilities: its token
-    __device__ __forceinline__ Weights(const Args& A, const Decision& D, const int seq)
+    Chosen c;
+    int32_t without;
+    __device__ __forceinline__ Weights(const Args& A, const Chosen& chosen, const int seq) : c(chosen)
     {
-        const int a = D.accepted;
-        p = row_of(A, seq, a);
-        scale = D.scale; p_max = D.row[a].max; p_inv = 1.0 / D.row[a].total;
-        q = nullptr; q_max = q_inv = 0.0; without = -1;
-        if (D.less && A.draft) { const Row& r = D.row[A.n_draft + 1 + a]; q = row_of(A, seq, A.n_draft + 1 + a); q_max = r.max; q_inv = 1.0 / r.total; }
-        else if (D.less) without = A.tokens[(int64_t)seq * A.n_draft + a];
+        p = row_of(A, seq, c.place);
+        q = c.less == 1 ? row_of(A, seq, A.n_draft + 1 + c.place) : p;
+        without = c.less == 2 ? A.tokens[(int64_t)seq * A.n_draft + c.place] : -1;
     }
-    __device__ __forceinline__ double operator()(const int i) const
+    // of logits x and y of the two rows, at index i
+    __device__ __forceinline__ double operator()(const float x, const float y, const int i) const
     {
-        double w = power_of_two(((double)logit<F32>(p, i) - p_max) * scale) * p_inv;
-        if (q) w = __builtin_fmax(w - power_of_two(((double)logit<F32>(q, i) - q_max) * scale) * q_inv, 0.0);
+        double w = power_of_two(((double)x - c.p_max) * c.scale) * c.p_inv;
+        if (c.less == 1) w = __builtin_fmax(w - power_of_two(((double)y - c.q_max) * c.scale) * c.q_inv, 0.0);
         return i == without ? 0.0 : w;
     }
 };
 
-// ---- second launch: the sum of a stretch of the drawn row ----
-
 template <bool F32>
-__global__ __launch_bounds__(kThreads) void sk_verify_stretches(const Args A, const int rows)
-{
-    __shared__ Decision D;
-    __shared__ double of_wave[kWaves];
-    const int stretch = blockIdx.x % A.stretches, seq = blockIdx.x / A.stretches;
-    decide<F32>(A, rows, seq, D);
-    if (D.greedy || !D.valid) return;
-    const Weights<F32> w(A, D, seq);
-    double sum = 0.0;
-#pragma unroll 4
-    for (int i = 0; i < kStretch / kThreads; ++i) {
-        const int t = stretch * kStretch + i * kThreads + threadIdx.x;
-        if (t < A.vocab) sum += w(t);
-    }
-    sum = wave_sum(sum);
-    if ((threadIdx.x & 63) == 0) of_wave[threadIdx.x >> 6] = sum;
-    __syncthreads();
-    if (threadIdx.x == 0) A.sums[(int64_t)seq * A.stretches + stretch] = of_wave[0] + of_wave[1] + of_wave[2] + of_wave[3];
-}
-
-// ---- third launch: the draw, and what a sequence's outputs are ----
-
-// The token that the sequence's last number finds in the running sum of the row's weights, for the whole workgroup.
-template <bool F32>
-__device__ __forceinline__ int draw(const Args& A, const Decision& D, const int seq)
+__global__ __launch_bounds__(kThreads) void sk_verify_stretches(const Args A)
 {
     constexpr int EACH = kStretch / kThreads;
-    __shared__ double of_thread[kThreads];
-    __shared__ int chosen;
-    __shared__ double left;
-    const int tid = threadIdx.x;
-    const Weights<F32> w(A, D, seq);
-    const double* sums = A.sums + (int64_t)seq * A.stretches;
-    if (tid == 0) {
-        double total = 0.0, before = 0.0, at_last = 0.0;
-        for (int c = 0; c < A.stretches; ++c) total += sums[c];
-        const double limit = __builtin_fmax((double)A.uniform[(int64_t)seq * (A.n_draft + 1) + A.n_draft], 0.0) * total;
-        int c = 0, last = 0;
-        for (; c < A.stretches; ++c) {
-            if (sums[c] > 0.0) { last = c; at_last = before; }
-            if (before + sums[c] > limit) break;
-            before += sums[c];
+    __shared__ Row row[kMaxRows];
+    __shared__ Chosen chosen;
+    __shared__ double of_wave[kWaves];
+    const int stretch = blockIdx.x % A.stretches, seq = blockIdx.x / A.stretches, tid = threadIdx.x, lane = tid & 63;
+    const float none = -__builtin_inff();
+    bool greedy;
+    const double scale = scale_of(A, seq, greedy);
+    const int32_t token = token_of_lane(A, seq);
+    const int n = drafted(A, token);
+    // a drafted token's logits, for the lanes of the first wave
+    float xp = none, xq = none, u = 0.f;
+    if (tid < n) {
+        xp = logit<F32>(row_of(A, seq, lane), token);
+        if (A.draft) xq = logit<F32>(row_of(A, seq, A.n_draft + 1 + lane), token);
+        u = A.uniform[(int64_t)seq * (A.n_draft + 1) + lane];
+    }
+    // the parts of a row meet in sixteen lanes (rows that were not computed hold anything, and are not looked at)
+    for (int r = tid >> 4; r < A.rows; r += kThreads / 16) {
+        const Part* p = A.part + ((int64_t)seq * A.rows + r) * A.parts;
+        float m = none;
+        double sum = 0.0;
+        int at = INT32_MAX;
+        for (int c = tid & 15; c < A.parts; c += 16) {
+            const Part o = p[c];
+            const float top = fmaxf(m, o.max);
+            const double t0 = top == none ? 0.0 : (double)top;
+            sum = sum * power_of_two(((double)m - t0) * scale) + o.sum * power_of_two(((double)o.max - t0) * scale);
+            at = o.max > m ? o.at : o.max == m ? min(at, o.at) : at;
+            m = top;
         }
-        if (c == A.stretches) { c = last; before = at_last; }
-        chosen = total > 0.0 ? c : -1; left = limit - before;
+        const float top = row_max(m);
+        const double t0 = top == none ? 0.0 : (double)top;
+        sum = row_sum(sum * power_of_two(((double)m - t0) * scale));
+        at = row_min(m == top ? at : INT32_MAX);
+        if ((tid & 15) == 0) row[r] = Row{sum > 0.0 ? sum : 0.0, top, at};      // (NaN: none)
     }
     __syncthreads();
-    // nothing is left of the target: p and q are one, and the drafted token is as good
-    if (chosen < 0) return A.tokens[(int64_t)seq * A.n_draft + D.accepted];
-    const int begin = chosen * kStretch + tid * EACH;
-    double mine = 0.0;
-    for (int i = 0; i < EACH; ++i)
-        if (begin + i < A.vocab) mine += w(begin + i);
-    of_thread[tid] = mine;
-    __syncthreads();
-    if (tid == 0) {
-        double before = 0.0, at_last = 0.0;
-        int t = 0, last = 0;
-        for (; t < kThreads; ++t) {
-            if (of_thread[t] > 0.0) { last = t; at_last = before; }
-            if (before + of_thread[t] > left) break;
-            before += of_thread[t];
+    if (tid < 64) {
+        bool stays = false;
+        if (lane < n && row[lane].total > 0.0) {
+            const Row p = row[lane];
+            if (greedy) stays = token == p.at;
+            else {
+                const double px = power_of_two(((double)xp - (double)p.max) * scale) / p.total;
+                double qx = 1.0;
+                bool known = true;
+                if (A.draft) {
+                    const Row q = row[A.n_draft + 1 + lane];
+                    known = q.total > 0.0;
+                    if (known) qx = power_of_two(((double)xq - (double)q.max) * scale) / q.total;
+                }
+                stays = known && (double)u * qx < px;
+            }
         }
-        if (t == kThreads) { t = last; before = at_last; }
-        const int from = chosen * kStretch + t * EACH;
-        int found = from;
-        for (int i = 0; i < EACH && from + i < A.vocab; ++i) {
-            const double x = w(from + i);
-            if (x > 0.0) found = from + i;         // (the last that counts, where roundings leave the sum below the limit)
-            before += x;
-            if (before > left && x > 0.0) break;
+        const uint64_t out = ~__ballot(stays);
+        const int a = min(n, (int)__builtin_ctzll(out));            // (lanes from n on are out)
+        const Row p = row[a];
+        const bool valid = p.total > 0.0;
+        if (lane == 0) {
+            Chosen c = {scale, (double)p.max, 1.0 / p.total, 0.0, 0.0, valid && !greedy ? a : -1, 0};
+            if (a < n && !A.draft) c.less = 2;
+            else if (a < n && !greedy && row[A.n_draft + 1 + a].total > 0.0) {
+                const Row q = row[A.n_draft + 1 + a];
+                c.less = 1; c.q_max = q.max; c.q_inv = 1.0 / q.total;
+            }
+            chosen = c;
+            if (stretch == 0) { A.chosen[seq] = c; A.n_accepted[seq] = a; }
         }
-        chosen = found;
+        if (stretch == 0 && lane <= A.n_draft) {   // everything but a token that is still to be drawn
+            const int32_t t = lane < a ? token : lane == a && valid && greedy ? p.at : -1;
+            const int64_t at = (int64_t)seq * (A.n_draft + 1) + lane;
+            A.out_tokens[at] = t;
+            if (A.logprob) {
+                float l = 0.f;
+                if (lane < a || (lane == a && valid && greedy)) {
+                    const Row r = row[lane];
+                    l = (float)(((double)logit<F32>(row_of(A, seq, lane), t) - (double)r.max) * (scale * 0.6931471805599453) - log(r.total));
+                } else if (lane == a && !valid) l = __builtin_nanf("");
+                A.logprob[at] = l;
+            }
+        }
     }
     __syncthreads();
-    return chosen;
+    if (chosen.place < 0) return;
+    const Weights<F32> w(A, chosen, seq);
+    float x[EACH], y[EACH];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int t = min(stretch * kStretch + i * kThreads + tid, A.vocab - 1);
+        x[i] = logit<F32>(w.p, t);
+        y[i] = logit<F32>(w.q, t);
+    }
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int t = stretch * kStretch + i * kThreads + tid;
+        if (t < A.vocab) sum += w(x[i], y[i], t);
+    }
+    sum = wave_sum(sum);
+    if (lane == 0) of_wave[tid >> 6] = sum;
+    __syncthreads();
+    if (tid == 0) A.sums[(int64_t)seq * A.stretches + stretch] = of_wave[0] + of_wave[1] + of_wave[2] + of_wave[3];
 }
 
+// ---- third launch: the draw ----
+
+// The token that the sequence's last number finds in the running sum of the row's weights: the stretch, by the first wave, then the thread, then its logit.
 template <bool F32>
-__global__ __launch_bounds__(kThreads) void sk_verify_draw(const Args A, const int rows)
+__global__ __launch_bounds__(kThreads) void sk_verify_draw(const Args A)
 {
-    __shared__ Decision D;
-    const int seq = blockIdx.x, tid = threadIdx.x;
-    decide<F32>(A, rows, seq, D);
-    const int a = D.accepted;
-    int token = -1;
-    if (D.valid) token = D.greedy ? D.row[a].at : draw<F32>(A, D, seq);
-    if (tid == 0) A.n_accepted[seq] = a;
-    if (tid <= A.n_draft) {
-        const int32_t t = tid < a ? A.tokens[(int64_t)seq * A.n_draft + tid] : tid == a ? token : -1;
-        A.out_tokens[(int64_t)seq * (A.n_draft + 1) + tid] = t;
-        if (A.logprob) {
-            float l = 0.f;
-            if (tid <= a) {
-                const Row r = D.row[tid];
-                l = t < 0 ? __builtin_nanf("") : (float)(((double)logit<F32>(row_of(A, seq, tid), t) - (double)r.max) * (D.scale * 0.6931471805599453) - log(r.total));
+    constexpr int EACH = kStretch / kThreads;      // logits of a thread, one behind the other
+    __shared__ double of_wave[kWaves], left_of;
+    __shared__ int chosen_stretch, token_of;
+    const int seq = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const Chosen c = A.chosen[seq];
+    if (c.place < 0) return;
+    if (wave == 0) {
+        const double* sums = A.sums + (int64_t)seq * A.stretches;
+        double total = 0.0;
+        for (int i = lane; i < A.stretches; i += 64) total += sums[i];
+        total = wave_sum(total);
+        const double limit = __builtin_fmax((double)A.uniform[(int64_t)seq * (A.n_draft + 1) + A.n_draft], 0.0) * total;
+        double before = 0.0, left = 0.0;
+        int found = -1;
+        for (int base = 0; base < A.stretches; base += 64) {
+            const double mine = base + lane < A.stretches ? sums[base + lane] : 0.0, mine_before = before + wave_sum_before(mine, lane);
+            // the first whose running sum exceeds the limit; until there is one, the last that counts (roundings, or a number from 1 on)
+            const uint64_t over = __ballot(mine > 0.0 && mine_before + mine > limit), some = __ballot(mine > 0.0);
+            if (some) {
+                const int l = over ? __builtin_ctzll(over) : 63 - __builtin_clzll(some);
+                found = base + l;
+                left = limit - of_lane(mine_before, l);
             }
-            A.logprob[(int64_t)seq * (A.n_draft + 1) + tid] = l;
+            if (over) break;
+            before = of_lane(mine_before, 63) + of_lane(mine, 63);
         }
+        if (lane == 0) { chosen_stretch = found; left_of = left; token_of = 0; }
+    }
+    __syncthreads();
+    int token;
+    // nothing is left of the target: p and q are one, and the drafted token is as good
+    if (chosen_stretch < 0) token = c.less ? A.tokens[(int64_t)seq * A.n_draft + c.place] : 0;
+    else {
+        const Weights<F32> w(A, c, seq);
+        const int begin = chosen_stretch * kStretch + tid * EACH;
+        float x[EACH], y[EACH];
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int t = min(begin + i, A.vocab - 1);
+            x[i] = logit<F32>(w.p, t);
+            y[i] = logit<F32>(w.q, t);
+        }
+        double weight[EACH], mine = 0.0;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) { weight[i] = begin + i < A.vocab ? w(x[i], y[i], begin + i) : 0.0; mine += weight[i]; }
+        double before = wave_sum_before(mine, lane);
+        if (lane == 63) of_wave[wave] = before + mine;
+        __syncthreads();
+        for (int i = 0; i < wave; ++i) before += of_wave[i];
+        // the thread in which the running sum passes what is left; if none, the last that counts: the highest of those that say so
+        const double left = left_of;
+        const uint64_t over = __ballot(mine > 0.0 && before + mine > left), some = __ballot(mine > 0.0);
+        const bool last = !over && some && lane == 63 - __builtin_clzll(some), first = over && lane == __builtin_ctzll(over);
+        if (first || last) {
+            int t = begin;
+            double sum = before;
+            bool passed = false;
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) {
+                if (!passed && weight[i] > 0.0) t = begin + i;
+                sum += weight[i];
+                passed |= weight[i] > 0.0 && sum > left;
+            }
+            // of several waves' answers the lowest that passes, or else the highest
+            if (first) atomicMax(&token_of, (1 << 30) | ((1 << 29) - t));
+            else atomicMax(&token_of, t);
+        }
+        __syncthreads();
+        token = token_of & (1 << 30) ? (1 << 29) - (token_of & ~(1 << 30)) : token_of;
+    }
+    if (tid == 0) {
+        const int64_t at = (int64_t)seq * (A.n_draft + 1) + c.place;
+        A.out_tokens[at] = token;
+        if (A.logprob) A.logprob[at] = (float)(((double)logit<F32>(row_of(A, seq, c.place), token) - c.p_max) * (c.scale * 0.6931471805599453) + log(c.p_inv));
     }
 }
 
 int64_t parts_of(const int dtype_bytes, const int32_t vocab)
 {
     const int n = 16 / dtype_bytes;
-    return ((int64_t)vocab + n - 1 + kPieces * kThreads * n - 1) / (kPieces * kThreads * n);
+    return ((int64_t)vocab + kPieces * kThreads * n - 1) / (kPieces * kThreads * n);
 }
 bool sizes_ok(const int32_t n_seq, const int32_t n_draft, const int32_t vocab)
 {
@@ -375,7 +465,7 @@ size_t sk_verify_workspace_bytes(int32_t n_seq, int32_t n_draft, int32_t vocab)
     if (!sizes_ok(n_seq, n_draft, vocab)) return 0;
     // (for either type of the logits: fp32 ones have more parts)
     const int64_t stretches = ((int64_t)vocab + kStretch - 1) / kStretch;
-    return size_t(n_seq) * (size_t(2 * n_draft + 1) * size_t(parts_of(4, vocab)) * sizeof(Part) + size_t(stretches) * 8);
+    return size_t(n_seq) * (size_t(2 * n_draft + 1) * size_t(parts_of(4, vocab)) * sizeof(Part) + sizeof(Chosen) + size_t(stretches) * 8);
 }
 
 int sk_verify(const void* target, int64_t target_stride, const void* draft, int64_t draft_stride, int dtype, int32_t n_seq, int32_t n_draft, int32_t vocab,
@@ -399,21 +489,22 @@ int sk_verify(const void* target, int64_t target_stride, const void* draft, int6
     A.n_draft = n_draft; A.vocab = vocab;
     A.parts = (int32_t)parts_of(el, vocab); A.stretches = (vocab + kStretch - 1) / kStretch;
     A.tokens = tokens; A.uniform = uniform; A.temperature = temperature;
-    const int rows = n_draft + 1 + (A.draft ? n_draft : 0);
+    const int rows = A.rows = n_draft + 1 + (A.draft ? n_draft : 0);
     A.part = (Part*)workspace;
-    A.sums = (double*)(A.part + (int64_t)n_seq * rows * A.parts);
+    A.chosen = (Chosen*)(A.part + (int64_t)n_seq * rows * A.parts);
+    A.sums = (double*)(A.chosen + n_seq);
     A.n_accepted = n_accepted; A.out_tokens = out_tokens; A.logprob = logprob;
     if ((int64_t)n_seq * rows * A.parts >= (int64_t(1) << 31) || (int64_t)n_seq * A.stretches >= (int64_t(1) << 31)) return SK_E_INVAL;
     hipStream_t st = (hipStream_t)hip_stream;
     const dim3 block(kThreads), first((unsigned)(n_seq * rows) * (unsigned)A.parts), second((unsigned)n_seq * (unsigned)A.stretches);
     if (dtype == SK_F32) {
-        hipLaunchKernelGGL(sk_verify_rows<true>, first, block, 0, st, A, rows);
-        hipLaunchKernelGGL(sk_verify_stretches<true>, second, block, 0, st, A, rows);
-        hipLaunchKernelGGL(sk_verify_draw<true>, dim3(n_seq), block, 0, st, A, rows);
+        hipLaunchKernelGGL(sk_verify_rows<true>, first, block, 0, st, A);
+        hipLaunchKernelGGL(sk_verify_stretches<true>, second, block, 0, st, A);
+        hipLaunchKernelGGL(sk_verify_draw<true>, dim3(n_seq), block, 0, st, A);
     } else {
-        hipLaunchKernelGGL(sk_verify_rows<false>, first, block, 0, st, A, rows);
-        hipLaunchKernelGGL(sk_verify_stretches<false>, second, block, 0, st, A, rows);
-        hipLaunchKernelGGL(sk_verify_draw<false>, dim3(n_seq), block, 0, st, A, rows);
+        hipLaunchKernelGGL(sk_verify_rows<false>, first, block, 0, st, A);
+        hipLaunchKernelGGL(sk_verify_stretches<false>, second, block, 0, st, A);
+        hipLaunchKernelGGL(sk_verify_draw<false>, dim3(n_seq), block, 0, st, A);
     }
     return sk_status_of((int)hipGetLastError());
 }
