@@ -22,18 +22,21 @@
 namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
-constexpr int kPieces = 8;                         // 16-byte pieces of a thread in the first launch
+constexpr int kEach = 32, kEachFew = 8;            // logits of a thread in the first launch; where there are few rows
 constexpr int kStretch = 4096;                     // logits of a workgroup in the second
 constexpr int kMaxRows = 2 * SK_VERIFY_MAX_DRAFT + 1;
 
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef u32x4 __attribute__((aligned(2))) u32x4_anywhere;      // (the hardware loads 16 bytes from any address)
 
-struct Part { double sum; float max; int32_t at; };       // of a part of a row: sum of 2^((x - max) scale), lowest index of max (greedy)
+// Of a part of a row, or of all of it: sum of 2^(x scale - e) with a whole number e next to the maximum's, so that parts meet without a rounding;
+// the lowest index of the maximum (greedy sequences).
+struct Part { double sum, e; float max; int32_t at; };
 
 // What the second launch leaves for the third, a sequence.
 struct Chosen {
-    double scale, p_max, p_inv, q_max, q_inv;
+    double scale, p_e, p_inv, q_e, q_inv;
+    float p_max, q_max;
     int32_t place;            // the row that is drawn from; -1: the token is known
     int32_t less;             // 0: p; 1: p - q; 2: p without the drafted token
 };
@@ -61,21 +64,45 @@ __device__ __forceinline__ double power_of_fraction(const double f)
     r = __builtin_fma(r, f, 0.2402265069564034); r = __builtin_fma(r, f, 0.6931471805599462);
     return __builtin_fma(r, f, 1.0);
 }
-// 2^d for d <= 0
-__device__ __forceinline__ double power_of_two(double d)
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+
+// From 2^50 on, x scale is a whole number and two different logits lie further apart than 2^1000: only the maximum counts.
+constexpr double kFar = 1125899906842624.0;
+
+// 2^(x scale - e), where e is no less than a whole number next to the row's largest x scale
+__device__ __forceinline__ double weight_of(const float x, const double scale, const double e, const float max)
 {
-    d = __builtin_fmax(d, -1100.0);                // (-inf, and NaN of -inf * 0: nothing)
+    if (__builtin_fabs(e) >= kFar) return x == max ? 1.0 : 0.0;
+    const double d = __builtin_fmax(__builtin_fma((double)x, scale, -e), -1100.0);      // (-inf, and NaN of -inf * 0: nothing)
     const double n = __builtin_rint(d);
     return __builtin_ldexp(power_of_fraction(d - n), (int)n);
 }
-// The same where 2^-1000 is as good as nothing: the integer part is rounded into the low bits of a sum and added to the exponent's.
-__device__ __forceinline__ double power_of_two_in_sum(double d)
+// The same for many, where 2^-1000 is as good as nothing and |e| is below 2^50: the integer part is rounded into the low bits of a sum and added to the exponent's.
+__device__ __forceinline__ double weight_in_sum(const float x, const double scale, const double e)
 {
-    d = __builtin_fmax(d, -1000.0);
+    const double d = __builtin_fmax(__builtin_fma((double)x, scale, -e), -1000.0);
     const double t = d + 6755399441055744.0;       // 1.5 * 2^52
-    const uint64_t r = __builtin_bit_cast(uint64_t, power_of_fraction(d - (t - 6755399441055744.0)));
-    const uint32_t n = (uint32_t)__builtin_bit_cast(uint64_t, t);
-    return __builtin_bit_cast(double, (uint64_t)((uint32_t)(r >> 32) + (n << 20)) << 32 | (uint32_t)r);
+    u32x2 r = __builtin_bit_cast(u32x2, power_of_fraction(d - (t - 6755399441055744.0)));
+    r.y += __builtin_bit_cast(u32x2, t).x << 20;
+    return __builtin_bit_cast(double, r);
+}
+// The logarithm of a token's probability
+__device__ __forceinline__ float log_probability(const float x, const double scale, const double e, const float max, const double inverse)
+{
+    const double d = __builtin_fabs(e) < kFar ? __builtin_fma((double)x, scale, -e) : ((double)x - (double)max) * scale;
+    return (float)(d * 0.6931471805599453 + log(inverse));
+}
+// A sum from exponent `from` to the larger one `to`
+__device__ __forceinline__ double at_exponent(const double sum, const double from, const double to)
+{
+    return __builtin_ldexp(sum, (int)__builtin_fmax(from - to, -2200.0));
+}
+// The exponent of a maximum; of none, lower than any other
+constexpr double kNoExponent = -1.0e300;
+__device__ __forceinline__ double exponent_of(const float max, const double scale)
+{
+    const double e = __builtin_rint((double)max * scale);
+    return max == -__builtin_inff() ? kNoExponent : e;
 }
 
 template <bool F32> __device__ __forceinline__ float logit(const unsigned char* row, const int i)
@@ -162,10 +189,10 @@ __device__ __forceinline__ const unsigned char* row_of(const Args& A, const int 
 
 // ---- first launch: maximum and sum of a part of a row ----
 
-template <bool F32>
+template <bool F32, int EACH>
 __global__ __launch_bounds__(kThreads) void sk_verify_rows(const Args A)
 {
-    constexpr int EL = F32 ? 4 : 2, N = 16 / EL;
+    constexpr int EL = F32 ? 4 : 2, N = 16 / EL, P = EACH / N;      // P pieces of 16 bytes
     __shared__ Part of_wave[kWaves];
     const int part = blockIdx.x % A.parts, row = blockIdx.x / A.parts, seq = row / A.rows, r = row - seq * A.rows;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -175,40 +202,43 @@ __global__ __launch_bounds__(kThreads) void sk_verify_rows(const Args A)
     if (r <= A.n_draft ? r > n : greedy || r - A.n_draft - 1 >= n) return;
     const unsigned char* x = row_of(A, seq, r);
     const float none = -__builtin_inff();
-    const int at0 = (part * kPieces * kThreads + (int)threadIdx.x) * N;      // piece i: N logits from at0 + i * kThreads * N on
-    float v[kPieces * N];
+    const int at0 = (part * P * kThreads + (int)threadIdx.x) * N;   // piece i: N logits from at0 + i * kThreads * N on
+    float v[EACH];
     if (A.vocab >= N) {
         // A piece that reaches behind the row is read N logits in front of its end, of which those count that are its own.
-        u32x4 w[kPieces];
+        u32x4 w[P];
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) w[i] = *(const u32x4_anywhere*)(x + (int64_t)min(at0 + i * kThreads * N, A.vocab - N) * EL);
+        for (int i = 0; i < P; ++i) w[i] = *(const u32x4_anywhere*)(x + (int64_t)min(at0 + i * kThreads * N, A.vocab - N) * EL);
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-            const int behind = at0 + i * kThreads * N - (A.vocab - N);
+        for (int i = 0; i < EACH; ++i) v[i] = F32 ? __uint_as_float(w[i / N][i % 4]) : __uint_as_float(i & 1 ? w[i / N][i / 2 % 4] & 0xffff0000u : w[i / N][i / 2 % 4] << 16);
+        if ((part + 1) * P * kThreads * N > A.vocab) {
 #pragma unroll
-            for (int e = 0; e < N; ++e) {
-                const float y = F32 ? __uint_as_float(w[i][e % 4]) : __uint_as_float(e & 1 ? w[i][e / 2 % 4] & 0xffff0000u : w[i][e / 2 % 4] << 16);
-                v[i * N + e] = e >= behind ? y : none;
-            }
+            for (int i = 0; i < EACH; ++i) v[i] = i % N >= at0 + i / N * kThreads * N - (A.vocab - N) ? v[i] : none;
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < kPieces * N; ++i) v[i] = i < N && at0 + i < A.vocab ? logit<F32>(x, at0 + i) : none;
+        for (int i = 0; i < EACH; ++i) v[i] = i < N && at0 + i < A.vocab ? logit<F32>(x, at0 + i) : none;
     }
     float m = none;
     bool bad = false;
 #pragma unroll
-    for (int i = 0; i < kPieces * N; ++i) { m = fmaxf(m, v[i]); bad |= !(v[i] < __builtin_inff()); }
+    for (int i = 0; i < EACH; i += 2) { m = fmaxf(m, fmaxf(v[i], v[i + 1])); bad |= __builtin_isunordered(v[i], v[i + 1]); }
     m = wave_max(m);
-    const double m0 = m == none ? 0.0 : (double)m;
+    bad |= m == __builtin_inff();
+    const double e = exponent_of(m, scale);
     double sum[2] = {0.0, 0.0};
+    if (__builtin_fabs(e) < kFar) {
 #pragma unroll
-    for (int i = 0; i < kPieces * N; ++i) sum[i & 1] += power_of_two_in_sum(((double)v[i] - m0) * scale);
+        for (int i = 0; i < EACH; ++i) sum[i & 1] += weight_in_sum(v[i], scale, e);
+    } else if (m != none) {
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) sum[0] += v[i] == m ? 1.0 : 0.0;
+    }
     double total = wave_sum(sum[0] + sum[1]);
     int at = INT32_MAX;
     if (greedy) {
 #pragma unroll
-        for (int i = kPieces * N - 1; i >= 0; --i)
+        for (int i = EACH - 1; i >= 0; --i)
             if (v[i] == m) {
                 const int first = at0 + i / N * kThreads * N;
                 at = (A.vocab >= N ? min(first, A.vocab - N) : first) + i % N;
@@ -216,23 +246,19 @@ __global__ __launch_bounds__(kThreads) void sk_verify_rows(const Args A)
 #pragma unroll
         for (int s = 1; s < 64; s *= 2) at = min(at, __shfl_xor(at, s, 64));
     }
-    if (m == none) total = 0.0;
     if (__ballot(bad)) total = __builtin_nan("");
-    if (lane == 0) of_wave[wave] = Part{total, m, at};
+    if (lane == 0) of_wave[wave] = Part{total, e, m, at};
     __syncthreads();
     if (threadIdx.x < 64) {                        // lanes 0 to 3 have the waves'
-        const Part p = lane < kWaves ? of_wave[lane] : Part{0.0, none, INT32_MAX};
+        const Part p = lane < kWaves ? of_wave[lane] : Part{0.0, kNoExponent, none, INT32_MAX};
         const float top = row_max(p.max);
-        const double t0 = top == none ? 0.0 : (double)top;
-        const double all = row_sum(p.sum * power_of_two(((double)p.max - t0) * scale));
+        const double to = exponent_of(top, scale), all = row_sum(at_exponent(p.sum, p.e, to));
         const int first = row_min(p.max == top ? p.at : INT32_MAX);
-        if (lane == 0) A.part[((int64_t)seq * A.rows + r) * A.parts + part] = Part{all, top, first};
+        if (lane == 0) A.part[((int64_t)seq * A.rows + r) * A.parts + part] = Part{all, to, top, first};
     }
 }
 
 // ---- second launch: which tokens stay, and the sums of the stretches of the row that is drawn from ----
-
-struct Row { double total; float max; int32_t at; };      // of a whole row: sum of 2^((x - max) scale); 0: no probabilities
 
 // What a logit of the row that is drawn from counts for.
 template <bool F32> struct Weights {
@@ -248,8 +274,8 @@ template <bool F32> struct Weights {
     // of logits x and y of the two rows, at index i
     __device__ __forceinline__ double operator()(const float x, const float y, const int i) const
     {
-        double w = power_of_two(((double)x - c.p_max) * c.scale) * c.p_inv;
-        if (c.less == 1) w = __builtin_fmax(w - power_of_two(((double)y - c.q_max) * c.scale) * c.q_inv, 0.0);
+        double w = weight_of(x, c.scale, c.p_e, c.p_max) * c.p_inv;
+        if (c.less == 1) w = __builtin_fmax(w - weight_of(y, c.scale, c.q_e, c.q_max) * c.q_inv, 0.0);
         return i == without ? 0.0 : w;
     }
 };
@@ -258,7 +284,7 @@ template <bool F32>
 __global__ __launch_bounds__(kThreads) void sk_verify_stretches(const Args A)
 {
     constexpr int EACH = kStretch / kThreads;
-    __shared__ Row row[kMaxRows];
+    __shared__ Part row[kMaxRows];                 // of whole rows; sum 0: no probabilities
     __shared__ Chosen chosen;
     __shared__ double of_wave[kWaves];
     const int stretch = blockIdx.x % A.stretches, seq = blockIdx.x / A.stretches, tid = threadIdx.x, lane = tid & 63;
@@ -277,51 +303,45 @@ __global__ __launch_bounds__(kThreads) void sk_verify_stretches(const Args A)
     // the parts of a row meet in sixteen lanes (rows that were not computed hold anything, and are not looked at)
     for (int r = tid >> 4; r < A.rows; r += kThreads / 16) {
         const Part* p = A.part + ((int64_t)seq * A.rows + r) * A.parts;
-        float m = none;
-        double sum = 0.0;
-        int at = INT32_MAX;
+        Part o = {0.0, kNoExponent, none, INT32_MAX};
         for (int c = tid & 15; c < A.parts; c += 16) {
-            const Part o = p[c];
-            const float top = fmaxf(m, o.max);
-            const double t0 = top == none ? 0.0 : (double)top;
-            sum = sum * power_of_two(((double)m - t0) * scale) + o.sum * power_of_two(((double)o.max - t0) * scale);
-            at = o.max > m ? o.at : o.max == m ? min(at, o.at) : at;
-            m = top;
+            const Part y = p[c];
+            const double to = __builtin_fmax(o.e, y.e);
+            o = Part{at_exponent(o.sum, o.e, to) + at_exponent(y.sum, y.e, to), to, fmaxf(o.max, y.max), y.max > o.max ? y.at : y.max == o.max ? min(o.at, y.at) : o.at};
         }
-        const float top = row_max(m);
-        const double t0 = top == none ? 0.0 : (double)top;
-        sum = row_sum(sum * power_of_two(((double)m - t0) * scale));
-        at = row_min(m == top ? at : INT32_MAX);
-        if ((tid & 15) == 0) row[r] = Row{sum > 0.0 ? sum : 0.0, top, at};      // (NaN: none)
+        const float top = row_max(o.max);
+        const double to = exponent_of(top, scale), sum = row_sum(at_exponent(o.sum, o.e, to));
+        const int at = row_min(o.max == top ? o.at : INT32_MAX);
+        if ((tid & 15) == 0) row[r] = Part{sum > 0.0 ? sum : 0.0, to, top, at};      // (NaN: none)
     }
     __syncthreads();
     if (tid < 64) {
         bool stays = false;
-        if (lane < n && row[lane].total > 0.0) {
-            const Row p = row[lane];
+        if (lane < n && row[lane].sum > 0.0) {
+            const Part p = row[lane];
             if (greedy) stays = token == p.at;
             else {
-                const double px = power_of_two(((double)xp - (double)p.max) * scale) / p.total;
+                const double px = weight_of(xp, scale, p.e, p.max) / p.sum;
                 double qx = 1.0;
                 bool known = true;
                 if (A.draft) {
-                    const Row q = row[A.n_draft + 1 + lane];
-                    known = q.total > 0.0;
-                    if (known) qx = power_of_two(((double)xq - (double)q.max) * scale) / q.total;
+                    const Part q = row[A.n_draft + 1 + lane];
+                    known = q.sum > 0.0;
+                    if (known) qx = weight_of(xq, scale, q.e, q.max) / q.sum;
                 }
                 stays = known && (double)u * qx < px;
             }
         }
         const uint64_t out = ~__ballot(stays);
         const int a = min(n, (int)__builtin_ctzll(out));            // (lanes from n on are out)
-        const Row p = row[a];
-        const bool valid = p.total > 0.0;
+        const Part p = row[a];
+        const bool valid = p.sum > 0.0;
         if (lane == 0) {
-            Chosen c = {scale, (double)p.max, 1.0 / p.total, 0.0, 0.0, valid && !greedy ? a : -1, 0};
+            Chosen c = {scale, p.e, 1.0 / p.sum, 0.0, 0.0, p.max, 0.f, valid && !greedy ? a : -1, 0};
             if (a < n && !A.draft) c.less = 2;
-            else if (a < n && !greedy && row[A.n_draft + 1 + a].total > 0.0) {
-                const Row q = row[A.n_draft + 1 + a];
-                c.less = 1; c.q_max = q.max; c.q_inv = 1.0 / q.total;
+            else if (a < n && !greedy && row[A.n_draft + 1 + a].sum > 0.0) {
+                const Part q = row[A.n_draft + 1 + a];
+                c.less = 1; c.q_e = q.e; c.q_inv = 1.0 / q.sum; c.q_max = q.max;
             }
             chosen = c;
             if (stretch == 0) { A.chosen[seq] = c; A.n_accepted[seq] = a; }
@@ -333,8 +353,8 @@ __global__ __launch_bounds__(kThreads) void sk_verify_stretches(const Args A)
             if (A.logprob) {
                 float l = 0.f;
                 if (lane < a || (lane == a && valid && greedy)) {
-                    const Row r = row[lane];
-                    l = (float)(((double)logit<F32>(row_of(A, seq, lane), t) - (double)r.max) * (scale * 0.6931471805599453) - log(r.total));
+                    const Part r = row[lane];
+                    l = log_probability(logit<F32>(row_of(A, seq, lane), t), scale, r.e, r.max, 1.0 / r.sum);
                 } else if (lane == a && !valid) l = __builtin_nanf("");
                 A.logprob[at] = l;
             }
@@ -441,15 +461,13 @@ __global__ __launch_bounds__(kThreads) void sk_verify_draw(const Args A)
     if (tid == 0) {
         const int64_t at = (int64_t)seq * (A.n_draft + 1) + c.place;
         A.out_tokens[at] = token;
-        if (A.logprob) A.logprob[at] = (float)(((double)logit<F32>(row_of(A, seq, c.place), token) - c.p_max) * (c.scale * 0.6931471805599453) + log(c.p_inv));
+        if (A.logprob) A.logprob[at] = log_probability(logit<F32>(row_of(A, seq, c.place), token), c.scale, c.p_e, c.p_max, c.p_inv);
     }
 }
 
-int64_t parts_of(const int dtype_bytes, const int32_t vocab)
-{
-    const int n = 16 / dtype_bytes;
-    return ((int64_t)vocab + kPieces * kThreads * n - 1) / (kPieces * kThreads * n);
-}
+int64_t parts_of(const int64_t each, const int32_t vocab) { return (vocab + each * kThreads - 1) / (each * kThreads); }
+// Logits of a thread
+int each_of(const int64_t rows, const int32_t vocab) { return rows * parts_of(kEach, vocab) < 1024 ? kEachFew : kEach; }
 bool sizes_ok(const int32_t n_seq, const int32_t n_draft, const int32_t vocab)
 {
     return n_seq > 0 && n_draft >= 0 && n_draft <= SK_VERIFY_MAX_DRAFT && vocab >= 1 && vocab <= SK_VERIFY_MAX_VOCAB &&
@@ -463,9 +481,11 @@ extern "C" {
 size_t sk_verify_workspace_bytes(int32_t n_seq, int32_t n_draft, int32_t vocab)
 {
     if (!sizes_ok(n_seq, n_draft, vocab)) return 0;
-    // (for either type of the logits: fp32 ones have more parts)
+    // (with a draft's rows or without them)
     const int64_t stretches = ((int64_t)vocab + kStretch - 1) / kStretch;
-    return size_t(n_seq) * (size_t(2 * n_draft + 1) * size_t(parts_of(4, vocab)) * sizeof(Part) + sizeof(Chosen) + size_t(stretches) * 8);
+    auto parts = [&](const int64_t rows) { return rows * n_seq * parts_of(each_of(rows * n_seq, vocab), vocab); };
+    const int64_t with = parts(2 * n_draft + 1), without = parts(n_draft + 1);
+    return size_t(with > without ? with : without) * sizeof(Part) + size_t(n_seq) * (sizeof(Chosen) + size_t(stretches) * 8);
 }
 
 int sk_verify(const void* target, int64_t target_stride, const void* draft, int64_t draft_stride, int dtype, int32_t n_seq, int32_t n_draft, int32_t vocab,
@@ -487,9 +507,11 @@ int sk_verify(const void* target, int64_t target_stride, const void* draft, int6
     A.target = (const unsigned char*)target; A.draft = n_draft > 0 ? (const unsigned char*)draft : nullptr;
     A.target_stride = target_stride * el; A.draft_stride = draft_stride * el;
     A.n_draft = n_draft; A.vocab = vocab;
-    A.parts = (int32_t)parts_of(el, vocab); A.stretches = (vocab + kStretch - 1) / kStretch;
+    A.stretches = (vocab + kStretch - 1) / kStretch;
     A.tokens = tokens; A.uniform = uniform; A.temperature = temperature;
     const int rows = A.rows = n_draft + 1 + (A.draft ? n_draft : 0);
+    const int each = each_of((int64_t)n_seq * rows, vocab);
+    A.parts = (int32_t)parts_of(each, vocab);
     A.part = (Part*)workspace;
     A.chosen = (Chosen*)(A.part + (int64_t)n_seq * rows * A.parts);
     A.sums = (double*)(A.chosen + n_seq);
@@ -498,11 +520,13 @@ int sk_verify(const void* target, int64_t target_stride, const void* draft, int6
     hipStream_t st = (hipStream_t)hip_stream;
     const dim3 block(kThreads), first((unsigned)(n_seq * rows) * (unsigned)A.parts), second((unsigned)n_seq * (unsigned)A.stretches);
     if (dtype == SK_F32) {
-        hipLaunchKernelGGL(sk_verify_rows<true>, first, block, 0, st, A);
+        if (each == kEach) hipLaunchKernelGGL((sk_verify_rows<true, kEach>), first, block, 0, st, A);
+        else hipLaunchKernelGGL((sk_verify_rows<true, kEachFew>), first, block, 0, st, A);
         hipLaunchKernelGGL(sk_verify_stretches<true>, second, block, 0, st, A);
         hipLaunchKernelGGL(sk_verify_draw<true>, dim3(n_seq), block, 0, st, A);
     } else {
-        hipLaunchKernelGGL(sk_verify_rows<false>, first, block, 0, st, A);
+        if (each == kEach) hipLaunchKernelGGL((sk_verify_rows<false, kEach>), first, block, 0, st, A);
+        else hipLaunchKernelGGL((sk_verify_rows<false, kEachFew>), first, block, 0, st, A);
         hipLaunchKernelGGL(sk_verify_stretches<false>, second, block, 0, st, A);
         hipLaunchKernelGGL(sk_verify_draw<false>, dim3(n_seq), block, 0, st, A);
     }
