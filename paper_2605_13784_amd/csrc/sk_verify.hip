@@ -22,8 +22,7 @@
 namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
-constexpr int kEach = 32, kEachFew = 8;            // logits of a thread in the first launch; where there are few rows
-constexpr int kStretch = 4096;                     // logits of a workgroup in the second
+constexpr int kEach = 32, kEachFew = 8;            // logits of a lane; where there are few rows.  A stretch is a wave's, a part a workgroup's
 constexpr int kMaxRows = 2 * SK_VERIFY_MAX_DRAFT + 1;
 
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
@@ -32,6 +31,7 @@ typedef u32x4 __attribute__((aligned(2))) u32x4_anywhere;      // (the hardware 
 // Of a part of a row, or of all of it: sum of 2^(x scale - e) with a whole number e next to the maximum's, so that parts meet without a rounding;
 // the lowest index of the maximum (greedy sequences).
 struct Part { double sum, e; float max; int32_t at; };
+struct Sum { double sum, e; };                     // of a stretch
 
 // What the second launch leaves for the third, a sequence.
 struct Chosen {
@@ -49,8 +49,9 @@ struct Args {
     const float* uniform;
     const float* temperature;
     Part* part;                                    // [sequence][target rows, then draft rows][part]
+    Sum* of_stretch;                               // [sequence][target rows][stretch]
     Chosen* chosen;                                // [sequence]
-    double* sums;                                  // [sequence][stretch]
+    double* sums;                                  // [sequence][stretch]: of the weights of the drawn row
     int32_t *n_accepted, *out_tokens;
     float* logprob;
 };
@@ -149,17 +150,18 @@ __device__ __forceinline__ double of_lane(const double x, const int lane)
     const uint64_t b = __builtin_bit_cast(uint64_t, x);
     return __builtin_bit_cast(double, (uint64_t)(uint32_t)__shfl((int)(b >> 32), lane, 64) << 32 | (uint32_t)__shfl((int)(uint32_t)b, lane, 64));
 }
-// Sum over the lanes in front of this one.
-__device__ __forceinline__ double wave_sum_before(double x, const int lane)
+// Sum over the lanes up to and with this one: within a row of 16 lanes by shifts of it, then the last lane of a row added to the rows behind it.
+template <int CTRL, int ROWS, bool BOUND> __device__ __forceinline__ double shifted(const double x)
 {
-    double sum = x;
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2) {
-        const double y = of_lane(sum, lane - m);
-        if (lane >= m) sum += y;
-    }
-    const double y = of_lane(sum, lane - 1);
-    return lane ? y : 0.0;
+    u32x2 b = __builtin_bit_cast(u32x2, x);
+    b.x = __builtin_amdgcn_update_dpp(0u, b.x, CTRL, ROWS, 0xf, BOUND);
+    b.y = __builtin_amdgcn_update_dpp(0u, b.y, CTRL, ROWS, 0xf, BOUND);
+    return __builtin_bit_cast(double, b);
+}
+__device__ __forceinline__ double wave_running_sum(double x)
+{
+    x += shifted<0x111, 0xf, true>(x); x += shifted<0x112, 0xf, true>(x); x += shifted<0x114, 0xf, true>(x); x += shifted<0x118, 0xf, true>(x);
+    x += shifted<0x142, 0xa, false>(x); return x + shifted<0x143, 0xc, false>(x);
 }
 
 // The exponent's factor of a sequence: log2(e) / T; greedy sequences, whose log probabilities are those of the logits as they are, have T = 1.
@@ -202,18 +204,18 @@ __global__ __launch_bounds__(kThreads) void sk_verify_rows(const Args A)
     if (r <= A.n_draft ? r > n : greedy || r - A.n_draft - 1 >= n) return;
     const unsigned char* x = row_of(A, seq, r);
     const float none = -__builtin_inff();
-    const int at0 = (part * P * kThreads + (int)threadIdx.x) * N;   // piece i: N logits from at0 + i * kThreads * N on
+    const int stretch = part * kWaves + wave, at0 = stretch * 64 * EACH + lane * N;      // piece i: N logits from at0 + i * 64 * N on
     float v[EACH];
     if (A.vocab >= N) {
         // A piece that reaches behind the row is read N logits in front of its end, of which those count that are its own.
         u32x4 w[P];
 #pragma unroll
-        for (int i = 0; i < P; ++i) w[i] = *(const u32x4_anywhere*)(x + (int64_t)min(at0 + i * kThreads * N, A.vocab - N) * EL);
+        for (int i = 0; i < P; ++i) w[i] = *(const u32x4_anywhere*)(x + (int64_t)min(at0 + i * 64 * N, A.vocab - N) * EL);
 #pragma unroll
         for (int i = 0; i < EACH; ++i) v[i] = F32 ? __uint_as_float(w[i / N][i % 4]) : __uint_as_float(i & 1 ? w[i / N][i / 2 % 4] & 0xffff0000u : w[i / N][i / 2 % 4] << 16);
-        if ((part + 1) * P * kThreads * N > A.vocab) {
+        if ((stretch + 1) * 64 * EACH > A.vocab) {
 #pragma unroll
-            for (int i = 0; i < EACH; ++i) v[i] = i % N >= at0 + i / N * kThreads * N - (A.vocab - N) ? v[i] : none;
+            for (int i = 0; i < EACH; ++i) v[i] = i % N >= at0 + i / N * 64 * N - (A.vocab - N) ? v[i] : none;
         }
     } else {
 #pragma unroll
@@ -240,14 +242,17 @@ __global__ __launch_bounds__(kThreads) void sk_verify_rows(const Args A)
 #pragma unroll
         for (int i = EACH - 1; i >= 0; --i)
             if (v[i] == m) {
-                const int first = at0 + i / N * kThreads * N;
+                const int first = at0 + i / N * 64 * N;
                 at = (A.vocab >= N ? min(first, A.vocab - N) : first) + i % N;
             }
 #pragma unroll
         for (int s = 1; s < 64; s *= 2) at = min(at, __shfl_xor(at, s, 64));
     }
     if (__ballot(bad)) total = __builtin_nan("");
-    if (lane == 0) of_wave[wave] = Part{total, e, m, at};
+    if (lane == 0) {
+        of_wave[wave] = Part{total, e, m, at};
+        if (r <= A.n_draft) A.of_stretch[((int64_t)seq * (A.n_draft + 1) + r) * A.stretches + stretch] = Sum{total, e};
+    }
     __syncthreads();
     if (threadIdx.x < 64) {                        // lanes 0 to 3 have the waves'
         const Part p = lane < kWaves ? of_wave[lane] : Part{0.0, kNoExponent, none, INT32_MAX};
@@ -280,14 +285,13 @@ template <bool F32> struct Weights {
     }
 };
 
-template <bool F32>
+template <bool F32, int EACH>
 __global__ __launch_bounds__(kThreads) void sk_verify_stretches(const Args A)
 {
-    constexpr int EACH = kStretch / kThreads;
+    constexpr int kParts = 4;
     __shared__ Part row[kMaxRows];                 // of whole rows; sum 0: no probabilities
     __shared__ Chosen chosen;
-    __shared__ double of_wave[kWaves];
-    const int stretch = blockIdx.x % A.stretches, seq = blockIdx.x / A.stretches, tid = threadIdx.x, lane = tid & 63;
+    const int wg = blockIdx.x % A.parts, seq = blockIdx.x / A.parts, tid = threadIdx.x, lane = tid & 63;
     const float none = -__builtin_inff();
     bool greedy;
     const double scale = scale_of(A, seq, greedy);
@@ -304,10 +308,17 @@ __global__ __launch_bounds__(kThreads) void sk_verify_stretches(const Args A)
     for (int r = tid >> 4; r < A.rows; r += kThreads / 16) {
         const Part* p = A.part + ((int64_t)seq * A.rows + r) * A.parts;
         Part o = {0.0, kNoExponent, none, INT32_MAX};
-        for (int c = tid & 15; c < A.parts; c += 16) {
-            const Part y = p[c];
-            const double to = __builtin_fmax(o.e, y.e);
-            o = Part{at_exponent(o.sum, o.e, to) + at_exponent(y.sum, y.e, to), to, fmaxf(o.max, y.max), y.max > o.max ? y.at : y.max == o.max ? min(o.at, y.at) : o.at};
+        for (int c0 = tid & 15; c0 < A.parts; c0 += 16 * kParts) {
+            Part y[kParts];
+#pragma unroll
+            for (int j = 0; j < kParts; ++j) y[j] = p[min(c0 + 16 * j, A.parts - 1)];
+#pragma unroll
+            for (int j = 0; j < kParts; ++j) {
+                if (c0 + 16 * j >= A.parts) continue;
+                const double to = __builtin_fmax(o.e, y[j].e);
+                o = Part{at_exponent(o.sum, o.e, to) + at_exponent(y[j].sum, y[j].e, to), to, fmaxf(o.max, y[j].max),
+                         y[j].max > o.max ? y[j].at : y[j].max == o.max ? min(o.at, y[j].at) : o.at};
+            }
         }
         const float top = row_max(o.max);
         const double to = exponent_of(top, scale), sum = row_sum(at_exponent(o.sum, o.e, to));
@@ -344,9 +355,9 @@ __global__ __launch_bounds__(kThreads) void sk_verify_stretches(const Args A)
                 c.less = 1; c.q_e = q.e; c.q_inv = 1.0 / q.sum; c.q_max = q.max;
             }
             chosen = c;
-            if (stretch == 0) { A.chosen[seq] = c; A.n_accepted[seq] = a; }
+            if (wg == 0) { A.chosen[seq] = c; A.n_accepted[seq] = a; }
         }
-        if (stretch == 0 && lane <= A.n_draft) {   // everything but a token that is still to be drawn
+        if (wg == 0 && lane <= A.n_draft) {   // everything but a token that is still to be drawn
             const int32_t t = lane < a ? token : lane == a && valid && greedy ? p.at : -1;
             const int64_t at = (int64_t)seq * (A.n_draft + 1) + lane;
             A.out_tokens[at] = t;
@@ -361,117 +372,152 @@ __global__ __launch_bounds__(kThreads) void sk_verify_stretches(const Args A)
         }
     }
     __syncthreads();
-    if (chosen.place < 0) return;
+    const int stretch = wg * kWaves + (tid >> 6);
+    // the target's own weights are known; without the drafted token, all but those of its stretch
+    if (chosen.place < 0 || chosen.less == 0) return;
     const Weights<F32> w(A, chosen, seq);
+    if (chosen.less == 2 && w.without / (64 * EACH) != stretch) return;
     float x[EACH], y[EACH];
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
-        const int t = min(stretch * kStretch + i * kThreads + tid, A.vocab - 1);
+        const int t = min(stretch * 64 * EACH + i * 64 + lane, A.vocab - 1);
         x[i] = logit<F32>(w.p, t);
         y[i] = logit<F32>(w.q, t);
     }
     double sum = 0.0;
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
-        const int t = stretch * kStretch + i * kThreads + tid;
+        const int t = stretch * 64 * EACH + i * 64 + lane;
         if (t < A.vocab) sum += w(x[i], y[i], t);
     }
     sum = wave_sum(sum);
-    if (lane == 0) of_wave[tid >> 6] = sum;
-    __syncthreads();
-    if (tid == 0) A.sums[(int64_t)seq * A.stretches + stretch] = of_wave[0] + of_wave[1] + of_wave[2] + of_wave[3];
+    if (lane == 0) A.sums[(int64_t)seq * A.stretches + stretch] = sum;
 }
 
 // ---- third launch: the draw ----
 
-// The token that the sequence's last number finds in the running sum of the row's weights: the stretch, by the first wave, then the thread, then its logit.
-template <bool F32>
+// The token that the sequence's last number finds in the running sum of the row's weights: the stretch, by every wave for itself, then the thread, then
+// its logit.  Where roundings leave the sum below the limit, or the number is 1 or more, the last that counts is taken at each step.
+template <bool F32, int STRETCH>
 __global__ __launch_bounds__(kThreads) void sk_verify_draw(const Args A)
 {
-    constexpr int EACH = kStretch / kThreads;      // logits of a thread, one behind the other
-    __shared__ double of_wave[kWaves], left_of;
-    __shared__ int chosen_stretch, token_of;
+    constexpr int EACH = STRETCH / kThreads, kSums = 4;       // logits of a thread, one behind the other; stretches of a lane that are asked for at once
+    __shared__ double of_wave[kWaves];
+    __shared__ uint64_t over_of[kWaves], some_of[kWaves];
     const int seq = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const double* sums = A.sums + (int64_t)seq * A.stretches;
+    const double u = __builtin_fmax((double)A.uniform[(int64_t)seq * (A.n_draft + 1) + A.n_draft], 0.0);
+    double first[kSums];
+#pragma unroll
+    for (int j = 0; j < kSums; ++j) first[j] = sums[min(64 * j + lane, A.stretches - 1)];
     const Chosen c = A.chosen[seq];
     if (c.place < 0) return;
-    if (wave == 0) {
-        const double* sums = A.sums + (int64_t)seq * A.stretches;
-        double total = 0.0;
-        for (int i = lane; i < A.stretches; i += 64) total += sums[i];
-        total = wave_sum(total);
-        const double limit = __builtin_fmax((double)A.uniform[(int64_t)seq * (A.n_draft + 1) + A.n_draft], 0.0) * total;
-        double before = 0.0, left = 0.0;
-        int found = -1;
-        for (int base = 0; base < A.stretches; base += 64) {
-            const double mine = base + lane < A.stretches ? sums[base + lane] : 0.0, mine_before = before + wave_sum_before(mine, lane);
-            // the first whose running sum exceeds the limit; until there is one, the last that counts (roundings, or a number from 1 on)
-            const uint64_t over = __ballot(mine > 0.0 && mine_before + mine > limit), some = __ballot(mine > 0.0);
-            if (some) {
-                const int l = over ? __builtin_ctzll(over) : 63 - __builtin_clzll(some);
-                found = base + l;
-                left = limit - of_lane(mine_before, l);
-            }
-            if (over) break;
-            before = of_lane(mine_before, 63) + of_lane(mine, 63);
-        }
-        if (lane == 0) { chosen_stretch = found; left_of = left; token_of = 0; }
+    const Weights<F32> w(A, c, seq);
+    const Sum* known = A.of_stretch + ((int64_t)seq * (A.n_draft + 1) + c.place) * A.stretches;
+    auto known_sum = [&](const int i, const double again) {
+        const Sum k = known[min(i, A.stretches - 1)];
+        return c.less == 2 && i == w.without / STRETCH ? again : at_exponent(k.sum, k.e, c.p_e) * c.p_inv;
+    };
+    if (c.less != 1) {
+#pragma unroll
+        for (int j = 0; j < kSums; ++j) first[j] = known_sum(64 * j + lane, first[j]);
     }
+    auto stretch_sum = [&](const int base) {
+        if (base + lane >= A.stretches) return 0.0;
+        if (base < 64 * kSums) return base < 128 ? (base ? first[1] : first[0]) : base == 128 ? first[2] : first[3];
+        return c.less == 1 ? sums[base + lane] : known_sum(base + lane, sums[base + lane]);
+    };
+    double total = 0.0;
+    for (int base = 0; base < A.stretches; base += 64) total += stretch_sum(base);
+    total = wave_sum(total);
+    const double limit = u * total;
+    double before = 0.0, left = 0.0;
+    int stretch = -1;
+    for (int base = 0; base < A.stretches; base += 64) {
+        const double mine = stretch_sum(base), running = before + wave_running_sum(mine);
+        const uint64_t over = __ballot(mine > 0.0 && running > limit), some = __ballot(mine > 0.0);
+        if (some) {
+            const int l = over ? __builtin_ctzll(over) : 63 - __builtin_clzll(some);
+            stretch = base + l;
+            left = limit - (l ? of_lane(running, l - 1) : before);
+        }
+        if (over) break;
+        before = of_lane(running, 63);
+    }
+    const int64_t to = (int64_t)seq * (A.n_draft + 1) + c.place;
+    if (stretch < 0) {                             // nothing is left of the target: p and q are one, and the drafted token is as good
+        if (tid == 0) {
+            const int token = c.less ? A.tokens[(int64_t)seq * A.n_draft + c.place] : 0;
+            A.out_tokens[to] = token;
+            if (A.logprob) A.logprob[to] = log_probability(logit<F32>(row_of(A, seq, c.place), token), c.scale, c.p_e, c.p_max, c.p_inv);
+        }
+        return;
+    }
+    const int begin = stretch * STRETCH + tid * EACH;
+    float x[EACH], y[EACH];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int t = min(begin + i, A.vocab - 1);
+        x[i] = logit<F32>(w.p, t);
+        y[i] = logit<F32>(w.q, t);
+    }
+    double weight[EACH], mine = 0.0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) { weight[i] = begin + i < A.vocab ? w(x[i], y[i], begin + i) : 0.0; mine += weight[i]; }
+    double running = wave_running_sum(mine);
+    if (lane == 63) of_wave[wave] = running;
     __syncthreads();
-    int token;
-    // nothing is left of the target: p and q are one, and the drafted token is as good
-    if (chosen_stretch < 0) token = c.less ? A.tokens[(int64_t)seq * A.n_draft + c.place] : 0;
-    else {
-        const Weights<F32> w(A, c, seq);
-        const int begin = chosen_stretch * kStretch + tid * EACH;
-        float x[EACH], y[EACH];
-#pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            const int t = min(begin + i, A.vocab - 1);
-            x[i] = logit<F32>(w.p, t);
-            y[i] = logit<F32>(w.q, t);
-        }
-        double weight[EACH], mine = 0.0;
-#pragma unroll
-        for (int i = 0; i < EACH; ++i) { weight[i] = begin + i < A.vocab ? w(x[i], y[i], begin + i) : 0.0; mine += weight[i]; }
-        double before = wave_sum_before(mine, lane);
-        if (lane == 63) of_wave[wave] = before + mine;
-        __syncthreads();
-        for (int i = 0; i < wave; ++i) before += of_wave[i];
-        // the thread in which the running sum passes what is left; if none, the last that counts: the highest of those that say so
-        const double left = left_of;
-        const uint64_t over = __ballot(mine > 0.0 && before + mine > left), some = __ballot(mine > 0.0);
-        const bool last = !over && some && lane == 63 - __builtin_clzll(some), first = over && lane == __builtin_ctzll(over);
-        if (first || last) {
-            int t = begin;
-            double sum = before;
-            bool passed = false;
-#pragma unroll
-            for (int i = 0; i < EACH; ++i) {
-                if (!passed && weight[i] > 0.0) t = begin + i;
-                sum += weight[i];
-                passed |= weight[i] > 0.0 && sum > left;
-            }
-            // of several waves' answers the lowest that passes, or else the highest
-            if (first) atomicMax(&token_of, (1 << 30) | ((1 << 29) - t));
-            else atomicMax(&token_of, t);
-        }
-        __syncthreads();
-        token = token_of & (1 << 30) ? (1 << 29) - (token_of & ~(1 << 30)) : token_of;
+    double in_front = 0.0;
+    for (int i = 0; i < wave; ++i) in_front += of_wave[i];
+    const uint64_t over = __ballot(mine > 0.0 && in_front + running > left), some = __ballot(mine > 0.0);
+    if (lane == 0) { over_of[wave] = over; some_of[wave] = some; }
+    __syncthreads();
+    int chosen_wave = -1, chosen_lane = 0;
+    for (int i = kWaves - 1; i >= 0; --i) {
+        if (over_of[i]) { chosen_wave = i; chosen_lane = __builtin_ctzll(over_of[i]); }
+        else if (some_of[i] && chosen_wave < 0) { chosen_wave = i; chosen_lane = 63 - __builtin_clzll(some_of[i]); }
     }
-    if (tid == 0) {
-        const int64_t at = (int64_t)seq * (A.n_draft + 1) + c.place;
-        A.out_tokens[at] = token;
-        if (A.logprob) A.logprob[at] = log_probability(logit<F32>(row_of(A, seq, c.place), token), c.scale, c.p_e, c.p_max, c.p_inv);
+    if (wave != chosen_wave || lane != chosen_lane) return;
+    double sum = in_front + running - mine;
+    int token = begin;
+    float its = x[0];
+    bool passed = false;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        if (!passed && weight[i] > 0.0) { token = begin + i; its = x[i]; }
+        sum += weight[i];
+        passed |= weight[i] > 0.0 && sum > left;
     }
+    A.out_tokens[to] = token;
+    if (A.logprob) A.logprob[to] = log_probability(its, c.scale, c.p_e, c.p_max, c.p_inv);
 }
 
 int64_t parts_of(const int64_t each, const int32_t vocab) { return (vocab + each * kThreads - 1) / (each * kThreads); }
-// Logits of a thread
+// Logits of a lane
 int each_of(const int64_t rows, const int32_t vocab) { return rows * parts_of(kEach, vocab) < 1024 ? kEachFew : kEach; }
 bool sizes_ok(const int32_t n_seq, const int32_t n_draft, const int32_t vocab)
 {
     return n_seq > 0 && n_draft >= 0 && n_draft <= SK_VERIFY_MAX_DRAFT && vocab >= 1 && vocab <= SK_VERIFY_MAX_VOCAB &&
            (int64_t)n_seq * (n_draft + 1) <= SK_VERIFY_MAX_ROWS;
+}
+// What a call keeps, in the order in which it lies in the workspace
+size_t lay_out(Args& A, unsigned char* at, const int32_t n_seq)
+{
+    const unsigned char* from = at;
+    const int64_t parts = (int64_t)n_seq * A.rows * A.parts, stretches = (int64_t)n_seq * A.stretches;
+    A.part = (Part*)at; at += parts * sizeof(Part);
+    A.of_stretch = (Sum*)at; at += stretches * (A.n_draft + 1) * sizeof(Sum);
+    A.chosen = (Chosen*)at; at += n_seq * sizeof(Chosen);
+    A.sums = (double*)at; at += stretches * sizeof(double);
+    return size_t(at - from);
+}
+int cut(Args& A, const int32_t n_seq, const int32_t n_draft, const int32_t vocab, const bool draft)
+{
+    A.n_draft = n_draft; A.vocab = vocab;
+    A.rows = n_draft + 1 + (draft ? n_draft : 0);
+    const int each = each_of((int64_t)n_seq * A.rows, vocab);
+    A.parts = (int32_t)parts_of(each, vocab); A.stretches = A.parts * kWaves;
+    return each;
 }
 
 }  // namespace
@@ -481,11 +527,14 @@ extern "C" {
 size_t sk_verify_workspace_bytes(int32_t n_seq, int32_t n_draft, int32_t vocab)
 {
     if (!sizes_ok(n_seq, n_draft, vocab)) return 0;
-    // (with a draft's rows or without them)
-    const int64_t stretches = ((int64_t)vocab + kStretch - 1) / kStretch;
-    auto parts = [&](const int64_t rows) { return rows * n_seq * parts_of(each_of(rows * n_seq, vocab), vocab); };
-    const int64_t with = parts(2 * n_draft + 1), without = parts(n_draft + 1);
-    return size_t(with > without ? with : without) * sizeof(Part) + size_t(n_seq) * (sizeof(Chosen) + size_t(stretches) * 8);
+    size_t most = 0;                               // with a draft's rows or without them, whose cut may be another
+    for (int draft = 0; draft < 2; ++draft) {
+        Args A = {};
+        cut(A, n_seq, n_draft, vocab, draft != 0);
+        const size_t bytes = lay_out(A, nullptr, n_seq);
+        if (bytes > most) most = bytes;
+    }
+    return most;
 }
 
 int sk_verify(const void* target, int64_t target_stride, const void* draft, int64_t draft_stride, int dtype, int32_t n_seq, int32_t n_draft, int32_t vocab,
@@ -506,30 +555,23 @@ int sk_verify(const void* target, int64_t target_stride, const void* draft, int6
     Args A;
     A.target = (const unsigned char*)target; A.draft = n_draft > 0 ? (const unsigned char*)draft : nullptr;
     A.target_stride = target_stride * el; A.draft_stride = draft_stride * el;
-    A.n_draft = n_draft; A.vocab = vocab;
-    A.stretches = (vocab + kStretch - 1) / kStretch;
     A.tokens = tokens; A.uniform = uniform; A.temperature = temperature;
-    const int rows = A.rows = n_draft + 1 + (A.draft ? n_draft : 0);
-    const int each = each_of((int64_t)n_seq * rows, vocab);
-    A.parts = (int32_t)parts_of(each, vocab);
-    A.part = (Part*)workspace;
-    A.chosen = (Chosen*)(A.part + (int64_t)n_seq * rows * A.parts);
-    A.sums = (double*)(A.chosen + n_seq);
+    const int each = cut(A, n_seq, n_draft, vocab, A.draft != nullptr);
+    lay_out(A, (unsigned char*)workspace, n_seq);
     A.n_accepted = n_accepted; A.out_tokens = out_tokens; A.logprob = logprob;
-    if ((int64_t)n_seq * rows * A.parts >= (int64_t(1) << 31) || (int64_t)n_seq * A.stretches >= (int64_t(1) << 31)) return SK_E_INVAL;
+    if ((int64_t)n_seq * A.rows * A.parts >= (int64_t(1) << 31)) return SK_E_INVAL;
     hipStream_t st = (hipStream_t)hip_stream;
-    const dim3 block(kThreads), first((unsigned)(n_seq * rows) * (unsigned)A.parts), second((unsigned)n_seq * (unsigned)A.stretches);
+    const dim3 block(kThreads), first((unsigned)n_seq * A.rows * A.parts), second((unsigned)n_seq * A.parts), third((unsigned)n_seq);
+#define SK_VERIFY(F32, EACH)                                                                    \
+    hipLaunchKernelGGL((sk_verify_rows<F32, EACH>), first, block, 0, st, A);                    \
+    hipLaunchKernelGGL((sk_verify_stretches<F32, EACH>), second, block, 0, st, A);              \
+    hipLaunchKernelGGL((sk_verify_draw<F32, 64 * EACH>), third, block, 0, st, A)
     if (dtype == SK_F32) {
-        if (each == kEach) hipLaunchKernelGGL((sk_verify_rows<true, kEach>), first, block, 0, st, A);
-        else hipLaunchKernelGGL((sk_verify_rows<true, kEachFew>), first, block, 0, st, A);
-        hipLaunchKernelGGL(sk_verify_stretches<true>, second, block, 0, st, A);
-        hipLaunchKernelGGL(sk_verify_draw<true>, dim3(n_seq), block, 0, st, A);
+        if (each == kEach) { SK_VERIFY(true, kEach); } else { SK_VERIFY(true, kEachFew); }
     } else {
-        if (each == kEach) hipLaunchKernelGGL((sk_verify_rows<false, kEach>), first, block, 0, st, A);
-        else hipLaunchKernelGGL((sk_verify_rows<false, kEachFew>), first, block, 0, st, A);
-        hipLaunchKernelGGL(sk_verify_stretches<false>, second, block, 0, st, A);
-        hipLaunchKernelGGL(sk_verify_draw<false>, dim3(n_seq), block, 0, st, A);
+        if (each == kEach) { SK_VERIFY(false, kEach); } else { SK_VERIFY(false, kEachFew); }
     }
+#undef SK_VERIFY
     return sk_status_of((int)hipGetLastError());
 }
 
