@@ -50,6 +50,7 @@ struct Args {
     const float* temperature;
     Part* part;                                    // [sequence][target rows, then draft rows][part]
     Sum* of_stretch;                               // [sequence][target rows][stretch]
+    float* given;                                  // [sequence][rows]: the logit of the row's drafted token
     Chosen* chosen;                                // [sequence]
     double* sums;                                  // [sequence][stretch]: of the weights of the drawn row
     int32_t *n_accepted, *out_tokens;
@@ -70,13 +71,16 @@ typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 // From 2^50 on, x scale is a whole number and two different logits lie further apart than 2^1000: only the maximum counts.
 constexpr double kFar = 1125899906842624.0;
 
-// 2^(x scale - e), where e is no less than a whole number next to the row's largest x scale
-__device__ __forceinline__ double weight_of(const float x, const double scale, const double e, const float max)
+// 2^(x scale - e), where e is no less than a whole number next to the row's largest x scale, and below 2^50 in magnitude
+__device__ __forceinline__ double near_weight(const float x, const double scale, const double e)
 {
-    if (__builtin_fabs(e) >= kFar) return x == max ? 1.0 : 0.0;
     const double d = __builtin_fmax(__builtin_fma((double)x, scale, -e), -1100.0);      // (-inf, and NaN of -inf * 0: nothing)
     const double n = __builtin_rint(d);
     return __builtin_ldexp(power_of_fraction(d - n), (int)n);
+}
+__device__ __forceinline__ double weight_of(const float x, const double scale, const double e, const float max)
+{
+    return __builtin_fabs(e) < kFar ? near_weight(x, scale, e) : x == max ? 1.0 : 0.0;
 }
 // The same for many, where 2^-1000 is as good as nothing and |e| is below 2^50: the integer part is rounded into the low bits of a sum and added to the exponent's.
 __device__ __forceinline__ double weight_in_sum(const float x, const double scale, const double e)
@@ -110,6 +114,13 @@ template <bool F32> __device__ __forceinline__ float logit(const unsigned char* 
 {
     if (F32) return ((const float*)row)[i];
     return __uint_as_float((uint32_t)((const uint16_t*)row)[i] << 16);
+}
+
+// Logit e of a piece of 16 bytes
+template <bool F32> __device__ __forceinline__ float element(const u32x4 w, const int e)
+{
+    if (F32) return __uint_as_float(w[e & 3]);
+    return __uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
 }
 
 // Sums and maxima over a row of 16 lanes and over a wave, in every lane, by lane exchanges within the vector unit.
@@ -198,7 +209,8 @@ __global__ __launch_bounds__(kThreads) void sk_verify_rows(const Args A)
     __shared__ Part of_wave[kWaves];
     const int part = blockIdx.x % A.parts, row = blockIdx.x / A.parts, seq = row / A.rows, r = row - seq * A.rows;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int n = drafted(A, token_of_lane(A, seq));
+    const int32_t tokens = token_of_lane(A, seq);
+    const int n = drafted(A, tokens);
     bool greedy;
     const double scale = scale_of(A, seq, greedy);
     if (r <= A.n_draft ? r > n : greedy || r - A.n_draft - 1 >= n) return;
@@ -206,13 +218,18 @@ __global__ __launch_bounds__(kThreads) void sk_verify_rows(const Args A)
     const float none = -__builtin_inff();
     const int stretch = part * kWaves + wave, at0 = stretch * 64 * EACH + lane * N;      // piece i: N logits from at0 + i * 64 * N on
     float v[EACH];
+    const int place = r <= A.n_draft ? r : r - A.n_draft - 1;
+    if (place < n) {
+        const int32_t t = __builtin_amdgcn_readlane(tokens, place);
+        if (t / (64 * EACH) == stretch && lane == 0) A.given[(int64_t)seq * A.rows + r] = logit<F32>(x, t);
+    }
     if (A.vocab >= N) {
         // A piece that reaches behind the row is read N logits in front of its end, of which those count that are its own.
         u32x4 w[P];
 #pragma unroll
         for (int i = 0; i < P; ++i) w[i] = *(const u32x4_anywhere*)(x + (int64_t)min(at0 + i * 64 * N, A.vocab - N) * EL);
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) v[i] = F32 ? __uint_as_float(w[i / N][i % 4]) : __uint_as_float(i & 1 ? w[i / N][i / 2 % 4] & 0xffff0000u : w[i / N][i / 2 % 4] << 16);
+        for (int i = 0; i < EACH; ++i) v[i] = element<F32>(w[i / N], i % N);
         if ((stretch + 1) * 64 * EACH > A.vocab) {
 #pragma unroll
             for (int i = 0; i < EACH; ++i) v[i] = i % N >= at0 + i / N * 64 * N - (A.vocab - N) ? v[i] : none;
@@ -276,6 +293,19 @@ template <bool F32> struct Weights {
         q = c.less == 1 ? row_of(A, seq, A.n_draft + 1 + c.place) : p;
         without = c.less == 2 ? A.tokens[(int64_t)seq * A.n_draft + c.place] : -1;
     }
+    // Where no exponent is far, as nearly always, what a logit has to pass holds no branch: `visit` is called with a function of two logits and an index.
+    template <class V> __device__ __forceinline__ void each(V visit) const
+    {
+        const bool near = __builtin_fabs(c.p_e) < kFar && __builtin_fabs(c.q_e) < kFar;
+        if (near && c.less == 1)
+            visit([&](const float x, const float y, int) __attribute__((always_inline)) {
+                return __builtin_fmax(near_weight(x, c.scale, c.p_e) * c.p_inv - near_weight(y, c.scale, c.q_e) * c.q_inv, 0.0);
+            });
+        else if (near)
+            visit([&](const float x, float, const int i) __attribute__((always_inline)) { return i == without ? 0.0 : near_weight(x, c.scale, c.p_e) * c.p_inv; });
+        else
+            visit([&](const float x, const float y, const int i) __attribute__((always_inline)) { return (*this)(x, y, i); });
+    }
     // of logits x and y of the two rows, at index i
     __device__ __forceinline__ double operator()(const float x, const float y, const int i) const
     {
@@ -288,10 +318,13 @@ template <bool F32> struct Weights {
 template <bool F32, int EACH>
 __global__ __launch_bounds__(kThreads) void sk_verify_stretches(const Args A)
 {
-    constexpr int kParts = 4;
+    // eight logits to a lane: a workgroup has one stretch, or four
+    constexpr int EL = F32 ? 4 : 2, N = 16 / EL, P = 8 / N, kParts = 4, kOfWg = kThreads * 8 / (64 * EACH);
+    static_assert(kOfWg == 1 || kOfWg == kWaves, "");
+    __shared__ double of_wave[kWaves];
     __shared__ Part row[kMaxRows];                 // of whole rows; sum 0: no probabilities
     __shared__ Chosen chosen;
-    const int wg = blockIdx.x % A.parts, seq = blockIdx.x / A.parts, tid = threadIdx.x, lane = tid & 63;
+    const int wgs = A.stretches / kOfWg, wg = blockIdx.x % wgs, seq = blockIdx.x / wgs, tid = threadIdx.x, lane = tid & 63;
     const float none = -__builtin_inff();
     bool greedy;
     const double scale = scale_of(A, seq, greedy);
@@ -300,8 +333,8 @@ __global__ __launch_bounds__(kThreads) void sk_verify_stretches(const Args A)
     // a drafted token's logits, for the lanes of the first wave
     float xp = none, xq = none, u = 0.f;
     if (tid < n) {
-        xp = logit<F32>(row_of(A, seq, lane), token);
-        if (A.draft) xq = logit<F32>(row_of(A, seq, A.n_draft + 1 + lane), token);
+        xp = A.given[(int64_t)seq * A.rows + lane];
+        if (A.draft) xq = A.given[(int64_t)seq * A.rows + A.n_draft + 1 + lane];
         u = A.uniform[(int64_t)seq * (A.n_draft + 1) + lane];
     }
     // the parts of a row meet in sixteen lanes (rows that were not computed hold anything, and are not looked at)
@@ -365,33 +398,51 @@ __global__ __launch_bounds__(kThreads) void sk_verify_stretches(const Args A)
                 float l = 0.f;
                 if (lane < a || (lane == a && valid && greedy)) {
                     const Part r = row[lane];
-                    l = log_probability(logit<F32>(row_of(A, seq, lane), t), scale, r.e, r.max, 1.0 / r.sum);
+                    l = log_probability(lane < a ? xp : p.max, scale, r.e, r.max, 1.0 / r.sum);
                 } else if (lane == a && !valid) l = __builtin_nanf("");
                 A.logprob[at] = l;
             }
         }
     }
     __syncthreads();
-    const int stretch = wg * kWaves + (tid >> 6);
+    const int sub = wg * kWaves + (tid >> 6), stretch = sub * 512 / (64 * EACH);
     // the target's own weights are known; without the drafted token, all but those of its stretch
     if (chosen.place < 0 || chosen.less == 0) return;
     const Weights<F32> w(A, chosen, seq);
     if (chosen.less == 2 && w.without / (64 * EACH) != stretch) return;
-    float x[EACH], y[EACH];
-#pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-        const int t = min(stretch * 64 * EACH + i * 64 + lane, A.vocab - 1);
-        x[i] = logit<F32>(w.p, t);
-        y[i] = logit<F32>(w.q, t);
-    }
     double sum = 0.0;
+    if (A.vocab >= N) {                            // pieces of 16 bytes as in the first launch
+        const int at0 = sub * 512 + lane * N, last = A.vocab - N;
+        u32x4 x[P], y[P];
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-        const int t = stretch * 64 * EACH + i * 64 + lane;
-        if (t < A.vocab) sum += w(x[i], y[i], t);
+        for (int i = 0; i < P; ++i) {
+            const int64_t at = (int64_t)min(at0 + i * 64 * N, last) * EL;
+            x[i] = *(const u32x4_anywhere*)(w.p + at);
+            y[i] = *(const u32x4_anywhere*)(w.q + at);
+        }
+        w.each([&](auto one) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+                const int first = at0 + i * 64 * N, from = min(first, last);
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const double z = one(element<F32>(x[i], e), element<F32>(y[i], e), from + e);
+                    sum += from + e >= first ? z : 0.0;
+                }
+            }
+        });
+    } else {
+        for (int i = lane; i < A.vocab && sub == 0; i += 64) sum += w(logit<F32>(w.p, i), logit<F32>(w.q, i), i);
     }
     sum = wave_sum(sum);
-    if (lane == 0) A.sums[(int64_t)seq * A.stretches + stretch] = sum;
+    double* to = A.sums + (int64_t)seq * A.stretches + stretch;
+    if (kOfWg == kWaves) {
+        if (lane == 0) *to = sum;
+        return;
+    }
+    if (lane == 0) of_wave[tid >> 6] = sum;
+    __syncthreads();
+    if (tid == 0) *to = of_wave[0] + of_wave[1] + of_wave[2] + of_wave[3];
 }
 
 // ---- third launch: the draw ----
@@ -462,8 +513,10 @@ __global__ __launch_bounds__(kThreads) void sk_verify_draw(const Args A)
         y[i] = logit<F32>(w.q, t);
     }
     double weight[EACH], mine = 0.0;
+    w.each([&](auto one) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) { weight[i] = begin + i < A.vocab ? w(x[i], y[i], begin + i) : 0.0; mine += weight[i]; }
+        for (int i = 0; i < EACH; ++i) { const double z = one(x[i], y[i], begin + i); weight[i] = begin + i < A.vocab ? z : 0.0; mine += weight[i]; }
+    });
     double running = wave_running_sum(mine);
     if (lane == 63) of_wave[wave] = running;
     __syncthreads();
@@ -507,6 +560,7 @@ size_t lay_out(Args& A, unsigned char* at, const int32_t n_seq)
     const int64_t parts = (int64_t)n_seq * A.rows * A.parts, stretches = (int64_t)n_seq * A.stretches;
     A.part = (Part*)at; at += parts * sizeof(Part);
     A.of_stretch = (Sum*)at; at += stretches * (A.n_draft + 1) * sizeof(Sum);
+    A.given = (float*)at; at += ((int64_t)n_seq * A.rows + 1) / 2 * 2 * sizeof(float);
     A.chosen = (Chosen*)at; at += n_seq * sizeof(Chosen);
     A.sums = (double*)at; at += stretches * sizeof(double);
     return size_t(at - from);
@@ -559,9 +613,9 @@ int sk_verify(const void* target, int64_t target_stride, const void* draft, int6
     const int each = cut(A, n_seq, n_draft, vocab, A.draft != nullptr);
     lay_out(A, (unsigned char*)workspace, n_seq);
     A.n_accepted = n_accepted; A.out_tokens = out_tokens; A.logprob = logprob;
-    if ((int64_t)n_seq * A.rows * A.parts >= (int64_t(1) << 31)) return SK_E_INVAL;
+    if ((int64_t)n_seq * A.rows * A.stretches >= (int64_t(1) << 31)) return SK_E_INVAL;
     hipStream_t st = (hipStream_t)hip_stream;
-    const dim3 block(kThreads), first((unsigned)n_seq * A.rows * A.parts), second((unsigned)n_seq * A.parts), third((unsigned)n_seq);
+    const dim3 block(kThreads), first((unsigned)n_seq * A.rows * A.parts), second((unsigned)n_seq * (each == kEach ? A.stretches : A.parts)), third((unsigned)n_seq);
 #define SK_VERIFY(F32, EACH)                                                                    \
     hipLaunchKernelGGL((sk_verify_rows<F32, EACH>), first, block, 0, st, A);                    \
     hipLaunchKernelGGL((sk_verify_stretches<F32, EACH>), second, block, 0, st, A);              \
