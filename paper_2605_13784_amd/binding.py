@@ -3,6 +3,7 @@ only.  PyTorch appears here for device memory and streams, nothing else; every s
 path runs in the library's HIP kernels.  There is no CPU fallback: if libsk.so is missing or
 a call fails, an exception is raised.
 """
+import array
 import ctypes
 import os
 import numpy as np
@@ -133,7 +134,7 @@ def lib():
     L.sk_pool_set_rotation.argtypes = [vp, i32, i32, P(ctypes.c_double), ctypes.c_float]
     L.sk_rotate.argtypes = [vp, vp, vp, i32, vp, i32, vp, vp, vp]
     L.sk_session_append_rotated.argtypes = [vp, i32, vp, vp, vp, i32, vp, i32, vp, vp, ctypes.c_int, vp, vp]
-    L.sk_batch_step_rotated.argtypes = [vp, i32, P(i32), P(i32), P(i32), vp, vp, vp, vp, vp, vp, ctypes.c_int, vp, vp]
+    L.sk_batch_step_rotated.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_int, vp, vp]
     L.sk_session_shift.argtypes = [vp, i32, i64, i64, i32, vp, i64, vp]
     L.sk_verify_workspace_bytes.restype = ctypes.c_size_t
     L.sk_verify_workspace_bytes.argtypes = [i32, i32, i32]
@@ -477,11 +478,13 @@ class Pool:
         assert positions is None or (positions.dtype is torch.int32 and positions.is_cuda and positions.numel() == n)
         if q is None:
             return None
-        assert q.dtype is self.torch_dtype and q.is_cuda and q.numel() == n * heads * self.d
+        size = n * heads * self.d
+        assert q.dtype is self.torch_dtype and q.is_cuda and q.numel() == size
         if q_out is None:
             q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
             _made(stream, q_out)
-        assert q_out.dtype is self.torch_dtype and q_out.is_cuda and q_out.numel() == q.numel()
+        else:
+            assert q_out.dtype is self.torch_dtype and q_out.is_cuda and q_out.numel() == size
         return q_out
 
     def sk_rotate(self, q, k=None, positions=None, pos0=0, q_out=None, k_out=None, stream=None):
@@ -515,9 +518,10 @@ class Pool:
         q_out = self._turns(q, q_out, self.Hq, T, positions, stream)
         if out is None:
             out, lse = self._out(T, out_dtype, want_lse, stream)
-        _ck(lib().sk_batch_step_rotated(self.h, n, (ctypes.c_int32 * n)(*map(int, session_ids)), (ctypes.c_int32 * n)(*map(int, ops)),
-                                        (ctypes.c_int32 * (n + 1))(*map(int, cu_tokens)), _p(positions), _p(q), _p(k), _p(v), _p(q_out), _p(out),
-                                        _dt(out_dtype), _p(lse), _stream(stream)), "sk_batch_step_rotated")
+        sid, op, cu = array.array("i", session_ids), array.array("i", ops), array.array("i", cu_tokens)
+        assert len(op) == n and len(cu) == n + 1
+        _ck(lib().sk_batch_step_rotated(self.h, n, sid.buffer_info()[0], op.buffer_info()[0], cu.buffer_info()[0], _p(positions), _p(q), _p(k), _p(v),
+                                        _p(q_out), _p(out), _dt(out_dtype), _p(lse), _stream(stream)), "sk_batch_step_rotated")
         return q_out, out, lse
 
     def sk_session_shift(self, sid, delta, first=0, count=None, stream=None):

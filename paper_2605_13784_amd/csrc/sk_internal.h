@@ -183,9 +183,20 @@ struct sk_rotation {
     uint64_t step[SK_ROTARY_MAX / 2];
 };
 
-// A call that turns its q and k on the way (sk_rotate.hip): the launches that stand in for the plain commit's.  `scatter` and
-// `scatter_args` commit or stage as sk_launch_scatter does, with k turned, and turn q into q_out; `rows` turns q and k (each may
-// be null) into q_out and k_out.
+// Where a stretch of tokens of one session goes, in the kernel arguments: its groups of 16 slots follow from it.
+#define SK_BLOCK_ARGS_MAX 480
+struct sk_block_list {
+    int32_t first;            // storage index of the first token
+    int32_t count;
+    int32_t blk0;             // first / block_tokens: the block that id[0] is
+    int32_t first_new;        // blocks from here on are entered in the device table
+    int32_t tbl_off;
+    int32_t id[SK_BLOCK_ARGS_MAX];
+};
+
+// A call that turns its q and k on the way (sk_rotate.hip): the launches that stand in for the plain commit's.  `scatter` commits or
+// stages as sk_launch_scatter does, with k turned, and turns q into q_out; `blocks` commits one stretch likewise; `rows` turns q and k
+// (each may be null) into q_out and k_out.
 struct sk_turned {
     const sk_rotation* rot;
     const int32_t* positions;     // DEVICE, one a token, or null: pos0, pos0 + 1, ..
@@ -196,8 +207,8 @@ struct sk_turned {
     int (*rows)(const sk_geom& g, const sk_turned& t, const void* q, const void* k, void* k_out, void* stream);
     int (*scatter)(const sk_geom& g, const sk_turned& t, const void* k, const void* v, const sk_scatter* items, int32_t n_items,
                    int32_t* tables_rw, unsigned char* kv_rw, unsigned char* eph_rw, void* stream);
-    int (*scatter_args)(const sk_geom& g, const sk_turned& t, const void* k, const void* v, const sk_scatter_list& items, int32_t n_items,
-                        int32_t* tables_rw, unsigned char* kv_rw, unsigned char* eph_rw, void* stream);
+    int (*blocks)(const sk_geom& g, const sk_turned& t, const void* k, const void* v, const sk_block_list& to,
+                  int32_t* tables_rw, unsigned char* kv_rw, void* stream);
 };
 
 // What an operator in a file of its own needs to know of a pool and one of its sessions (sk_pool.cpp).
@@ -240,12 +251,16 @@ struct sk_shift {
     int64_t len;              // storage end
     int64_t blk0, n_blk;      // blocks that hold [lo, hi)
     int64_t n_fresh;          // of those, how many are replaced
-    const int32_t* list;      // pinned: n_blk pairs of a block and what it is replaced by (itself, if it is not; n_fresh > 0, device pools)
+    // n_blk pairs of a block and what it is replaced by, itself if it is not (n_fresh > 0, device pools): up to SK_SHIFT_ARGS_MAX of
+    // them in `pairs`, more in pinned memory
+    const int32_t* list;
+    int32_t* pairs;           // the caller's, 2 * SK_SHIFT_ARGS_MAX
     int slot;
     int32_t* tables_rw;
     unsigned char* kv_rw;
 };
-int sk_shift_begin(sk_pool* p, int32_t id, int64_t lo, int64_t hi, sk_shift* out);
+#define SK_SHIFT_ARGS_MAX 360
+int sk_shift_begin(sk_pool* p, int32_t id, int64_t lo, int64_t hi, int32_t* pairs, sk_shift* out);
 void sk_shift_listed(sk_pool* p, const sk_shift& e, void* stream);
 void sk_shift_end(sk_pool* p, const sk_shift& e);
 

@@ -922,8 +922,7 @@ int scatter_reserve(sk_pool* p, int64_t n_items, ScatterSlot& ss)
     return ring_acquire(p, &ss.slot, &ss.host);
 }
 
-int scatter_launch(sk_pool* p, const ScatterSlot& ss, const std::vector<sk_scatter>& items, const void* k, const void* v, hipStream_t st,
-                   const sk_turned* turned = nullptr)
+int scatter_launch(sk_pool* p, const ScatterSlot& ss, const std::vector<sk_scatter>& items, const void* k, const void* v, hipStream_t st)
 {
     if (items.empty()) return SK_OK;
     unsigned char* ws = (unsigned char*)p->d.workspace;
@@ -932,9 +931,8 @@ int scatter_launch(sk_pool* p, const ScatterSlot& ss, const std::vector<sk_scatt
         if (!p->device) return SK_OK;
         sk_scatter_list lst;
         memcpy(lst.item, items.data(), items.size() * sizeof(sk_scatter));
-        int32_t* tables = (int32_t*)(ws + p->L.off_tables);
-        int e = turned ? turned->scatter_args(p->geom, *turned, k, v, lst, (int32_t)items.size(), tables, (unsigned char*)p->d.kv_mem, ws + p->L.off_eph, st)
-                       : sk_launch_scatter_args(p->geom, k, v, lst, (int32_t)items.size(), tables, (unsigned char*)p->d.kv_mem, ws + p->L.off_eph, st);
+        int e = sk_launch_scatter_args(p->geom, k, v, lst, (int32_t)items.size(), (int32_t*)(ws + p->L.off_tables),
+                                       (unsigned char*)p->d.kv_mem, ws + p->L.off_eph, st);
         if (e) { g_last_hip = e; return SK_E_HIP; }
         p->stats.launches++;
         return SK_OK;
@@ -961,12 +959,41 @@ int scatter_launch(sk_pool* p, const ScatterSlot& ss, const std::vector<sk_scatt
     } else if (inject(p, SK_SITE_UPLOAD)) return SK_E_HIP;
     if (inject(p, SK_SITE_SCATTER)) return SK_E_HIP;
     if (!p->device) return SK_OK;
-    int32_t* tables = (int32_t*)(ws + p->L.off_tables);
-    int e = turned ? turned->scatter(p->geom, *turned, k, v, list, (int32_t)items.size(), tables, (unsigned char*)p->d.kv_mem, ws + p->L.off_eph, st)
-                   : sk_launch_scatter(p->geom, k, v, list, (int32_t)items.size(), tables, (unsigned char*)p->d.kv_mem, ws + p->L.off_eph, st);
+    int e = sk_launch_scatter(p->geom, k, v, list, (int32_t)items.size(),
+                              (int32_t*)(ws + p->L.off_tables), (unsigned char*)p->d.kv_mem, ws + p->L.off_eph, st);
     if (in_place) ring_busy(p, ss.slot, st);         // whatever e is: an error that an earlier call left behind shows up here too, with the kernel on the stream
     if (e) { g_last_hip = e; return SK_E_HIP; }
     p->stats.launches++;
+    return SK_OK;
+}
+
+// The commit of T tokens that are turned on the way, behind position n of session s: in stretches whose blocks travel in the kernel arguments,
+// so that no list is read over the host link and no slot of pinned memory has to be waited for.  us per commit, alone in a stream, list in
+// pinned memory -> blocks in the arguments: COMMIT_FIGURES
+int commit_turned(sk_pool* p, const Session* s, int32_t id, int64_t n, int32_t T, int64_t first_new, const sk_turned& t, const void* k, const void* v, hipStream_t st,
+                  bool* enqueued)
+{
+    const int64_t B = p->d.block_tokens, row = int64_t(p->d.n_kv_heads) * p->d.head_dim * p->L.elem, q_row = int64_t(p->d.n_q_heads) * p->d.head_dim * p->L.elem;
+    sk_block_list to;
+    for (int64_t done = 0; done < T; done += to.count) {
+        to.first = int32_t(n + done); to.blk0 = int32_t(to.first / B);
+        to.count = (int32_t)std::min<int64_t>(T - done, (to.blk0 + SK_BLOCK_ARGS_MAX) * B - to.first);
+        to.first_new = (int32_t)first_new; to.tbl_off = int32_t(int64_t(id) * p->L.max_blocks_per_session);
+        memcpy(to.id, s->blocks.data() + to.blk0, size_t((to.first + to.count + B - 1) / B - to.blk0) * 4);
+        if (inject(p, SK_SITE_SCATTER)) return SK_E_HIP;
+        if (!p->device) { *enqueued = true; continue; }
+        sk_turned part = t;
+        part.n_tok = to.count;
+        part.pos0 = t.positions ? 0 : int32_t(t.pos0 + done);
+        part.positions = t.positions ? t.positions + done : nullptr;
+        part.q = t.q ? (const unsigned char*)t.q + done * q_row : nullptr;
+        part.q_out = t.q ? (unsigned char*)t.q_out + done * q_row : nullptr;
+        const int e = t.blocks(p->geom, part, (const unsigned char*)k + done * row, (const unsigned char*)v + done * row, to,
+                               (int32_t*)((unsigned char*)p->d.workspace + p->L.off_tables), (unsigned char*)p->d.kv_mem, st);
+        if (e) { g_last_hip = e; return SK_E_HIP; }
+        *enqueued = true;
+        p->stats.launches++;
+    }
     return SK_OK;
 }
 
@@ -1465,7 +1492,7 @@ void sk_evict_end(sk_pool* p, const sk_evict& e)
     p->stats.tokens_evicted += e.n_evict;
 }
 
-int sk_shift_begin(sk_pool* p, int32_t id, int64_t lo, int64_t hi, sk_shift* out)
+int sk_shift_begin(sk_pool* p, int32_t id, int64_t lo, int64_t hi, int32_t* pairs, sk_shift* out)
 {
     sk_shift& e = *out;
     const Session& s = p->sessions[(size_t)id];
@@ -1480,17 +1507,20 @@ int sk_shift_begin(sk_pool* p, int32_t id, int64_t lo, int64_t hi, sk_shift* out
     e.kv_rw = (unsigned char*)p->d.kv_mem;
     if (e.n_fresh == 0) return SK_OK;
     if (size_t(e.n_blk) * 8 > p->L.meta_bytes) return SK_E_WORKSPACE;
-    unsigned char* host;
-    const int rc = ring_acquire(p, &e.slot, &host);
-    if (rc) return rc;
+    int32_t* to = pairs;
+    if (e.n_blk <= SK_SHIFT_ARGS_MAX) e.pairs = pairs;
+    else {
+        unsigned char* host;
+        const int rc = ring_acquire(p, &e.slot, &host);
+        if (rc) return rc;
+        e.list = to = (int32_t*)host;
+    }
     size_t next = 0;
-    if (host)
-        for (int64_t b = 0; b < e.n_blk; ++b) {
-            const int32_t blk = s.blocks[size_t(e.blk0 + b)];
-            ((int32_t*)host)[2 * b] = blk;
-            ((int32_t*)host)[2 * b + 1] = p->refcnt[(size_t)blk] > 1 ? p->free_blocks[next++] : blk;
-        }
-    e.list = (const int32_t*)host;
+    for (int64_t b = 0; b < e.n_blk && p->device; ++b) {
+        const int32_t blk = s.blocks[size_t(e.blk0 + b)];
+        to[2 * b] = blk;
+        to[2 * b + 1] = p->refcnt[(size_t)blk] > 1 ? p->free_blocks[next++] : blk;
+    }
     return SK_OK;
 }
 
@@ -1727,8 +1757,9 @@ static int append(sk_pool* p, int32_t id, const void* q, const void* k, const vo
     }
     const bool in_place = attend && plan.L.own_mode != SK_OWN_NONE;
     const bool one_launch = in_place && scatter_groups(n, L) <= SK_COMMIT_ITEMS;      // the attention launch commits too
+    const bool commits_turned = turned && !in_place;
     ScatterSlot ss;
-    { int rc = scatter_reserve(p, scatter_groups(n, L), ss); if (rc) return rc; }
+    if (!commits_turned) { int rc = scatter_reserve(p, scatter_groups(n, L), ss); if (rc) return rc; }
     if (in_place && turned) {                   // the launches behind find k turned in the staging area
         const size_t bytes = size_t(L) * p->d.n_kv_heads * p->d.head_dim * p->L.elem;
         unsigned char* to = p->device ? (unsigned char*)p->d.workspace + p->L.off_eph : nullptr;
@@ -1746,15 +1777,17 @@ static int append(sk_pool* p, int32_t id, const void* q, const void* k, const vo
     int64_t first_new = 0;
     { int rc = grow_session(p, s, L, u, &first_new, st); if (rc) return rc; }
     std::vector<sk_scatter> items;
-    build_scatter(p, s, id, n, 0, L, first_new, false, 0, items);
+    if (!commits_turned) build_scatter(p, s, id, n, 0, L, first_new, false, 0, items);
     int rc;
+    bool committing = false;                    // a launch that points the device table at a private copy is on the stream
     if (in_place) { plan.own_k = k; plan.own_v = v; }
     if (one_launch) {
         plan.commit_items = (int32_t)items.size();
         memcpy(plan.commit.item, items.data(), items.size() * sizeof(sk_scatter));
         rc = inject(p, SK_SITE_SCATTER) ? SK_E_HIP : SK_OK;
-    } else rc = scatter_launch(p, ss, items, k, v, st, in_place ? nullptr : turned);
-    if (rc) { rollback(p, u, false); return rc; }
+    } else if (commits_turned) rc = commit_turned(p, s, id, n, L, first_new, *turned, k, v, st, &committing);
+    else rc = scatter_launch(p, ss, items, k, v, st);
+    if (rc) { rollback(p, u, committing); return rc; }
     if (attend) {
         rc = launch_regular(p, plan, turned ? turned->q_out : q, out, out_dtype, lse, st);
         if (rc) { rollback(p, u, !one_launch || plan.enqueued); return rc; }

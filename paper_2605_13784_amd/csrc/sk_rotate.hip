@@ -241,26 +241,39 @@ struct CommitArgs {
     sk_rotation rot;
 };
 
-template <int D, bool F32, int HEADS>
-__device__ __forceinline__ void commit_or_turn(const CommitArgs& A, const sk_scatter* items)
+// `item(i)` is the i-th group that the launch commits; behind their workgroups lie those of q.
+template <int D, bool F32, int HEADS, class ITEM>
+__device__ __forceinline__ void commit_or_turn(const CommitArgs& A, ITEM item)
 {
     __shared__ __attribute__((aligned(16))) uint16_t vt[F32 ? 8 : 16 * (D + 8)];
     const int wg = blockIdx.x;
     if (wg >= A.commit_wgs) { turn_rows<D, F32, HEADS>(A.rot, A.positions, A.pos0, A.n_tok, A.g.Hq, A.q, A.q_out, wg - A.commit_wgs); return; }
     const int i = A.by_heads.mul ? (int)(__umulhi((uint32_t)wg, A.by_heads.mul) >> A.by_heads.shift) : wg, head = wg - i * A.g.Hkv;
-    const sk_scatter it = items[i];                // at once: the list may lie in host memory
+    const sk_scatter it = item(i);
     if (it.to_eph == SK_COPY_LIST) {
         const int at = head * 256 + threadIdx.x;
-        if (at < it.count) ((u32x4*)(A.eph_rw + it.dst_off))[at] = ((const u32x4*)items)[it.src_tok0 + at];
+        if (at < it.count) ((u32x4*)(A.eph_rw + it.dst_off))[at] = ((const u32x4*)A.items)[it.src_tok0 + at];
         return;
     }
     commit_group<D, F32>(A.g, A.rot, A.positions, A.pos0, A.k, A.v, it, head, A.tables_rw, it.to_eph ? A.eph_rw : A.kv_rw, vt);
 }
 
+// Groups of a list, which may lie in host memory: read at once
 template <int D, bool F32, int HEADS>
-__global__ __launch_bounds__(256) void sk_turn_commit(const CommitArgs A) { commit_or_turn<D, F32, HEADS>(A, A.items); }
+__global__ __launch_bounds__(256) void sk_turn_commit(const CommitArgs A)
+{
+    commit_or_turn<D, F32, HEADS>(A, [&](const int i) { return A.items[i]; });
+}
+// Groups of a stretch of tokens
 template <int D, bool F32, int HEADS>
-__global__ __launch_bounds__(256) void sk_turn_commit_args(const CommitArgs A, const sk_scatter_list L) { commit_or_turn<D, F32, HEADS>(A, L.item); }
+__global__ __launch_bounds__(256) void sk_turn_commit_blocks(const CommitArgs A, const sk_block_list L)
+{
+    commit_or_turn<D, F32, HEADS>(A, [&](const int i) {
+        const int group = (L.first >> 4) + i, t0 = max(L.first, 16 * group), t1 = min(L.first + L.count, 16 * group + 16), b = t0 >> A.g.log2B;
+        const int32_t block = L.id[b - L.blk0];
+        return sk_scatter{(int64_t)block * A.g.blk_stride, t0 - L.first, t1 - t0, t0 & (A.g.B - 1), 0, b >= L.first_new ? L.tbl_off + b : -1, block};
+    });
+}
 
 // ---- keys in the cache, turned on ---------------------------------------------------------------------
 
@@ -270,7 +283,8 @@ struct ShiftArgs {
     sk_geom g;
     unsigned char* kv_rw;
     int32_t* tables_rw;
-    const int32_t* list;          // pairs of a block and what it is replaced by, from blk0 on; null: nothing is replaced
+    const int32_t* list;          // pairs of a block and what it is replaced by, from blk0 on, where they are not in the arguments
+    int32_t replaces;             // 0: no block is replaced
     int32_t tbl_off, blk0;
     int32_t start, end;           // storage indices: the first of a group, and behind the last token
     int32_t lo, hi;               // turned: [lo, hi) without [hole_lo, hole_hi)
@@ -284,7 +298,7 @@ struct ShiftArgs {
 
 // Workgroup (64 tokens, KV head).
 template <int D, bool F32>
-__global__ __launch_bounds__(256) void sk_turn_cached(const ShiftArgs A)
+__device__ __forceinline__ void turn_cached(const ShiftArgs& A, const int32_t* list)
 {
     constexpr int U = D / 16, ROWB = D * (F32 ? 4 : 2), ROWS = 256 / U, N = kShiftTokens / ROWS;
     constexpr int GB = 16 * ROWB;                  // bytes of a group's V
@@ -293,7 +307,7 @@ __global__ __launch_bounds__(256) void sk_turn_cached(const ShiftArgs A)
     unsigned char* kv = A.kv_rw + (int64_t)head * A.g.head_stride;
     auto block_of = [&](const int t, int& from, int& to) {
         const int b = t >> A.g.log2B;
-        if (A.list) { from = A.list[2 * (b - A.blk0)]; to = A.list[2 * (b - A.blk0) + 1]; }
+        if (A.replaces) { from = list[2 * (b - A.blk0)]; to = list[2 * (b - A.blk0) + 1]; }
         else from = to = A.g.tables[A.tbl_off + b];
     };
     const Place at = place_of<F32>(A.rot, unit);
@@ -316,7 +330,7 @@ __global__ __launch_bounds__(256) void sk_turn_cached(const ShiftArgs A)
         }
     }
     // V of blocks that are replaced: whole groups of 16 slots
-    if (A.list) {
+    if (A.replaces) {
         constexpr int PV = GB / 16;                // pieces of a group
 #pragma unroll
         for (int i = 0; i < kShiftTokens / 16 * PV / 256; ++i) {
@@ -330,7 +344,7 @@ __global__ __launch_bounds__(256) void sk_turn_cached(const ShiftArgs A)
         }
         if (head == 0 && tid < kShiftTokens / 16) {
             const int t = t0 + 16 * tid;
-            if (t < A.end && (t & (A.g.B - 1)) == 0) A.tables_rw[A.tbl_off + (t >> A.g.log2B)] = A.list[2 * ((t >> A.g.log2B) - A.blk0) + 1];
+            if (t < A.end && (t & (A.g.B - 1)) == 0) A.tables_rw[A.tbl_off + (t >> A.g.log2B)] = list[2 * ((t >> A.g.log2B) - A.blk0) + 1];
         }
     }
 #pragma unroll
@@ -345,6 +359,12 @@ __global__ __launch_bounds__(256) void sk_turn_cached(const ShiftArgs A)
         store_unit<F32>(to_row[i], at, u[i]);
     }
 }
+
+template <int D, bool F32>
+__global__ __launch_bounds__(256) void sk_turn_cached(const ShiftArgs A) { turn_cached<D, F32>(A, A.list); }
+struct PairList { int32_t pair[2 * SK_SHIFT_ARGS_MAX]; };
+template <int D, bool F32>
+__global__ __launch_bounds__(256) void sk_turn_cached_args(const ShiftArgs A, const PairList L) { turn_cached<D, F32>(A, L.pair); }
 
 // ---- launches -----------------------------------------------------------------------------------------
 
@@ -377,7 +397,7 @@ int launch_rows(const sk_geom& g, const sk_turned& t, const void* q, const void*
     return (int)hipGetLastError();
 }
 
-int launch_commit(const sk_geom& g, const sk_turned& t, const void* k, const void* v, const sk_scatter* items, const sk_scatter_list* args, int32_t n_items,
+int launch_commit(const sk_geom& g, const sk_turned& t, const void* k, const void* v, const sk_scatter* items, const sk_block_list* to, int32_t n_items,
                   int32_t* tables_rw, unsigned char* kv_rw, unsigned char* eph_rw, void* stream)
 {
     CommitArgs A;
@@ -391,8 +411,8 @@ int launch_commit(const sk_geom& g, const sk_turned& t, const void* k, const voi
     const dim3 grid((unsigned)A.commit_wgs + (t.q ? row_wgs(g, t.n_tok, g.Hq, four ? 4 : 1) : 0)), block(256);
     hipStream_t st = (hipStream_t)stream;
 #define SK_COMMIT(D, F32)                                                                                       \
-    if (args) { if (four) hipLaunchKernelGGL((sk_turn_commit_args<D, F32, 4>), grid, block, 0, st, A, *args);   \
-                else hipLaunchKernelGGL((sk_turn_commit_args<D, F32, 1>), grid, block, 0, st, A, *args); }      \
+    if (to) { if (four) hipLaunchKernelGGL((sk_turn_commit_blocks<D, F32, 4>), grid, block, 0, st, A, *to);     \
+              else hipLaunchKernelGGL((sk_turn_commit_blocks<D, F32, 1>), grid, block, 0, st, A, *to); }        \
     else if (four) hipLaunchKernelGGL((sk_turn_commit<D, F32, 4>), grid, block, 0, st, A);                      \
     else hipLaunchKernelGGL((sk_turn_commit<D, F32, 1>), grid, block, 0, st, A)
     SK_BY_SHAPE(g, SK_COMMIT);
@@ -404,10 +424,9 @@ int launch_scatter(const sk_geom& g, const sk_turned& t, const void* k, const vo
 {
     return launch_commit(g, t, k, v, items, nullptr, n_items, tables_rw, kv_rw, eph_rw, stream);
 }
-int launch_scatter_args(const sk_geom& g, const sk_turned& t, const void* k, const void* v, const sk_scatter_list& items, int32_t n_items,
-                        int32_t* tables_rw, unsigned char* kv_rw, unsigned char* eph_rw, void* stream)
+int launch_blocks(const sk_geom& g, const sk_turned& t, const void* k, const void* v, const sk_block_list& to, int32_t* tables_rw, unsigned char* kv_rw, void* stream)
 {
-    return launch_commit(g, t, k, v, nullptr, &items, n_items, tables_rw, kv_rw, eph_rw, stream);
+    return launch_commit(g, t, k, v, nullptr, &to, (to.first + to.count + 15) / 16 - to.first / 16, tables_rw, kv_rw, nullptr, stream);
 }
 
 bool aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
@@ -416,7 +435,7 @@ sk_turned make_turned(const sk_rotation* rot, const void* q, void* q_out, const 
 {
     sk_turned t;
     t.rot = rot; t.positions = positions; t.pos0 = pos0; t.n_tok = n_tok; t.q = q; t.q_out = q_out;
-    t.rows = launch_rows; t.scatter = launch_scatter; t.scatter_args = launch_scatter_args;
+    t.rows = launch_rows; t.scatter = launch_scatter; t.blocks = launch_blocks;
     return t;
 }
 
@@ -501,7 +520,8 @@ int sk_session_shift(sk_pool* p, int32_t id, int64_t first, int64_t count, int32
     auto stored = [&](const int64_t j) { return j < V.frozen ? j : j - V.frozen + V.win; };
     const int64_t lo = stored(first), hi = stored(first + count - 1) + 1;
     sk_shift E;
-    rc = sk_shift_begin(p, id, lo, hi, &E);
+    PairList pairs;
+    rc = sk_shift_begin(p, id, lo, hi, pairs.pair, &E);
     if (rc) return rc;
     if (sk_injected(p, SK_SITE_SCATTER)) return SK_E_HIP;
     if (V.device) {
@@ -509,16 +529,18 @@ int sk_session_shift(sk_pool* p, int32_t id, int64_t first, int64_t count, int32
         int e = (int)hipGetLastError();
         if (e) return sk_note_hip_error(e);
         ShiftArgs A = {};
-        A.g = V.g; A.kv_rw = E.kv_rw; A.tables_rw = E.tables_rw; A.list = E.list; A.tbl_off = V.tbl_off; A.blk0 = (int32_t)E.blk0;
+        A.g = V.g; A.kv_rw = E.kv_rw; A.tables_rw = E.tables_rw; A.list = E.list; A.replaces = E.n_fresh > 0; A.tbl_off = V.tbl_off; A.blk0 = (int32_t)E.blk0;
         // of replaced blocks everything that holds tokens, otherwise the groups of the stretch
-        const int64_t start = E.list ? E.blk0 * V.g.B : lo / 16 * 16, behind = (E.blk0 + E.n_blk) * V.g.B;
-        const int64_t end = E.list ? (behind < E.len ? behind : E.len) : hi;
+        const int64_t start = A.replaces ? E.blk0 * V.g.B : lo / 16 * 16, behind = (E.blk0 + E.n_blk) * V.g.B;
+        const int64_t end = A.replaces ? (behind < E.len ? behind : E.len) : hi;
         A.start = (int32_t)start; A.end = (int32_t)end; A.lo = (int32_t)lo; A.hi = (int32_t)hi;
         A.hole_lo = (int32_t)V.frozen; A.hole_hi = (int32_t)V.win;
         A.delta = delta; A.deltas = deltas; A.delta_stride = delta_stride; A.first = (int32_t)first;
         A.rot = *sk_rotation_of(p);
         const dim3 grid((unsigned)((end - start + kShiftTokens - 1) / kShiftTokens * V.g.Hkv)), block(256);
-#define SK_SHIFT(D, F32) hipLaunchKernelGGL((sk_turn_cached<D, F32>), grid, block, 0, (hipStream_t)hip_stream, A)
+#define SK_SHIFT(D, F32)                                                                                                        \
+    if (E.pairs) hipLaunchKernelGGL((sk_turn_cached_args<D, F32>), grid, block, 0, (hipStream_t)hip_stream, A, pairs);            \
+    else hipLaunchKernelGGL((sk_turn_cached<D, F32>), grid, block, 0, (hipStream_t)hip_stream, A)
         SK_BY_SHAPE(V.g, SK_SHIFT);
 #undef SK_SHIFT
         e = (int)hipGetLastError();

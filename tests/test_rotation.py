@@ -129,6 +129,42 @@ def test_append_rotated_on_the_host():
     pool.sk_pool_inject_failure(0, 0)
 
 
+def test_a_list_of_shared_blocks_in_pinned_memory():
+    pool = _host_pool(1000)
+    pool.sk_pool_set_rotation(np.ones(32))
+    a = pool.sk_session_create()
+    pool.reserve(a, 4096), pool.reserve(a, 16 * 400 - 4096)
+    b = pool.sk_session_fork(a, 16 * 400)
+    before = pool.sk_session_block_table(b)
+    for site in (sk.SK_SITE_RING, sk.SK_SITE_SCATTER):
+        pool.sk_pool_inject_failure(site)
+        assert _status(pool.sk_session_shift, b, 7) == sk.SK_E_HIP
+        assert pool.sk_session_block_table(b) == before and pool.sk_pool_blocks_free() == 600
+    pool.sk_session_shift(b, 7)
+    assert not set(pool.sk_session_block_table(b)) & set(before) and pool.sk_pool_blocks_free() == 200
+
+
+@pytest.mark.parametrize("launch,kept", [(1, 0), (2, 1), (3, 1)])
+def test_a_long_append_that_fails_between_its_launches(launch, kept):
+    """Its blocks travel in the arguments of several launches.  The copy of a shared last block stays once a launch has pointed the device's
+    table at it; everything else is taken back."""
+    pool = sk.Pool("bf16", 4, 2, 64, 16, 2000, max_sessions=2, max_batch_tokens=20000, metadata_only=True)
+    pool.sk_pool_set_rotation(np.ones(32))
+    a = pool.sk_session_create()
+    pool.reserve(a, 40)
+    b = pool.sk_session_fork(a, 48 - 8)
+    pool.sk_session_truncate(a, 20)                            # ends inside a block that the fork holds too
+    tables, free = pool.sk_session_block_table(a), pool.sk_pool_blocks_free()
+    pool.sk_pool_inject_failure(sk.SK_SITE_SCATTER, launch)
+    L = sk.lib()
+    assert L.sk_session_append_rotated(pool.h, a, None, None, None, 18000, None, 0, None, None, sk.SK_F32, None, None) == sk.SK_E_HIP
+    assert pool.sk_session_length(a) == 20 and pool.sk_pool_blocks_free() == free - kept
+    now = pool.sk_session_block_table(a)
+    assert now[:1] == tables[:1] and (now[1] != tables[1]) == bool(kept)
+    assert L.sk_session_append_rotated(pool.h, a, None, None, None, 18000, None, 0, None, None, sk.SK_F32, None, None) == sk.SK_OK
+    assert pool.sk_session_length(a) == 18020 and pool.sk_session_length(b) == 40
+
+
 def test_shared_blocks_are_replaced_and_others_are_not():
     pool = _host_pool(24)
     pool.sk_pool_set_rotation(np.ones(32))
@@ -148,9 +184,6 @@ def test_shared_blocks_are_replaced_and_others_are_not():
     pool.sk_session_shift(a, 7, first=40, count=1)             # the other holder's block 2 has one holder
     assert pool.sk_session_block_table(a) == ta
     pool.sk_pool_inject_failure(sk.SK_SITE_SCATTER)
-    assert _status(pool.sk_session_shift, b, 7) == sk.SK_E_HIP
-    assert pool.sk_session_block_table(b) == now
-    pool.sk_pool_inject_failure(sk.SK_SITE_RING)
     assert _status(pool.sk_session_shift, b, 7) == sk.SK_E_HIP
     assert pool.sk_session_block_table(b) == now
     # more shared blocks than are free: refused, nothing changed
@@ -306,6 +339,45 @@ def test_append_is_a_rotation_and_an_append(layer, block, rotary, interleaved):
     n = pools[0].sk_session_length(sids[0])
     got_q = pools[0].sk_session_append_rotated(sids[0], q, k, v)[0]
     assert torch.equal(got_q, pools[1].sk_rotate(q, pos0=n)[0])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_an_append_whose_blocks_take_several_launches(dtype):
+    layer, T = (dtype, 2, 1, 64), 9000
+    pools = [_pool(layer, 64, False, n_blocks=700, max_batch_tokens=T) for _ in range(2)]
+    gen = synth.generator(23)
+    q, k, v = (x.cuda() for x in _rows(gen, T, layer))
+    sids = [p.sk_session_create() for p in pools]
+    for p, s in zip(pools, sids):
+        p.sk_session_append(s, None, k[:5].contiguous(), v[:5].contiguous())
+    for positions, pos0 in ((None, 77), (torch.randint(0, 1 << 20, (T,), generator=gen, dtype=torch.int32).cuda(), 0)):
+        got_q, _, _ = pools[0].sk_session_append_rotated(sids[0], q, k, v, positions=positions, pos0=pos0, attend=False)
+        want_q, want_k = pools[1].sk_rotate(q, k, positions=positions, pos0=pos0)
+        pools[1].sk_session_append(sids[1], None, want_k, v)
+        assert torch.equal(got_q, want_q)
+        _same(pools[0], sids[0], pools[1], sids[1])
+        for p, s in zip(pools, sids):
+            p.sk_session_truncate(s, 5)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("by", ["all", "head"])
+def test_shift_of_more_shared_blocks_than_travel_in_the_arguments(by):
+    layer = ("bf16", 2, 2, 64)
+    pool = _pool(layer, 64, False, n_blocks=1100, max_sessions=2)
+    gen = synth.generator(24)
+    source, k, v = _cached(pool, gen, 8000, layer)
+    for first in (0, 3000):                                    # 500 shared blocks; 313
+        fork = pool.sk_session_fork(source, 8000)
+        delta = _deltas(gen, by, 2, 8000 - first)
+        pool.sk_session_shift(fork, delta if by == "all" else delta.cuda(), first=first)
+        got_k, got_v = (x.cpu() for x in pool.sk_session_gather(fork))
+        assert torch.equal(got_v, v) and torch.equal(got_k[:first], k[:first])
+        _check(got_k[first:], k[first:], np.full((8000 - first, 2), delta) if by == "all" else delta.numpy().T, 64, False, "bf16")
+        src_k, src_v = (x.cpu() for x in pool.sk_session_gather(source))
+        assert torch.equal(src_k, k) and torch.equal(src_v, v)
+        pool.sk_session_destroy(fork)
 
 
 @pytest.mark.gpu
