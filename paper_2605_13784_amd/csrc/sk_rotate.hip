@@ -53,14 +53,23 @@ __device__ __forceinline__ f32x2 cos_sin(const uint32_t phase)
     return f32x2{__uint_as_float(__float_as_uint(a) ^ ((quadrant + 1) & 2) << 30), __uint_as_float(__float_as_uint(b) ^ (quadrant & 2) << 30)};
 }
 
-// cos and sin of the eight pairs from pair0 on
+// Steps of the eight pairs of a unit, asked for ahead of the rows that they turn (units that do not turn have some too)
+struct Steps { uint64_t of[8]; };
+__device__ __forceinline__ Steps steps_of(const sk_rotation& rot, const int unit)
+{
+    Steps s;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s.of[i] = rot.step[8 * unit + i];
+    return s;
+}
+// cos and sin of those pairs
 struct Turn { float c[8], s[8]; };
-__device__ __forceinline__ Turn turn_of(const sk_rotation& rot, const int pair0, const int32_t position, const float factor)
+__device__ __forceinline__ Turn turn_of(const Steps& steps, const int32_t position, const float factor)
 {
     Turn t;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const f32x2 cs = cos_sin(phase_of(position, rot.step[pair0 + i]));
+        const f32x2 cs = cos_sin(phase_of(position, steps.of[i]));
         t.c[i] = cs.x * factor; t.s[i] = cs.y * factor;
     }
     return t;
@@ -150,6 +159,8 @@ __device__ __forceinline__ void turn_rows(const sk_rotation& rot, const int32_t*
     const int head_groups = (n_heads + HEADS - 1) / HEADS, stretch = wg / head_groups, head0 = (wg - stretch * head_groups) * HEADS;
     const int unit = threadIdx.x % U, tok = stretch * TOK + threadIdx.x / U;
     if (tok >= n_tok) return;
+    const Steps steps = steps_of(rot, unit);
+    const int32_t position = positions ? positions[tok] : pos0 + tok;
     const bool turns = 16 * unit < rot.rotary;
     const Place at = place_of<F32>(rot, unit);
     const int64_t row = ((int64_t)tok * n_heads + head0) * ROWB;
@@ -158,7 +169,7 @@ __device__ __forceinline__ void turn_rows(const sk_rotation& rot, const int32_t*
     for (int h = 0; h < HEADS; ++h)
         if (head0 + h < n_heads) u[h] = load_unit<F32>((const unsigned char*)x + row + h * ROWB, at);
     if (turns) {
-        const Turn t = turn_of(rot, 8 * unit, positions ? positions[tok] : pos0 + tok, rot.factor);
+        const Turn t = turn_of(steps, position, rot.factor);
 #pragma unroll
         for (int h = 0; h < HEADS; ++h) u[h] = turned<F32>(u[h], t, rot.interleaved);
     }
@@ -188,6 +199,9 @@ __device__ __forceinline__ void commit_group(const sk_geom& g, const sk_rotation
     unsigned char* vdst = dst + (it.to_eph ? g.eph_v_off : g.v_off);
     if (it.tbl_index >= 0 && head == 0 && tid == 0) tables_rw[it.tbl_index] = it.block_id;
     const bool mine = row < it.count;
+    const Steps steps = steps_of(rot, unit);
+    int32_t position = pos0 + it.src_tok0 + row;
+    if (mine && positions) position = positions[it.src_tok0 + row];
     const Place at = place_of<F32>(rot, unit);
     Unit<F32> u;
     if (mine) u = load_unit<F32>((const unsigned char*)k + ((int64_t)(it.src_tok0 + row) * g.Hkv + head) * ROWB, at);
@@ -199,8 +213,7 @@ __device__ __forceinline__ void commit_group(const sk_geom& g, const sk_rotation
         if (r < it.count) y[i] = *(const u32x4*)((const unsigned char*)v + ((int64_t)(it.src_tok0 + r) * g.Hkv + head) * ROWB + (p % PR) * 16);
     }
     if (mine) {
-        const int tok = it.src_tok0 + row;
-        if (16 * unit < rot.rotary) u = turned<F32>(u, turn_of(rot, 8 * unit, positions ? positions[tok] : pos0 + tok, rot.factor), rot.interleaved);
+        if (16 * unit < rot.rotary) u = turned<F32>(u, turn_of(steps, position, rot.factor), rot.interleaved);
         store_unit<F32>(dst + (it.dst_slot0 + row) * ROWB, at, u);
     }
 #pragma unroll
@@ -312,14 +325,18 @@ __device__ __forceinline__ void turn_cached(const ShiftArgs& A, const int32_t* l
     };
     const Place at = place_of<F32>(A.rot, unit);
     const bool turns = 16 * unit < A.rot.rotary;
+    const Steps steps = steps_of(A.rot, unit);
     Unit<F32> u[N];
     unsigned char* to_row[N];
     bool moves[N], writes[N];
+    int32_t by[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const int t = t0 + tid / U + i * ROWS;
         moves[i] = turns && t >= A.lo && t < A.hi && !(t >= A.hole_lo && t < A.hole_hi);
         writes[i] = false;
+        by[i] = A.delta;
+        if (moves[i] && A.deltas) by[i] = A.deltas[head * A.delta_stride + (t >= A.hole_hi ? t - (A.hole_hi - A.hole_lo) : t) - A.first];
         if (t < A.end) {
             int from, to;
             block_of(t, from, to);
@@ -347,15 +364,13 @@ __device__ __forceinline__ void turn_cached(const ShiftArgs& A, const int32_t* l
             if (t < A.end && (t & (A.g.B - 1)) == 0) A.tables_rw[A.tbl_off + (t >> A.g.log2B)] = list[2 * ((t >> A.g.log2B) - A.blk0) + 1];
         }
     }
+    // one turn for all, or one a row
+    Turn turn = turn_of(steps, by[0], 1.f);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
+        if (i > 0 && A.deltas) turn = turn_of(steps, by[i], 1.f);
         if (!writes[i]) continue;
-        if (moves[i]) {
-            const int t = t0 + tid / U + i * ROWS;
-            int32_t d = A.delta;
-            if (A.deltas) d = A.deltas[head * A.delta_stride + (t >= A.hole_hi ? t - (A.hole_hi - A.hole_lo) : t) - A.first];
-            if (d != 0) u[i] = turned<F32>(u[i], turn_of(A.rot, 8 * unit, d, 1.f), A.rot.interleaved);
-        }
+        if (moves[i] && by[i] != 0) u[i] = turned<F32>(u[i], turn, A.rot.interleaved);
         store_unit<F32>(to_row[i], at, u[i]);
     }
 }
