@@ -445,7 +445,7 @@ int sk_logprobs(const void* logits, int dtype, int32_t rows, int32_t vocab, int6
  * the last token that has a weight; where p - q leaves nothing, the drafted token is drawn).  Greedy: the largest logit's.
  * Outputs, DEVICE: n_accepted int32 [n_seq], the tokens that stay; out_tokens int32 [n_seq][n_draft + 1], those, the one drawn, then -1;
  * logprob float [n_seq][n_draft + 1] (may be NULL), the target's log probability at the temperature (greedy: at 1) of each, 0 behind them.
- * They overlap no input.  A target row that has no probabilities (NaN or +inf among its logits, or nothing but -inf) keeps no token and draws -1, log probability
+ * They overlap neither an input nor each other nor the workspace (SK_E_INVAL).  A target row that has no probabilities (NaN or +inf among its logits, or nothing but -inf) keeps no token and draws -1, log probability
  * NaN; a draft row that has none keeps no token and takes nothing off p.  Rows behind a sequence's draft are not read, nor are draft rows of greedy sequences.
  * Sums and exponentials are held in 64 bits.  workspace: DEVICE scratch of sk_verify_workspace_bytes(..) bytes, 16-byte aligned, owned by the
  * caller; calls that overlap in time need one each.  Kernels only: the call can be captured in a HIP graph.

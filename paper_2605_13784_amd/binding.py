@@ -635,29 +635,37 @@ def sk_verify(target, tokens, uniform, draft=None, temperature=None, workspace=N
     strided, evenly over sequences and places.  Returns (n_accepted [n_seq], tokens [n_seq, n_draft + 1], logprob [n_seq, n_draft + 1])."""
     assert target.is_cuda and target.dtype in (torch.float32, torch.bfloat16) and target.dim() == 3
     n_seq, places, vocab = target.shape
-    n_draft = places - 1
+    n_draft, on = places - 1, target.get_device()
 
     def rows(x, n):                                          # address and row stride of [n_seq, n, vocab]
-        assert x.is_cuda and x.dtype is target.dtype and x.shape == (n_seq, n, vocab) and (x.stride(2) == 1 or vocab == 1)
-        stride = x.stride(1) if n > 1 else x.stride(0) if n_seq > 1 else vocab
-        assert n <= 1 or n_seq <= 1 or x.stride(0) == n * stride
-        return x.data_ptr() if x.numel() else None, stride
+        s0, s1, s2 = x.stride()
+        stride = s1 if n > 1 else s0 if n_seq > 1 else vocab
+        assert (s2 == 1 or vocab == 1) and (n <= 1 or n_seq <= 1 or s0 == n * stride)
+        return x.data_ptr() if n_seq else None, stride
 
     pt, st = rows(target, places)
-    pd, sd = (None, 0) if draft is None or n_draft == 0 else rows(draft, n_draft)
-    for t, kind, shape in ((tokens, torch.int32, (n_seq, n_draft)), (uniform, torch.float32, (n_seq, places)), (temperature, torch.float32, (n_seq,))):
-        assert (t is None and kind is torch.float32 and shape == (n_seq,)) or (t.is_cuda and t.dtype is kind and t.shape == shape)
+    pd, sd = None, 0
+    if draft is not None:
+        assert draft.dtype is target.dtype and draft.shape == (n_seq, n_draft, vocab) and draft.get_device() == on
+        pd, sd = rows(draft, n_draft) if n_draft else (None, 0)
+    assert tokens.dtype is torch.int32 and tokens.shape == (n_seq, n_draft) and tokens.get_device() == on
+    assert uniform.dtype is torch.float32 and uniform.shape == (n_seq, places) and uniform.get_device() == on
+    assert temperature is None or (temperature.dtype is torch.float32 and temperature.shape == (n_seq,) and temperature.get_device() == on)
     if outputs is None:
         outputs = verify_outputs(n_seq, n_draft, target.device)
         _made(stream, *outputs)
-    n_accepted, out_tokens, logprob = outputs
-    for t, kind, n in ((n_accepted, torch.int32, n_seq), (out_tokens, torch.int32, n_seq * places), (logprob, torch.float32, n_seq * places)):
-        assert (t is None and kind is torch.float32) or (t.is_cuda and t.dtype is kind and t.numel() == n)
+        n_accepted, out_tokens, logprob = outputs
+    else:
+        n_accepted, out_tokens, logprob = outputs
+        assert n_accepted.dtype is torch.int32 and n_accepted.numel() == n_seq and n_accepted.get_device() == on
+        assert out_tokens.dtype is torch.int32 and out_tokens.numel() == n_seq * places and out_tokens.get_device() == on
+        assert logprob is None or (logprob.dtype is torch.float32 and logprob.numel() == n_seq * places and logprob.get_device() == on)
+    L = lib()
     if workspace is None:
-        workspace = torch.empty(max(lib().sk_verify_workspace_bytes(n_seq, n_draft, vocab), 16), dtype=torch.uint8, device=target.device)
+        workspace = torch.empty(max(L.sk_verify_workspace_bytes(n_seq, n_draft, vocab), 16), dtype=torch.uint8, device=target.device)
         _made(stream, workspace)
-    _ck(lib().sk_verify(pt, st, pd, sd, _dt(target.dtype), n_seq, n_draft, vocab, _p(tokens), _p(uniform), _p(temperature), _p(workspace),
-                        workspace.numel() * workspace.element_size(), _p(n_accepted), _p(out_tokens), _p(logprob), _stream(stream)), "sk_verify")
+    _ck(L.sk_verify(pt, st, pd, sd, SK_F32 if target.dtype is torch.float32 else SK_BF16, n_seq, n_draft, vocab, _p(tokens), _p(uniform), _p(temperature),
+                    _p(workspace), workspace.numel() * workspace.element_size(), _p(n_accepted), _p(out_tokens), _p(logprob), _stream(stream)), "sk_verify")
     return outputs
 
 

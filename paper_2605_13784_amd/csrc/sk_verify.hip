@@ -554,16 +554,17 @@ bool sizes_ok(const int32_t n_seq, const int32_t n_draft, const int32_t vocab)
            (int64_t)n_seq * (n_draft + 1) <= SK_VERIFY_MAX_ROWS;
 }
 // What a call keeps, in the order in which it lies in the workspace
-size_t lay_out(Args& A, unsigned char* at, const int32_t n_seq)
+size_t lay_out(Args& A, void* workspace, const int32_t n_seq)
 {
-    const unsigned char* from = at;
     const int64_t parts = (int64_t)n_seq * A.rows * A.parts, stretches = (int64_t)n_seq * A.stretches;
-    A.part = (Part*)at; at += parts * sizeof(Part);
-    A.of_stretch = (Sum*)at; at += stretches * (A.n_draft + 1) * sizeof(Sum);
-    A.given = (float*)at; at += ((int64_t)n_seq * A.rows + 1) / 2 * 2 * sizeof(float);
-    A.chosen = (Chosen*)at; at += n_seq * sizeof(Chosen);
-    A.sums = (double*)at; at += stretches * sizeof(double);
-    return size_t(at - from);
+    uintptr_t at = (uintptr_t)workspace;
+    auto take = [&](const int64_t n, const size_t bytes) { const uintptr_t p = at; at += size_t(n) * bytes; return (void*)p; };
+    A.part = (Part*)take(parts, sizeof(Part));
+    A.of_stretch = (Sum*)take(stretches * (A.n_draft + 1), sizeof(Sum));
+    A.given = (float*)take(((int64_t)n_seq * A.rows + 1) / 2 * 2, sizeof(float));
+    A.chosen = (Chosen*)take(n_seq, sizeof(Chosen));
+    A.sums = (double*)take(stretches, sizeof(double));
+    return size_t(at - (uintptr_t)workspace);
 }
 int cut(Args& A, const int32_t n_seq, const int32_t n_draft, const int32_t vocab, const bool draft)
 {
@@ -605,13 +606,26 @@ int sk_verify(const void* target, int64_t target_stride, const void* draft, int6
     auto off = [](const void* p, const uintptr_t to) { return ((uintptr_t)p & (to - 1)) != 0; };
     if (off(target, el) || off(draft, el) || off(tokens, 4) || off(uniform, 4) || off(temperature, 4) || off(n_accepted, 4) || off(out_tokens, 4) || off(logprob, 4)) return SK_E_INVAL;
     if (!workspace || off(workspace, 16)) return SK_E_INVAL;
-    if (workspace_bytes < sk_verify_workspace_bytes(n_seq, n_draft, vocab)) return SK_E_WORKSPACE;
+    const size_t scratch = sk_verify_workspace_bytes(n_seq, n_draft, vocab);
+    if (workspace_bytes < scratch) return SK_E_WORKSPACE;
+    {   // what is written, first, lies apart from everything else
+        const int64_t places = (int64_t)n_seq * (n_draft + 1), drafts = (int64_t)n_seq * n_draft;
+        struct { const void* at; size_t bytes; } a[] = {
+            {n_accepted, size_t(n_seq) * 4}, {out_tokens, size_t(places) * 4}, {logprob, size_t(places) * 4}, {workspace, scratch},
+            {target, size_t((places - 1) * target_stride + vocab) * el}, {draft, drafts ? size_t((drafts - 1) * draft_stride + vocab) * el : 0},
+            {tokens, size_t(drafts) * 4}, {uniform, size_t(places) * 4}, {temperature, size_t(n_seq) * 4}};
+        for (int i = 0; i < 4; ++i)
+            for (int j = i + 1; j < 9; ++j) {
+                const uintptr_t x = (uintptr_t)a[i].at, y = (uintptr_t)a[j].at;
+                if (x && y && x < y + a[j].bytes && y < x + a[i].bytes) return SK_E_INVAL;
+            }
+    }
     Args A;
     A.target = (const unsigned char*)target; A.draft = n_draft > 0 ? (const unsigned char*)draft : nullptr;
     A.target_stride = target_stride * el; A.draft_stride = draft_stride * el;
     A.tokens = tokens; A.uniform = uniform; A.temperature = temperature;
     const int each = cut(A, n_seq, n_draft, vocab, A.draft != nullptr);
-    lay_out(A, (unsigned char*)workspace, n_seq);
+    lay_out(A, workspace, n_seq);
     A.n_accepted = n_accepted; A.out_tokens = out_tokens; A.logprob = logprob;
     if ((int64_t)n_seq * A.rows * A.stretches >= (int64_t(1) << 31)) return SK_E_INVAL;
     hipStream_t st = (hipStream_t)hip_stream;

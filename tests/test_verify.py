@@ -105,9 +105,10 @@ def _case(gen, n, k, V, dtype, near=1.0, spread=2.5):
 
 def test_refusals_without_a_gpu():
     L = sk.lib()
-    p = 4096                                                  # an address that no call below gets as far as using
+    p = 1 << 24                                               # addresses that no call below gets as far as using
+    q, r = 2 * p, 3 * p
     good = dict(target=p, target_stride=100, draft=p, draft_stride=100, dtype=sk.SK_F32, n_seq=3, n_draft=2, vocab=100, tokens=p, uniform=p, temperature=p,
-                ws=p, ws_bytes=1 << 20, n_accepted=p, out_tokens=p, logprob=p, stream=None)
+                ws=q, ws_bytes=1 << 20, n_accepted=r, out_tokens=r + 64, logprob=r + 128, stream=None)
 
     def call(**kw):
         return L.sk_verify(*{**good, **kw}.values())
@@ -115,8 +116,11 @@ def test_refusals_without_a_gpu():
     for bad in (dict(n_seq=-1), dict(n_draft=-1), dict(n_draft=sk.SK_VERIFY_MAX_DRAFT + 1), dict(vocab=0), dict(vocab=-5), dict(target_stride=99),
                 dict(draft_stride=99), dict(vocab=sk.SK_VERIFY_MAX_VOCAB + 1, target_stride=1 << 22, draft_stride=1 << 22), dict(n_seq=sk.SK_VERIFY_MAX_ROWS),
                 dict(target=None), dict(tokens=None), dict(uniform=None), dict(n_accepted=None), dict(out_tokens=None), dict(target=p + 2),
-                dict(draft=p + 1), dict(dtype=sk.SK_BF16, target=p + 1), dict(tokens=p + 2), dict(uniform=p + 1), dict(temperature=p + 2), dict(ws=p + 8), dict(ws=None),
-                dict(n_accepted=p + 2), dict(out_tokens=p + 1), dict(logprob=p + 2), dict(target_stride=1 << 41)):
+                dict(draft=p + 1), dict(dtype=sk.SK_BF16, target=p + 1), dict(tokens=p + 2), dict(uniform=p + 1), dict(temperature=p + 2), dict(ws=q + 8), dict(ws=None),
+                dict(n_accepted=r + 2), dict(out_tokens=r + 65), dict(logprob=r + 130), dict(target_stride=1 << 41),
+                # outputs over inputs, over each other, over the workspace, and that over an input
+                dict(n_accepted=p + 3596), dict(out_tokens=p + 2000), dict(logprob=p), dict(out_tokens=r + 8), dict(logprob=r + 96), dict(n_accepted=q + 16),
+                dict(ws=p + 16), dict(tokens=r + 80), dict(uniform=r + 160), dict(temperature=r)):
         assert call(**bad) == sk.SK_E_INVAL, bad
     assert call(dtype=2) == sk.SK_E_DTYPE
     need = L.sk_verify_workspace_bytes(3, 2, 100)
