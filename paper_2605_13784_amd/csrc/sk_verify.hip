@@ -23,6 +23,8 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kEach = 32, kEachFew = 8;            // logits of a lane; where there are few rows.  A stretch is a wave's, a part a workgroup's
+constexpr int kFirstPlaces = 2;                    // places whose rows come first, where there are many rows
+constexpr int64_t kPartsInTwo = 8192;              // parts of rows from which they do
 constexpr int kMaxRows = 2 * SK_VERIFY_MAX_DRAFT + 1;
 
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
@@ -51,6 +53,8 @@ struct Args {
     Part* part;                                    // [sequence][target rows, then draft rows][part]
     Sum* of_stretch;                               // [sequence][target rows][stretch]
     float* given;                                  // [sequence][rows]: the logit of the row's drafted token
+    int32_t* ended;                                // [sequence]: nothing behind place0 counts (where rows come in two launches)
+    int32_t place0, places, drafts;                // of a launch of rows: its first place, target rows and draft rows of a sequence
     Chosen* chosen;                                // [sequence]
     double* sums;                                  // [sequence][stretch]: of the weights of the drawn row
     int32_t *n_accepted, *out_tokens;
@@ -207,18 +211,19 @@ __global__ __launch_bounds__(kThreads) void sk_verify_rows(const Args A)
 {
     constexpr int EL = F32 ? 4 : 2, N = 16 / EL, P = EACH / N;      // P pieces of 16 bytes
     __shared__ Part of_wave[kWaves];
-    const int part = blockIdx.x % A.parts, row = blockIdx.x / A.parts, seq = row / A.rows, r = row - seq * A.rows;
+    const int part = blockIdx.x % A.parts, row = blockIdx.x / A.parts, rows = A.places + A.drafts, seq = row / rows, of_seq = row - seq * rows;
+    const int place = A.place0 + (of_seq < A.places ? of_seq : of_seq - A.places), r = of_seq < A.places ? place : A.n_draft + 1 + place;
+    if (A.place0 > 0 && A.ended[seq]) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int32_t tokens = token_of_lane(A, seq);
     const int n = drafted(A, tokens);
     bool greedy;
     const double scale = scale_of(A, seq, greedy);
-    if (r <= A.n_draft ? r > n : greedy || r - A.n_draft - 1 >= n) return;
+    if (r <= A.n_draft ? place > n : greedy || place >= n) return;
     const unsigned char* x = row_of(A, seq, r);
     const float none = -__builtin_inff();
     const int stretch = part * kWaves + wave, at0 = stretch * 64 * EACH + lane * N;      // piece i: N logits from at0 + i * 64 * N on
     float v[EACH];
-    const int place = r <= A.n_draft ? r : r - A.n_draft - 1;
     if (place < n) {
         const int32_t t = __builtin_amdgcn_readlane(tokens, place);
         if (t / (64 * EACH) == stretch && lane == 0) A.given[(int64_t)seq * A.rows + r] = logit<F32>(x, t);
@@ -280,7 +285,76 @@ __global__ __launch_bounds__(kThreads) void sk_verify_rows(const Args A)
     }
 }
 
-// ---- second launch: which tokens stay, and the sums of the stretches of the row that is drawn from ----
+// ---- which tokens stay ----
+
+// Whole rows from their parts, which meet in sixteen lanes each: those of the first `places` places (rows that were not computed hold anything, and are
+// not looked at).  sum 0: no probabilities.
+__device__ __forceinline__ void join_rows(const Args& A, const int seq, const int places, const double scale, Part* row)
+{
+    constexpr int kParts = 4;                      // of a lane, asked for at once
+    const int tid = threadIdx.x, n = places + (A.draft ? min(places, A.n_draft) : 0);
+    for (int i = tid >> 4; i < n; i += kThreads / 16) {
+        const int r = i < places ? i : A.n_draft + 1 + i - places;
+        const Part* p = A.part + ((int64_t)seq * A.rows + r) * A.parts;
+        Part o = {0.0, kNoExponent, -__builtin_inff(), INT32_MAX};
+        for (int c0 = tid & 15; c0 < A.parts; c0 += 16 * kParts) {
+            Part y[kParts];
+#pragma unroll
+            for (int j = 0; j < kParts; ++j) y[j] = p[min(c0 + 16 * j, A.parts - 1)];
+#pragma unroll
+            for (int j = 0; j < kParts; ++j) {
+                if (c0 + 16 * j >= A.parts) continue;
+                const double to = __builtin_fmax(o.e, y[j].e);
+                o = Part{at_exponent(o.sum, o.e, to) + at_exponent(y[j].sum, y[j].e, to), to, fmaxf(o.max, y[j].max),
+                         y[j].max > o.max ? y[j].at : y[j].max == o.max ? min(o.at, y[j].at) : o.at};
+            }
+        }
+        const float top = row_max(o.max);
+        const double to = exponent_of(top, scale), sum = row_sum(at_exponent(o.sum, o.e, to));
+        const int at = row_min(o.max == top ? o.at : INT32_MAX);
+        if ((tid & 15) == 0) row[r] = Part{sum > 0.0 ? sum : 0.0, to, top, at};      // (NaN: none)
+    }
+}
+
+// A drafted token's logits in its two rows, and its number, for the lanes of a wave
+__device__ __forceinline__ void given_of(const Args& A, const int seq, const int lane, float& xp, float& xq, float& u)
+{
+    xp = A.given[(int64_t)seq * A.rows + lane];
+    xq = A.draft ? A.given[(int64_t)seq * A.rows + A.n_draft + 1 + lane] : 0.f;
+    u = A.uniform[(int64_t)seq * (A.n_draft + 1) + lane];
+}
+__device__ __forceinline__ bool token_stays(const Args& A, const int place, const int32_t token, const bool greedy, const double scale, const float xp, const float xq,
+                                            const float u, const Part* row)
+{
+    const Part p = row[place];
+    if (!(p.sum > 0.0)) return false;
+    if (greedy) return token == p.at;
+    const double px = weight_of(xp, scale, p.e, p.max) / p.sum;
+    if (!A.draft) return (double)u < px;
+    const Part q = row[A.n_draft + 1 + place];
+    return q.sum > 0.0 && (double)u * (weight_of(xq, scale, q.e, q.max) / q.sum) < px;
+}
+
+// Where rows come in two launches: which sequences' drafts end within the first, for good or by a token that does not stay.
+__global__ __launch_bounds__(kThreads) void sk_verify_ends(const Args A)
+{
+    __shared__ Part row[kMaxRows];
+    const int seq = blockIdx.x, tid = threadIdx.x;
+    bool greedy;
+    const double scale = scale_of(A, seq, greedy);
+    const int32_t token = token_of_lane(A, seq);
+    const int n = min(drafted(A, token), A.place0);
+    float xp = 0.f, xq = 0.f, u = 0.f;
+    if (tid < n) given_of(A, seq, tid, xp, xq, u);
+    join_rows(A, seq, A.place0, scale, row);
+    __syncthreads();
+    if (tid < 64) {
+        const uint64_t out = ~__ballot(tid < n && token_stays(A, tid, token, greedy, scale, xp, xq, u, row));
+        if (tid == 0) A.ended[seq] = (int)__builtin_ctzll(out) < A.place0;
+    }
+}
+
+// ---- second launch: the sums of the stretches of the row that is drawn from ----
 
 // What a logit of the row that is drawn from counts for.
 template <bool F32> struct Weights {
@@ -319,10 +393,10 @@ template <bool F32, int EACH>
 __global__ __launch_bounds__(kThreads) void sk_verify_stretches(const Args A)
 {
     // eight logits to a lane: a workgroup has one stretch, or four
-    constexpr int EL = F32 ? 4 : 2, N = 16 / EL, P = 8 / N, kParts = 4, kOfWg = kThreads * 8 / (64 * EACH);
+    constexpr int EL = F32 ? 4 : 2, N = 16 / EL, P = 8 / N, kOfWg = kThreads * 8 / (64 * EACH);
     static_assert(kOfWg == 1 || kOfWg == kWaves, "");
     __shared__ double of_wave[kWaves];
-    __shared__ Part row[kMaxRows];                 // of whole rows; sum 0: no probabilities
+    __shared__ Part row[kMaxRows];
     __shared__ Chosen chosen;
     const int wgs = A.stretches / kOfWg, wg = blockIdx.x % wgs, seq = blockIdx.x / wgs, tid = threadIdx.x, lane = tid & 63;
     const float none = -__builtin_inff();
@@ -332,50 +406,11 @@ __global__ __launch_bounds__(kThreads) void sk_verify_stretches(const Args A)
     const int n = drafted(A, token);
     // a drafted token's logits, for the lanes of the first wave
     float xp = none, xq = none, u = 0.f;
-    if (tid < n) {
-        xp = A.given[(int64_t)seq * A.rows + lane];
-        if (A.draft) xq = A.given[(int64_t)seq * A.rows + A.n_draft + 1 + lane];
-        u = A.uniform[(int64_t)seq * (A.n_draft + 1) + lane];
-    }
-    // the parts of a row meet in sixteen lanes (rows that were not computed hold anything, and are not looked at)
-    for (int r = tid >> 4; r < A.rows; r += kThreads / 16) {
-        const Part* p = A.part + ((int64_t)seq * A.rows + r) * A.parts;
-        Part o = {0.0, kNoExponent, none, INT32_MAX};
-        for (int c0 = tid & 15; c0 < A.parts; c0 += 16 * kParts) {
-            Part y[kParts];
-#pragma unroll
-            for (int j = 0; j < kParts; ++j) y[j] = p[min(c0 + 16 * j, A.parts - 1)];
-#pragma unroll
-            for (int j = 0; j < kParts; ++j) {
-                if (c0 + 16 * j >= A.parts) continue;
-                const double to = __builtin_fmax(o.e, y[j].e);
-                o = Part{at_exponent(o.sum, o.e, to) + at_exponent(y[j].sum, y[j].e, to), to, fmaxf(o.max, y[j].max),
-                         y[j].max > o.max ? y[j].at : y[j].max == o.max ? min(o.at, y[j].at) : o.at};
-            }
-        }
-        const float top = row_max(o.max);
-        const double to = exponent_of(top, scale), sum = row_sum(at_exponent(o.sum, o.e, to));
-        const int at = row_min(o.max == top ? o.at : INT32_MAX);
-        if ((tid & 15) == 0) row[r] = Part{sum > 0.0 ? sum : 0.0, to, top, at};      // (NaN: none)
-    }
+    if (tid < n) given_of(A, seq, lane, xp, xq, u);
+    join_rows(A, seq, A.n_draft + 1, scale, row);
     __syncthreads();
     if (tid < 64) {
-        bool stays = false;
-        if (lane < n && row[lane].sum > 0.0) {
-            const Part p = row[lane];
-            if (greedy) stays = token == p.at;
-            else {
-                const double px = weight_of(xp, scale, p.e, p.max) / p.sum;
-                double qx = 1.0;
-                bool known = true;
-                if (A.draft) {
-                    const Part q = row[A.n_draft + 1 + lane];
-                    known = q.sum > 0.0;
-                    if (known) qx = weight_of(xq, scale, q.e, q.max) / q.sum;
-                }
-                stays = known && (double)u * qx < px;
-            }
-        }
+        const bool stays = lane < n && token_stays(A, lane, token, greedy, scale, xp, xq, u, row);
         const uint64_t out = ~__ballot(stays);
         const int a = min(n, (int)__builtin_ctzll(out));            // (lanes from n on are out)
         const Part p = row[a];
@@ -561,7 +596,8 @@ size_t lay_out(Args& A, void* workspace, const int32_t n_seq)
     auto take = [&](const int64_t n, const size_t bytes) { const uintptr_t p = at; at += size_t(n) * bytes; return (void*)p; };
     A.part = (Part*)take(parts, sizeof(Part));
     A.of_stretch = (Sum*)take(stretches * (A.n_draft + 1), sizeof(Sum));
-    A.given = (float*)take(((int64_t)n_seq * A.rows + 1) / 2 * 2, sizeof(float));
+    A.given = (float*)take((int64_t)n_seq * A.rows, sizeof(float));
+    A.ended = (int32_t*)take(n_seq + ((n_seq * (int64_t)A.rows + n_seq) & 1), sizeof(int32_t));
     A.chosen = (Chosen*)take(n_seq, sizeof(Chosen));
     A.sums = (double*)take(stretches, sizeof(double));
     return size_t(at - (uintptr_t)workspace);
@@ -629,10 +665,25 @@ int sk_verify(const void* target, int64_t target_stride, const void* draft, int6
     A.n_accepted = n_accepted; A.out_tokens = out_tokens; A.logprob = logprob;
     if ((int64_t)n_seq * A.rows * A.stretches >= (int64_t(1) << 31)) return SK_E_INVAL;
     hipStream_t st = (hipStream_t)hip_stream;
-    const dim3 block(kThreads), first((unsigned)n_seq * A.rows * A.parts), second((unsigned)n_seq * (each == kEach ? A.stretches : A.parts)), third((unsigned)n_seq);
-#define SK_VERIFY(F32, EACH)                                                                    \
-    hipLaunchKernelGGL((sk_verify_rows<F32, EACH>), first, block, 0, st, A);                    \
-    hipLaunchKernelGGL((sk_verify_stretches<F32, EACH>), second, block, 0, st, A);              \
+    const dim3 block(kThreads), second((unsigned)n_seq * (each == kEach ? A.stretches : A.stretches / kWaves)), third((unsigned)n_seq);
+    // Where there are many rows, those of the first two places come first, and the others only of sequences whose draft is still standing.  us per call, all
+    // rows at once -> in two launches, fp32 rows of 128,256 logits with their draft's:
+    //   accepted of the drafted       nearly all        0.7 of them       0.3               0.05
+    //   64 x 4 (9,216 parts)           92 ->  94          80 ->  84        87 ->  75         86 ->  65
+    //   64 x 8 (17,408)               156 -> 171         151 -> 135       159 -> 101        152 ->  70
+    //   32 x 4 (4,608)                 45 ->  54          47 ->  52        51 ->  49         50 ->  39
+    //   64 x 3, bf16 (7,168)           62 ->  70          66 ->  67        72 ->  66         74 ->  60
+    const bool in_two = each == kEach && n_draft > kFirstPlaces && (int64_t)n_seq * A.rows * A.parts >= kPartsInTwo;
+    const int split = in_two ? kFirstPlaces : 0;
+#define SK_VERIFY(F32, EACH)                                                                                                                 \
+    for (int from = 0; from <= n_draft;) {                                                                                                   \
+        const int to = from == 0 && split ? split : n_draft + 1;                                                                             \
+        A.place0 = from; A.places = to - from; A.drafts = !A.draft ? 0 : to <= n_draft ? A.places : A.places - 1;                            \
+        hipLaunchKernelGGL((sk_verify_rows<F32, EACH>), dim3((unsigned)n_seq * (A.places + A.drafts) * A.parts), block, 0, st, A);           \
+        A.place0 = from = to;                                                                                                                \
+        if (to <= n_draft) hipLaunchKernelGGL(sk_verify_ends, third, block, 0, st, A);                                                       \
+    }                                                                                                                                        \
+    hipLaunchKernelGGL((sk_verify_stretches<F32, EACH>), second, block, 0, st, A);                                                           \
     hipLaunchKernelGGL((sk_verify_draw<F32, 64 * EACH>), third, block, 0, st, A)
     if (dtype == SK_F32) {
         if (each == kEach) { SK_VERIFY(true, kEach); } else { SK_VERIFY(true, kEachFew); }

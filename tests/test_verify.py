@@ -242,6 +242,33 @@ def test_rows_that_start_anywhere(dtype, shift, pad):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("drawn", [True, False])
+def test_many_rows_whose_later_places_wait_for_the_first(dtype, drawn):
+    """600 sequences of up to 4 drafted tokens over 16,400 logits: sequences that end at every place, by a token that does not stay, by the draft's end and greedily,
+    some of them in rows without probabilities behind the place where they end (which do not count)."""
+    gen = synth.generator(40)
+    n, k, V = 600, 4, 16400
+    x, y, tokens, u = _case(gen, n, k, V, dtype, near=0.4)
+    for s in range(n):
+        if s % 7 < k:
+            tokens[s, s % 7] = -1
+        if s % 11 == 0:
+            x[s, 3] = float("nan")
+        if s % 13 == 0:
+            y[s, 2] = -float("inf")
+        if s % 17 == 0:
+            x[s, 1] = -float("inf")
+    if not drawn:
+        tokens[:, 0] = torch.where(tokens[:, 0] >= 0, x[:, 0].float().argmax(1).to(torch.int32), tokens[:, 0])
+    temperature = torch.where(torch.arange(n) % 5 == 0, 0.0, 1.0)
+    for s in range(0, n, 10):
+        tokens[s] = torch.nan_to_num(x[s, :k].float(), nan=0.0).argmax(1)
+    accepted = _check(x, tokens, u, draft=y if drawn else None, temperature=temperature)
+    assert set(accepted) == set(range(k + 1))
+
+
+@pytest.mark.gpu
 def test_what_it_draws_has_the_targets_distribution():
     """Frequencies of the first token over 2^17 sequences, for a draft that is far from the target, a looked-up token and none: within 5 deviations."""
     gen = synth.generator(35)
