@@ -150,7 +150,9 @@ template <bool F32> __device__ __forceinline__ Unit<F32> turned(const Unit<F32>&
 // ---- rows beside the cache --------------------------------------------------------------------------
 
 // Workgroup `wg` of those that turn [n_tok][n_heads][D] x into y: a stretch of tokens and HEADS heads, for which a thread forms its
-// sines and cosines once.
+// sines and cosines once.  A thread has eight pairs, both halves of each: nothing is exchanged, and a row is read and written in whole lines.
+// Bound: memory for long calls (4,096 tokens of 32/8 heads of 128: 84 MB in 14.5 us, 5.8 TB/s with the last-level cache's help), the launch and one round trip
+// for short ones (32 tokens: 3.3 us of the device's time, 0.35 of them for the steps, which come with the arguments).
 template <int D, bool F32, int HEADS>
 __device__ __forceinline__ void turn_rows(const sk_rotation& rot, const int32_t* positions, const int32_t pos0, const int n_tok, const int n_heads,
                                           const void* x, void* y, const int wg)
@@ -189,6 +191,8 @@ __global__ __launch_bounds__(256) void sk_turn_rows(const void* q, void* q_out, 
 // ---- the commit, turning on the way -------------------------------------------------------------------
 
 // One (16-token group, KV head) of a commit or staging list, as the plain commit does it but for k.
+// Bound: as above (256 tokens of 32/8 heads of 128: 4.6 us of the device's time, q's rows with them, against 4.8 for the plain commit alone;
+// 4,096: 100 MB in 19 us, 5.3 TB/s).
 template <int D, bool F32>
 __device__ __forceinline__ void commit_group(const sk_geom& g, const sk_rotation& rot, const int32_t* positions, const int32_t pos0, const void* k, const void* v,
                                              const sk_scatter& it, const int head, int32_t* tables_rw, unsigned char* base, uint16_t* vt)
@@ -309,7 +313,10 @@ struct ShiftArgs {
     sk_rotation rot;
 };
 
-// Workgroup (64 tokens, KV head).
+// Workgroup (64 tokens, KV head): K rows are read, turned and written where they lie, or with their whole group, and its V, to the block that
+// replaces theirs.  One difference for all takes one set of sines and cosines a thread; one a row takes one each (some 250 operations, which hide behind the
+// rows' way).  Bound: memory.  131,072 tokens of 8 heads of 128 in a fork's shared blocks: 1.07 GB in 202 us, 5.3 TB/s, what a plain copy
+// reaches; 64 tokens to a workgroup 202 us, 128 211; 2,600 tokens 7.1 and 8.9 us.
 template <int D, bool F32>
 __device__ __forceinline__ void turn_cached(const ShiftArgs& A, const int32_t* list)
 {
@@ -395,17 +402,23 @@ unsigned row_wgs(const sk_geom& g, const int n_tok, const int n_heads, const int
     return unsigned((n_tok + tok - 1) / tok) * unsigned((n_heads + heads - 1) / heads);
 }
 
-// Heads of a thread: four where one each would give more workgroups than the chip holds at once.
-bool four_heads(const sk_geom& g, const int n_tok) { return row_wgs(g, n_tok, g.Hq, 1) >= 2048; }
+// Heads of a thread: two where one each gives more workgroups than the chip runs at a time.  us per call in a stream of them, one head a thread -> two -> four:
+//                          512 tokens          1,024               2,048                4,096                 8,192
+//   bf16 32/8 d 128  rows   5.1 -> 5.2 -> 5.1   6.3 -> 5.6 -> 5.8   9.6 ->  8.0 ->  8.0  16.0 -> 14.5 -> 12.9  27.1 -> 27.1 -> 25.7
+//                  commit   6.4 -> 6.5 -> 6.5   7.3 -> 6.6 -> 6.7  11.4 ->  9.4 -> 10.8  17.9 -> 17.9 -> 19.0  34.2 -> 35.2 -> 36.2
+//   bf16 32/8 d 64 commit   6.4 -> 6.4 -> 6.3   6.6 -> 6.4 -> 6.4   7.4 ->  6.8 ->  6.8  11.6 -> 10.5 -> 10.8  22.3 -> 22.1 -> 24.9
+//   fp32 8/2 d 128 commit   6.3 -> 6.5 -> 6.6   6.4 -> 6.7 -> 6.4   6.5 ->  6.7 ->  7.3  10.4 ->  9.2 -> 11.3  22.0 -> 20.8 -> 25.6
+// (one is kept below for the calls that wait for each other: half the rows to a thread)
+bool two_heads(const sk_geom& g, const int n_tok) { return row_wgs(g, n_tok, g.Hq, 1) >= 1024; }
 
 int launch_rows(const sk_geom& g, const sk_turned& t, const void* q, const void* k, void* k_out, void* stream)
 {
-    const bool four = four_heads(g, t.n_tok);
-    const unsigned q_wgs = q ? row_wgs(g, t.n_tok, g.Hq, four ? 4 : 1) : 0, k_wgs = k ? row_wgs(g, t.n_tok, g.Hkv, four ? 4 : 1) : 0;
+    const bool two = two_heads(g, t.n_tok);
+    const unsigned q_wgs = q ? row_wgs(g, t.n_tok, g.Hq, two ? 2 : 1) : 0, k_wgs = k ? row_wgs(g, t.n_tok, g.Hkv, two ? 2 : 1) : 0;
     if (q_wgs + k_wgs == 0) return 0;
     hipStream_t st = (hipStream_t)stream;
 #define SK_ROWS(D, F32)                                                                                                                        \
-    if (four) hipLaunchKernelGGL((sk_turn_rows<D, F32, 4>), dim3(q_wgs + k_wgs), dim3(256), 0, st, q, t.q_out, g.Hq, k, k_out, g.Hkv, t.positions, t.pos0, t.n_tok, (int)q_wgs, *t.rot); \
+    if (two) hipLaunchKernelGGL((sk_turn_rows<D, F32, 2>), dim3(q_wgs + k_wgs), dim3(256), 0, st, q, t.q_out, g.Hq, k, k_out, g.Hkv, t.positions, t.pos0, t.n_tok, (int)q_wgs, *t.rot); \
     else hipLaunchKernelGGL((sk_turn_rows<D, F32, 1>), dim3(q_wgs + k_wgs), dim3(256), 0, st, q, t.q_out, g.Hq, k, k_out, g.Hkv, t.positions, t.pos0, t.n_tok, (int)q_wgs, *t.rot)
     SK_BY_SHAPE(g, SK_ROWS);
 #undef SK_ROWS
@@ -422,13 +435,13 @@ int launch_commit(const sk_geom& g, const sk_turned& t, const void* k, const voi
     A.commit_wgs = n_items * g.Hkv;
     A.items = items; A.tables_rw = tables_rw; A.kv_rw = kv_rw; A.eph_rw = eph_rw;
     A.rot = *t.rot;
-    const bool four = four_heads(g, t.n_tok);
-    const dim3 grid((unsigned)A.commit_wgs + (t.q ? row_wgs(g, t.n_tok, g.Hq, four ? 4 : 1) : 0)), block(256);
+    const bool two = two_heads(g, t.n_tok);
+    const dim3 grid((unsigned)A.commit_wgs + (t.q ? row_wgs(g, t.n_tok, g.Hq, two ? 2 : 1) : 0)), block(256);
     hipStream_t st = (hipStream_t)stream;
 #define SK_COMMIT(D, F32)                                                                                       \
-    if (to) { if (four) hipLaunchKernelGGL((sk_turn_commit_blocks<D, F32, 4>), grid, block, 0, st, A, *to);     \
+    if (to) { if (two) hipLaunchKernelGGL((sk_turn_commit_blocks<D, F32, 2>), grid, block, 0, st, A, *to);     \
               else hipLaunchKernelGGL((sk_turn_commit_blocks<D, F32, 1>), grid, block, 0, st, A, *to); }        \
-    else if (four) hipLaunchKernelGGL((sk_turn_commit<D, F32, 4>), grid, block, 0, st, A);                      \
+    else if (two) hipLaunchKernelGGL((sk_turn_commit<D, F32, 2>), grid, block, 0, st, A);                      \
     else hipLaunchKernelGGL((sk_turn_commit<D, F32, 1>), grid, block, 0, st, A)
     SK_BY_SHAPE(g, SK_COMMIT);
 #undef SK_COMMIT
