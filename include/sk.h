@@ -247,8 +247,7 @@ int sk_session_truncate(sk_pool* pool, int32_t id, int64_t new_length);
  * of the sliding Region 1); more than the session holds there gives SK_E_INVAL and changes
  * nothing.  Attention then runs over [Region 0 ; what is left of Region 1]; the order of the
  * retained tokens is kept, and sk_session_length / gather / truncate count retained tokens only.
- * Re-encoding positions after an eviction is the caller's concern (as for every K the cache is
- * given).  Metadata only: blocks that hold nothing but evicted tokens return to the free list at
+ * Positions stay what they were: sk_session_shift moves them, where the pool knows the layer's rotation.  Metadata only: blocks that hold nothing but evicted tokens return to the free list at
  * once; evicted tokens that share a block with retained ones stay in kv_mem and are skipped by
  * the kernels.  The only device work is a copy of the moved part of the session's block table,
  * ordered on hip_stream (which must be the stream of the session's other calls).
@@ -289,8 +288,8 @@ int sk_batch_attention_mass(sk_pool* pool, int32_t n_items, const int32_t* sessi
  * any number.  per_head != 0: every KV head by its own row of mass_in, so that token j of the session is another one for each head
  * (their number is the same: the session has one length); per_head == 0: the same tokens for all heads, by the sum of the rows,
  * added in fp32 in the order of the heads.  The others keep their order and move together, K and V bit for bit, in front of
- * them the frozen tokens; sk_session_length falls by n_evict, blocks behind the new end return to the free list, and positions are the
- * caller's concern as for sk_session_evict_oldest.
+ * them the frozen tokens; sk_session_length falls by n_evict, blocks behind the new end return to the free list, and positions stay
+ * what they were as for sk_session_evict_oldest.
  * mass_in, mass_out: DEVICE float [Hkv][stride] as sk_session_attention_mass keeps them (4-byte aligned, strides at least the length).
  * mass_out[g][j] receives the sums of the tokens that stay, in their new places, and 0 in the n_evict places behind the new end.
  * It may be mass_in (same pointer and stride; no other overlap) or NULL (the caller keeps no sums).
@@ -326,7 +325,7 @@ int sk_session_evict_lowest(sk_pool* pool, int32_t id, const float* mass_in, int
  * places in the cache.  q_out [tokens][Hq][d] receives q turned, which is what the call attends with and what
  * sk_session_attention_mass needs afterwards; it may be q (same pointer), and overlaps no other array of the call (SK_E_INVAL).
  *
- * sk_rotate: q and k (either NULL, with its output) into q_out and k_out (which may be k), for sk_session_query and
+ * sk_rotate: q and k (either NULL, with its output; n_tok * Hq at most 2^30) into q_out and k_out (which may be k), for sk_session_query and
  * sk_session_query_shared_prefix, whose arguments they then are.  One kernel; can be captured and replayed, with other contents of q, k, positions too.
  * sk_session_append_rotated: sk_session_append, with k turned on its way into the cache, v bit for bit, q turned into q_out.  q and q_out may be
  * NULL together (and then out): commit only; out may be NULL alone: q is turned, nothing attends.  Otherwise as there.

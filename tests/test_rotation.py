@@ -342,6 +342,45 @@ def test_append_is_a_rotation_and_an_append(layer, block, rotary, interleaved):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("switch", ["SK_FORCE_SIMPLE", "SK_NO_SMALL", "SK_FUSE", "SK_NO_256"])
+@pytest.mark.parametrize("layer", [("bf16", 8, 2, 128), ("bf16", 16, 1, 64)])
+def test_append_whatever_kernel_attends(monkeypatch, switch, layer):
+    monkeypatch.setenv(switch, "1")
+    pools = [_pool(layer, 64, False, n_blocks=200) for _ in range(2)]
+    gen = synth.generator(26)
+    sids = [p.sk_session_create() for p in pools]
+    for T in (1, 20, 150, 400, 7):
+        q, k, v = (x.cuda() for x in _rows(gen, T, layer))
+        got_q, out, lse = pools[0].sk_session_append_rotated(sids[0], q, k, v, pos0=5 * T)
+        want_q, want_k = pools[1].sk_rotate(q, k, pos0=5 * T)
+        want = pools[1].sk_session_append(sids[1], want_q, want_k, v)
+        assert torch.equal(got_q, want_q) and torch.equal(out, want[0]) and torch.equal(lse, want[1])
+        _same(pools[0], sids[0], pools[1], sids[1])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layer", [("bf16", 8, 2, 128), ("f32", 4, 4, 64)])
+def test_an_append_behind_a_shared_last_block(layer):
+    """The session's end lies in a block that a fork holds too: the append takes a copy of its own, and the fork reads what it read."""
+    pool, plain = _pool(layer, 64, False, max_sessions=2), _pool(layer, 64, False, max_sessions=2)
+    gen = synth.generator(27)
+    a, k, v = _cached(pool, gen, 100, layer)
+    fork = pool.sk_session_fork(a, 96)
+    pool.sk_session_truncate(a, 87)
+    ref = plain.sk_session_create()
+    plain.sk_session_append(ref, None, k[:87].cuda(), v[:87].cuda())
+    for T in (1, 50):
+        q, k1, v1 = (x.cuda() for x in _rows(gen, T, layer))
+        got = pool.sk_session_append_rotated(a, q, k1, v1, pos0=3)
+        want_q, want_k = plain.sk_rotate(q, k1, pos0=3)
+        want = plain.sk_session_append(ref, want_q, want_k, v1)
+        assert torch.equal(got[0], want_q) and torch.equal(got[1], want[0]) and torch.equal(got[2], want[1])
+        _same(pool, a, plain, ref)
+        got_k, got_v = (x.cpu() for x in pool.sk_session_gather(fork))
+        assert torch.equal(got_k, k[:96]) and torch.equal(got_v, v[:96])
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_an_append_whose_blocks_take_several_launches(dtype):
     layer, T = (dtype, 2, 1, 64), 9000
