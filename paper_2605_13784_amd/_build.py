@@ -6,7 +6,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libsk.so")
 SOURCES = ["sk_kernels.hip", "sk_top2.hip", "sk_logprobs.hip", "sk_mass.hip", "sk_evict.hip", "sk_rotate.hip", "sk_verify.hip", "sk_probe.hip", "sk_pool.cpp"]
-HEADERS = ["sk_internal.h", "sk_order.h", os.path.join("..", "..", "include", "sk.h")]
+HEADERS = ["sk_internal.h", "sk_order.h", "sk_turn.h", os.path.join("..", "..", "include", "sk.h")]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

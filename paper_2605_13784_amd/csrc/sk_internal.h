@@ -209,6 +209,8 @@ struct sk_turned {
                    int32_t* tables_rw, unsigned char* kv_rw, unsigned char* eph_rw, void* stream);
     int (*blocks)(const sk_geom& g, const sk_turned& t, const void* k, const void* v, const sk_block_list& to,
                   int32_t* tables_rw, unsigned char* kv_rw, void* stream);
+    // the launch that attends, commits and turns at once, for calls that it takes (null: not this one)
+    int (*small)(const sk_launch& L, const sk_commit& C, const sk_turned& t, int32_t n_workgroups, void* stream, void* ev_start, void* ev_stop);
 };
 
 // What an operator in a file of its own needs to know of a pool and one of its sessions (sk_pool.cpp).
@@ -307,6 +309,12 @@ int sk_launch_scatter_args(const sk_geom& g, const void* k, const void* v, const
                            unsigned char* eph_rw, void* stream);
 int sk_launch_attention(const sk_launch& L, int variant, int32_t n_workgroups, void* stream, void* ev_start, void* ev_stop);
 int sk_launch_attention_small(const sk_launch& L, const sk_commit& C, int32_t n_workgroups, void* stream, void* ev_start, void* ev_stop);
+int sk_launch_attention_small_turned(const sk_launch& L, const sk_commit& C, const sk_turned& t, int32_t n_workgroups, void* stream, void* ev_start, void* ev_stop);
+// Which rotations it does: whose pairs a lane holds both elements of; its table has room for 16 tokens.
+static inline bool sk_small_turns(const sk_geom& g, const sk_rotation& r, int64_t n_tok)
+{
+    return g.elem == 2 && n_tok <= 16 && (r.interleaved || r.rotary == g.d || 2 * r.rotary == g.d);
+}
 int sk_launch_combine(const sk_launch& L, int32_t n_row_tiles, int32_t max_parts, int64_t part_stride, void* stream, void* ev_start, void* ev_stop);
 int sk_launch_gather(const sk_geom& g, int32_t tbl_off, int64_t first, int64_t count,
                      void* k_out, void* v_out, void* stream);

@@ -4,7 +4,9 @@
 #include <hip/hip_runtime.h>
 #include <hip/hip_ext.h>
 #include <stdint.h>
+#include <type_traits>
 #include "sk_internal.h"
+#include "sk_turn.h"
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
@@ -1632,6 +1634,14 @@ struct sk_small_args {
     sk_launch P;
     sk_commit C;
 };
+// ... and, behind them, those of the kernel that turns its rows by their positions
+struct sk_small_turn {
+    const int32_t* positions;     // or null: pos0, pos0 + 1, ..
+    void* q_out;
+    int32_t pos0, pad;
+    sk_rotation rot;
+};
+struct sk_small_turned_args { sk_small_args A; sk_small_turn T; };
 // Byte offset at which argument N of a kernel lies in its argument block: each behind the one in front, aligned as its type.
 template <int N, class... A>
 constexpr size_t sk_argument_offset(void (*)(A...))
@@ -1643,11 +1653,14 @@ constexpr size_t sk_argument_offset(void (*)(A...))
 }
 // The first arguments are in registers when a wave starts: what the first loads need (`table`: of the session; `shape`: see
 // sk_launch_attention_small), which go out before the argument block, that nobody has read yet, has arrived.
-template <int D>
-__global__ __launch_bounds__(256, 2) void sk_attn_bf16_small(const int32_t* const table, const unsigned char* const q, const unsigned char* const kv,
-                                                             const uint32_t head_pages, const int32_t Hkv, const uint32_t shape, const uint32_t pad_mul,
-                                                             const uint32_t g_magic, const int32_t n_parts, const int32_t chunk, const int32_t kv_len,
-                                                             const sk_launch, const sk_commit)
+//
+// TURN: q and the call's own k are turned by their positions (sk_turn.h) as they arrive, and q as turned is written out by the workgroups of the first
+// part.  Sines and cosines of the call's tokens, at most 16, are formed once in a workgroup and lie in LDS, in the half of a wave's quarter of the exchange area
+// that the own tokens' values leave free; all that happens while the first keys are on their way.
+template <int D, bool TURN>
+__device__ __forceinline__ void sk_attn_small_body(const int32_t* const table, const unsigned char* const q, const unsigned char* const kv,
+                                                   const uint32_t head_pages, const int32_t Hkv, const uint32_t shape, const uint32_t pad_mul,
+                                                   const uint32_t g_magic, const int32_t n_parts, const int32_t chunk, const int32_t kv_len)
 {
     constexpr int NKS = D / 16, NMT = D / 32, NWV = 4, CPR = D / 4;      // CPR: float4 chunks of an output row
     constexpr int ROWB = D * 2, LOG2_TOK_BYTES = D == 128 ? 8 : 7;
@@ -1664,7 +1677,10 @@ __global__ __launch_bounds__(256, 2) void sk_attn_bf16_small(const int32_t* cons
         typedef const __attribute__((address_space(4))) unsigned char* args_ptr;
         const sk_commit& C = *(const sk_commit*)((args_ptr)__builtin_amdgcn_kernarg_segment_ptr() + offsetof(sk_small_args, C));
         const int i = blockIdx.x - C.first_wg, item = sk_divide(i, P.by_heads);
-        sk_commit_group<D>(P.g, P.own_k, P.own_v, C.item[item], i - item * Hkv, C.tables_rw, C.kv_rw, (uint16_t*)&tr[0][0][0]);
+        if constexpr (TURN) {
+            const sk_small_turn& T = *(const sk_small_turn*)((args_ptr)__builtin_amdgcn_kernarg_segment_ptr() + offsetof(sk_small_turned_args, T));
+            sk_turn::commit_group<D, false>(P.g, T.rot, T.positions, T.pos0, P.own_k, P.own_v, C.item[item], i - item * Hkv, C.tables_rw, C.kv_rw, (uint16_t*)&tr[0][0][0]);
+        } else sk_commit_group<D>(P.g, P.own_k, P.own_v, C.item[item], i - item * Hkv, C.tables_rw, C.kv_rw, (uint16_t*)&tr[0][0][0]);
         return;
     }
     if (head >= Hkv) return;
@@ -1729,6 +1745,71 @@ __global__ __launch_bounds__(256, 2) void sk_attn_bf16_small(const int32_t* cons
         sk_touch_arguments<offsetof(sk_small_args, C)>();
         const sk_launch P = sk_late_argument<sk_launch, offsetof(sk_small_args, P)>();
         const float c_scale = P.g.scale_log2e;
+
+        // Rows as this kernel's lanes hold them (piece ks: 8 elements from dimension 16 ks + 8 kg on), turned by what the table holds for a token.
+        auto trig = [&](const int token, const int pair) __attribute__((always_inline)) -> const float4* {
+            return (const float4*)((const unsigned char*)&tr[n_cached & (NWV - 1)][0][0] + 32 * ROWB) + (token * (D / 2) + pair) / 2;
+        };
+        auto turn = [&](auto (&x)[NKS], const int token) __attribute__((always_inline)) {
+            typedef const __attribute__((address_space(4))) unsigned char* args_ptr;
+            const sk_small_turn& T = *(const sk_small_turn*)((args_ptr)__builtin_amdgcn_kernarg_segment_ptr() + offsetof(sk_small_turned_args, T));
+            typedef std::remove_reference_t<decltype(x[0])> piece;
+            auto halves = [&](const auto apart) __attribute__((always_inline)) {
+                constexpr int A = decltype(apart)::value;
+#pragma unroll
+                for (int ks = 0; ks < A; ++ks) {
+                    sk_turn::Unit<false> u;
+                    u.x[0] = __builtin_bit_cast(sk_turn::u32x4, x[ks]); u.x[1] = __builtin_bit_cast(sk_turn::u32x4, x[ks + A]);
+                    sk_turn::Turn t;
+                    const float4* cs = trig(token, 16 * ks + 8 * kg);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) { const float4 y = cs[i]; t.c[2 * i] = y.x; t.s[2 * i] = y.y; t.c[2 * i + 1] = y.z; t.s[2 * i + 1] = y.w; }
+                    u = sk_turn::turned<false>(u, t, false);
+                    x[ks] = __builtin_bit_cast(piece, u.x[0]); x[ks + A] = __builtin_bit_cast(piece, u.x[1]);
+                }
+            };
+            if (!T.rot.interleaved) {
+                if (T.rot.rotary == D) halves(sk_int<NKS / 2>{});
+                else halves(sk_int<NKS / 4>{});
+            } else {
+#pragma unroll
+                for (int ks = 0; ks < NKS; ks += 2) {         // two pieces: eight pairs
+                    sk_turn::Unit<false> u;
+                    u.x[0] = __builtin_bit_cast(sk_turn::u32x4, x[ks]); u.x[1] = __builtin_bit_cast(sk_turn::u32x4, x[ks + 1]);
+                    sk_turn::Turn t;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const float4* cs = trig(token, 8 * (ks + h) + 4 * kg);
+                        const float4 y = cs[0], z = cs[1];
+                        t.c[4 * h] = y.x; t.s[4 * h] = y.y; t.c[4 * h + 1] = y.z; t.s[4 * h + 1] = y.w;
+                        t.c[4 * h + 2] = z.x; t.s[4 * h + 2] = z.y; t.c[4 * h + 3] = z.z; t.s[4 * h + 3] = z.w;
+                    }
+                    u = sk_turn::turned<false>(u, t, true);
+                    if (16 * ks < T.rot.rotary) x[ks] = __builtin_bit_cast(piece, u.x[0]);
+                    if (16 * ks + 16 < T.rot.rotary) x[ks + 1] = __builtin_bit_cast(piece, u.x[1]);
+                }
+            }
+        };
+        if constexpr (TURN) {
+            typedef const __attribute__((address_space(4))) unsigned char* args_ptr;
+            const sk_small_turn& T = *(const sk_small_turn*)((args_ptr)__builtin_amdgcn_kernarg_segment_ptr() + offsetof(sk_small_turned_args, T));
+            if (alone) sk_lds_barrier();                      // (a second time round: the exchange area has been read)
+            float2* table_at = (float2*)trig(0, 0);
+            for (int t = wave; t < n_tok; t += NWV)
+                if (lane < T.rot.rotary / 2) {
+                    const int32_t position = T.positions ? T.positions[t] : T.pos0 + t;
+                    const sk_turn::f32x2 cs = sk_turn::cos_sin(sk_turn::phase_of(position, T.rot.step[lane]));
+                    table_at[t * (D / 2) + lane] = make_float2(cs.x * T.rot.factor, cs.y * T.rot.factor);
+                }
+            sk_lds_barrier();
+            turn(qreg, tok);
+            sk_lds_barrier();                                 // (a wave that has nothing to do writes to its quarter at once)
+            if (part == 0 && wave == 0 && r < nrows) {
+                sk_u32x4* to = (sk_u32x4*)((unsigned char*)T.q_out + ((size_t)tok * (Hkv * G) + hq) * ROWB);
+#pragma unroll
+                for (int ks = 0; ks < NKS; ++ks) to[ks * 2 + kg] = __builtin_bit_cast(sk_u32x4, qreg[ks]);
+            }
+        }
 
         f32x16 oacc[NMT];
 #pragma unroll
@@ -1841,6 +1922,7 @@ __global__ __launch_bounds__(256, 2) void sk_attn_bf16_small(const int32_t* cons
                 if (vkey < own_cnt) x = *(const uint4*)((const unsigned char*)P.own_v + ((size_t)vkey * Hkv + head) * ROWB + cc * 16);
                 rows[c] = x;
             }
+            if constexpr (TURN) turn(ka, key);
             scores();
             mask(0, P.pos0 < SK_NO_CAUSAL ? tok : own_cnt - 1, 0, 0);
             softmax();
@@ -1878,6 +1960,23 @@ __global__ __launch_bounds__(256, 2) void sk_attn_bf16_small(const int32_t* cons
         part = alone ? part + 1 : 0;
         alone = true;
     }
+}
+
+template <int D>
+__global__ __launch_bounds__(256, 2) void sk_attn_bf16_small(const int32_t* const table, const unsigned char* const q, const unsigned char* const kv,
+                                                             const uint32_t head_pages, const int32_t Hkv, const uint32_t shape, const uint32_t pad_mul,
+                                                             const uint32_t g_magic, const int32_t n_parts, const int32_t chunk, const int32_t kv_len,
+                                                             const sk_launch, const sk_commit)
+{
+    sk_attn_small_body<D, false>(table, q, kv, head_pages, Hkv, shape, pad_mul, g_magic, n_parts, chunk, kv_len);
+}
+template <int D>
+__global__ __launch_bounds__(256, 2) void sk_turned_small(const int32_t* const table, const unsigned char* const q, const unsigned char* const kv,
+                                                          const uint32_t head_pages, const int32_t Hkv, const uint32_t shape, const uint32_t pad_mul,
+                                                          const uint32_t g_magic, const int32_t n_parts, const int32_t chunk, const int32_t kv_len,
+                                                          const sk_launch, const sk_commit, const sk_small_turn)
+{
+    sk_attn_small_body<D, true>(table, q, kv, head_pages, Hkv, shape, pad_mul, g_magic, n_parts, chunk, kv_len);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -2535,7 +2634,7 @@ int sk_launch_attention(const sk_launch& L, int variant, int32_t n_workgroups, v
 
 // The kernels that can read the call's own K/V in place and commit them: sk_attn_bf16_small, and sk_attn_f32 (every call
 // of an fp32 pool; a batched one with own_mode none and nothing to commit).
-int sk_launch_attention_small(const sk_launch& L, const sk_commit& C, int32_t n_workgroups, void* stream, void* ev_start, void* ev_stop)
+static int sk_small_launch(const sk_launch& L, const sk_commit& C, const sk_turned* turned, int32_t n_workgroups, void* stream, void* ev_start, void* ev_stop)
 {
     if (n_workgroups <= 0) return 0;
     hipStream_t st = (hipStream_t)stream;
@@ -2545,6 +2644,7 @@ int sk_launch_attention_small(const sk_launch& L, const sk_commit& C, int32_t n_
         else hipLaunchKernelGGL(kernel, dim3(n_workgroups), dim3(256), 0, st, __VA_ARGS__);                         \
     } while (0)
     if (L.g.elem == 4) {
+        if (turned) return (int)hipErrorInvalidValue;
         if (L.g.d == 128) SK_LAUNCH_SMALL(sk_attn_f32<128>, L, C);
         else if (L.g.d == 64) SK_LAUNCH_SMALL(sk_attn_f32<64>, L, C);
         else return (int)hipErrorInvalidValue;
@@ -2565,12 +2665,32 @@ int sk_launch_attention_small(const sk_launch& L, const sk_commit& C, int32_t n_
     static_assert(sk_argument_offset<11>(kernel) == offsetof(sk_small_args, P) && sk_argument_offset<12>(kernel) == offsetof(sk_small_args, C) &&
                   sk_argument_offset<6>(kernel) == offsetof(sk_small_args, pad_mul), "the kernel reads its arguments through sk_small_args");
 #define SK_SMALL_ARGS table, q, L.g.kv, pages, L.g.Hkv, shape, L.by_pad.mul, L.g.g_magic, L.n_splits, L.chunk, L.kv_len, L, C
+    if (turned) {
+        constexpr void (*kernel)(const int32_t*, const unsigned char*, const unsigned char*, uint32_t, int32_t, uint32_t, uint32_t, uint32_t, int32_t, int32_t,
+                                 int32_t, sk_launch, sk_commit, sk_small_turn) = sk_turned_small<128>;
+        static_assert(sk_argument_offset<11>(kernel) == offsetof(sk_small_args, P) && sk_argument_offset<12>(kernel) == offsetof(sk_small_args, C) &&
+                      sk_argument_offset<13>(kernel) == offsetof(sk_small_turned_args, T), "the kernel reads its arguments through sk_small_turned_args");
+        if (!sk_small_turns(L.g, *turned->rot, L.n_tok) || L.own_cnt != L.n_tok) return (int)hipErrorInvalidValue;
+        const sk_small_turn T = {turned->positions, turned->q_out, turned->pos0, 0, *turned->rot};
+        if (L.g.d == 128) SK_LAUNCH_SMALL(sk_turned_small<128>, SK_SMALL_ARGS, T);
+        else if (L.g.d == 64) SK_LAUNCH_SMALL(sk_turned_small<64>, SK_SMALL_ARGS, T);
+        else return (int)hipErrorInvalidValue;
+        return (int)hipGetLastError();
+    }
     if (L.g.d == 128) SK_LAUNCH_SMALL(sk_attn_bf16_small<128>, SK_SMALL_ARGS);
     else if (L.g.d == 64) SK_LAUNCH_SMALL(sk_attn_bf16_small<64>, SK_SMALL_ARGS);
     else return (int)hipErrorInvalidValue;
 #undef SK_SMALL_ARGS
 #undef SK_LAUNCH_SMALL
     return (int)hipGetLastError();
+}
+int sk_launch_attention_small(const sk_launch& L, const sk_commit& C, int32_t n_workgroups, void* stream, void* ev_start, void* ev_stop)
+{
+    return sk_small_launch(L, C, nullptr, n_workgroups, stream, ev_start, ev_stop);
+}
+int sk_launch_attention_small_turned(const sk_launch& L, const sk_commit& C, const sk_turned& t, int32_t n_workgroups, void* stream, void* ev_start, void* ev_stop)
+{
+    return sk_small_launch(L, C, &t, n_workgroups, stream, ev_start, ev_stop);
 }
 
 // max_parts: the most parts of a row tile of the launch; part_stride: slots from one part to the next.

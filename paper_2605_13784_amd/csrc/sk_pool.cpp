@@ -325,6 +325,7 @@ struct RegPlan {
     const void *own_k = nullptr, *own_v = nullptr;     // SMALL: the call's own K/V
     sk_commit commit;                                  // SMALL: what an append commits in the same launch
     int32_t commit_items = 0;
+    const sk_turned* turned = nullptr;                 // SMALL: the launch turns its rows itself
     bool enqueued = false;                             // set by launch_regular once the attention kernel is on the stream
 };
 
@@ -854,7 +855,8 @@ int launch_regular(sk_pool* p, RegPlan& R, const void* q, void* out, int out_dty
         R.commit.first_wg = R.commit_items > 0 ? R.wgs : INT32_MAX;
         R.commit.tables_rw = (int32_t*)((unsigned char*)p->d.workspace + p->L.off_tables);
         R.commit.kv_rw = (unsigned char*)p->d.kv_mem;
-        e = sk_launch_attention_small(R.L, R.commit, R.wgs + R.commit_items * p->d.n_kv_heads, st, e0, e1);
+        const int32_t wgs = R.wgs + R.commit_items * p->d.n_kv_heads;
+        e = R.turned ? R.turned->small(R.L, R.commit, *R.turned, wgs, st, e0, e1) : sk_launch_attention_small(R.L, R.commit, wgs, st, e0, e1);
     } else e = sk_launch_attention(R.L, R.v.id, R.wgs, st, e0, e1);
     if (e) { g_last_hip = e; return SK_E_HIP; }
     p->stats.launches++;
@@ -1010,6 +1012,13 @@ bool results_over_own(const sk_pool* p, int64_t T, const void* k, const void* v,
     const size_t kv = size_t(T) * p->d.n_kv_heads * p->d.head_dim * p->L.elem, rows = size_t(T) * p->d.n_q_heads;
     const size_t n_out = rows * p->d.head_dim * (out_dtype == SK_F32 ? 4 : 2);
     return overlap(out, n_out, k, kv) || overlap(out, n_out, v, kv) || overlap(lse, rows * 4, k, kv) || overlap(lse, rows * 4, v, kv);
+}
+
+// ... or over its q or positions.
+bool over_inputs(const sk_pool* p, int64_t T, const void* q, const int32_t* positions, const void* out, int out_dtype, const float* lse)
+{
+    const size_t rows = size_t(T) * p->d.n_q_heads, n_q = rows * p->d.head_dim * p->L.elem, n_out = rows * p->d.head_dim * (out_dtype == SK_F32 ? 4 : 2);
+    return overlap(out, n_out, q, n_q) || overlap(lse, rows * 4, q, n_q) || overlap(out, n_out, positions, size_t(T) * 4) || overlap(lse, rows * 4, positions, size_t(T) * 4);
 }
 
 // Turns a call's q and k, k into the staging area, in a launch of its own.
@@ -1758,9 +1767,13 @@ static int append(sk_pool* p, int32_t id, const void* q, const void* k, const vo
     const bool in_place = attend && plan.L.own_mode != SK_OWN_NONE;
     const bool one_launch = in_place && scatter_groups(n, L) <= SK_COMMIT_ITEMS;      // the attention launch commits too
     const bool commits_turned = turned && !in_place;
+    // A short call's launch turns the rows as well, where nothing that it writes is read by another of its workgroups.  One token at 2,600 cached, 32/8 heads of
+    // 128 dims: TURNED_FIGURES
+    const bool turns_inside = turned && one_launch && plan.v.id == SK_KV_SMALL && turned->small && turned->q != turned->q_out &&
+                              !over_inputs(p, L, q, turned->positions, out, out_dtype, lse);
     ScatterSlot ss;
     if (!commits_turned) { int rc = scatter_reserve(p, scatter_groups(n, L), ss); if (rc) return rc; }
-    if (in_place && turned) {                   // the launches behind find k turned in the staging area
+    if (in_place && turned && !turns_inside) {  // the launches behind find k turned in the staging area
         const size_t bytes = size_t(L) * p->d.n_kv_heads * p->d.head_dim * p->L.elem;
         unsigned char* to = p->device ? (unsigned char*)p->d.workspace + p->L.off_eph : nullptr;
         int rc = turn_rows(p, *turned, k, to, st);
@@ -1789,7 +1802,8 @@ static int append(sk_pool* p, int32_t id, const void* q, const void* k, const vo
     else rc = scatter_launch(p, ss, items, k, v, st);
     if (rc) { rollback(p, u, committing); return rc; }
     if (attend) {
-        rc = launch_regular(p, plan, turned ? turned->q_out : q, out, out_dtype, lse, st);
+        plan.turned = turns_inside ? turned : nullptr;
+        rc = launch_regular(p, plan, turned && !turns_inside ? turned->q_out : q, out, out_dtype, lse, st);
         if (rc) { rollback(p, u, !one_launch || plan.enqueued); return rc; }
     }
     p->stats.tokens_appended += L;

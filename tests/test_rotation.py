@@ -359,6 +359,43 @@ def test_append_whatever_kernel_attends(monkeypatch, switch, layer):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("distrust", ["0", "1"])
+@pytest.mark.parametrize("layer", [("bf16", 8, 8, 128), ("bf16", 8, 2, 64), ("bf16", 32, 8, 128), ("bf16", 7, 1, 128), ("bf16", 32, 1, 64)])
+@pytest.mark.parametrize("rotary,interleaved", [(128, False), (64, False), (32, False), (128, True), (48, True), (16, True)])
+def test_short_appends_whose_attention_turns_them(monkeypatch, distrust, layer, rotary, interleaved):
+    """Up to 16 tokens and 32 rows a KV head: one launch, as far as its lanes hold both elements of a pair.  Sessions of no tokens, of a few, of several parts,
+    with evicted ones; also with the last workgroup computing every part again."""
+    monkeypatch.setenv("SK_SMALL_DISTRUST", distrust)
+    rotary = min(rotary, layer[3])
+    pools = [_pool(layer, rotary, interleaved, n_blocks=400, max_sessions=1, factor=1.125) for _ in range(2)]
+    gen = synth.generator(28, stream=rotary + layer[1])
+    sids = [p.sk_session_create() for p in pools]
+    G = layer[1] // layer[2]
+    for n in (0, 5, 33, 700, 4000):
+        for T in sorted({1, 2, min(16, 32 // G), min(17, max(1, 32 // G)), min(32, max(1, 32 // G))}):
+            q, k, v = (x.cuda() for x in _rows(gen, T, layer))
+            positions = torch.randint(-5, 1 << 20, (T,), generator=gen, dtype=torch.int32).cuda() if T % 2 else None
+            before = pools[0].sk_pool_get_stats()["launches"]
+            got_q, out, lse = pools[0].sk_session_append_rotated(sids[0], q, k, v, positions=positions, pos0=n)
+            launches = pools[0].sk_pool_get_stats()["launches"] - before - (not pools[0].sk_pool_last_launch()["fused_merge"] and pools[0].sk_pool_last_launch()["n_splits"] > 1)
+            inside = T <= 16 and T * G <= 32 and (interleaved or rotary in (layer[3], layer[3] // 2))
+            assert launches == (1 if inside else 2)
+            want_q, want_k = pools[1].sk_rotate(q, k, positions=positions, pos0=n)
+            want, want_lse = pools[1].sk_session_append(sids[1], want_q, want_k, v)
+            assert torch.equal(got_q, want_q) and torch.equal(out, want) and torch.equal(lse, want_lse), (n, T)
+            _same(pools[0], sids[0], pools[1], sids[1])
+        if n == 33:
+            for p, s in zip(pools, sids):
+                p.sk_session_freeze(s, 3)
+                p.sk_session_evict_oldest(s, 9)
+        grow = max(0, n * 2 - pools[0].sk_session_length(sids[0]))
+        if grow:
+            _, k, v = (x.cuda() for x in _rows(gen, min(grow, 4000), layer))
+            for p, s in zip(pools, sids):
+                p.sk_session_append(s, None, k, v)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("layer", [("bf16", 8, 2, 128), ("f32", 4, 4, 64)])
 def test_an_append_behind_a_shared_last_block(layer):
     """The session's end lies in a block that a fork holds too: the append takes a copy of its own, and the fork reads what it read."""
