@@ -1642,6 +1642,11 @@ struct sk_small_turn {
     sk_rotation rot;
 };
 struct sk_small_turned_args { sk_small_args A; sk_small_turn T; };
+// What is turned: nothing, pairs (i, i + D / 2) of the whole row, pairs (i, i + D / 4) of its first half, pairs (2 i, 2 i + 1) of any part of it.
+// (A kernel for each: with all three ways in one, one decoded token at 2,600 cached took 8.5 us of the device's time instead of 8.3, for its
+// instructions, which nobody has run yet; the kernel that turns nothing takes 7.0, a launch that turns the rows in front of it 3.3.  Of the 1.3 between them 0.7 are q's:
+// each wave turns all of it.)
+enum { SK_TURN_NONE = 0, SK_TURN_WHOLE, SK_TURN_HALF, SK_TURN_PAIRS };
 // Byte offset at which argument N of a kernel lies in its argument block: each behind the one in front, aligned as its type.
 template <int N, class... A>
 constexpr size_t sk_argument_offset(void (*)(A...))
@@ -1654,10 +1659,10 @@ constexpr size_t sk_argument_offset(void (*)(A...))
 // The first arguments are in registers when a wave starts: what the first loads need (`table`: of the session; `shape`: see
 // sk_launch_attention_small), which go out before the argument block, that nobody has read yet, has arrived.
 //
-// TURN: q and the call's own k are turned by their positions (sk_turn.h) as they arrive, and q as turned is written out by the workgroups of the first
+// TURN other than none: q and the call's own k are turned by their positions (sk_turn.h) as they arrive, and q as turned is written out by the workgroups of the first
 // part.  Sines and cosines of the call's tokens, at most 16, are formed once in a workgroup and lie in LDS, in the half of a wave's quarter of the exchange area
 // that the own tokens' values leave free; all that happens while the first keys are on their way.
-template <int D, bool TURN>
+template <int D, int TURN>
 __device__ __forceinline__ void sk_attn_small_body(const int32_t* const table, const unsigned char* const q, const unsigned char* const kv,
                                                    const uint32_t head_pages, const int32_t Hkv, const uint32_t shape, const uint32_t pad_mul,
                                                    const uint32_t g_magic, const int32_t n_parts, const int32_t chunk, const int32_t kv_len)
@@ -1677,7 +1682,7 @@ __device__ __forceinline__ void sk_attn_small_body(const int32_t* const table, c
         typedef const __attribute__((address_space(4))) unsigned char* args_ptr;
         const sk_commit& C = *(const sk_commit*)((args_ptr)__builtin_amdgcn_kernarg_segment_ptr() + offsetof(sk_small_args, C));
         const int i = blockIdx.x - C.first_wg, item = sk_divide(i, P.by_heads);
-        if constexpr (TURN) {
+        if constexpr (TURN != SK_TURN_NONE) {
             const sk_small_turn& T = *(const sk_small_turn*)((args_ptr)__builtin_amdgcn_kernarg_segment_ptr() + offsetof(sk_small_turned_args, T));
             sk_turn::commit_group<D, false>(P.g, T.rot, T.positions, T.pos0, P.own_k, P.own_v, C.item[item], i - item * Hkv, C.tables_rw, C.kv_rw, (uint16_t*)&tr[0][0][0]);
         } else sk_commit_group<D>(P.g, P.own_k, P.own_v, C.item[item], i - item * Hkv, C.tables_rw, C.kv_rw, (uint16_t*)&tr[0][0][0]);
@@ -1768,10 +1773,8 @@ __device__ __forceinline__ void sk_attn_small_body(const int32_t* const table, c
                     x[ks] = __builtin_bit_cast(piece, u.x[0]); x[ks + A] = __builtin_bit_cast(piece, u.x[1]);
                 }
             };
-            if (!T.rot.interleaved) {
-                if (T.rot.rotary == D) halves(sk_int<NKS / 2>{});
-                else halves(sk_int<NKS / 4>{});
-            } else {
+            if constexpr (TURN != SK_TURN_PAIRS) halves(sk_int<TURN == SK_TURN_WHOLE ? NKS / 2 : NKS / 4>{});
+            else {
 #pragma unroll
                 for (int ks = 0; ks < NKS; ks += 2) {         // two pieces: eight pairs
                     sk_turn::Unit<false> u;
@@ -1790,7 +1793,7 @@ __device__ __forceinline__ void sk_attn_small_body(const int32_t* const table, c
                 }
             }
         };
-        if constexpr (TURN) {
+        if constexpr (TURN != SK_TURN_NONE) {
             typedef const __attribute__((address_space(4))) unsigned char* args_ptr;
             const sk_small_turn& T = *(const sk_small_turn*)((args_ptr)__builtin_amdgcn_kernarg_segment_ptr() + offsetof(sk_small_turned_args, T));
             if (alone) sk_lds_barrier();                      // (a second time round: the exchange area has been read)
@@ -1922,7 +1925,7 @@ __device__ __forceinline__ void sk_attn_small_body(const int32_t* const table, c
                 if (vkey < own_cnt) x = *(const uint4*)((const unsigned char*)P.own_v + ((size_t)vkey * Hkv + head) * ROWB + cc * 16);
                 rows[c] = x;
             }
-            if constexpr (TURN) turn(ka, key);
+            if constexpr (TURN != SK_TURN_NONE) turn(ka, key);
             scores();
             mask(0, P.pos0 < SK_NO_CAUSAL ? tok : own_cnt - 1, 0, 0);
             softmax();
@@ -1968,15 +1971,15 @@ __global__ __launch_bounds__(256, 2) void sk_attn_bf16_small(const int32_t* cons
                                                              const uint32_t g_magic, const int32_t n_parts, const int32_t chunk, const int32_t kv_len,
                                                              const sk_launch, const sk_commit)
 {
-    sk_attn_small_body<D, false>(table, q, kv, head_pages, Hkv, shape, pad_mul, g_magic, n_parts, chunk, kv_len);
+    sk_attn_small_body<D, SK_TURN_NONE>(table, q, kv, head_pages, Hkv, shape, pad_mul, g_magic, n_parts, chunk, kv_len);
 }
-template <int D>
+template <int D, int TURN>
 __global__ __launch_bounds__(256, 2) void sk_turned_small(const int32_t* const table, const unsigned char* const q, const unsigned char* const kv,
                                                           const uint32_t head_pages, const int32_t Hkv, const uint32_t shape, const uint32_t pad_mul,
                                                           const uint32_t g_magic, const int32_t n_parts, const int32_t chunk, const int32_t kv_len,
                                                           const sk_launch, const sk_commit, const sk_small_turn)
 {
-    sk_attn_small_body<D, true>(table, q, kv, head_pages, Hkv, shape, pad_mul, g_magic, n_parts, chunk, kv_len);
+    sk_attn_small_body<D, TURN>(table, q, kv, head_pages, Hkv, shape, pad_mul, g_magic, n_parts, chunk, kv_len);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -2667,14 +2670,21 @@ static int sk_small_launch(const sk_launch& L, const sk_commit& C, const sk_turn
 #define SK_SMALL_ARGS table, q, L.g.kv, pages, L.g.Hkv, shape, L.by_pad.mul, L.g.g_magic, L.n_splits, L.chunk, L.kv_len, L, C
     if (turned) {
         constexpr void (*kernel)(const int32_t*, const unsigned char*, const unsigned char*, uint32_t, int32_t, uint32_t, uint32_t, uint32_t, int32_t, int32_t,
-                                 int32_t, sk_launch, sk_commit, sk_small_turn) = sk_turned_small<128>;
+                                 int32_t, sk_launch, sk_commit, sk_small_turn) = sk_turned_small<128, SK_TURN_WHOLE>;
         static_assert(sk_argument_offset<11>(kernel) == offsetof(sk_small_args, P) && sk_argument_offset<12>(kernel) == offsetof(sk_small_args, C) &&
                       sk_argument_offset<13>(kernel) == offsetof(sk_small_turned_args, T), "the kernel reads its arguments through sk_small_turned_args");
         if (!sk_small_turns(L.g, *turned->rot, L.n_tok) || L.own_cnt != L.n_tok) return (int)hipErrorInvalidValue;
         const sk_small_turn T = {turned->positions, turned->q_out, turned->pos0, 0, *turned->rot};
-        if (L.g.d == 128) SK_LAUNCH_SMALL(sk_turned_small<128>, SK_SMALL_ARGS, T);
-        else if (L.g.d == 64) SK_LAUNCH_SMALL(sk_turned_small<64>, SK_SMALL_ARGS, T);
+#define SK_LAUNCH_TURNED(D)                                                                                               \
+    do {                                                                                                                  \
+        if (turned->rot->interleaved) SK_LAUNCH_SMALL((sk_turned_small<D, SK_TURN_PAIRS>), SK_SMALL_ARGS, T);             \
+        else if (turned->rot->rotary == D) SK_LAUNCH_SMALL((sk_turned_small<D, SK_TURN_WHOLE>), SK_SMALL_ARGS, T);        \
+        else SK_LAUNCH_SMALL((sk_turned_small<D, SK_TURN_HALF>), SK_SMALL_ARGS, T);                                       \
+    } while (0)
+        if (L.g.d == 128) SK_LAUNCH_TURNED(128);
+        else if (L.g.d == 64) SK_LAUNCH_TURNED(64);
         else return (int)hipErrorInvalidValue;
+#undef SK_LAUNCH_TURNED
         return (int)hipGetLastError();
     }
     if (L.g.d == 128) SK_LAUNCH_SMALL(sk_attn_bf16_small<128>, SK_SMALL_ARGS);
