@@ -325,7 +325,7 @@ int sk_session_evict_lowest(sk_pool* pool, int32_t id, const float* mass_in, int
  * places in the cache.  q_out [tokens][Hq][d] receives q turned, which is what the call attends with and what
  * sk_session_attention_mass needs afterwards; it may be q (same pointer), and overlaps no other array of the call (SK_E_INVAL).
  *
- * sk_rotate: q and k (either NULL, with its output; n_tok * Hq at most 2^30) into q_out and k_out (which may be k), for sk_session_query and
+ * sk_rotate: q and k (either NULL, with its output; n_tok * Hq at most 2^27) into q_out and k_out (which may be k), for sk_session_query and
  * sk_session_query_shared_prefix, whose arguments they then are.  One kernel; can be captured and replayed, with other contents of q, k, positions too.
  * sk_session_append_rotated: sk_session_append, with k turned on its way into the cache, v bit for bit, q turned into q_out.  q and q_out may be
  * NULL together (and then out): commit only; out may be NULL alone: q is turned, nothing attends.  Otherwise as there.

@@ -309,11 +309,12 @@ int sk_rotate(sk_pool* p, const void* q, const void* k, int32_t n_tok, const int
     if (!p || !sk_rotation_of(p)->rotary || n_tok < 0) return SK_E_INVAL;
     if (n_tok == 0) return SK_OK;
     sk_geom g;
-    if (!sk_geom_of(p, &g)) return SK_E_NODEVICE;
+    const bool device = sk_geom_of(p, &g);
+    if ((int64_t)n_tok * g.Hq > (int64_t(1) << 27)) return SK_E_INVAL;      // (a grid has fewer than 2^32 threads)
+    if (!device) return SK_E_NODEVICE;
     if ((!q && !k) || (!q) != (!q_out) || (!k) != (!k_out)) return SK_E_INVAL;
     if (!aligned(q, 16) || !aligned(k, 16) || !aligned(q_out, 16) || !aligned(k_out, 16) || !aligned(positions, 4)) return SK_E_INVAL;
     if (!positions && pos0 > INT32_MAX - (n_tok - 1)) return SK_E_INVAL;
-    if ((int64_t)n_tok * g.Hq > (int64_t(1) << 30)) return SK_E_INVAL;
     const sk_turned t = make_turned(g, sk_rotation_of(p), q, q_out, positions, pos0, n_tok);
     if (!sk_turned_apart(g, t, n_tok, k, nullptr, k_out, nullptr, SK_F32, nullptr)) return SK_E_INVAL;
     if (sk_injected(p, SK_SITE_SCATTER)) return SK_E_HIP;

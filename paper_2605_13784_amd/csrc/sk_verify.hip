@@ -27,6 +27,7 @@ constexpr int kEach = 32, kEachFew = 8;            // logits of a lane; where th
 constexpr int kFirstPlaces = 2;                    // places whose rows come first, where there are many rows
 constexpr int64_t kPartsInTwo = 8192;              // parts of rows from which they do
 constexpr int kMaxRows = 2 * SK_VERIFY_MAX_DRAFT + 1;
+constexpr int64_t kMaxWgs = (int64_t(1) << 32) / kThreads - 1;      // of a launch, which has fewer than 2^32 threads
 
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef u32x4 __attribute__((aligned(2))) u32x4_anywhere;      // (the hardware loads 16 bytes from any address)
@@ -622,6 +623,39 @@ int cut(Args& A, const int32_t n_seq, const int32_t n_draft, const int32_t vocab
     return each;
 }
 
+// The launches of n_seq sequences
+int launch(Args& A, const int each, const int dtype, const int32_t n_seq, void* workspace, hipStream_t st)
+{
+    lay_out(A, workspace, n_seq);
+    const dim3 block(kThreads), second((unsigned)n_seq * (each == kEach ? A.stretches : A.stretches / kWaves)), third((unsigned)n_seq);
+    // Where there are many rows, those of the first two places come first, and the others only of sequences whose draft is still standing.  us per call, all
+    // rows at once -> in two launches, fp32 rows of 128,256 logits with their draft's:
+    //   accepted of the drafted       nearly all        0.7 of them       0.3               0.05
+    //   64 x 4 (9,216 parts)           92 ->  94          80 ->  84        87 ->  75         86 ->  65
+    //   64 x 8 (17,408)               156 -> 171         151 -> 135       159 -> 101        152 ->  70
+    //   32 x 4 (4,608)                 45 ->  54          47 ->  52        51 ->  49         50 ->  39
+    //   64 x 3, bf16 (7,168)           62 ->  70          66 ->  67        72 ->  66         74 ->  60
+    const bool in_two = each == kEach && A.n_draft > kFirstPlaces && (int64_t)n_seq * A.rows * A.parts >= kPartsInTwo;
+    const int split = in_two ? kFirstPlaces : 0;
+#define SK_VERIFY(F32, EACH)                                                                                                                 \
+    for (int from = 0; from <= A.n_draft;) {                                                                                                 \
+        const int to = from == 0 && split ? split : A.n_draft + 1;                                                                           \
+        A.place0 = from; A.places = to - from; A.drafts = !A.draft ? 0 : to <= A.n_draft ? A.places : A.places - 1;                          \
+        hipLaunchKernelGGL((sk_verify_rows<F32, EACH>), dim3((unsigned)n_seq * (A.places + A.drafts) * A.parts), block, 0, st, A);           \
+        A.place0 = from = to;                                                                                                                \
+        if (to <= A.n_draft) hipLaunchKernelGGL(sk_verify_ends, third, block, 0, st, A);                                                     \
+    }                                                                                                                                        \
+    hipLaunchKernelGGL((sk_verify_stretches<F32, EACH>), second, block, 0, st, A);                                                           \
+    hipLaunchKernelGGL((sk_verify_draw<F32, 64 * EACH>), third, block, 0, st, A)
+    if (dtype == SK_F32) {
+        if (each == kEach) { SK_VERIFY(true, kEach); } else { SK_VERIFY(true, kEachFew); }
+    } else {
+        if (each == kEach) { SK_VERIFY(false, kEach); } else { SK_VERIFY(false, kEachFew); }
+    }
+#undef SK_VERIFY
+    return (int)hipGetLastError();
+}
+
 }  // namespace
 
 extern "C" {
@@ -672,37 +706,23 @@ int sk_verify(const void* target, int64_t target_stride, const void* draft, int6
     A.target_stride = target_stride * el; A.draft_stride = draft_stride * el;
     A.tokens = tokens; A.uniform = uniform; A.temperature = temperature;
     const int each = cut(A, n_seq, n_draft, vocab, A.draft != nullptr);
-    lay_out(A, workspace, n_seq);
     A.n_accepted = n_accepted; A.out_tokens = out_tokens; A.logprob = logprob;
-    if ((int64_t)n_seq * A.rows * A.stretches >= (int64_t(1) << 31)) return SK_E_INVAL;
     hipStream_t st = (hipStream_t)hip_stream;
-    const dim3 block(kThreads), second((unsigned)n_seq * (each == kEach ? A.stretches : A.stretches / kWaves)), third((unsigned)n_seq);
-    // Where there are many rows, those of the first two places come first, and the others only of sequences whose draft is still standing.  us per call, all
-    // rows at once -> in two launches, fp32 rows of 128,256 logits with their draft's:
-    //   accepted of the drafted       nearly all        0.7 of them       0.3               0.05
-    //   64 x 4 (9,216 parts)           92 ->  94          80 ->  84        87 ->  75         86 ->  65
-    //   64 x 8 (17,408)               156 -> 171         151 -> 135       159 -> 101        152 ->  70
-    //   32 x 4 (4,608)                 45 ->  54          47 ->  52        51 ->  49         50 ->  39
-    //   64 x 3, bf16 (7,168)           62 ->  70          66 ->  67        72 ->  66         74 ->  60
-    const bool in_two = each == kEach && n_draft > kFirstPlaces && (int64_t)n_seq * A.rows * A.parts >= kPartsInTwo;
-    const int split = in_two ? kFirstPlaces : 0;
-#define SK_VERIFY(F32, EACH)                                                                                                                 \
-    for (int from = 0; from <= n_draft;) {                                                                                                   \
-        const int to = from == 0 && split ? split : n_draft + 1;                                                                             \
-        A.place0 = from; A.places = to - from; A.drafts = !A.draft ? 0 : to <= n_draft ? A.places : A.places - 1;                            \
-        hipLaunchKernelGGL((sk_verify_rows<F32, EACH>), dim3((unsigned)n_seq * (A.places + A.drafts) * A.parts), block, 0, st, A);           \
-        A.place0 = from = to;                                                                                                                \
-        if (to <= n_draft) hipLaunchKernelGGL(sk_verify_ends, third, block, 0, st, A);                                                       \
-    }                                                                                                                                        \
-    hipLaunchKernelGGL((sk_verify_stretches<F32, EACH>), second, block, 0, st, A);                                                           \
-    hipLaunchKernelGGL((sk_verify_draw<F32, 64 * EACH>), third, block, 0, st, A)
-    if (dtype == SK_F32) {
-        if (each == kEach) { SK_VERIFY(true, kEach); } else { SK_VERIFY(true, kEachFew); }
-    } else {
-        if (each == kEach) { SK_VERIFY(false, kEach); } else { SK_VERIFY(false, kEachFew); }
+    // Sequences of a launch: all, except where its grid would be too large (2^20 rows of more than 24,576 logits).
+    const int32_t second_wgs = each == kEach ? A.stretches : A.stretches / kWaves, all = n_seq;
+    const int32_t at_once = (int32_t)(kMaxWgs / (second_wgs > A.rows * A.parts ? second_wgs : A.rows * A.parts));
+    for (int32_t s0 = 0; s0 < all; s0 += n_seq) {
+        n_seq = all - s0 < at_once ? all - s0 : at_once;
+        const int e = launch(A, each, dtype, n_seq, workspace, st);
+        if (e) return sk_status_of(e);
+        const int64_t places = (int64_t)n_seq * (n_draft + 1), drafts = (int64_t)n_seq * n_draft;
+        A.target += places * A.target_stride; A.uniform += places; A.out_tokens += places; A.n_accepted += n_seq;
+        if (A.draft) A.draft += drafts * A.draft_stride;
+        if (A.tokens) A.tokens += drafts;
+        if (A.temperature) A.temperature += n_seq;
+        if (A.logprob) A.logprob += places;
     }
-#undef SK_VERIFY
-    return sk_status_of((int)hipGetLastError());
+    return SK_OK;
 }
 
 }  // extern "C"

@@ -90,6 +90,9 @@ def test_a_rotation_is_checked():
     pool.sk_pool_set_rotation(np.ones(32), interleaved=True)
     assert L.sk_rotate(pool.h, p, None, 1, None, 0, p, None, None) == sk.SK_E_NODEVICE
     assert L.sk_rotate(pool.h, p, None, -1, None, 0, p, None, None) == sk.SK_E_INVAL
+    most = (1 << 27) // pool.Hq
+    assert L.sk_rotate(pool.h, p, None, most + 1, None, 0, p, None, None) == sk.SK_E_INVAL
+    assert L.sk_rotate(pool.h, p, None, most, None, 0, p, None, None) == sk.SK_E_NODEVICE
     assert L.sk_rotate(pool.h, None, None, 0, None, 0, None, None, None) == sk.SK_OK
     assert _status(pool.sk_session_shift, sid, 1) == sk.SK_OK
 

@@ -269,6 +269,35 @@ def test_many_rows_whose_later_places_wait_for_the_first(dtype, drawn):
 
 
 @pytest.mark.gpu
+def test_more_rows_than_one_grid_has_workgroups_for():
+    """2^20 rows of 32,769 bf16 logits (68.7 GB, offsets far behind 32 bits): more than 2^24 workgroups, so that the last sequences are a second run of launches.
+    Every stretch of sequences gives what a call of its own gives, and rows on both sides of the border what the definition does."""
+    n, V, step = 1 << 20, 4 * 8192 + 1, 1 << 16
+    if torch.cuda.mem_get_info()[0] < 80 << 30:
+        pytest.skip("needs 80 GiB of device memory")
+    gen = torch.Generator(device="cuda").manual_seed(41)
+    some = (2.5 * torch.randn((4099, V), generator=gen, device="cuda")).bfloat16()
+    target = torch.empty((n, 1, V), dtype=torch.bfloat16, device="cuda")
+    for i in range(0, n, 4099):
+        target[i:i + 4099, 0] = some[:min(4099, n - i)]
+    u = torch.rand((n, 1), generator=gen, device="cuda")
+    temperature = 0.5 + torch.rand(n, generator=gen, device="cuda")
+    temperature[::5] = 0.0                                    # greedy
+    tokens = torch.empty((n, 0), dtype=torch.int32, device="cuda")
+    accepted, out, logp = sk.sk_verify(target, tokens, u, temperature=temperature)
+    torch.cuda.synchronize()
+    assert not accepted.any()
+    for i in range(0, n, step):
+        one = sk.sk_verify(target[i:i + step], tokens[i:i + step], u[i:i + step], temperature=temperature[i:i + step])
+        assert torch.equal(one[1], out[i:i + step]) and torch.equal(one[2], logp[i:i + step]), i
+    border = ((1 << 24) - 1) // 20                            # sequences of the first run
+    for i in [0, 1, border - 2, border - 1, border, border + 1, n - 1]:
+        _, t, lp, near = _define(target[i].float().cpu().numpy(), None, [], u[i].cpu().numpy(), float(temperature[i]))
+        assert near > 2.0 ** -40 and int(out[i, 0]) == t[0] and abs(float(logp[i, 0]) - lp[0]) <= 2.0 ** -24 * abs(lp[0]) + 2.0 ** -40 * (1 + abs(lp[0])), i
+    del target, some
+
+
+@pytest.mark.gpu
 def test_what_it_draws_has_the_targets_distribution():
     """Frequencies of the first token over 2^17 sequences, for a draft that is far from the target, a looked-up token and none: within 5 deviations."""
     gen = synth.generator(35)
