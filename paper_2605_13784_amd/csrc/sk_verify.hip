@@ -8,8 +8,9 @@
 // bits, which the vector unit adds and multiplies at the rate of 32-bit ones.  Exponentials of 32 bits are off by up to 2^-23 of themselves, and the border between any two
 // of 128,256 tokens would move by as much of the total; a number that falls between the old place and the new finds another token.
 //
-// Three launches: maxima and sums of all rows, in parts; the sums of the stretches of the one row per sequence that is drawn from; the draw.  Where
-// there are many rows, the first is two, with a small one between them.
+// Maxima and sums of all rows, in parts; the sums of the stretches of the one row per sequence that is drawn from; the draw.  Where there are few rows, that is two
+// launches, the draw being the business of the workgroup that is its sequence's last to have a sum; where there are many, three, of which the first is two with a small
+// one between them.
 #include <hip/hip_runtime.h>
 #include <cstring>
 
@@ -24,6 +25,7 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kEach = 32, kEachFew = 8;            // logits of a lane; where there are few rows.  A stretch is a wave's, a part a workgroup's
+constexpr int kApart = 64;                         // words from a sequence's count of workgroups to the next: additions to one line wait for each other
 constexpr int kFirstPlaces = 2;                    // places whose rows come first, where there are many rows
 constexpr int64_t kPartsInTwo = 8192;              // parts of rows from which they do
 constexpr int kMaxRows = 2 * SK_VERIFY_MAX_DRAFT + 1;
@@ -37,7 +39,7 @@ typedef u32x4 __attribute__((aligned(2))) u32x4_anywhere;      // (the hardware 
 struct Part { double sum, e; float max; int32_t at; };
 struct Sum { double sum, e; };                     // of a stretch
 
-// What the second launch leaves for the third, a sequence.
+// What a sequence draws from.
 struct Chosen {
     double scale, p_e, p_inv, q_e, q_inv;
     float p_max, q_max;
@@ -57,7 +59,8 @@ struct Args {
     float* given;                                  // [sequence][rows]: the logit of the row's drafted token
     int32_t* ended;                                // [sequence]: nothing behind place0 counts (where rows come in two launches)
     int32_t place0, places, drafts;                // of a launch of rows: its first place, target rows and draft rows of a sequence
-    Chosen* chosen;                                // [sequence]
+    Chosen* chosen;                                // [sequence], for a launch of draws
+    uint32_t* arrived;                             // [sequence][kApart]: workgroups that have their sums, where the last one draws (few rows)
     double* sums;                                  // [sequence][stretch]: of the weights of the drawn row
     int32_t *n_accepted, *out_tokens;
     float* logprob;
@@ -219,6 +222,7 @@ __global__ __launch_bounds__(kThreads) void sk_verify_rows(const Args A)
     const int part = blockIdx.x % A.parts, row = blockIdx.x / A.parts, rows = A.places + A.drafts, seq = row / rows, of_seq = row - seq * rows;
     const int place = A.place0 + (of_seq < A.places ? of_seq : of_seq - A.places), r = of_seq < A.places ? place : A.n_draft + 1 + place;
     if (A.place0 > 0 && A.ended[seq]) return;
+    if (EACH == kEachFew && part == 0 && of_seq == 0 && threadIdx.x == 0) A.arrived[seq * kApart] = 0;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int32_t tokens = token_of_lane(A, seq);
     const int n = drafted(A, tokens);
@@ -359,10 +363,11 @@ __global__ __launch_bounds__(kThreads) void sk_verify_ends(const Args A)
     }
 }
 
-// ---- second launch: the sums of the stretches of the row that is drawn from ----
+// ---- second launch: the sums of the stretches of the row that is drawn from, and the draw ----
 //
-// Every workgroup finds by itself which row that is (a launch for it would cost as much).  Bound: four round trips one behind the other (5 us for one sequence of 128,256 logits),
-// then two rows' way and their exponentials: 64 sequences 22 us, of which reading 66 MB takes 13.
+// Every workgroup finds by itself which row that is (a launch for it would cost as much).  Bound: round trips one behind the other, four to the sums (5 us for one sequence of 128,256
+// logits), four more to the drawn token (8.7; in a launch of its own 5.3 + 3.4 and the gap between them, and 2.5 us more of the host).  Where there are many rows, two rows' way and
+// their exponentials: 64 sequences 22 us, of which reading 66 MB takes 13; there a workgroup that waits until its sum has arrived keeps another from starting (38 us with the draw, 29 in two launches).
 
 // What a logit of the row that is drawn from counts for.
 template <bool F32> struct Weights {
@@ -397,122 +402,25 @@ template <bool F32> struct Weights {
     }
 };
 
-template <bool F32, int EACH>
-__global__ __launch_bounds__(kThreads) void sk_verify_stretches(const Args A)
-{
-    // eight logits to a lane: a workgroup has one stretch, or four
-    constexpr int EL = F32 ? 4 : 2, N = 16 / EL, P = 8 / N, kOfWg = kThreads * 8 / (64 * EACH);
-    static_assert(kOfWg == 1 || kOfWg == kWaves, "");
-    __shared__ double of_wave[kWaves];
-    __shared__ Part row[kMaxRows];
-    __shared__ Chosen chosen;
-    const int wgs = A.stretches / kOfWg, wg = blockIdx.x % wgs, seq = blockIdx.x / wgs, tid = threadIdx.x, lane = tid & 63;
-    const float none = -__builtin_inff();
-    bool greedy;
-    const double scale = scale_of(A, seq, greedy);
-    const int32_t token = token_of_lane(A, seq);
-    const int n = drafted(A, token);
-    // a drafted token's logits, for the lanes of the first wave
-    float xp = none, xq = none, u = 0.f;
-    if (tid < n) given_of(A, seq, lane, xp, xq, u);
-    join_rows(A, seq, A.n_draft + 1, scale, row);
-    __syncthreads();
-    if (tid < 64) {
-        const bool stays = lane < n && token_stays(A, lane, token, greedy, scale, xp, xq, u, row);
-        const uint64_t out = ~__ballot(stays);
-        const int a = min(n, (int)__builtin_ctzll(out));            // (lanes from n on are out)
-        const Part p = row[a];
-        const bool valid = p.sum > 0.0;
-        if (lane == 0) {
-            Chosen c = {scale, p.e, 1.0 / p.sum, 0.0, 0.0, p.max, 0.f, valid && !greedy ? a : -1, 0};
-            if (a < n && !A.draft) c.less = 2;
-            else if (a < n && !greedy && row[A.n_draft + 1 + a].sum > 0.0) {
-                const Part q = row[A.n_draft + 1 + a];
-                c.less = 1; c.q_e = q.e; c.q_inv = 1.0 / q.sum; c.q_max = q.max;
-            }
-            chosen = c;
-            if (wg == 0) { A.chosen[seq] = c; A.n_accepted[seq] = a; }
-        }
-        if (wg == 0 && lane <= A.n_draft) {   // everything but a token that is still to be drawn
-            const int32_t t = lane < a ? token : lane == a && valid && greedy ? p.at : -1;
-            const int64_t at = (int64_t)seq * (A.n_draft + 1) + lane;
-            A.out_tokens[at] = t;
-            if (A.logprob) {
-                float l = 0.f;
-                if (lane < a || (lane == a && valid && greedy)) {
-                    const Part r = row[lane];
-                    l = log_probability(lane < a ? xp : p.max, scale, r.e, r.max, 1.0 / r.sum);
-                } else if (lane == a && !valid) l = __builtin_nanf("");
-                A.logprob[at] = l;
-            }
-        }
-    }
-    __syncthreads();
-    const int sub = wg * kWaves + (tid >> 6), stretch = sub * 512 / (64 * EACH);
-    // the target's own weights are known; without the drafted token, all but those of its stretch
-    if (chosen.place < 0 || chosen.less == 0) return;
-    const Weights<F32> w(A, chosen, seq);
-    if (chosen.less == 2 && w.without / (64 * EACH) != stretch) return;
-    double sum = 0.0;
-    if (A.vocab >= N) {                            // pieces of 16 bytes as in the first launch
-        const int at0 = sub * 512 + lane * N, last = A.vocab - N;
-        u32x4 x[P], y[P];
-#pragma unroll
-        for (int i = 0; i < P; ++i) {
-            const int64_t at = (int64_t)min(at0 + i * 64 * N, last) * EL;
-            x[i] = *(const u32x4_anywhere*)(w.p + at);
-            y[i] = *(const u32x4_anywhere*)(w.q + at);
-        }
-        w.each([&](auto one) __attribute__((always_inline)) {
-#pragma unroll
-            for (int i = 0; i < P; ++i) {
-                const int first = at0 + i * 64 * N, from = min(first, last);
-#pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const double z = one(element<F32>(x[i], e), element<F32>(y[i], e), from + e);
-                    sum += from + e >= first ? z : 0.0;
-                }
-            }
-        });
-    } else {
-        for (int i = lane; i < A.vocab && sub == 0; i += 64) sum += w(logit<F32>(w.p, i), logit<F32>(w.q, i), i);
-    }
-    sum = wave_sum(sum);
-    double* to = A.sums + (int64_t)seq * A.stretches + stretch;
-    if (kOfWg == kWaves) {
-        if (lane == 0) *to = sum;
-        return;
-    }
-    if (lane == 0) of_wave[tid >> 6] = sum;
-    __syncthreads();
-    if (tid == 0) *to = of_wave[0] + of_wave[1] + of_wave[2] + of_wave[3];
-}
-
-// ---- third launch: the draw ----
-//
-// Bound: three round trips (3.5 us for one sequence, 7 for 64).
+constexpr int kSums = 4;                           // stretches of a lane that are asked for at once
 
 // The token that the sequence's last number finds in the running sum of the row's weights: the stretch, by every wave for itself, then the thread, then
-// its logit.  Where roundings leave the sum below the limit, or the number is 1 or more, the last that counts is taken at each step.
-template <bool F32, int STRETCH>
-__global__ __launch_bounds__(kThreads) void sk_verify_draw(const Args A)
+// its logit.  Where roundings leave the sum below the limit, or the number is 1 or more, the last that counts is taken at each step.  `summed(i)` is what has been added up
+// for stretch i if less is 1, or 2 and the drafted token is in it; `first` holds it for the first ones.
+template <bool F32, int STRETCH, class SUMMED>
+__device__ __forceinline__ void draw(const Args& A, const int seq, const Weights<F32>& w, const float number, const SUMMED summed, double (&first)[kSums])
 {
-    constexpr int EACH = STRETCH / kThreads, kSums = 4;       // logits of a thread, one behind the other; stretches of a lane that are asked for at once
+    constexpr int EACH = STRETCH / kThreads;       // logits of a thread, one behind the other
     __shared__ double of_wave[kWaves];
     __shared__ uint64_t over_of[kWaves], some_of[kWaves];
-    const int seq = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const double* sums = A.sums + (int64_t)seq * A.stretches;
-    const double u = __builtin_fmax((double)A.uniform[(int64_t)seq * (A.n_draft + 1) + A.n_draft], 0.0);
-    double first[kSums];
-#pragma unroll
-    for (int j = 0; j < kSums; ++j) first[j] = sums[min(64 * j + lane, A.stretches - 1)];
-    const Chosen c = A.chosen[seq];
-    if (c.place < 0) return;
-    const Weights<F32> w(A, c, seq);
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const Chosen& c = w.c;
+    // The target's own sums.  One below 2^-1000 is none: its logits may all be below the least double.
     const Sum* known = A.of_stretch + ((int64_t)seq * (A.n_draft + 1) + c.place) * A.stretches;
     auto known_sum = [&](const int i, const double again) {
         const Sum k = known[min(i, A.stretches - 1)];
-        return c.less == 2 && i == w.without / STRETCH ? again : at_exponent(k.sum, k.e, c.p_e) * c.p_inv;
+        const double x = at_exponent(k.sum, k.e, c.p_e) * c.p_inv;
+        return c.less == 2 && i == w.without / STRETCH ? again : x < 0x1p-1000 ? 0.0 : x;
     };
     if (c.less != 1) {
 #pragma unroll
@@ -521,12 +429,12 @@ __global__ __launch_bounds__(kThreads) void sk_verify_draw(const Args A)
     auto stretch_sum = [&](const int base) {
         if (base + lane >= A.stretches) return 0.0;
         if (base < 64 * kSums) return base < 128 ? (base ? first[1] : first[0]) : base == 128 ? first[2] : first[3];
-        return c.less == 1 ? sums[base + lane] : known_sum(base + lane, sums[base + lane]);
+        return c.less == 1 ? summed(base + lane) : known_sum(base + lane, summed(base + lane));
     };
     double total = 0.0;
     for (int base = 0; base < A.stretches; base += 64) total += stretch_sum(base);
     total = wave_sum(total);
-    const double limit = u * total;
+    const double limit = __builtin_fmax((double)number, 0.0) * total;
     double before = 0.0, left = 0.0;
     int stretch = -1;
     for (int base = 0; base < A.stretches; base += 64) {
@@ -590,10 +498,142 @@ __global__ __launch_bounds__(kThreads) void sk_verify_draw(const Args A)
     if (A.logprob) A.logprob[to] = log_probability(its, c.scale, c.p_e, c.p_max, c.p_inv);
 }
 
+template <bool F32, int EACH>
+__global__ __launch_bounds__(kThreads) void sk_verify_stretches(const Args A)
+{
+    // eight logits to a lane: a workgroup has one stretch, or four
+    constexpr int EL = F32 ? 4 : 2, N = 16 / EL, P = 8 / N, kOfThisWg = kThreads * 8, kOfWg = kOfThisWg / (64 * EACH);
+    constexpr bool kDraws = EACH == kEachFew;
+    static_assert(kOfWg == (kDraws ? kWaves : 1), "");
+    __shared__ double of_wave[kWaves];
+    __shared__ Part row[kMaxRows];
+    __shared__ Chosen chosen;
+    __shared__ int draws;
+    const int wgs = A.stretches / kOfWg, wg = blockIdx.x % wgs, seq = blockIdx.x / wgs, tid = threadIdx.x, lane = tid & 63;
+    const float none = -__builtin_inff();
+    bool greedy;
+    const double scale = scale_of(A, seq, greedy);
+    const int32_t token = token_of_lane(A, seq);
+    const int n = drafted(A, token);
+    // a drafted token's logits, for the lanes of the first wave
+    float xp = none, xq = none, u = 0.f;
+    const float number = A.uniform[(int64_t)seq * (A.n_draft + 1) + A.n_draft];
+    if (tid < n) given_of(A, seq, lane, xp, xq, u);
+    join_rows(A, seq, A.n_draft + 1, scale, row);
+    __syncthreads();
+    if (tid < 64) {
+        const bool stays = lane < n && token_stays(A, lane, token, greedy, scale, xp, xq, u, row);
+        const uint64_t out = ~__ballot(stays);
+        const int a = min(n, (int)__builtin_ctzll(out));            // (lanes from n on are out)
+        const Part p = row[a];
+        const bool valid = p.sum > 0.0;
+        if (lane == 0) {
+            Chosen c = {scale, p.e, 1.0 / p.sum, 0.0, 0.0, p.max, 0.f, valid && !greedy ? a : -1, 0};
+            if (a < n && !A.draft) c.less = 2;
+            else if (a < n && !greedy && row[A.n_draft + 1 + a].sum > 0.0) {
+                const Part q = row[A.n_draft + 1 + a];
+                c.less = 1; c.q_e = q.e; c.q_inv = 1.0 / q.sum; c.q_max = q.max;
+            }
+            chosen = c;
+            if (wg == 0) { if (!kDraws) A.chosen[seq] = c; A.n_accepted[seq] = a; }
+        }
+        if (wg == 0 && lane <= A.n_draft && (lane != a || !valid || greedy)) {       // everything but a token that is still to be drawn
+            const int32_t t = lane < a ? token : lane == a && valid && greedy ? p.at : -1;
+            const int64_t at = (int64_t)seq * (A.n_draft + 1) + lane;
+            A.out_tokens[at] = t;
+            if (A.logprob) {
+                float l = 0.f;
+                if (lane < a || (lane == a && valid && greedy)) {
+                    const Part r = row[lane];
+                    l = log_probability(lane < a ? xp : p.max, scale, r.e, r.max, 1.0 / r.sum);
+                } else if (lane == a && !valid) l = __builtin_nanf("");
+                A.logprob[at] = l;
+            }
+        }
+    }
+    __syncthreads();
+    // The target's own sums are known; without the drafted token, all but those of its stretch.
+    if (chosen.place < 0 || (chosen.less == 0 && !(kDraws && wg == 0))) return;
+    const Weights<F32> w(A, chosen, seq);
+    if (w.c.less == 2 && w.without / kOfThisWg != wg) return;
+    double again = 0.0, *sums = A.sums + (int64_t)seq * A.stretches;
+    if (w.c.less > 0) {
+        const int sub = wg * kWaves + (tid >> 6);
+        double sum = 0.0;
+        if (A.vocab >= N) {                        // pieces of 16 bytes as in the first launch
+            const int at0 = sub * 512 + lane * N, last = A.vocab - N;
+            u32x4 x[P], y[P];
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+                const int64_t at = (int64_t)min(at0 + i * 64 * N, last) * EL;
+                x[i] = *(const u32x4_anywhere*)(w.p + at);
+                y[i] = *(const u32x4_anywhere*)(w.q + at);
+            }
+            w.each([&](auto one) __attribute__((always_inline)) {
+#pragma unroll
+                for (int i = 0; i < P; ++i) {
+                    const int first = at0 + i * 64 * N, from = min(first, last);
+#pragma unroll
+                    for (int e = 0; e < N; ++e) {
+                        const double z = one(element<F32>(x[i], e), element<F32>(y[i], e), from + e);
+                        sum += from + e >= first ? z : 0.0;
+                    }
+                }
+            });
+        } else {
+            for (int i = lane; i < A.vocab && sub == 0; i += 64) sum += w(logit<F32>(w.p, i), logit<F32>(w.q, i), i);
+        }
+        sum = wave_sum(sum);
+        if (lane == 0) of_wave[tid >> 6] = sum;
+        __syncthreads();
+        if (!kDraws) {                             // the workgroup is one stretch
+            if (tid == 0) sums[wg] = of_wave[0] + of_wave[1] + of_wave[2] + of_wave[3];
+            return;
+        }
+        if (w.c.less == 2) again = of_wave[w.without / (64 * EACH) % kWaves];
+        else {
+            // Sums leave by stores that write through, and have arrived behind the wait, before the workgroup is counted: whoever counts the last one finds all.  Nobody waits.
+            if (tid == 0) {
+#pragma unroll
+                for (int i = 0; i < kWaves; ++i) __hip_atomic_store(&sums[wg * kWaves + i], of_wave[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                asm volatile("" : : : "memory");
+                __builtin_amdgcn_s_waitcnt(0);
+                asm volatile("" : : : "memory");
+                draws = __hip_atomic_fetch_add(&A.arrived[seq * kApart], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1u == (uint32_t)wgs;
+            }
+            __syncthreads();
+            if (!draws) return;
+        }
+    }
+    if (!kDraws) return;
+    auto summed = [&](const int i) { return w.c.less == 1 ? __hip_atomic_load(&sums[min(i, A.stretches - 1)], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : again; };
+    double first[kSums];
+#pragma unroll
+    for (int j = 0; j < kSums; ++j) first[j] = summed(64 * j + lane);
+    draw<F32, 64 * EACH>(A, seq, w, number, summed, first);
+}
+
+// The draw in a launch of its own, where there are many rows.  Bound: three round trips (7 us for 64 sequences).
+template <bool F32>
+__global__ __launch_bounds__(kThreads) void sk_verify_draw(const Args A)
+{
+    const int seq = blockIdx.x, lane = threadIdx.x & 63;
+    const double* sums = A.sums + (int64_t)seq * A.stretches;
+    auto summed = [&](const int i) { return sums[min(i, A.stretches - 1)]; };
+    const float number = A.uniform[(int64_t)seq * (A.n_draft + 1) + A.n_draft];
+    double first[kSums];
+#pragma unroll
+    for (int j = 0; j < kSums; ++j) first[j] = summed(64 * j + lane);
+    const Chosen c = A.chosen[seq];
+    if (c.place < 0) return;
+    draw<F32, 64 * kEach>(A, seq, Weights<F32>(A, c, seq), number, summed, first);
+}
+
 int64_t parts_of(const int64_t each, const int32_t vocab) { return (vocab + each * kThreads - 1) / (each * kThreads); }
-// Logits of a lane.  us per call, eight -> 32, fp32 rows of 128,256 logits with their draft's: 1 x 4 14 -> 15.4, 4 x 4 17.7 -> 18.4, 7 x 4 (1,008 parts of 32) 22.3 ->
-// 22.3, 10 x 4 27 -> 26, 14 x 4 32 -> 30, 24 x 4 45 -> 41; bf16 rows of 50,257 16 x 3 19 -> 20.6, 64 x 3 40 -> 37; without a draft 64 x 0 22.5 -> 21 (1,024 parts),
-// 300 x 0 rows of 32,000 (1,200) 23.8 -> 25.3.
+// Logits of a lane.  us per call in a stream of them, eight (two launches) -> 32 (three), fp32 rows of 128,256 logits with their draft's: 1 x 4 13.1 -> 15.2, 4 x 4 16.8 ->
+// 18.2, 7 x 4 (1,008 parts of 32) 21.3 -> 21.8, 10 x 4 26.0 -> 25.8, 14 x 4 29.9 -> 29.9, 24 x 4 44.5 -> 41; bf16 rows of 50,257 16 x 3 17.6 -> 20.2, 64 x 3 40.6 -> 36.7; without a
+// draft 16 x 0 11.1 -> 13.6, 40 x 0 15.9 -> 17.5, 64 x 0 (1,024 parts) 20.4 -> 20.8, 300 x 0 rows of 32,000 (1,200) 31 -> 25.  Eight and a launch of draws of its own: 1 x 4 13.8, 4 x 4
+// 17.5, 16 x 0 13.8; with counts next to each other 4 x 4 18.8, 10 x 4 29.5.
 int each_of(const int64_t rows, const int32_t vocab) { return rows * parts_of(kEach, vocab) < 1024 ? kEachFew : kEach; }
 bool sizes_ok(const int32_t n_seq, const int32_t n_draft, const int32_t vocab)
 {
@@ -601,7 +641,7 @@ bool sizes_ok(const int32_t n_seq, const int32_t n_draft, const int32_t vocab)
            (int64_t)n_seq * (n_draft + 1) <= SK_VERIFY_MAX_ROWS;
 }
 // What a call keeps, in the order in which it lies in the workspace
-size_t lay_out(Args& A, void* workspace, const int32_t n_seq)
+size_t lay_out(Args& A, const int each, void* workspace, const int32_t n_seq)
 {
     const int64_t parts = (int64_t)n_seq * A.rows * A.parts, stretches = (int64_t)n_seq * A.stretches;
     uintptr_t at = (uintptr_t)workspace;
@@ -610,6 +650,7 @@ size_t lay_out(Args& A, void* workspace, const int32_t n_seq)
     A.of_stretch = (Sum*)take(stretches * (A.n_draft + 1), sizeof(Sum));
     A.given = (float*)take((int64_t)n_seq * A.rows, sizeof(float));
     A.ended = (int32_t*)take(n_seq + ((n_seq * (int64_t)A.rows + n_seq) & 1), sizeof(int32_t));
+    A.arrived = (uint32_t*)take(each == kEachFew ? n_seq * kApart : 0, sizeof(uint32_t));
     A.chosen = (Chosen*)take(n_seq, sizeof(Chosen));
     A.sums = (double*)take(stretches, sizeof(double));
     return size_t(at - (uintptr_t)workspace);
@@ -626,8 +667,8 @@ int cut(Args& A, const int32_t n_seq, const int32_t n_draft, const int32_t vocab
 // The launches of n_seq sequences
 int launch(Args& A, const int each, const int dtype, const int32_t n_seq, void* workspace, hipStream_t st)
 {
-    lay_out(A, workspace, n_seq);
-    const dim3 block(kThreads), second((unsigned)n_seq * (each == kEach ? A.stretches : A.stretches / kWaves)), third((unsigned)n_seq);
+    lay_out(A, each, workspace, n_seq);
+    const dim3 block(kThreads), second((unsigned)n_seq * (each == kEach ? A.stretches : A.stretches / kWaves)), each_seq((unsigned)n_seq);
     // Where there are many rows, those of the first two places come first, and the others only of sequences whose draft is still standing.  us per call, all
     // rows at once -> in two launches, fp32 rows of 128,256 logits with their draft's:
     //   accepted of the drafted       nearly all        0.7 of them       0.3               0.05
@@ -643,10 +684,10 @@ int launch(Args& A, const int each, const int dtype, const int32_t n_seq, void* 
         A.place0 = from; A.places = to - from; A.drafts = !A.draft ? 0 : to <= A.n_draft ? A.places : A.places - 1;                          \
         hipLaunchKernelGGL((sk_verify_rows<F32, EACH>), dim3((unsigned)n_seq * (A.places + A.drafts) * A.parts), block, 0, st, A);           \
         A.place0 = from = to;                                                                                                                \
-        if (to <= A.n_draft) hipLaunchKernelGGL(sk_verify_ends, third, block, 0, st, A);                                                     \
+        if (to <= A.n_draft) hipLaunchKernelGGL(sk_verify_ends, each_seq, block, 0, st, A);                                                     \
     }                                                                                                                                        \
     hipLaunchKernelGGL((sk_verify_stretches<F32, EACH>), second, block, 0, st, A);                                                           \
-    hipLaunchKernelGGL((sk_verify_draw<F32, 64 * EACH>), third, block, 0, st, A)
+    if (EACH != kEachFew) hipLaunchKernelGGL(sk_verify_draw<F32>, each_seq, block, 0, st, A)
     if (dtype == SK_F32) {
         if (each == kEach) { SK_VERIFY(true, kEach); } else { SK_VERIFY(true, kEachFew); }
     } else {
@@ -666,8 +707,8 @@ size_t sk_verify_workspace_bytes(int32_t n_seq, int32_t n_draft, int32_t vocab)
     size_t most = 0;                               // with a draft's rows or without them, whose cut may be another
     for (int draft = 0; draft < 2; ++draft) {
         Args A = {};
-        cut(A, n_seq, n_draft, vocab, draft != 0);
-        const size_t bytes = lay_out(A, nullptr, n_seq);
+        const int each = cut(A, n_seq, n_draft, vocab, draft != 0);
+        const size_t bytes = lay_out(A, each, nullptr, n_seq);
         if (bytes > most) most = bytes;
     }
     return most;

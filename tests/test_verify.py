@@ -226,6 +226,23 @@ def test_numbers_at_the_ends_of_their_range():
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [3, 1100])
+def test_weights_below_the_least_double(dtype, n):
+    """2,048 logits that lie 2^-1075.3 below the largest: none of them has a weight, though all together would have 2^-1064."""
+    V, T = 6000, 1.4426950408889634 / 1075.3
+    x = torch.full((n, 2, V), -float("inf"), dtype=synth.torch_dtype(dtype))
+    x[:, :, :2048] = -1.0
+    x[:, :, 5000] = 0.0
+    temperature = torch.full((n,), T, dtype=torch.float32)
+    # a number of 0 finds the first token that has a weight, behind the draft and behind nothing; a number of 1 rejects the only one that has: nothing remains but the token
+    u = torch.tensor([[0.0, 0.0], [1.0, 0.0], [0.5, 2.0 ** -149]]).repeat((n + 2) // 3, 1)[:n]
+    tokens = torch.full((n, 1), 5000, dtype=torch.int32)
+    _check(x, tokens, u, temperature=temperature, least=-1.0)
+    _check(x[:, 1:], tokens[:, :0], u[:, 1:], temperature=temperature, least=-1.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("shift,pad", [(0, 1), (1, 0), (3, 5), (7, 2)])
 def test_rows_that_start_anywhere(dtype, shift, pad):
     gen = synth.generator(34, stream=shift)
