@@ -441,7 +441,7 @@ int sk_logprobs(const void* logits, int dtype, int32_t rows, int32_t vocab, int6
  * Drafted token x at place i stays, if all in front do, when uniform[s][i] * q(x) < p(x); greedy: when it is the target's largest logit's (lowest index
  * among equals).  Behind those that stay one token is drawn, at the first place whose drafted token does not stay with the weights max(p - q, 0), behind the
  * whole draft with p: the lowest t whose running sum of weights exceeds uniform[s][n_draft] times their total (a number below 0, or NaN, counts as 0, one from 1 on draws
- * the last token that has a weight; weights whose sum over hundreds of tokens is below 2^-1000 of the total may count as none; where p - q leaves nothing, the drafted token is drawn).  Greedy: the largest logit's.
+ * the last token that has a weight; weights below 2^-960 of the total may count as none; where p - q leaves nothing, the drafted token is drawn).  Greedy: the largest logit's.
  * Outputs, DEVICE: n_accepted int32 [n_seq], the tokens that stay; out_tokens int32 [n_seq][n_draft + 1], those, the one drawn, then -1;
  * logprob float [n_seq][n_draft + 1] (may be NULL), the target's log probability at the temperature (greedy: at 1) of each, 0 behind them.
  * They overlap neither an input nor each other nor the workspace (SK_E_INVAL).  A target row that has no probabilities (NaN or +inf among its logits, or nothing but -inf) keeps no token and draws -1, log probability

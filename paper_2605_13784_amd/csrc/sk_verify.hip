@@ -91,15 +91,26 @@ __device__ __forceinline__ double weight_of(const float x, const double scale, c
 {
     return __builtin_fabs(e) < kFar ? near_weight(x, scale, e) : x == max ? 1.0 : 0.0;
 }
-// The same for many, where 2^-1000 is as good as nothing and |e| is below 2^50: the integer part is rounded into the low bits of a sum and added to the exponent's.
-__device__ __forceinline__ double weight_in_sum(const float x, const double scale, const double e)
+// The same for many, where |e| is below 2^50 and no x scale further from e than 2^10: the distance is rounded into the low bits of a sum, from where its integer part is
+// added to the exponent's.  `base` is that sum's other part.
+constexpr double kRounds = 6755399441055744.0;     // 1.5 * 2^52
+constexpr double kLeast = -1000.0;
+__device__ __forceinline__ double weight_within(const float x, const double scale, const double base)
 {
-    const double d = __builtin_fmax(__builtin_fma((double)x, scale, -e), -1000.0);
-    const double t = d + 6755399441055744.0;       // 1.5 * 2^52
-    u32x2 r = __builtin_bit_cast(u32x2, power_of_fraction(d - (t - 6755399441055744.0)));
+    const double t = __builtin_fma((double)x, scale, base);
+    u32x2 r = __builtin_bit_cast(u32x2, power_of_fraction(__builtin_fma((double)x, scale, base - t)));
     r.y += __builtin_bit_cast(u32x2, t).x << 20;
     return __builtin_bit_cast(double, r);
 }
+// The same wherever x is, what lies further below e counting 2^-1000
+__device__ __forceinline__ double weight_or_least(const float x, const double scale, const double e)
+{
+    const double d = __builtin_fmax(__builtin_fma((double)x, scale, -e), kLeast), t = d + kRounds;
+    u32x2 r = __builtin_bit_cast(u32x2, power_of_fraction(d - (t - kRounds)));
+    r.y += __builtin_bit_cast(u32x2, t).x << 20;
+    return __builtin_bit_cast(double, r);
+}
+constexpr double kNothing = 0x1p-980;              // what the least makes of a row's weights, and more, is taken off the drawn ones: nothing is left of it, and others do not feel it
 // The logarithm of a token's probability
 __device__ __forceinline__ float log_probability(const float x, const double scale, const double e, const float max, const double inverse)
 {
@@ -118,6 +129,10 @@ __device__ __forceinline__ double exponent_of(const float max, const double scal
     const double e = __builtin_rint((double)max * scale);
     return max == -__builtin_inff() ? kNoExponent : e;
 }
+
+// Maximum and minimum of three (the library's take an instruction more for each operand, for the sake of signalling NaNs: a row that has one has no probabilities, whatever these say)
+__device__ __forceinline__ float max_of(const float a, const float b, const float c) { float r; asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c)); return r; }
+__device__ __forceinline__ float min_of(const float a, const float b, const float c) { float r; asm("v_min3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c)); return r; }
 
 template <bool F32> __device__ __forceinline__ float logit(const unsigned char* row, const int i)
 {
@@ -232,54 +247,70 @@ __global__ __launch_bounds__(kThreads) void sk_verify_rows(const Args A)
     const unsigned char* x = row_of(A, seq, r);
     const float none = -__builtin_inff();
     const int stretch = part * kWaves + wave, at0 = stretch * 64 * EACH + lane * N;      // piece i: N logits from at0 + i * 64 * N on
-    float v[EACH];
     if (place < n) {
         const int32_t t = __builtin_amdgcn_readlane(tokens, place);
         if (t / (64 * EACH) == stretch && lane == 0) A.given[(int64_t)seq * A.rows + r] = logit<F32>(x, t);
     }
-    if (A.vocab >= N) {
-        // A piece that reaches behind the row is read N logits in front of its end, of which those count that are its own.
-        u32x4 w[P];
-#pragma unroll
-        for (int i = 0; i < P; ++i) w[i] = *(const u32x4_anywhere*)(x + (int64_t)min(at0 + i * 64 * N, A.vocab - N) * EL);
-#pragma unroll
-        for (int i = 0; i < EACH; ++i) v[i] = element<F32>(w[i / N], i % N);
-        if ((stretch + 1) * 64 * EACH > A.vocab) {
-#pragma unroll
-            for (int i = 0; i < EACH; ++i) v[i] = i % N >= at0 + i / N * 64 * N - (A.vocab - N) ? v[i] : none;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < EACH; ++i) v[i] = i < N && at0 + i < A.vocab ? logit<F32>(x, at0 + i) : none;
-    }
-    float m = none;
-    bool bad = false;
-#pragma unroll
-    for (int i = 0; i < EACH; i += 2) { m = fmaxf(m, fmaxf(v[i], v[i + 1])); bad |= __builtin_isunordered(v[i], v[i + 1]); }
-    m = wave_max(m);
-    bad |= m == __builtin_inff();
-    const double e = exponent_of(m, scale);
-    double sum[2] = {0.0, 0.0};
-    if (__builtin_fabs(e) < kFar) {
-#pragma unroll
-        for (int i = 0; i < EACH; ++i) sum[i & 1] += weight_in_sum(v[i], scale, e);
-    } else if (m != none) {
-#pragma unroll
-        for (int i = 0; i < EACH; ++i) sum[0] += v[i] == m ? 1.0 : 0.0;
-    }
-    double total = wave_sum(sum[0] + sum[1]);
+    float m;
+    double e, total;
     int at = INT32_MAX;
-    if (greedy) {
+    // of a lane's logits, the i-th of which is index(i) of the row
+    auto sum_up = [&](auto& v, auto index) __attribute__((always_inline)) {
+        constexpr int M = sizeof(v) / sizeof(float);
+        m = v[0];
+        float low = v[0];
 #pragma unroll
-        for (int i = EACH - 1; i >= 0; --i)
-            if (v[i] == m) {
-                const int first = at0 + i / N * 64 * N;
-                at = (A.vocab >= N ? min(first, A.vocab - N) : first) + i % N;
+        for (int i = 1; i < M; i += 2) { const int k = i + 1 < M ? i + 1 : i; m = max_of(m, v[i], v[k]); low = min_of(low, v[i], v[k]); }
+        m = wave_max(m);
+        e = exponent_of(m, scale);
+        double sum[2] = {0.0, 0.0};
+        if (__builtin_fabs(e) < kFar && __all(__builtin_fma((double)low, scale, -e) >= kLeast)) {        // (a NaN makes the sum one)
+            const double base = kRounds - e;
+#pragma unroll
+            for (int i = 0; i < M; ++i) sum[i & 1] += weight_within(v[i], scale, base);
+        } else {
+            bool bad = m == __builtin_inff();
+#pragma unroll
+            for (int i = 0; i < M; ++i) bad |= v[i] != v[i];
+            if (__builtin_fabs(e) < kFar) {
+#pragma unroll
+                for (int i = 0; i < M; ++i) sum[i & 1] += weight_or_least(v[i], scale, e);
+            } else if (m != none) {
+#pragma unroll
+                for (int i = 0; i < M; ++i) sum[0] += v[i] == m ? 1.0 : 0.0;
             }
+            if (bad) sum[0] = __builtin_nan("");
+        }
+        total = wave_sum(sum[0] + sum[1]);
+        if (greedy) {
 #pragma unroll
-        for (int s = 1; s < 64; s *= 2) at = min(at, __shfl_xor(at, s, 64));
+            for (int i = M - 1; i >= 0; --i) at = v[i] == m ? index(i) : at;
+#pragma unroll
+            for (int s = 1; s < 64; s *= 2) at = min(at, __shfl_xor(at, s, 64));
+        }
+    };
+    if (A.vocab >= N) {
+        float v[EACH];
+        u32x4 w[P];
+        const int last = A.vocab - N;
+        if ((stretch + 1) * 64 * EACH <= A.vocab) {
+            const unsigned char* from = x + (int64_t)at0 * EL;
+#pragma unroll
+            for (int i = 0; i < P; ++i) w[i] = *(const u32x4_anywhere*)(from + i * 1024);
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) v[i] = element<F32>(w[i / N], i % N);
+        } else {
+            // A piece that reaches behind the row is read N logits in front of its end, of which those count that are its own.
+#pragma unroll
+            for (int i = 0; i < P; ++i) w[i] = *(const u32x4_anywhere*)(x + (int64_t)min(at0 + i * 64 * N, last) * EL);
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) v[i] = i % N >= at0 + i / N * 64 * N - last ? element<F32>(w[i / N], i % N) : none;
+        }
+        sum_up(v, [&](const int i) { return min(at0 + i / N * 64 * N, last) + i % N; });
+    } else {
+        float v[1] = {stretch == 0 && lane < A.vocab ? logit<F32>(x, lane) : none};
+        sum_up(v, [&](int) { return lane; });
     }
-    if (__ballot(bad)) total = __builtin_nan("");
     if (lane == 0) {
         of_wave[wave] = Part{total, e, m, at};
         if (r <= A.n_draft) A.of_stretch[((int64_t)seq * (A.n_draft + 1) + r) * A.stretches + stretch] = Sum{total, e};
@@ -386,19 +417,23 @@ template <bool F32> struct Weights {
         const bool near = __builtin_fabs(c.p_e) < kFar && __builtin_fabs(c.q_e) < kFar;
         if (near && c.less == 1)
             visit([&](const float x, const float y, int) __attribute__((always_inline)) {
-                return __builtin_fmax(near_weight(x, c.scale, c.p_e) * c.p_inv - near_weight(y, c.scale, c.q_e) * c.q_inv, 0.0);
+                return __builtin_fmax(__builtin_fma(weight_or_least(x, c.scale, c.p_e), c.p_inv, -kNothing) - weight_or_least(y, c.scale, c.q_e) * c.q_inv, 0.0);
             });
         else if (near)
-            visit([&](const float x, float, const int i) __attribute__((always_inline)) { return i == without ? 0.0 : near_weight(x, c.scale, c.p_e) * c.p_inv; });
+            visit([&](const float x, float, const int i) __attribute__((always_inline)) {
+                const double w = __builtin_fmax(__builtin_fma(weight_or_least(x, c.scale, c.p_e), c.p_inv, -kNothing), 0.0);
+                return i == without ? 0.0 : w;
+            });
         else
             visit([&](const float x, const float y, const int i) __attribute__((always_inline)) { return (*this)(x, y, i); });
     }
     // of logits x and y of the two rows, at index i
     __device__ __forceinline__ double operator()(const float x, const float y, const int i) const
     {
-        double w = weight_of(x, c.scale, c.p_e, c.p_max) * c.p_inv;
-        if (c.less == 1) w = __builtin_fmax(w - weight_of(y, c.scale, c.q_e, c.q_max) * c.q_inv, 0.0);
-        return i == without ? 0.0 : w;
+        auto weight = [&](const float z, const double e, const float max) { return __builtin_fabs(e) < kFar ? weight_or_least(z, c.scale, e) : z == max ? 1.0 : 0.0; };
+        double w = __builtin_fma(weight(x, c.p_e, c.p_max), c.p_inv, -kNothing);
+        if (c.less == 1) w -= weight(y, c.q_e, c.q_max) * c.q_inv;
+        return i == without ? 0.0 : __builtin_fmax(w, 0.0);
     }
 };
 
@@ -415,12 +450,12 @@ __device__ __forceinline__ void draw(const Args& A, const int seq, const Weights
     __shared__ uint64_t over_of[kWaves], some_of[kWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const Chosen& c = w.c;
-    // The target's own sums.  One below 2^-1000 is none: its logits may all be below the least double.
+    // The target's own sums.  One below 2^-960 is none: all of its logits, 2^11 at most, may be nothing.
     const Sum* known = A.of_stretch + ((int64_t)seq * (A.n_draft + 1) + c.place) * A.stretches;
     auto known_sum = [&](const int i, const double again) {
         const Sum k = known[min(i, A.stretches - 1)];
         const double x = at_exponent(k.sum, k.e, c.p_e) * c.p_inv;
-        return c.less == 2 && i == w.without / STRETCH ? again : x < 0x1p-1000 ? 0.0 : x;
+        return c.less == 2 && i == w.without / STRETCH ? again : x < 0x1p-960 ? 0.0 : x;
     };
     if (c.less != 1) {
 #pragma unroll
