@@ -226,9 +226,10 @@ __device__ __forceinline__ const unsigned char* row_of(const Args& A, const int 
 
 // ---- first launch: maximum and sum of a part of a row ----
 
-// Bound: vector instructions, some 20 a logit of which 17 are of 64 bits, beside HBM.  576 rows of 128,256 fp32 logits (295 MB) in 61-68 us, 4.5 TB/s: 58 with
-// all rows from the cache, 43 (6.9 TB/s) without the exponentials.  16 logits a lane 70, 64 64.5; several parts a workgroup, the next one's loads in flight
-// while it computes, 72-77 (a third fewer waves); loads ahead of the look at the sequence 67.
+// Bound: vector instructions beside HBM.  256 rows of 128,256 fp32 logits (131 MB) in 27.6 us, 4.8 TB/s; 19.6 instructions to a wave's 64 logits, of which the loop's 14 of 64 bits and one
+// of 32, take 76 % of the cycles.  With every logit's distance clamped, and the copies that a maximum of two and a row of three logits in the same code cost, 24.5 instructions and 30.5 us.  Of
+// 576 rows in one launch, at that time 61-68 us: 16 logits a lane 70, 64 64.5; several parts a workgroup, the next one's loads in flight while it computes, 72-77 (a third fewer waves);
+// loads ahead of the look at the sequence 67; without the exponentials 43 (6.9 TB/s).
 template <bool F32, int EACH>
 __global__ __launch_bounds__(kThreads) void sk_verify_rows(const Args A)
 {
@@ -398,7 +399,7 @@ __global__ __launch_bounds__(kThreads) void sk_verify_ends(const Args A)
 //
 // Every workgroup finds by itself which row that is (a launch for it would cost as much).  Bound: round trips one behind the other, four to the sums (5 us for one sequence of 128,256
 // logits), four more to the drawn token (8.7; in a launch of its own 5.3 + 3.4 and the gap between them, and 2.5 us more of the host).  Where there are many rows, two rows' way and
-// their exponentials: 64 sequences 22 us, of which reading 66 MB takes 13; there a workgroup that waits until its sum has arrived keeps another from starting (38 us with the draw, 29 in two launches).
+// their exponentials: 64 sequences 22.6 us, of which reading 66 MB takes 13; there a workgroup that waits until its sum has arrived keeps another from starting (38 us with the draw, 29 in two launches).
 
 // What a logit of the row that is drawn from counts for.
 template <bool F32> struct Weights {
@@ -665,10 +666,10 @@ __global__ __launch_bounds__(kThreads) void sk_verify_draw(const Args A)
 }
 
 int64_t parts_of(const int64_t each, const int32_t vocab) { return (vocab + each * kThreads - 1) / (each * kThreads); }
-// Logits of a lane.  us per call in a stream of them, eight (two launches) -> 32 (three), fp32 rows of 128,256 logits with their draft's: 1 x 4 13.1 -> 15.2, 4 x 4 16.8 ->
-// 18.2, 7 x 4 (1,008 parts of 32) 21.3 -> 21.8, 10 x 4 26.0 -> 25.8, 14 x 4 29.9 -> 29.9, 24 x 4 44.5 -> 41; bf16 rows of 50,257 16 x 3 17.6 -> 20.2, 64 x 3 40.6 -> 36.7; without a
-// draft 16 x 0 11.1 -> 13.6, 40 x 0 15.9 -> 17.5, 64 x 0 (1,024 parts) 20.4 -> 20.8, 300 x 0 rows of 32,000 (1,200) 31 -> 25.  Eight and a launch of draws of its own: 1 x 4 13.8, 4 x 4
-// 17.5, 16 x 0 13.8; with counts next to each other 4 x 4 18.8, 10 x 4 29.5.
+// Logits of a lane.  us per call in a stream of them, eight (two launches) -> 32 (three), fp32 rows of 128,256 logits with their draft's: 1 x 4 12.7 -> 15.2, 4 x 4 16.5 -> 17.5, 7 x 4 (1,008
+// parts of 32) 20.9 -> 21.4, 10 x 4 25.0 -> 24.9, 14 x 4 29.0 -> 29.0, 24 x 4 43 -> 38; bf16 rows of 50,257 16 x 3 17.0 -> 19.5, 64 x 3 39.5 -> 34.4; without a draft 16 x 0 10.9 -> 13.4, 40 x 0 15.3 ->
+// 17.0, 64 x 0 (1,024 parts) 19.8 -> 20.4, 300 x 0 rows of 32,000 (1,200) 30 -> 25.  Eight, and the draws in a launch of their own: 1 x 4 13.8, 4 x 4 17.5, 16 x 0 13.8; with sequences' counts
+// next to each other 4 x 4 18.8, 10 x 4 29.5.
 int each_of(const int64_t rows, const int32_t vocab) { return rows * parts_of(kEach, vocab) < 1024 ? kEachFew : kEach; }
 bool sizes_ok(const int32_t n_seq, const int32_t n_draft, const int32_t vocab)
 {
@@ -707,10 +708,10 @@ int launch(Args& A, const int each, const int dtype, const int32_t n_seq, void* 
     // Where there are many rows, those of the first two places come first, and the others only of sequences whose draft is still standing.  us per call, all
     // rows at once -> in two launches, fp32 rows of 128,256 logits with their draft's:
     //   accepted of the drafted       nearly all        0.7 of them       0.3               0.05
-    //   64 x 4 (9,216 parts)           92 ->  94          80 ->  84        87 ->  75         86 ->  65
-    //   64 x 8 (17,408)               156 -> 171         151 -> 135       159 -> 101        152 ->  70
-    //   32 x 4 (4,608)                 45 ->  54          47 ->  52        51 ->  49         50 ->  39
-    //   64 x 3, bf16 (7,168)           62 ->  70          66 ->  67        72 ->  66         74 ->  60
+    //   64 x 4 (9,216 parts)           83 ->  89          76 ->  79        80 ->  74         80 ->  65
+    //   64 x 8 (17,408)               143 -> 146         138 -> 126       140 ->  99        139 ->  69
+    //   32 x 4 (4,608)                 41 ->  50          44 ->  50        47 ->  48         46 ->  40
+    //   64 x 3, bf16 (7,168)           57 ->  65          62 ->  66        68 ->  66         69 ->  60
     const bool in_two = each == kEach && A.n_draft > kFirstPlaces && (int64_t)n_seq * A.rows * A.parts >= kPartsInTwo;
     const int split = in_two ? kFirstPlaces : 0;
 #define SK_VERIFY(F32, EACH)                                                                                                                 \
