@@ -10,7 +10,7 @@
 //
 // Maxima and sums of all rows, in parts; the sums of the stretches of the one row per sequence that is drawn from; the draw.  Where there are few rows, that is two
 // launches, the draw being the business of the workgroup that is its sequence's last to have a sum; where there are many, three, of which the first is two with a small
-// one between them.
+// one between them, and the second has a small one in front.
 #include <hip/hip_runtime.h>
 #include <cstring>
 
@@ -28,6 +28,7 @@ constexpr int kEach = 32, kEachFew = 8;            // logits of a lane; where th
 constexpr int kApart = 64;                         // words from a sequence's count of workgroups to the next: additions to one line wait for each other
 constexpr int kFirstPlaces = 2;                    // places whose rows come first, where there are many rows
 constexpr int64_t kPartsInTwo = 8192;              // parts of rows from which they do
+constexpr int64_t kAtATime = 2048;                 // workgroups that the chip runs at a time, eight to each of 256 units
 constexpr int kMaxRows = 2 * SK_VERIFY_MAX_DRAFT + 1;
 constexpr int64_t kMaxWgs = (int64_t(1) << 32) / kThreads - 1;      // of a launch, which has fewer than 2^32 threads
 
@@ -226,7 +227,7 @@ __device__ __forceinline__ const unsigned char* row_of(const Args& A, const int 
 
 // ---- first launch: maximum and sum of a part of a row ----
 
-// Bound: vector instructions beside HBM.  256 rows of 128,256 fp32 logits (131 MB) in 27.6 us, 4.8 TB/s; 19.6 instructions to a wave's 64 logits, of which the loop's 14 of 64 bits and one
+// Bound: vector instructions beside HBM.  256 rows of 128,256 fp32 logits (131 MB) in 27 us, 4.9 TB/s; 19.6 instructions to a wave's 64 logits, of which the loop's 14 of 64 bits and one
 // of 32, take 76 % of the cycles.  With every logit's distance clamped, and the copies that a maximum of two and a row of three logits in the same code cost, 24.5 instructions and 30.5 us.  Of
 // 576 rows in one launch, at that time 61-68 us: 16 logits a lane 70, 64 64.5; several parts a workgroup, the next one's loads in flight while it computes, 72-77 (a third fewer waves);
 // loads ahead of the look at the sequence 67; without the exponentials 43 (6.9 TB/s).
@@ -397,9 +398,10 @@ __global__ __launch_bounds__(kThreads) void sk_verify_ends(const Args A)
 
 // ---- second launch: the sums of the stretches of the row that is drawn from, and the draw ----
 //
-// Every workgroup finds by itself which row that is (a launch for it would cost as much).  Bound: round trips one behind the other, four to the sums (5 us for one sequence of 128,256
-// logits), four more to the drawn token (8.7; in a launch of its own 5.3 + 3.4 and the gap between them, and 2.5 us more of the host).  Where there are many rows, two rows' way and
-// their exponentials: 64 sequences 22.6 us, of which reading 66 MB takes 13; there a workgroup that waits until its sum has arrived keeps another from starting (38 us with the draw, 29 in two launches).
+// Every workgroup finds by itself which row that is (a launch for it would cost as much), unless there are many.  Bound: round trips one behind the other, four to the sums (5 us for one
+// sequence of 128,256 logits), four more to the drawn token (8.7; in a launch of its own 5.3 + 3.4 and the gap between them, and 2.5 us more of the host).  Where there are many rows, two rows' way and
+// their exponentials: 64 sequences 14.0 us, of which reading 66 MB takes 13 (21.7 where every workgroup decides); there a workgroup that waits until its sum has arrived keeps another from
+// starting (38 us with the draw, 29 in two launches).
 
 // What a logit of the row that is drawn from counts for.
 template <bool F32> struct Weights {
@@ -534,18 +536,10 @@ __device__ __forceinline__ void draw(const Args& A, const int seq, const Weights
     if (A.logprob) A.logprob[to] = log_probability(its, c.scale, c.p_e, c.p_max, c.p_inv);
 }
 
-template <bool F32, int EACH>
-__global__ __launch_bounds__(kThreads) void sk_verify_stretches(const Args A)
+// By a workgroup: how many of a sequence's tokens stay, and what it draws from; everything that it returns but a token that is still to be drawn.
+__device__ __forceinline__ void decide(const Args& A, const int seq, const bool writes, Part* row, Chosen& chosen)
 {
-    // eight logits to a lane: a workgroup has one stretch, or four
-    constexpr int EL = F32 ? 4 : 2, N = 16 / EL, P = 8 / N, kOfThisWg = kThreads * 8, kOfWg = kOfThisWg / (64 * EACH);
-    constexpr bool kDraws = EACH == kEachFew;
-    static_assert(kOfWg == (kDraws ? kWaves : 1), "");
-    __shared__ double of_wave[kWaves];
-    __shared__ Part row[kMaxRows];
-    __shared__ Chosen chosen;
-    __shared__ int draws;
-    const int wgs = A.stretches / kOfWg, wg = blockIdx.x % wgs, seq = blockIdx.x / wgs, tid = threadIdx.x, lane = tid & 63;
+    const int tid = threadIdx.x, lane = tid & 63;
     const float none = -__builtin_inff();
     bool greedy;
     const double scale = scale_of(A, seq, greedy);
@@ -553,7 +547,6 @@ __global__ __launch_bounds__(kThreads) void sk_verify_stretches(const Args A)
     const int n = drafted(A, token);
     // a drafted token's logits, for the lanes of the first wave
     float xp = none, xq = none, u = 0.f;
-    const float number = A.uniform[(int64_t)seq * (A.n_draft + 1) + A.n_draft];
     if (tid < n) given_of(A, seq, lane, xp, xq, u);
     join_rows(A, seq, A.n_draft + 1, scale, row);
     __syncthreads();
@@ -571,9 +564,9 @@ __global__ __launch_bounds__(kThreads) void sk_verify_stretches(const Args A)
                 c.less = 1; c.q_e = q.e; c.q_inv = 1.0 / q.sum; c.q_max = q.max;
             }
             chosen = c;
-            if (wg == 0) { if (!kDraws) A.chosen[seq] = c; A.n_accepted[seq] = a; }
+            if (writes) A.n_accepted[seq] = a;
         }
-        if (wg == 0 && lane <= A.n_draft && (lane != a || !valid || greedy)) {       // everything but a token that is still to be drawn
+        if (writes && lane <= A.n_draft && (lane != a || !valid || greedy)) {       // everything but a token that is still to be drawn
             const int32_t t = lane < a ? token : lane == a && valid && greedy ? p.at : -1;
             const int64_t at = (int64_t)seq * (A.n_draft + 1) + lane;
             A.out_tokens[at] = t;
@@ -587,7 +580,35 @@ __global__ __launch_bounds__(kThreads) void sk_verify_stretches(const Args A)
             }
         }
     }
-    __syncthreads();
+}
+
+// ... in a launch of its own, where there are many workgroups
+__global__ __launch_bounds__(kThreads) void sk_verify_decide(const Args A)
+{
+    __shared__ Part row[kMaxRows];
+    decide(A, blockIdx.x, true, row, A.chosen[blockIdx.x]);
+}
+
+template <bool F32, int EACH, bool DECIDES>
+__global__ __launch_bounds__(kThreads) void sk_verify_stretches(const Args A)
+{
+    // eight logits to a lane: a workgroup has one stretch, or four
+    constexpr int EL = F32 ? 4 : 2, N = 16 / EL, P = 8 / N, kOfThisWg = kThreads * 8, kOfWg = kOfThisWg / (64 * EACH);
+    constexpr bool kDraws = EACH == kEachFew;
+    static_assert(kOfWg == (kDraws ? kWaves : 1) && (DECIDES || !kDraws), "");
+    __shared__ double of_wave[kWaves];
+    __shared__ int draws;
+    Chosen chosen;
+    const int wgs = A.stretches / kOfWg, wg = blockIdx.x % wgs, seq = blockIdx.x / wgs, tid = threadIdx.x, lane = tid & 63;
+    const float number = A.uniform[(int64_t)seq * (A.n_draft + 1) + A.n_draft];
+    if constexpr (DECIDES) {
+        __shared__ Part row[kMaxRows];
+        __shared__ Chosen found;
+        decide(A, seq, wg == 0, row, found);
+        __syncthreads();
+        chosen = found;
+        if (!kDraws && wg == 0 && tid == 0) A.chosen[seq] = chosen;
+    } else chosen = A.chosen[seq];
     // The target's own sums are known; without the drafted token, all but those of its stretch.
     if (chosen.place < 0 || (chosen.less == 0 && !(kDraws && wg == 0))) return;
     const Weights<F32> w(A, chosen, seq);
@@ -714,6 +735,10 @@ int launch(Args& A, const int each, const int dtype, const int32_t n_seq, void* 
     //   64 x 3, bf16 (7,168)           57 ->  65          62 ->  66        68 ->  66         69 ->  60
     const bool in_two = each == kEach && A.n_draft > kFirstPlaces && (int64_t)n_seq * A.rows * A.parts >= kPartsInTwo;
     const int split = in_two ? kFirstPlaces : 0;
+    // Where its workgroups are more than run at a time, the second launch finds the row that is drawn from decided by one in front of it.  us per call, 0.7 to 0.05 of the drafted
+    // accepted, by every workgroup -> by a launch: 14 x 4 (896 workgroups) 28.8 -> 30.4, 24 x 4 (1,536) 37.9 -> 38.3, 32 x 4 (2,048) 43-45 -> 43-45, 64 x 3 bf16 (4,096) 60-64 -> 57-62, 64 x 4 (4,096) 62-79 -> 59-74,
+    // 64 x 8 67-123 -> 63-117, 128 x 2 (8,192) 87-102 -> 84-97.
+    const bool apart = (int64_t)second.x > kAtATime;
 #define SK_VERIFY(F32, EACH)                                                                                                                 \
     for (int from = 0; from <= A.n_draft;) {                                                                                                 \
         const int to = from == 0 && split ? split : A.n_draft + 1;                                                                           \
@@ -722,7 +747,10 @@ int launch(Args& A, const int each, const int dtype, const int32_t n_seq, void* 
         A.place0 = from = to;                                                                                                                \
         if (to <= A.n_draft) hipLaunchKernelGGL(sk_verify_ends, each_seq, block, 0, st, A);                                                     \
     }                                                                                                                                        \
-    hipLaunchKernelGGL((sk_verify_stretches<F32, EACH>), second, block, 0, st, A);                                                           \
+    if (EACH == kEach && apart) {                                                                                                            \
+        hipLaunchKernelGGL(sk_verify_decide, each_seq, block, 0, st, A);                                                                     \
+        hipLaunchKernelGGL((sk_verify_stretches<F32, EACH, EACH == kEachFew>), second, block, 0, st, A);                                     \
+    } else hipLaunchKernelGGL((sk_verify_stretches<F32, EACH, true>), second, block, 0, st, A);                                              \
     if (EACH != kEachFew) hipLaunchKernelGGL(sk_verify_draw<F32>, each_seq, block, 0, st, A)
     if (dtype == SK_F32) {
         if (each == kEach) { SK_VERIFY(true, kEach); } else { SK_VERIFY(true, kEachFew); }
