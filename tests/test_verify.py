@@ -167,10 +167,7 @@ def test_temperatures_and_drafts_that_end_early(dtype):
     _check(x, tokens, u, temperature=temperature)
 
 
-@pytest.mark.gpu
-@pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("V", [3, 40, 5000, 9001])
-def test_masks_equal_logits_and_rows_without_probabilities(dtype, V):
+def _odd_rows(dtype, V):
     gen = synth.generator(32, stream=V)
     n, k = 16, 2
     x, y, tokens, u = _case(gen, n, k, V, dtype, near=0.5)
@@ -197,12 +194,33 @@ def test_masks_equal_logits_and_rows_without_probabilities(dtype, V):
     y[14, :, :-1] = -inf
     tokens[14] = V - 1
     x[15, :, 0] = 3.0e38 if dtype == "f32" else 3.0e38
+    return x, y, tokens, u
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [3, 40, 5000, 9001])
+def test_masks_equal_logits_and_rows_without_probabilities(dtype, V):
+    x, y, tokens, u = _odd_rows(dtype, V)
+    n = 16
     temperature = torch.ones(n)
     _check(x, tokens, u, draft=y, temperature=temperature)
     _check(x, tokens, u, temperature=temperature)
     _check(x, tokens, u, draft=y, temperature=torch.zeros(n))
     tokens[:, 0] = torch.where(torch.isnan(x[:, 0].float()), torch.zeros(()), x[:, 0].float()).argmax(1)
     _check(x, tokens, u, draft=y, temperature=torch.full((n,), 0.0))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [3, 40, 9001])
+def test_masks_equal_logits_and_rows_without_probabilities_among_many_rows(dtype, V):
+    x, y, tokens, u = (t.repeat((20,) + (1,) * (t.dim() - 1)) for t in _odd_rows(dtype, V))
+    u[16:] = torch.rand((304, 3), generator=synth.generator(42))
+    temperature = torch.ones(320)
+    temperature[160:240] = 0.0
+    _check(x, tokens, u, draft=y, temperature=temperature)
+    _check(x, tokens, u, temperature=temperature)
 
 
 @pytest.mark.gpu
