@@ -315,7 +315,8 @@ int sk_session_evict_lowest(sk_pool* pool, int32_t id, const float* mass_in, int
  * keys in step when positions change.  Pair i of the first rotary_dim dimensions of a row at position p turns by the angle p * inv_freq[i]:
  *   (a, b) -> factor * (a cos - b sin, a sin + b cos)
  * the pairs being (i, i + rotary_dim / 2), or (2 i, 2 i + 1) if interleaved != 0; the other dimensions stay as they are.  Angles are exact to
- * 2^-31 of a turn at any position of 32 bits (negative ones turn backwards), products are fp32, and a turned element is rounded once to the pool's type.
+ * 2^-31 of a turn at any position of 32 bits (negative ones turn backwards) and any frequency that sk_pool_set_rotation takes, sines, cosines (2^-22) and products are fp32, and a turned element
+ * is rounded once to the pool's type.
  *
  * sk_pool_set_rotation gives a pool its rotation (HOST inv_freq, rotary_dim / 2 of them, finite, at most 10^6 in magnitude; copied).  rotary_dim: a
  * multiple of 16 up to head_dim (SK_E_SHAPE).  It may be set again; what is cached stays as it is.  Metadata-only pools take it too.  Without

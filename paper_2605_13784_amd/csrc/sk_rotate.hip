@@ -268,6 +268,20 @@ int launch_blocks(const sk_geom& g, const sk_turned& t, const void* k, const voi
     return launch_commit(g, t, k, v, nullptr, &to, (to.first + to.count + 15) / 16 - to.first / 16, tables_rw, kv_rw, nullptr, stream);
 }
 
+// The part of a turn, in 2^-64, that a pair of frequency f (at most 2^20) turns a position: f / (2 pi) less its whole turns, to the nearest.  f is a 53-bit m over 2^s, with s
+// from 33 on, and m / (2 pi) is formed in whole numbers, from 128 bits of 1 / (2 pi), before anything is dropped: whole turns take no bits off what is left of them.  (A quotient of 64 bits
+// has lost 19 of them at f = 10^6, which is 1.3e-4 rad at position 2^31.)
+uint64_t step_of(const double f)
+{
+    constexpr uint64_t kInverseHigh = 0x28be60db9391054aull, kInverseLow = 0x7f09d5f47d4d3770ull;
+    int e;
+    const uint64_t m = (uint64_t)std::ldexp(std::frexp(std::fabs(f), &e), 53);
+    const int s = 53 - e;
+    const unsigned __int128 turns = (unsigned __int128)m * kInverseHigh + (uint64_t)((unsigned __int128)m * kInverseLow >> 64);      // f / (2 pi) in 2^-(64 + s), by less than one too few
+    const uint64_t step = s > 127 ? 0 : (uint64_t)((turns + ((unsigned __int128)1 << (s - 1))) >> s);
+    return f < 0 ? 0 - step : step;
+}
+
 bool aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 
 sk_turned make_turned(const sk_geom& g, const sk_rotation* rot, const void* q, void* q_out, const int32_t* positions, int32_t pos0, int32_t n_tok)
@@ -294,12 +308,7 @@ int sk_pool_set_rotation(sk_pool* p, int32_t rotary_dim, int32_t interleaved, co
         if (!(std::fabs(inv_freq[i]) <= 1e6)) return SK_E_INVAL;
     sk_rotation r = {};
     r.rotary = rotary_dim; r.interleaved = interleaved != 0; r.factor = factor;
-    for (int i = 0; i < rotary_dim / 2; ++i) {
-        // the part of a turn a position, in 64 bits of mantissa; 2^64 itself is none
-        const long double turns = (long double)inv_freq[i] / 6.283185307179586476925286766559005768L;
-        const long double part = turns - floorl(turns), scaled = roundl(part * 18446744073709551616.0L);
-        r.step[i] = scaled >= 18446744073709551616.0L ? 0 : (uint64_t)scaled;
-    }
+    for (int i = 0; i < rotary_dim / 2; ++i) r.step[i] = step_of(inv_freq[i]);
     *sk_rotation_of(p) = r;
     return SK_OK;
 }

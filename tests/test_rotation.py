@@ -5,6 +5,8 @@ one from the phase's lower bits and 2^-34 from the step (times 2 pi: below 2^-28
 to a float, 2^-23 with the constant and the product by it; the series' next terms are below 2^-28, its last operations round by 2^-24 each and the inner
 ones by less than that together.  So a sine or cosine is within 2^-22 of itself absolutely, with the factor's product 2^-24 more, and the two
 products and their sum round by 2^-24 of |x| + |y| at most three times: 2^-21 factor (|x| + |y|).  Then one rounding to the pool's type."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -197,6 +199,76 @@ def test_shared_blocks_are_replaced_and_others_are_not():
     for s in (a, b, c):
         pool.sk_session_destroy(s)
     assert pool.sk_pool_blocks_free() == 24
+
+
+def _inverse_turn(bits=400):
+    """1 / (2 pi) in units of 2^-bits, pi by Machin's formula in whole numbers."""
+    one = 1 << (bits + 64)
+
+    def arctan_of_inverse(n):
+        term, total, k = one // n, 0, 1
+        while term:
+            total += term // k if k % 4 == 1 else -(term // k)
+            term //= n * n
+            k += 2
+        return total
+
+    return (one << bits) // (8 * (4 * arctan_of_inverse(5) - arctan_of_inverse(239)))
+
+
+def _turns(frequency, position, bits=400):
+    """The part of a turn, in units of 2^-bits, that a pair of a frequency has turned at a position."""
+    num, den = float(frequency).as_integer_ratio()
+    return int(position) * num * _INVERSE_TURN // den % (1 << bits)
+
+
+_INVERSE_TURN = _inverse_turn()
+FAST = np.array([(-1) ** i * 10.0 ** (6 * i / 63) for i in range(62)] + [2 * np.pi, 1e6])      # every frequency that a pool takes, above 1
+
+
+def _steps(pool):
+    """What the library keeps of a pool's frequencies (sk_rotation_of in csrc/sk_internal.h): the pairs' parts of a turn a position, in 2^-64."""
+    of = getattr(sk.lib(), "_Z14sk_rotation_ofP7sk_pool")
+    of.restype, of.argtypes = ctypes.c_void_p, [ctypes.c_void_p]
+    at = of(pool.h)
+    rotary = ctypes.c_int32.from_address(at).value
+    return list((ctypes.c_uint64 * (rotary // 2)).from_address(at + 16))
+
+
+def test_steps_against_whole_numbers():
+    """A step is the nearest 64-bit fraction of a turn, whatever the frequency: half a unit, and no more than 2^-20 of one from what forms it."""
+    pool = sk.Pool("bf16", 4, 2, 128, 16, 32, metadata_only=True)
+    lists = [FAST, -FAST, _freqs(128), np.concatenate([10.0 ** -np.arange(0, 32), -10.0 ** -np.arange(0, 32)]),
+             np.array([0.0, -0.0, 5e-324, 1.0, 2.0 ** -52, np.pi, -np.pi, 2 * np.pi, np.nextafter(2 * np.pi, 0), np.nextafter(2 * np.pi, 7), 999999.9999, -1e6, 2.0 ** 19, 710.0, 355.0, 1e-19])]
+    for f in lists:
+        pool.sk_pool_set_rotation(f)
+        steps = _steps(pool)
+        assert len(steps) == f.size
+        for x, step in zip(f, steps):
+            off = (step << 336) - _turns(x, 1)
+            off = (off + (1 << 399)) % (1 << 400) - (1 << 399)
+            assert abs(off) <= (1 << 335) + (1 << 316), (x, off / 2.0 ** 336)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_fast_pairs_at_far_positions(interleaved, sign):
+    """Frequencies up to the largest that a pool takes, positions up to the largest there are: angles of up to 3.4e8 turns."""
+    pool = sk.Pool("f32", 1, 1, 128, 16, 4)
+    pool.sk_pool_set_rotation(sign * FAST, interleaved=interleaved)
+    positions = [1, -1, 7, 1000, 4097, 131071, -131072, 10 ** 7, 10 ** 9, 2 ** 31 - 1, -2 ** 31 + 1, -2 ** 31]
+    q = synth.draw(synth.generator(39), (len(positions), 1, 128), "f32")
+    got, _ = pool.sk_rotate(q.cuda(), positions=torch.tensor(positions, dtype=torch.int32, device="cuda"))
+    got = got.cpu().double().numpy()[:, 0]
+    x = q.double().numpy()[:, 0]
+    a, b = (x[:, ::2], x[:, 1::2]) if interleaved else (x[:, :64], x[:, 64:])
+    angle = 2 * np.pi * np.array([[_turns(sign * f, p) / 2 ** 400 for f in FAST] for p in positions])
+    size = np.abs(a) + np.abs(b)
+    for y, want in ((got[:, ::2] if interleaved else got[:, :64], a * np.cos(angle) - b * np.sin(angle)),
+                    (got[:, 1::2] if interleaved else got[:, 64:], a * np.sin(angle) + b * np.cos(angle))):
+        tol = 2.0 ** -21 * size
+        assert np.all(np.abs(y - want) <= tol + HALF_STEP["f32"] * (np.abs(want) + tol)), (np.abs(y - want) / size).max()
 
 
 # ---- rows beside the cache ---------------------------------------------------------------------------
