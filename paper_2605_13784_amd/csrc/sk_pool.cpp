@@ -1769,8 +1769,8 @@ static int append(sk_pool* p, int32_t id, const void* q, const void* k, const vo
     const bool commits_turned = turned && !in_place;
     // A short call's launch turns the rows as well, where nothing that it writes is read by another of its workgroups.  One token at 2,600 cached, 32/8 heads of
     // 128 dims, us per call: in a launch in front 10.7, inside 8.1.
-    const bool turns_inside = turned && one_launch && plan.v.id == SK_KV_SMALL && turned->small && turned->q != turned->q_out &&
-                              !over_inputs(p, L, q, turned->positions, out, out_dtype, lse);
+    const bool turns_inside = turned && one_launch && plan.v.id == SK_KV_SMALL && turned->small &&
+                              (!p->device || (turned->q != turned->q_out && !over_inputs(p, L, q, turned->positions, out, out_dtype, lse)));
     ScatterSlot ss;
     if (!commits_turned) { int rc = scatter_reserve(p, scatter_groups(n, L), ss); if (rc) return rc; }
     if (in_place && turned && !turns_inside) {  // the launches behind find k turned in the staging area

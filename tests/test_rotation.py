@@ -134,6 +134,29 @@ def test_append_rotated_on_the_host():
     pool.sk_pool_inject_failure(0, 0)
 
 
+def test_a_short_append_comes_past_as_many_sites_as_it_has_launches():
+    """A metadata-only pool visits the sites of failures as a device pool does: once where the attention launch turns the rows and commits them,
+    twice where a launch in front of it turns them (the commit is the attention launch's in both)."""
+    for pairs, launches in ((32, 1), (16, 1), (8, 2)):
+        pool = _host_pool(8)
+        pool.sk_pool_set_rotation(np.ones(pairs))
+        sid = pool.sk_session_create()
+        pool.reserve(sid, 20)
+        L = sk.lib()
+
+        def append():
+            return L.sk_session_append_rotated(pool.h, sid, None, None, None, 1, None, 20, None, None, sk.SK_F32, None, None)
+
+        before = pool.sk_session_block_table(sid), pool.sk_pool_blocks_free()
+        for countdown in range(1, launches + 1):
+            pool.sk_pool_inject_failure(sk.SK_SITE_SCATTER, countdown)
+            assert append() == sk.SK_E_HIP
+            assert pool.sk_session_length(sid) == 20 and (pool.sk_session_block_table(sid), pool.sk_pool_blocks_free()) == before
+        pool.sk_pool_inject_failure(sk.SK_SITE_SCATTER, launches + 1)
+        assert append() == sk.SK_OK and pool.sk_session_length(sid) == 21
+        pool.sk_pool_inject_failure(0, 0)
+
+
 def test_a_list_of_shared_blocks_in_pinned_memory():
     pool = _host_pool(1000)
     pool.sk_pool_set_rotation(np.ones(32))
