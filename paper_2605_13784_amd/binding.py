@@ -487,6 +487,16 @@ class Pool:
             assert q_out.dtype is self.torch_dtype and q_out.is_cuda and q_out.numel() == size
         return q_out
 
+    def _own(self, x, n):
+        """Checks k or v of a call that reads n tokens of it."""
+        assert x.dtype is self.torch_dtype and x.is_cuda and x.numel() >= n * self.Hkv * self.d
+
+    def _results(self, out, lse, out_dtype, n):
+        """Checks a caller's outputs of a call of n tokens (which may have room for more)."""
+        rows = n * self.Hq
+        assert out is None or (out.dtype is (torch.float32 if _dt(out_dtype) == SK_F32 else torch.bfloat16) and out.is_cuda and out.numel() >= rows * self.d)
+        assert lse is None or (lse.dtype is torch.float32 and lse.is_cuda and lse.numel() >= rows)
+
     def sk_rotate(self, q, k=None, positions=None, pos0=0, q_out=None, k_out=None, stream=None):
         """q [tokens, Hq, d] and k [tokens, Hkv, d] (either None) turned by int32 positions [tokens], or pos0, pos0 + 1, ..  -> (q_out, k_out)"""
         n = int((k if q is None else q).shape[0])
@@ -504,9 +514,12 @@ class Pool:
             pos0 = 0 if positions is not None else self._length(sid)
         if self.kv_mem is not None:
             q_out = self._turns(q, q_out, self.Hq, L, positions, stream)
-            assert k.dtype is self.torch_dtype and v.dtype is self.torch_dtype and k.numel() == v.numel() == L * self.Hkv * self.d
+            self._own(k, L), self._own(v, L)
+            assert k.numel() == v.numel() == L * self.Hkv * self.d
             if q is not None and attend and out is None:
                 out, lse = self._out(L, out_dtype, want_lse, stream)
+            else:
+                self._results(out, lse, out_dtype, L)
         _ck(lib().sk_session_append_rotated(self.h, sid, _p(q), _p(k), _p(v), L, _p(positions), int(pos0), _p(q_out), _p(out), _dt(out_dtype), _p(lse),
                                             _stream(stream) if self.kv_mem is not None else None), "sk_session_append_rotated")
         return q_out, out, lse
@@ -516,10 +529,19 @@ class Pool:
         """sk_batch_step with q and k turned on the way by int32 positions [tokens] -> (q_out, out, lse)"""
         n, T = len(session_ids), int(cu_tokens[-1])
         q_out = self._turns(q, q_out, self.Hq, T, positions, stream)
-        if out is None:
-            out, lse = self._out(T, out_dtype, want_lse, stream)
         sid, op, cu = array.array("i", session_ids), array.array("i", ops), array.array("i", cu_tokens)
         assert len(op) == n and len(cu) == n + 1
+        read = n                                             # behind the last item whose k and v are read
+        while read and op[read - 1] == SK_OP_QUERY_A:
+            read -= 1
+        if cu[read]:
+            for x in (k, v):
+                if x is not None:                            # (left out: refused by the call)
+                    self._own(x, cu[read])
+        if out is None:
+            out, lse = self._out(T, out_dtype, want_lse, stream)
+        else:
+            self._results(out, lse, out_dtype, T)
         _ck(lib().sk_batch_step_rotated(self.h, n, sid.buffer_info()[0], op.buffer_info()[0], cu.buffer_info()[0], _p(positions), _p(q), _p(k), _p(v),
                                         _p(q_out), _p(out), _dt(out_dtype), _p(lse), _stream(stream)), "sk_batch_step_rotated")
         return q_out, out, lse

@@ -157,6 +157,72 @@ def test_a_short_append_comes_past_as_many_sites_as_it_has_launches():
         pool.sk_pool_inject_failure(0, 0)
 
 
+class _OnCard:
+    """What the binding looks at of a tensor, with nothing behind it."""
+    is_cuda = True
+
+    def __init__(self, n, dtype=torch.bfloat16, is_cuda=True):
+        self.n, self.dtype, self.is_cuda = n, dtype, is_cuda
+
+    shape = property(lambda self: (self.n // 128,))
+
+    def numel(self):
+        return self.n
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return 1 << 24
+
+
+def test_the_binding_checks_the_arrays_of_rotated_calls():
+    """A type or a length that is not the call's own would have kernels read and write behind an array: refused in the binding, which knows them.
+    (Nothing is computed: the pool holds metadata only.)"""
+    pool = _host_pool(64)                                      # 4 query heads, 2 KV heads of 64: 256 and 128 elements a token
+    pool.sk_pool_set_rotation(np.ones(32))
+    sids = [pool.sk_session_create() for _ in range(3)]
+    for sid in sids:
+        pool.reserve(sid, 20)
+    T = 9
+    good = dict(positions=_OnCard(T, torch.int32), q=_OnCard(T * 256), k=_OnCard(T * 128), v=_OnCard(T * 128), q_out=_OnCard(T * 256), out=_OnCard(T * 256, torch.float32),
+                lse=_OnCard(T * 4, torch.float32))
+    wrong = [dict(k=_OnCard(T * 128, torch.float32)), dict(v=_OnCard(T * 128, torch.float16)), dict(k=_OnCard(T * 128, is_cuda=False)), dict(v=_OnCard(T * 128, is_cuda=False)),
+             dict(out=_OnCard(T * 256)), dict(out=_OnCard(T * 256 - 4, torch.float32)), dict(out=_OnCard(T * 256, torch.float32, False)), dict(lse=_OnCard(T * 4)),
+             dict(lse=_OnCard(T * 4 - 1, torch.float32)), dict(lse=_OnCard(T * 4, torch.float32, False)), dict(q=_OnCard(T * 256, torch.float32)), dict(q_out=_OnCard(T * 256 - 64)),
+             dict(positions=_OnCard(T - 1, torch.int32)), dict(positions=_OnCard(T, torch.int64))]
+
+    def step(ops, **kw):
+        return pool.sk_batch_step_rotated(sids, ops, [0, 4, 6, T], **{**good, **kw}, stream=0)
+
+    A, B, C = sk.SK_OP_APPEND, sk.SK_OP_QUERY_A, sk.SK_OP_QUERY_B
+    step([A, B, C])
+    step([B, B, B], out=_OnCard(50 * 256, torch.float32), lse=_OnCard(50 * 4, torch.float32))           # room for more
+    for bad in wrong + [dict(k=_OnCard(T * 128 - 128)), dict(v=_OnCard(128))]:
+        with pytest.raises(AssertionError):
+            step([A, B, C], **bad)
+    # what no item reads of k and v may be missing
+    assert step([A, C, B], k=_OnCard(6 * 128), v=_OnCard(6 * 128))
+    assert step([B, B, B], k=None, v=None)
+    with pytest.raises(AssertionError):
+        step([A, C, B], k=_OnCard(6 * 128), v=_OnCard(5 * 128))
+    assert [pool.sk_session_length(s) for s in sids] == [28, 20, 20]
+
+    pool.kv_mem = True                                         # (the binding checks arrays of pools that have memory)
+    try:
+        def append(**kw):
+            a = {**good, **kw}
+            return pool.sk_session_append_rotated(sids[1], a.pop("q"), a.pop("k"), a.pop("v"), pos0=0, **a, stream=0)
+
+        append()
+        for bad in wrong + [dict(v=_OnCard(T * 128 + 128)), dict(v=_OnCard(T * 128 - 128))]:
+            with pytest.raises(AssertionError):
+                append(**bad)
+        assert pool.sk_session_length(sids[1]) == 29
+    finally:
+        pool.kv_mem = None
+
+
 def test_a_list_of_shared_blocks_in_pinned_memory():
     pool = _host_pool(1000)
     pool.sk_pool_set_rotation(np.ones(32))
