@@ -498,7 +498,8 @@ class Pool:
         assert lse is None or (lse.dtype is torch.float32 and lse.is_cuda and lse.numel() >= rows)
 
     def sk_rotate(self, q, k=None, positions=None, pos0=0, q_out=None, k_out=None, stream=None):
-        """q [tokens, Hq, d] and k [tokens, Hkv, d] (either None) turned by int32 positions [tokens], or pos0, pos0 + 1, ..  -> (q_out, k_out)"""
+        """q [tokens, Hq, d] and k [tokens, Hkv, d] (either None) turned by int32 positions [tokens], or pos0, pos0 + 1, ..: of no session, so
+        that rows that an append would put at its session's length need pos0=sk_session_length(sid).  -> (q_out, k_out)"""
         n = int((k if q is None else q).shape[0])
         q_out = self._turns(q, q_out, self.Hq, n, positions, stream)
         k_out = self._turns(k, k_out, self.Hkv, n, positions, stream)
@@ -507,8 +508,11 @@ class Pool:
 
     def sk_session_append_rotated(self, sid, q, k, v, positions=None, pos0=None, q_out=None, out=None, lse=None, attend=True, out_dtype="f32",
                                   want_lse=True, stream=None):
-        """sk_session_append with q and k turned on the way; pos0 left out: the session's length.  attend=False: q is turned, nothing attends.
-        -> (q_out, out, lse)"""
+        """sk_session_append with q and k turned on the way.  attend=False: q is turned, nothing attends.  -> (q_out, out, lse)
+
+        positions and pos0 left out: the new tokens' positions follow the session's length, the right ones where the cached tokens' are 0, 1, ..  They are not where
+        tokens have left the session (sk_session_evict_oldest, sk_session_evict_lowest) and sk_session_shift has not moved what stays: there the
+        length is a position that a cached key has, and the caller gives its own.  Nor are they where earlier appends got other positions."""
         L = int(k.shape[0])
         if pos0 is None:
             pos0 = 0 if positions is not None else self._length(sid)
