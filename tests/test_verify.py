@@ -304,6 +304,73 @@ def test_many_rows_whose_later_places_wait_for_the_first(dtype, drawn):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("drawn", [True, False])
+@pytest.mark.parametrize("n,k,V", [(1, 4, 151936), (2, 3, 131073), (2, 2, 262144), (3, 1, 202048), (1, 0, 1 << 21), (1, 1, 1 << 21)])
+def test_rows_of_more_stretches_than_a_lane_keeps(dtype, drawn, n, k, V):
+    """Behind 131,072 logits a row of the few-rows form has more than 256 stretches of 512 (four a lane) and 64 parts of 2,048 (four for each of sixteen lanes)."""
+    gen = synth.generator(50, stream=n * 1000 + k * 100 + V % 97)
+    x, y, tokens, u = _case(gen, n, k, V, dtype, near=0.7)
+    if not drawn and k:
+        tokens[:, 0] = x[:, 0].float().argmax(1)
+    _check(x, tokens, u, draft=y if drawn else None)
+
+
+def _behind(gen, n, k, V, at, dtype):
+    """Rows whose probabilities lie in the last logits, from `at` on; what is in front has none (sequences 0, 3, ..), next to none (1, 4, ..) or half (2, 5, ..)."""
+    x, y, tokens, u = _case(gen, n, k, V, dtype, near=0.7)
+    tail = V - at
+    for rows in (x, y):
+        rows[0::3, :, :at] = -float("inf")
+        rows[1::3, :, :at] -= 60.0
+        rows[2::3, :, at:] += float(np.log(at / tail))         # as much as in front
+    for i in range(k):
+        g = -torch.log(-torch.log(torch.rand((n, V), generator=gen).clamp(1e-9, 1 - 1e-7)))
+        tokens[:, i] = (y[:, i].float() + g).argmax(1)
+    return x, y, tokens, u
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,k,V,at", [(6, 2, 133000, 131072), (3, 3, 151936, 151936 - 300), (3, 1, 262144, 262143), (9, 0, 132100, 131072),
+                                      (9, 16, 524288 + 700, 524288), (40, 1, 524288 + 9000, 524288 + 8192), (200, 0, 524288 + 33, 524288)])
+def test_rows_whose_weight_lies_in_their_last_stretches(dtype, n, k, V, at):
+    """Behind stretch 256 and part 64, of either form (32 logits a lane have them from 524,288 on): draws, what is left of a drafted token, a looked-up token that is
+    rejected there, the maximum of a greedy sequence and its lowest index among equals."""
+    rows = n * (2 * k + 1)
+    gen = synth.generator(51, stream=n * 100 + k)
+    x, y, tokens, u = _behind(gen, n, k, V, at, dtype)
+    places = min(n, 8 if rows > 30 else n)
+    some = list(range(places))                                 # (the definition in 64 bits takes 0.1 s a row)
+
+    def check(**kw):
+        got = sk.sk_verify(x.cuda(), tokens.cuda(), u.cuda(), **{a: b.cuda() for a, b in kw.items()})
+        for s in some:
+            temperature = kw.get("temperature")
+            a, t, lp, near = _define(x[s].float().numpy(), kw["draft"][s].float().numpy() if "draft" in kw else None, tokens[s].numpy(), u[s].numpy(),
+                                     None if temperature is None else temperature[s])
+            assert near > 2.0 ** -40
+            assert int(got[0][s]) == a and got[1][s].tolist() == t + [-1] * (k + 1 - len(t)), s
+            lp = np.array(lp)
+            assert np.all(np.abs(got[2][s, :len(lp)].cpu().numpy() - lp) <= 2.0 ** -24 * np.abs(lp) + 2.0 ** -40 * (1 + np.abs(lp)))
+        return got
+
+    got = check(**({"draft": y} if k else {}))
+    assert (got[1][:, 0] >= at).float().mean() >= 0.5
+    if k:
+        u[:, :k] = 0.9375                                      # looked-up tokens that do not stay: each has half its row's weight or less
+        tokens[:, 0] = x[:, 0, at:].float().argmax(1).int() + at
+        check()
+    x[:, :, V - 1] = x.float().amax(2).to(x.dtype)             # greedy: two largest ones, the lower in front
+    if k:
+        tokens[:] = torch.from_numpy(np.argmax(x[:, :k].float().numpy(), 2)).int()
+    got = check(temperature=torch.zeros(n))
+    assert (got[0] == k).all()
+    x[:, :, V - 1] += 1.0
+    check(temperature=torch.zeros(n))
+
+
+@pytest.mark.gpu
 def test_more_rows_than_one_grid_has_workgroups_for():
     """2^20 rows of 32,769 bf16 logits (68.7 GB, offsets far behind 32 bits): more than 2^24 workgroups, so that the last sequences are a second run of launches.
     Every stretch of sequences gives what a call of its own gives, and rows on both sides of the border what the definition does."""
