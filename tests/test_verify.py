@@ -371,6 +371,36 @@ def test_rows_whose_weight_lies_in_their_last_stretches(dtype, n, k, V, at):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype,n,k,V,drawn", [("f32", 512, 8, 5000, True), ("bf16", 512, 8, 5000, True), ("f32", 512, 16, 5000, False), ("bf16", 512, 16, 5000, False),
+                                               ("f32", 32, 8, 128256, True)])
+def test_later_places_wait_and_every_workgroup_decides(dtype, n, k, V, drawn):
+    """8,192 parts and more, so that places come in two launches, with few enough sequences and stretches that every workgroup of the sums finds what is drawn from by itself: parts of
+    rows that nobody computed hold what the workspace held before, NaN here.  Sequences end at every place."""
+    gen = synth.generator(52, stream=n + k)
+    x, y, tokens, u = _case(gen, n, k, V, dtype, near=0.3)
+    for s in range(n):
+        e = s % (k + 2)
+        if not drawn:                                          # (looked up: what the target likes best, and numbers that let it stay)
+            tokens[s] = x[s, :k].float().argmax(1)
+            u[s, :k] *= 0.001
+        if e < k:
+            if s % 4 == 0:
+                tokens[s, e] = -1
+            elif s % 4 == 1:                                   # nothing in the target
+                x[s, e, int(tokens[s, e])] = -float("inf")
+            elif s % 4 == 2:
+                x[s, e] = float("nan")
+            else:
+                u[s, e] = 2.0                                  # (stays only where p > 2 q)
+            if s % 5 == 0:
+                x[s, e + 1:] = float("nan")                    # behind the end: not looked at
+    temperature = torch.where(torch.arange(n) % 7 == 3, 0.0, 1.0)
+    need = sk.lib().sk_verify_workspace_bytes(n, k, V)
+    accepted = _check(x, tokens, u, draft=y if drawn else None, temperature=temperature, workspace=torch.full((need,), 255, dtype=torch.uint8, device="cuda"))
+    assert len(set(accepted)) > min(k, 6)
+
+
+@pytest.mark.gpu
 def test_more_rows_than_one_grid_has_workgroups_for():
     """2^20 rows of 32,769 bf16 logits (68.7 GB, offsets far behind 32 bits): more than 2^24 workgroups, so that the last sequences are a second run of launches.
     Every stretch of sequences gives what a call of its own gives, and rows on both sides of the border what the definition does."""
