@@ -670,7 +670,7 @@ __global__ __launch_bounds__(kThreads) void sk_verify_stretches(const Args A)
     draw<F32, 64 * EACH>(A, seq, w, number, summed, first);
 }
 
-// The draw in a launch of its own, where there are many rows.  Bound: three round trips (7 us for 64 sequences).
+// The draw in a launch of its own, where there are many rows.  Bound: three round trips (6.2 us for 64 sequences).
 template <bool F32>
 __global__ __launch_bounds__(kThreads) void sk_verify_draw(const Args A)
 {
@@ -727,12 +727,19 @@ int launch(Args& A, const int each, const int dtype, const int32_t n_seq, void* 
     lay_out(A, each, workspace, n_seq);
     const dim3 block(kThreads), second((unsigned)n_seq * (each == kEach ? A.stretches : A.stretches / kWaves)), each_seq((unsigned)n_seq);
     // Where there are many rows, those of the first two places come first, and the others only of sequences whose draft is still standing.  us per call, all
-    // rows at once -> in two launches, fp32 rows of 128,256 logits with their draft's:
-    //   accepted of the drafted       nearly all        0.7 of them       0.3               0.05
-    //   64 x 4 (9,216 parts)           83 ->  89          76 ->  79        80 ->  74         80 ->  65
-    //   64 x 8 (17,408)               143 -> 146         138 -> 126       140 ->  99        139 ->  69
-    //   32 x 4 (4,608)                 41 ->  50          44 ->  50        47 ->  48         46 ->  40
-    //   64 x 3, bf16 (7,168)           57 ->  65          62 ->  66        68 ->  66         69 ->  60
+    // rows at once -> in two launches, rows of 128,256 logits with their draft's, by what share of the drafted tokens is accepted (each row at the nearest one measured):
+    //   accepted of the drafted            0.95-0.98     0.8           0.65          0.4           0.2           0.05
+    //   64 x 4 (9,216 parts)                72 ->  80     70 ->  76     74 ->  72     78 ->  69     79 ->  66     79 ->  59
+    //   64 x 8 (17,408)                    120 -> 132    126 -> 131    130 -> 124    136 -> 121    138 -> 104    137 ->  64
+    //   128 x 4 (18,432)                   129 -> 141    138 -> 139    142 -> 140    151 -> 127    154 -> 113    155 ->  99
+    //   128 x 4, bf16                      113 -> 127    125 -> 117    132 -> 115    140 -> 109    144 -> 103    144 ->  95
+    //   256 x 4, bf16 of 32,000 (9,216)     63 ->  69     63 ->  71     65 ->  70     69 ->  67     71 ->  63     73 ->  60
+    //   64 x 16 of 50,257 (14,784)         104 -> 117    104 -> 117        -         107 -> 103    109 ->  74    108 ->  56
+    //   32 x 8 (8,704)                      64 ->  73     65 ->  67     65 ->  66     67 ->  61     69 ->  56     70 ->  48
+    //   64 x 3, bf16 (7,168)                52 ->  57     52 ->  58     54 ->  59     57 ->  60     61 ->  58     61 ->  57
+    //   32 x 4 (4,608)                      40 ->  49     41 ->  49     43 ->  49     45 ->  48     46 ->  47     46 ->  40
+    // A token that stays with 0.9, 0.8 or 0.7, if those in front do, makes that share 0.77, 0.59 and 0.44 for four drafted tokens, 0.64, 0.42 and 0.27 for eight.  From the border on the
+    // two launches cost up to 14 % where nearly everything stays, and save from about 0.6 on downwards, up to half; below it they rarely save.
     const bool in_two = each == kEach && A.n_draft > kFirstPlaces && (int64_t)n_seq * A.rows * A.parts >= kPartsInTwo;
     const int split = in_two ? kFirstPlaces : 0;
     // Where its workgroups are more than run at a time, the second launch finds the row that is drawn from decided by one in front of it.  us per call, 0.7 to 0.05 of the drafted
